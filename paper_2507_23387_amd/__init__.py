@@ -42,14 +42,25 @@ _EXPORTS = (
     "workspace",
 )
 
-__all__ = list(_EXPORTS)
+# The layers around the product (layers.py).
+_LAYERS = (
+    "AdamW",
+    "layer_norm",
+    "layer_norm_backward",
+)
+
+__all__ = list(_EXPORTS + _LAYERS)
 
 
 def __getattr__(name):
-    if name in _EXPORTS or name == "binding":
-        import importlib
+    import importlib
 
-        # Raises ImportError if libsgemmcube.so is missing.
-        binding = importlib.import_module(__name__ + ".binding")
-        return binding if name == "binding" else getattr(binding, name)
+    # Raises ImportError if libsgemmcube.so is missing.
+    if name in ("binding", "layers"):
+        return importlib.import_module(f"{__name__}.{name}")
+    if name in _EXPORTS + _LAYERS:
+        module = importlib.import_module(__name__ + (".binding" if name in _EXPORTS else ".layers"))
+        # Bound here, so that the next use does not come through this function.
+        globals()[name] = value = getattr(module, name)
+        return value
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

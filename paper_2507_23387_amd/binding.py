@@ -48,6 +48,22 @@ EXPORTS = (
     "sgemm_cube_block_k",
 )
 
+# Every symbol include/sgemm_cube_layers.h declares.
+LAYER_EXPORTS = (
+    "sgemm_cube_layer_norm", "sgemm_cube_layer_norm_backward",
+    "sgemm_cube_layer_norm_backward_workspace_size",
+    "sgemm_cube_adamw", "sgemm_cube_adamw_values",
+)
+ADAMW_BLOCK = 256
+
+
+class AdamwTensor(ctypes.Structure):
+    """sgemm_cube_adamw_tensor_t"""
+    _fields_ = [("count", ctypes.c_int64), ("param", ctypes.c_void_p), ("grad", ctypes.c_void_p),
+                ("exp_avg", ctypes.c_void_p), ("exp_avg_sq", ctypes.c_void_p),
+                ("exp_avg_scale", ctypes.c_void_p), ("exp_avg_sq_scale", ctypes.c_void_p),
+                ("weight_decay", ctypes.c_double)]
+
 
 class SgemmCubeError(RuntimeError):
     def __init__(self, status: int, what: str):
@@ -63,6 +79,7 @@ def _load() -> ctypes.CDLL:
     lib = ctypes.CDLL(LIB_PATH)
     i64, ptr, f32, i32, sz, u32 = (ctypes.c_int64, ctypes.c_void_p, ctypes.c_float,
                                    ctypes.c_int, ctypes.c_size_t, ctypes.c_uint)
+    f64 = ctypes.c_double
     sig = {
         "sgemm_cube": (i32, [i64, i64, i64, ptr, i64, ptr, i64, ptr, i64, f32, i32, ptr]),
         "sgemm_cube_ws": (i32, [i64, i64, i64, ptr, i64, ptr, i64, ptr, i64, f32, i32, ptr, sz,
@@ -88,6 +105,13 @@ def _load() -> ctypes.CDLL:
         "sgemm_cube_hgemm": (i32, [i64, i64, i64, ptr, i64, ptr, i64, ptr, i64, ptr]),
         "sgemm_cube_status_string": (ctypes.c_char_p, [i32]),
         "sgemm_cube_block_k": (i32, []),
+        "sgemm_cube_layer_norm": (i32, [i64, i64, i32, ptr, i64, ptr, ptr, f32, ptr, i64, ptr,
+                                        ptr, ptr]),
+        "sgemm_cube_layer_norm_backward": (i32, [i64, i64, i32, ptr, i64, ptr, i64, ptr, ptr,
+                                                 ptr, ptr, i64, ptr, ptr, ptr, sz, ptr]),
+        "sgemm_cube_layer_norm_backward_workspace_size": (sz, [i64, i64]),
+        "sgemm_cube_adamw": (i32, [i64, ptr, i32, i32, f64, f64, f64, f64, f64, i64, ptr]),
+        "sgemm_cube_adamw_values": (i32, [i64, ptr, ptr, ptr, ptr]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -187,6 +211,35 @@ def sgemm_cube_status_string(status: int) -> str:
 
 def sgemm_cube_block_k() -> int:
     return int(_lib.sgemm_cube_block_k())
+
+
+def sgemm_cube_layer_norm(rows, cols, dtype, X, ldx, weight, bias, eps, Y, ldy, mean, rstd,
+                          stream) -> int:
+    return _lib.sgemm_cube_layer_norm(rows, cols, dtype, X, ldx, weight, bias, eps, Y, ldy, mean,
+                                      rstd, stream)
+
+
+def sgemm_cube_layer_norm_backward(rows, cols, dtype, dY, lddy, X, ldx, weight, mean, rstd, dX,
+                                   lddx, dweight, dbias, ws, ws_bytes, stream) -> int:
+    return _lib.sgemm_cube_layer_norm_backward(rows, cols, dtype, dY, lddy, X, ldx, weight, mean,
+                                               rstd, dX, lddx, dweight, dbias, ws, ws_bytes,
+                                               stream)
+
+
+def sgemm_cube_layer_norm_backward_workspace_size(rows, cols) -> int:
+    return int(_lib.sgemm_cube_layer_norm_backward_workspace_size(rows, cols))
+
+
+def sgemm_cube_adamw(tensors, list, grad_dtype, state_bits, lr, beta1, beta2, eps, grad_scale,
+                     step, stream) -> int:
+    """list: a ctypes array of AdamwTensor (or its address)."""
+    return _lib.sgemm_cube_adamw(tensors, list, grad_dtype, state_bits, lr, beta1, beta2, eps,
+                                 grad_scale, step, stream)
+
+
+def sgemm_cube_adamw_values(tensors, list, exp_avg, exp_avg_sq, stream) -> int:
+    """exp_avg, exp_avg_sq: ctypes arrays of c_void_p (or their addresses)."""
+    return _lib.sgemm_cube_adamw_values(tensors, list, exp_avg, exp_avg_sq, stream)
 
 
 # --- torch marshalling --------------------------------------------------------

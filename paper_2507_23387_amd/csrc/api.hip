@@ -9,6 +9,7 @@
 
 #include "internal.h"
 #include "sgemm_cube.h"
+#include "validate.h"
 
 namespace sgc {
 
@@ -38,55 +39,6 @@ Planes plan_planes(int64_t M, int64_t N, int64_t K, void* base, bool prescale) {
 }
 
 namespace {
-
-// Largest dimension the kernels index with 32-bit tile arithmetic; also keeps
-// every grid dimension within its hardware limit.
-constexpr int64_t kMaxDim = (int64_t{1} << 30);
-
-bool valid_order(int order) {
-  return order == SGEMM_CUBE_ELEMENTWISE || order == SGEMM_CUBE_TERMWISE ||
-         order == SGEMM_CUBE_ELEMENTWISE_CROSS_FIRST;
-}
-
-// Public accumulation order -> internal kernel variant.
-int variant_of(int order) {
-  switch (order) {
-    case SGEMM_CUBE_ELEMENTWISE: return kElementwise;
-    case SGEMM_CUBE_TERMWISE: return kTermwise;
-    default: return kCrossFirst;
-  }
-}
-
-bool valid_scale(float s) {
-  if (!std::isfinite(s) || s < 1.0f || s > 16777216.0f) return false;
-  int e = 0;
-  return std::frexp(s, &e) == 0.5f;  // exact power of two
-}
-
-// Bytes spanned by a rows x cols row-major matrix with leading dimension ld.
-uint64_t span_bytes(int64_t rows, int64_t cols, int64_t ld, uint64_t elem) {
-  if (rows <= 0 || cols <= 0) return 0;
-  return (static_cast<uint64_t>(rows - 1) * static_cast<uint64_t>(ld) +
-          static_cast<uint64_t>(cols)) * elem;
-}
-
-bool overlap(const void* p, uint64_t pn, const void* q, uint64_t qn) {
-  if (pn == 0 || qn == 0) return false;
-  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
-  return a < b + qn && b < a + pn;
-}
-
-// Grid limits: GEMM workgroups (at most (Mp / 256) * (Np / 128) of the wide
-// kernels) must fit an int, and B has at most 65535 panels (Np / 128).
-bool round_up_tiles_exceed(int64_t M, int64_t N) {
-  const int64_t Mp = round_up(M, kRowPad), Np = round_up(N, kRowPad);
-  return (Mp / 256) * (Np / 128) > INT32_MAX || Np / kPanel > 65535;
-}
-
-// ld * rows must not overflow int64 when forming addresses.
-bool ld_ok(int64_t rows, int64_t ld) {
-  return rows <= 1 || ld <= INT64_MAX / 8 / rows;
-}
 
 int validate_gemm(int64_t M, int64_t N, int64_t K, const float* A, int64_t lda, const float* B,
                   int64_t ldb, const float* C, int64_t ldc, float scale, bool check_scale) {

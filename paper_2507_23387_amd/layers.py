@@ -1,0 +1,208 @@
+"""The layers around the FP32-accuracy product (include/sgemm_cube_layers.h) on
+torch tensors: marshalling only, like binding.py.  Every call checks its
+tensors, takes its results and workspace from torch's allocator, enqueues the
+library's kernels on the current torch stream and returns; nothing is kept
+between calls, and a non-zero status raises SgemmCubeError.  There is no
+autograd here: the backward functions are called by the program.
+"""
+from __future__ import annotations
+
+import torch
+
+from . import binding
+from .binding import _check, _stream
+
+_DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+
+
+def _tensor(t, name, dtype, device=None):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in dtype:
+        raise TypeError(f"{name} must be a CUDA/HIP tensor of type "
+                        + " or ".join(str(d).removeprefix("torch.") for d in dtype))
+    if t.get_device() != (torch.cuda.current_device() if device is None else device):
+        raise ValueError(f"{name} must be on the current device, with the other operands")
+    return t
+
+
+def _matrix(t, name, shape=None, dtype=(torch.float32,)):
+    """(address, leading dimension) of a 2-D tensor whose columns are adjacent."""
+    _tensor(t, name, dtype)
+    if t.dim() != 2 or (shape is not None and t.shape != shape):
+        raise ValueError(f"{name} must be 2-D" if shape is None else
+                         f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
+    rows, cols = t.shape
+    if (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols):
+        raise ValueError(f"{name} must be row-major: unit column stride, rows apart")
+    return t.data_ptr(), max(t.stride(0) if rows > 1 else cols, 1)
+
+
+def _vector(t, name, n):
+    """Address of a contiguous FP32 vector of n values, or None."""
+    if t is None:
+        return None
+    _tensor(t, name, (torch.float32,))
+    if t.dim() != 1 or t.numel() != n or (n > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name} must be a contiguous vector of {n} values")
+    return t.data_ptr()
+
+
+def _bytes(n, device):
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+
+
+def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, keep_stats: bool = False, out=None):
+    """Layer norm of the rows of x (float32, float16 or bfloat16), rounded once to
+    x's type; weight and bias are float32.  With keep_stats=True returns
+    (y, mean, rstd), what layer_norm_backward needs.  out may be x."""
+    px, ldx = _matrix(x, "x", dtype=_DTYPES)
+    rows, cols = x.shape
+    pw, pb = _vector(weight, "weight", cols), _vector(bias, "bias", cols)
+    y = out if out is not None else torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+    py, ldy = _matrix(y, "out", x.shape, (x.dtype,))
+    mean = rstd = None
+    if keep_stats:
+        mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device)
+    _check(binding.sgemm_cube_layer_norm(
+        rows, cols, _DTYPES[x.dtype], px, ldx, pw, pb, eps, py, ldy,
+        mean.data_ptr() if keep_stats else None, rstd.data_ptr() if keep_stats else None,
+        _stream()), "sgemm_cube_layer_norm")
+    return (y, mean, rstd) if keep_stats else y
+
+
+def layer_norm_backward(dy, x, weight, mean, rstd, out=None):
+    """(dx, dweight, dbias) of layer_norm at x, with the mean and rstd that it
+    kept.  out may be dy; dweight and dbias are float32."""
+    px, ldx = _matrix(x, "x", dtype=_DTYPES)
+    rows, cols = x.shape
+    pdy, lddy = _matrix(dy, "dy", x.shape, (x.dtype,))
+    pw = _vector(weight, "weight", cols)
+    pm, pr = _vector(mean, "mean", rows), _vector(rstd, "rstd", rows)
+    dx = out if out is not None else torch.empty((rows, cols), dtype=x.dtype, device=x.device)
+    pdx, lddx = _matrix(dx, "out", x.shape, (x.dtype,))
+    dw, db = torch.empty((2, cols), dtype=torch.float32, device=x.device)
+    ws = _bytes(binding.sgemm_cube_layer_norm_backward_workspace_size(rows, cols), x.device)
+    _check(binding.sgemm_cube_layer_norm_backward(
+        rows, cols, _DTYPES[x.dtype], pdy, lddy, px, ldx, pw, pm, pr, pdx, lddx, dw.data_ptr(),
+        db.data_ptr(), ws.data_ptr(), ws.numel(), _stream()), "sgemm_cube_layer_norm_backward")
+    return dx, dw, db
+
+
+def _flat(t, name, n, dtype):
+    """Address of a contiguous tensor of n values."""
+    _tensor(t, name, dtype)
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous and hold {n} values")
+    return t.data_ptr()
+
+
+class AdamW:
+    """AdamW with decoupled weight decay over a program's tensors, one kernel
+    launch for up to 48 of them (sgemm_cube_adamw).
+
+    params        contiguous float32 tensors, updated in place
+    weight_decay  one number, or one per tensor
+    state_bits    32: float32 states; 8: int8 and uint8 codes with a float32
+                  scale per 256 values
+    states        dict of lists with one contiguous tensor per parameter, to go
+                  on from: "exp_avgs", "exp_avg_sqs" (32 bits: float32; 8 bits:
+                  int8 and uint8) and, for 8 bits, "exp_avg_scales" and
+                  "exp_avg_sq_scales".  They are used in place.  Without it the
+                  states start at zero.  The attribute `states` holds them.
+
+    The object keeps the tensors' addresses, so a parameter or state must stay
+    in its memory; gradients are given to each step.
+    """
+
+    def __init__(self, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8,
+                 weight_decay=0.01, state_bits: int = 32, states=None, step: int = 0):
+        if state_bits not in (8, 32):
+            raise ValueError("state_bits must be 8 or 32")
+        self.params = list(params)
+        self.lr, self.betas, self.eps = lr, tuple(betas), eps
+        self.state_bits, self.steps = state_bits, step
+        n = len(self.params)
+        decay = list(weight_decay) if hasattr(weight_decay, "__len__") else [weight_decay] * n
+        if len(decay) != n:
+            raise ValueError(f"weight_decay must be one number or {n}")
+        self.states = self._zero_states() if states is None else dict(states)
+        kinds = self._kinds()
+        if set(self.states) != set(kinds):
+            raise ValueError(f"states must hold {', '.join(kinds)}")
+        self._list = (binding.AdamwTensor * n)()
+        self._device = None
+        for i, p in enumerate(self.params):
+            count = p.numel() if isinstance(p, torch.Tensor) else 0
+            entry = self._list[i]
+            entry.count, entry.weight_decay = count, decay[i]
+            entry.param = _flat(p, f"params[{i}]", count, (torch.float32,))
+            for key, (field, dtype, scale) in kinds.items():
+                if len(self.states[key]) != n:
+                    raise ValueError(f"states[{key!r}] must hold {n} tensors")
+                size = -(-count // binding.ADAMW_BLOCK) if scale else count
+                setattr(entry, field, _flat(self.states[key][i], f"states[{key!r}][{i}]", size,
+                                            (dtype,)))
+            self._device = p.get_device()
+        self._counts = [p.numel() for p in self.params]
+
+    def _kinds(self):
+        """states' keys: (field of the list's entries, type, one value per block)."""
+        f32 = torch.float32
+        if self.state_bits == 32:
+            return {"exp_avgs": ("exp_avg", f32, False), "exp_avg_sqs": ("exp_avg_sq", f32, False)}
+        return {"exp_avgs": ("exp_avg", torch.int8, False),
+                "exp_avg_sqs": ("exp_avg_sq", torch.uint8, False),
+                "exp_avg_scales": ("exp_avg_scale", f32, True),
+                "exp_avg_sq_scales": ("exp_avg_sq_scale", f32, True)}
+
+    def _zero_states(self):
+        block = binding.ADAMW_BLOCK
+        return {key: [torch.zeros(-(-p.numel() // block) if scale else p.numel(), dtype=dtype,
+                                  device=p.device) for p in self.params]
+                for key, (_, dtype, scale) in self._kinds().items()}
+
+    def step(self, grads, step: int | None = None, grad_scale: float = 1.0):
+        """One step from grads (contiguous tensors of one type: float32, float16 or
+        bfloat16), multiplied by grad_scale first.  step: its number, by default
+        one more than the last."""
+        grads = list(grads)
+        if len(grads) != len(self._counts):
+            raise ValueError(f"grads must hold {len(self._counts)} tensors")
+        number = self.steps + 1 if step is None else step
+        dtype = grads[0].dtype if grads and isinstance(grads[0], torch.Tensor) else torch.float32
+        if dtype not in _DTYPES:
+            raise TypeError("grads must be float32, float16 or bfloat16")
+        self._on_device()
+        for i, (g, n, entry) in enumerate(zip(grads, self._counts, self._list)):
+            entry.grad = _flat(g, f"grads[{i}]", n, (dtype,))
+        _check(binding.sgemm_cube_adamw(
+            len(grads), self._list, _DTYPES[dtype], self.state_bits, self.lr, self.betas[0],
+            self.betas[1], self.eps, grad_scale, number, _stream()), "sgemm_cube_adamw")
+        self.steps = number
+
+    def state_values(self, out=None):
+        """(exp_avgs, exp_avg_sqs) as lists of float32 tensors in the parameters'
+        shapes, as a checkpoint holds them; out: a pair of lists to write to.
+        With 32-bit states, the states themselves (or copies in out)."""
+        if out is None and self.state_bits == 32:
+            return self.states["exp_avgs"], self.states["exp_avg_sqs"]
+        if out is None:
+            out = tuple([torch.empty_like(p) for p in self.params] for _ in range(2))
+        n = len(self._counts)
+        if len(out) != 2 or len(out[0]) != n or len(out[1]) != n:
+            raise ValueError(f"out must be a pair of lists of {n} tensors")
+        self._on_device()
+        addresses = [(binding.ctypes.c_void_p * n)(*(
+            _flat(t, f"out[{k}][{i}]", self._counts[i], (torch.float32,))
+            for i, t in enumerate(out[k]))) for k in range(2)]
+        if self.state_bits == 32:
+            for k, key in enumerate(("exp_avgs", "exp_avg_sqs")):
+                for t, s in zip(out[k], self.states[key]):
+                    t.view(-1).copy_(s.view(-1))
+            return out
+        _check(binding.sgemm_cube_adamw_values(n, self._list, *addresses, _stream()),
+               "sgemm_cube_adamw_values")
+        return out
+
+    def _on_device(self):
+        if self._device is not None and torch.cuda.current_device() != self._device:
+            raise ValueError("the parameters are not on the current device")

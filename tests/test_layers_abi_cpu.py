@@ -1,0 +1,120 @@
+"""Host-side checks of the layers' C-ABI (no GPU needed): the library exports
+what include/sgemm_cube_layers.h declares and rejects invalid arguments before
+touching the device."""
+import ctypes
+import os
+import re
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HEADER = os.path.join(ROOT, "include", "sgemm_cube_layers.h")
+INVALID, NOT_SUPPORTED = 1, 2
+FAKE = 1 << 40  # a non-null address that is never dereferenced
+GIB = 1 << 30
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2507_23387_amd import binding
+
+    return binding
+
+
+def test_header_and_exports(lib):
+    text = re.sub(r"/\*.*?\*/", "", open(HEADER).read(), flags=re.S)
+    declared = sorted(set(re.findall(r"\b(sgemm_cube\w*)\s*\(", text)))
+    assert declared == sorted(lib.LAYER_EXPORTS)
+    raw = ctypes.CDLL(lib.LIB_PATH)
+    assert all(hasattr(raw, name) for name in declared)
+
+
+def test_header_compiles_as_c():
+    import subprocess
+
+    src = b'#include "sgemm_cube_layers.h"\nint main(void) { return SGEMM_CUBE_F32; }\n'
+    subprocess.run(["gcc", "-x", "c", "-std=c11", "-fsyntax-only", "-D__HIP_PLATFORM_AMD__",
+                    "-I", os.path.join(ROOT, "include"), "-I", "/opt/rocm/include", "-"],
+                   input=src, check=True)
+
+
+def test_layer_norm_validation(lib):
+    X, Y, W, B, MU, RS = (FAKE + i * GIB for i in range(6))
+
+    def call(rows=4, cols=8, dtype=0, X=X, ldx=8, W=W, B=B, eps=1e-5, Y=Y, ldy=8, mu=MU, rs=RS):
+        return lib.sgemm_cube_layer_norm(rows, cols, dtype, X, ldx, W, B, eps, Y, ldy, mu, rs, 0)
+
+    for kw in (dict(rows=-1), dict(cols=-1), dict(dtype=3), dict(dtype=-1), dict(ldx=7),
+               dict(ldy=7), dict(X=None), dict(Y=None), dict(X=X + 2), dict(Y=Y + 2),
+               dict(W=W + 2), dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")),
+               dict(Y=X + 32), dict(Y=X, ldy=9), dict(W=Y), dict(mu=Y), dict(rs=MU + 8),
+               dict(mu=X), dict(rs=B), dict(rows=1 << 60, ldx=1 << 10)):
+        assert call(**kw) == INVALID, kw
+    assert call(rows=(1 << 30) + 1, Y=FAKE << 1, mu=FAKE << 2, rs=FAKE << 3) == NOT_SUPPORTED
+    assert call(rows=0) == 0 and call(rows=0, X=None, Y=None, mu=None, rs=None) == 0
+    assert call(cols=0, mu=None, rs=None) == 0
+
+
+def test_layer_norm_backward_validation(lib):
+    DY, X, W, MU, RS, DX, DW, DB, WS = (FAKE + i * GIB for i in range(9))
+    need = lib.sgemm_cube_layer_norm_backward_workspace_size(4, 8)
+    assert need > 0 and need % 256 == 0
+    assert lib.sgemm_cube_layer_norm_backward_workspace_size(0, 8) == 0
+    assert lib.sgemm_cube_layer_norm_backward_workspace_size(4, -8) == 0
+
+    def call(rows=4, cols=8, dtype=1, DY=DY, lddy=8, X=X, ldx=8, W=W, MU=MU, RS=RS, DX=DX, lddx=8,
+             DW=DW, DB=DB, WS=WS, n=need):
+        return lib.sgemm_cube_layer_norm_backward(rows, cols, dtype, DY, lddy, X, ldx, W, MU, RS,
+                                                  DX, lddx, DW, DB, WS, n, 0)
+
+    for kw in (dict(rows=-1), dict(dtype=5), dict(lddy=7), dict(ldx=7), dict(lddx=7),
+               dict(DY=None), dict(X=None), dict(DX=None), dict(MU=None), dict(RS=None),
+               dict(DY=DY + 1), dict(DX=DY + 16), dict(DX=X), dict(DX=DY, lddx=9), dict(DW=DB),
+               dict(DW=X), dict(DB=MU), dict(n=need - 1), dict(WS=None), dict(WS=WS + 8),
+               dict(WS=X), dict(DW=WS), dict(DX=WS)):
+        assert call(**kw) == INVALID, kw
+    assert call(cols=0) == 0
+
+
+def test_adamw_validation(lib):
+    P, G, M, V, MS, VS = (FAKE + i * GIB for i in range(6))
+    inf, nan = float("inf"), float("nan")
+
+    def call(bits=32, dtype=0, lr=1e-3, b1=0.9, b2=0.99, eps=1e-8, scale=1.0, step=1, tensors=1,
+             **entry):
+        e = dict(count=1000, param=P, grad=G, exp_avg=M, exp_avg_sq=V, exp_avg_scale=MS,
+                 exp_avg_sq_scale=VS, weight_decay=0.1) | entry
+        array = (lib.AdamwTensor * 1)(lib.AdamwTensor(**e))
+        return lib.sgemm_cube_adamw(tensors, array, dtype, bits, lr, b1, b2, eps, scale, step, 0)
+
+    for bits in (8, 32):
+        for kw in (dict(bits=16), dict(dtype=3), dict(lr=nan), dict(lr=inf), dict(b1=1.0),
+                   dict(b1=-0.1), dict(b2=nan), dict(eps=-1.0), dict(eps=inf), dict(scale=inf),
+                   dict(step=0), dict(count=-1), dict(param=None), dict(grad=None),
+                   dict(exp_avg=None), dict(exp_avg_sq=None), dict(param=P + 2), dict(grad=G + 2),
+                   dict(weight_decay=nan), dict(param=G), dict(param=M + 4), dict(exp_avg=V),
+                   dict(grad=V - 8), dict(tensors=-1)):
+            assert call(**(dict(bits=bits) | kw)) == INVALID, (bits, kw)
+        assert call(bits=bits, count=(1 << 35) + 1) == NOT_SUPPORTED
+        assert call(bits=bits, count=0, param=None, grad=None) == 0
+        assert call(bits=bits, tensors=0) == 0
+    for kw in (dict(exp_avg_scale=None), dict(exp_avg_sq_scale=None), dict(exp_avg_scale=MS + 1),
+               dict(exp_avg_scale=VS), dict(exp_avg_scale=P)):
+        assert call(bits=8, **kw) == INVALID, kw
+    assert lib.sgemm_cube_adamw(1, None, 0, 32, 1e-3, 0.9, 0.9, 0.0, 1.0, 1, 0) == INVALID
+
+
+def test_adamw_values_validation(lib):
+    M, V, MS, VS, A, B = (FAKE + i * GIB for i in range(6))
+
+    def call(tensors=1, out=(A, B), **entry):
+        e = dict(count=1000, exp_avg=M, exp_avg_sq=V, exp_avg_scale=MS, exp_avg_sq_scale=VS) | entry
+        array = (lib.AdamwTensor * 1)(lib.AdamwTensor(**e))
+        a, b = ((ctypes.c_void_p * 1)(x) for x in out)
+        return lib.sgemm_cube_adamw_values(tensors, array, a, b, 0)
+
+    for kw in (dict(out=(None, B)), dict(out=(A, None)), dict(out=(A + 2, B)), dict(out=(A, A)),
+               dict(out=(M, B)), dict(out=(A, VS)), dict(exp_avg=None), dict(exp_avg_scale=None),
+               dict(count=-1), dict(tensors=-1)):
+        assert call(**kw) == INVALID, kw
+    assert call(count=0) == 0 and call(tensors=0) == 0
