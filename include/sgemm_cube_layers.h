@@ -18,6 +18,71 @@
 extern "C" {
 #endif
 
+/* Activations, and their derivatives in the backward pass. */
+typedef enum {
+  SGEMM_CUBE_ACT_NONE = 0,
+  SGEMM_CUBE_ACT_RELU = 1,      /* max(z, 0), derivative 0 at 0 */
+  SGEMM_CUBE_ACT_GELU = 2,      /* z Phi(z), Phi the normal distribution */
+  SGEMM_CUBE_ACT_GELU_TANH = 3, /* z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2 */
+  SGEMM_CUBE_ACT_SILU = 4       /* z / (1 + exp(-z)) */
+} sgemm_cube_activation_t;
+
+/*
+ * A linear layer with its epilogue:
+ *   Z = X W + bias,   Y = act(Z) + R,
+ * the product by the three-product method of sgemm_cube.h, the epilogue in 32
+ * bits.
+ *   M, N, K      >= 0.  M == 0 or N == 0: nothing is done.  K == 0: X W = 0.
+ *   X, ldx       row-major M x K, ldx >= max(1, K).
+ *   W, ldw       transpose_w == 0: row-major K x N, ldw >= max(1, N);
+ *                otherwise row-major N x K (its rows the outputs), ldw >=
+ *                max(1, K).
+ *   bias         NULL, or N values.
+ *   activation   sgemm_cube_activation_t.
+ *   R, ldr       NULL, or row-major M x N, ldr >= max(1, N) (ignored without R).
+ *                May be Y itself (same pointer and leading dimension).
+ *   Y, ldy       row-major M x N, ldy >= max(1, N).
+ *   Z, ldz       NULL, or row-major M x N that receives Z, what the backward
+ *                pass needs of a layer with an activation.
+ *   scale, accum_order  as for sgemm_cube.
+ *   ws, ws_bytes at least sgemm_cube_linear_workspace_size(M, N, K) bytes,
+ *                256-byte aligned, as for sgemm_cube_ws.
+ * Outputs must not overlap each other, an input or the workspace, but for R.
+ * As for sgemm_cube there is no range guard: entries of X and W with a
+ * magnitude of 65520 or more give infinities or NaN in their rows and columns.
+ */
+int sgemm_cube_linear(int64_t M, int64_t N, int64_t K, const float* X, int64_t ldx,
+                      const float* W, int64_t ldw, int transpose_w, const float* bias,
+                      int activation, const float* R, int64_t ldr, float* Y, int64_t ldy,
+                      float* Z, int64_t ldz, float scale, int accum_order, void* ws,
+                      size_t ws_bytes, hipStream_t stream);
+size_t sgemm_cube_linear_workspace_size(int64_t M, int64_t N, int64_t K);
+
+/*
+ * Gradients of the linear layer: with D = dY act'(Z), entry by entry,
+ *   dX = D W^T,   dW = X^T D,   dbias_j = sum_i D_ij
+ * (the residual's gradient is dY itself).  Gradients are often far below what
+ * FP16 holds, so D is multiplied by a power of two, found from its largest
+ * finite magnitude, before it is split, and dX and dW are scaled back; X and W
+ * are taken as they are, as in the forward pass.
+ *   dY, lddy     row-major M x N.
+ *   Z, ldz       row-major M x N; NULL (and ldz ignored) without an activation.
+ *   X, W         as in the forward pass.
+ *   dX, lddx     NULL, or row-major M x K, overwritten.
+ *   dW, lddw     NULL, or of W's shape and layout, overwritten (zeros for M == 0).
+ *   dbias        NULL, or N values, overwritten (zeros for M == 0).
+ *   ws, ws_bytes at least sgemm_cube_linear_backward_workspace_size(M, N, K)
+ *                bytes, 256-byte aligned, as for sgemm_cube_ws.
+ * Outputs must not overlap each other, an input or the workspace.
+ */
+int sgemm_cube_linear_backward(int64_t M, int64_t N, int64_t K, const float* dY, int64_t lddy,
+                               const float* Z, int64_t ldz, const float* X, int64_t ldx,
+                               const float* W, int64_t ldw, int transpose_w, int activation,
+                               float* dX, int64_t lddx, float* dW, int64_t lddw, float* dbias,
+                               float scale, int accum_order, void* ws, size_t ws_bytes,
+                               hipStream_t stream);
+size_t sgemm_cube_linear_backward_workspace_size(int64_t M, int64_t N, int64_t K);
+
 /* Element types of a layer norm's rows. */
 typedef enum {
   SGEMM_CUBE_F32 = 0,

@@ -47,6 +47,8 @@ _LAYERS = (
     "AdamW",
     "layer_norm",
     "layer_norm_backward",
+    "linear",
+    "linear_backward",
 )
 
 __all__ = list(_EXPORTS + _LAYERS)

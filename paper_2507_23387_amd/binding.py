@@ -50,11 +50,14 @@ EXPORTS = (
 
 # Every symbol include/sgemm_cube_layers.h declares.
 LAYER_EXPORTS = (
+    "sgemm_cube_linear", "sgemm_cube_linear_workspace_size",
+    "sgemm_cube_linear_backward", "sgemm_cube_linear_backward_workspace_size",
     "sgemm_cube_layer_norm", "sgemm_cube_layer_norm_backward",
     "sgemm_cube_layer_norm_backward_workspace_size",
     "sgemm_cube_adamw", "sgemm_cube_adamw_values",
 )
 ADAMW_BLOCK = 256
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 
 
 class AdamwTensor(ctypes.Structure):
@@ -105,6 +108,13 @@ def _load() -> ctypes.CDLL:
         "sgemm_cube_hgemm": (i32, [i64, i64, i64, ptr, i64, ptr, i64, ptr, i64, ptr]),
         "sgemm_cube_status_string": (ctypes.c_char_p, [i32]),
         "sgemm_cube_block_k": (i32, []),
+        "sgemm_cube_linear": (i32, [i64, i64, i64, ptr, i64, ptr, i64, i32, ptr, i32, ptr, i64,
+                                    ptr, i64, ptr, i64, f32, i32, ptr, sz, ptr]),
+        "sgemm_cube_linear_workspace_size": (sz, [i64, i64, i64]),
+        "sgemm_cube_linear_backward": (i32, [i64, i64, i64, ptr, i64, ptr, i64, ptr, i64, ptr,
+                                             i64, i32, i32, ptr, i64, ptr, i64, ptr, f32, i32,
+                                             ptr, sz, ptr]),
+        "sgemm_cube_linear_backward_workspace_size": (sz, [i64, i64, i64]),
         "sgemm_cube_layer_norm": (i32, [i64, i64, i32, ptr, i64, ptr, ptr, f32, ptr, i64, ptr,
                                         ptr, ptr]),
         "sgemm_cube_layer_norm_backward": (i32, [i64, i64, i32, ptr, i64, ptr, i64, ptr, ptr,
@@ -211,6 +221,28 @@ def sgemm_cube_status_string(status: int) -> str:
 
 def sgemm_cube_block_k() -> int:
     return int(_lib.sgemm_cube_block_k())
+
+
+def sgemm_cube_linear(M, N, K, X, ldx, W, ldw, transpose_w, bias, activation, R, ldr, Y, ldy, Z,
+                      ldz, scale, accum_order, ws, ws_bytes, stream) -> int:
+    return _lib.sgemm_cube_linear(M, N, K, X, ldx, W, ldw, transpose_w, bias, activation, R, ldr,
+                                  Y, ldy, Z, ldz, scale, accum_order, ws, ws_bytes, stream)
+
+
+def sgemm_cube_linear_workspace_size(M, N, K) -> int:
+    return int(_lib.sgemm_cube_linear_workspace_size(M, N, K))
+
+
+def sgemm_cube_linear_backward(M, N, K, dY, lddy, Z, ldz, X, ldx, W, ldw, transpose_w, activation,
+                               dX, lddx, dW, lddw, dbias, scale, accum_order, ws, ws_bytes,
+                               stream) -> int:
+    return _lib.sgemm_cube_linear_backward(M, N, K, dY, lddy, Z, ldz, X, ldx, W, ldw, transpose_w,
+                                           activation, dX, lddx, dW, lddw, dbias, scale,
+                                           accum_order, ws, ws_bytes, stream)
+
+
+def sgemm_cube_linear_backward_workspace_size(M, N, K) -> int:
+    return int(_lib.sgemm_cube_linear_backward_workspace_size(M, N, K))
 
 
 def sgemm_cube_layer_norm(rows, cols, dtype, X, ldx, weight, bias, eps, Y, ldy, mean, rstd,

@@ -38,6 +38,13 @@ Planes plan_planes(int64_t M, int64_t N, int64_t K, void* base, bool prescale) {
   return p;
 }
 
+// A fresh stamp for every split of an operand (see launch_split); 0 is skipped.
+static std::atomic<uint32_t> g_stamp{0};
+uint32_t next_stamp() {
+  uint32_t s = g_stamp.fetch_add(1, std::memory_order_relaxed) + 1;
+  return s ? s : g_stamp.fetch_add(1, std::memory_order_relaxed) + 1;
+}
+
 namespace {
 
 int validate_gemm(int64_t M, int64_t N, int64_t K, const float* A, int64_t lda, const float* B,
@@ -55,13 +62,6 @@ int validate_gemm(int64_t M, int64_t N, int64_t K, const float* A, int64_t lda, 
   if (M > kMaxDim || N > kMaxDim || K > kMaxDim) return SGEMM_CUBE_ERR_NOT_SUPPORTED;
   if (round_up_tiles_exceed(M, N)) return SGEMM_CUBE_ERR_NOT_SUPPORTED;
   return SGEMM_CUBE_OK;
-}
-
-// A fresh stamp for every split of an operand (see launch_split); 0 is skipped.
-std::atomic<uint32_t> g_stamp{0};
-uint32_t next_stamp() {
-  uint32_t s = g_stamp.fetch_add(1, std::memory_order_relaxed) + 1;
-  return s ? s : g_stamp.fetch_add(1, std::memory_order_relaxed) + 1;
 }
 
 size_t ws_size(int64_t M, int64_t N, int64_t K, bool prescale = false) {

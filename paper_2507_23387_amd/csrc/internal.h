@@ -182,6 +182,9 @@ hipError_t launch_split(const Planes& p, int64_t M, int64_t N, int64_t K, const 
                         const RangeOpts& opt, uint32_t a_stamp, uint32_t b_stamp, SplitPlanes what,
                         hipStream_t stream);
 
+// A fresh stamp for every split of an operand (never 0).
+uint32_t next_stamp();
+
 // Pre-scaling: enqueue the row maxima of |A| and column maxima of |B| (finite
 // entries only) into p.row_max / p.col_max.
 hipError_t launch_absmax(const Planes& p, int64_t M, int64_t N, int64_t K, const float* A,

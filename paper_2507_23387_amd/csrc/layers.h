@@ -11,6 +11,106 @@ namespace sgc {
 enum Dtype : int { kF32 = 0, kF16 = 1, kBF16 = 2 };
 inline int dtype_bytes(int dtype) { return dtype == kF32 ? 4 : 2; }
 
+// --- linear layer ---------------------------------------------------------------
+
+// One matrix of a split launch: S is rows x cols row-major, times act'(Z) where z
+// is not null.  Its planes with S's rows as rows (k = cols) go to row_*, those
+// with its columns as rows (k = rows) to col_*; either may be null.  kp_row =
+// cols and kp_col = rows rounded up to 64.  With max_bits the values are first
+// multiplied by the power of two that brings the magnitude of those bits to
+// 2^target (one target for each kind of planes).  `range`: the header of B-side
+// planes, whose flag words get `stamp` as launch_split's do (null: none).
+struct SplitJob {
+  const float* s;
+  int64_t ld;
+  const float* z;
+  int64_t ldz;
+  int activation;
+  int64_t rows, cols;
+  uint16_t* row_hi;
+  uint16_t* row_lo;
+  uint16_t* col_hi;
+  uint16_t* col_lo;
+  const uint32_t* max_bits;
+  int row_target, col_target;
+  uint32_t* row_range;
+  uint32_t* col_range;
+  uint32_t row_stamp, col_stamp;
+};
+constexpr int kSplitJobs = 3;
+hipError_t launch_split_jobs(const SplitJob* jobs, int count, float scale, hipStream_t stream);
+
+// The sums of D = dY act'(Z)'s columns in `dbias` (null: none) and the bits of
+// its largest finite magnitude in *max_bits.  `partial` holds
+// column_slabs(M, N) x (N + ceil(N / kColumnStrip)) floats.
+constexpr int kColumnStrip = 128;
+int64_t column_slabs(int64_t M, int64_t N);
+struct ColumnArgs {
+  int64_t M, N;
+  const float* dy;
+  int64_t lddy;
+  const float* z;  // null: D = dY
+  int64_t ldz;
+  int activation;
+  float* dbias;
+  uint32_t* max_bits;
+  float* partial;
+};
+hipError_t launch_columns(const ColumnArgs& a, hipStream_t stream);
+
+// What follows a product P: Y = act(Z) + R, Z = 2^-shift P + bias.
+struct Epilogue {
+  const float* bias;  // null: none
+  int activation;
+  const float* r;     // null: none
+  int64_t ldr;
+  float* z;           // null: not kept
+  int64_t ldz;
+  const uint32_t* max_bits;  // shift = prescale_shift(*max_bits, target); null: 0
+  int target;
+};
+hipError_t launch_epilogue(const Epilogue& e, int64_t M, int64_t N, const float* P, int64_t ldp,
+                           float* Y, int64_t ldy, hipStream_t stream);
+
+struct LinearArgs {
+  int64_t M, N, K;
+  const float* x;
+  int64_t ldx;
+  const float* w;
+  int64_t ldw;
+  bool transpose_w;
+  Epilogue e;
+  float* y;
+  int64_t ldy;
+  float scale;
+  int variant;
+};
+size_t linear_ws(int64_t M, int64_t N, int64_t K);
+hipError_t launch_linear(const LinearArgs& a, void* ws, hipStream_t stream);
+
+struct LinearGradArgs {
+  int64_t M, N, K;
+  const float* dy;
+  int64_t lddy;
+  const float* z;  // null: no activation
+  int64_t ldz;
+  const float* x;
+  int64_t ldx;
+  const float* w;
+  int64_t ldw;
+  bool transpose_w;
+  int activation;
+  float* dx;  // null: not wanted, as dw and dbias
+  int64_t lddx;
+  float* dw;
+  int64_t lddw;
+  float* dbias;
+  float scale;
+  int variant;
+};
+size_t linear_grad_ws(int64_t M, int64_t N, int64_t K);
+hipError_t launch_linear_grad(const LinearGradArgs& a, void* ws, hipStream_t stream);
+
 struct NormArgs {
   int64_t rows, cols;
   const void* x;

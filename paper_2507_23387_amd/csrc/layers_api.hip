@@ -61,6 +61,13 @@ int check_adamw_list(int64_t tensors, const sgemm_cube_adamw_tensor_t* list, int
   return SGEMM_CUBE_OK;
 }
 
+bool valid_activation(int a) { return a >= SGEMM_CUBE_ACT_NONE && a <= SGEMM_CUBE_ACT_SILU; }
+
+// Limits of the kernels of an M x N x K product.
+bool product_exceeds(int64_t M, int64_t N, int64_t K) {
+  return M > kMaxDim || N > kMaxDim || K > kMaxDim || round_up_tiles_exceed(M, N);
+}
+
 size_t norm_grad_ws(int64_t rows, int64_t cols) {
   return static_cast<size_t>(round_up(norm_slabs(rows, cols) * 2 * cols * 4, 256));
 }
@@ -70,6 +77,87 @@ size_t norm_grad_ws(int64_t rows, int64_t cols) {
 
 #pragma GCC visibility push(default)
 extern "C" {
+
+size_t sgemm_cube_linear_workspace_size(int64_t M, int64_t N, int64_t K) {
+  if (M < 0 || N < 0 || K < 0 || sgc::product_exceeds(M, N, K)) return 0;
+  return sgc::linear_ws(M, N, K);
+}
+
+int sgemm_cube_linear(int64_t M, int64_t N, int64_t K, const float* X, int64_t ldx,
+                      const float* W, int64_t ldw, int transpose_w, const float* bias,
+                      int activation, const float* R, int64_t ldr, float* Y, int64_t ldy,
+                      float* Z, int64_t ldz, float scale, int accum_order, void* ws,
+                      size_t ws_bytes, hipStream_t stream) {
+  using namespace sgc;
+  if (M < 0 || N < 0 || K < 0 || !valid_order(accum_order) || !valid_activation(activation) ||
+      !valid_scale(scale))
+    return kInvalid;
+  const int64_t wr = transpose_w ? N : K, wc = transpose_w ? K : N;
+  if (!matrix_ok(M, K, X, ldx, 4) || !matrix_ok(wr, wc, W, ldw, 4) || !vector_ok(bias) ||
+      (R && !matrix_ok(M, N, R, ldr, 4)) || !matrix_ok(M, N, Y, ldy, 4) ||
+      (Z && !matrix_ok(M, N, Z, ldz, 4)))
+    return kInvalid;
+  if (product_exceeds(M, N, K)) return SGEMM_CUBE_ERR_NOT_SUPPORTED;
+  const size_t need = linear_ws(M, N, K);
+  if (!workspace_ok(ws, ws_bytes, need)) return kInvalid;
+  const Span x{X, span_bytes(M, K, ldx, 4)}, w{W, span_bytes(wr, wc, ldw, 4)};
+  const Span b{bias, 4 * static_cast<uint64_t>(N)}, r{R, span_bytes(M, N, ldr, 4)};
+  const Span y{Y, span_bytes(M, N, ldy, 4)}, z{Z, span_bytes(M, N, ldz, 4)}, wsp{ws, need};
+  const bool in_place = R == Y && ldr == ldy;
+  if (hits(y, {x, w, b, z, wsp}) || (!in_place && hits(y, {r})) || hits(z, {x, w, b, r, wsp}) ||
+      hits(wsp, {x, w, b, r}))
+    return kInvalid;
+  if (M == 0 || N == 0) return SGEMM_CUBE_OK;
+  LinearArgs a{M, N, K, X, ldx, W, ldw, transpose_w != 0, Epilogue{}, Y, ldy, scale,
+               variant_of(accum_order)};
+  a.e.bias = bias;
+  a.e.activation = activation;
+  a.e.r = R, a.e.ldr = ldr;
+  a.e.z = Z, a.e.ldz = ldz;
+  return status_of(launch_linear(a, ws, stream));
+}
+
+size_t sgemm_cube_linear_backward_workspace_size(int64_t M, int64_t N, int64_t K) {
+  using namespace sgc;
+  if (M < 0 || N < 0 || K < 0 || product_exceeds(M, K, N) || product_exceeds(K, N, M) ||
+      product_exceeds(N, K, M))
+    return 0;
+  return linear_grad_ws(M, N, K);
+}
+
+int sgemm_cube_linear_backward(int64_t M, int64_t N, int64_t K, const float* dY, int64_t lddy,
+                               const float* Z, int64_t ldz, const float* X, int64_t ldx,
+                               const float* W, int64_t ldw, int transpose_w, int activation,
+                               float* dX, int64_t lddx, float* dW, int64_t lddw, float* dbias,
+                               float scale, int accum_order, void* ws, size_t ws_bytes,
+                               hipStream_t stream) {
+  using namespace sgc;
+  if (M < 0 || N < 0 || K < 0 || !valid_order(accum_order) || !valid_activation(activation) ||
+      !valid_scale(scale))
+    return kInvalid;
+  const int64_t wr = transpose_w ? N : K, wc = transpose_w ? K : N;
+  const bool act = activation != SGEMM_CUBE_ACT_NONE;
+  if (!matrix_ok(M, N, dY, lddy, 4) || (act && !matrix_ok(M, N, Z, ldz, 4)) ||
+      !matrix_ok(M, K, X, ldx, 4) || !matrix_ok(wr, wc, W, ldw, 4) ||
+      (dX && !matrix_ok(M, K, dX, lddx, 4)) || (dW && !matrix_ok(wr, wc, dW, lddw, 4)) ||
+      !vector_ok(dbias))
+    return kInvalid;
+  if (product_exceeds(M, K, N) || product_exceeds(K, N, M) || product_exceeds(N, K, M))
+    return SGEMM_CUBE_ERR_NOT_SUPPORTED;
+  const size_t need = linear_grad_ws(M, N, K);
+  if (!workspace_ok(ws, ws_bytes, need)) return kInvalid;
+  if (!act) Z = nullptr;
+  const Span dy{dY, span_bytes(M, N, lddy, 4)}, z{Z, span_bytes(M, N, ldz, 4)};
+  const Span x{X, span_bytes(M, K, ldx, 4)}, w{W, span_bytes(wr, wc, ldw, 4)};
+  const Span dx{dX, span_bytes(M, K, lddx, 4)}, dw{dW, span_bytes(wr, wc, lddw, 4)};
+  const Span db{dbias, 4 * static_cast<uint64_t>(N)}, wsp{ws, need};
+  if (hits(dx, {dy, z, x, w, dw, db, wsp}) || hits(dw, {dy, z, x, w, db, wsp}) ||
+      hits(db, {dy, z, x, w, wsp}) || hits(wsp, {dy, z, x, w}))
+    return kInvalid;
+  const LinearGradArgs a{M, N, K, dY, lddy, Z, ldz, X, ldx, W, ldw, transpose_w != 0, activation,
+                         dX, lddx, dW, lddw, dbias, scale, variant_of(accum_order)};
+  return status_of(launch_linear_grad(a, ws, stream));
+}
 
 int sgemm_cube_layer_norm(int64_t rows, int64_t cols, int dtype, const void* X, int64_t ldx,
                           const float* weight, const float* bias, float eps, void* Y,

@@ -1,0 +1,173 @@
+// The linear layer and its gradients: workspace, operands and launches.
+#include <algorithm>
+#include <cmath>
+
+#include "layers.h"
+
+namespace sgc {
+namespace {
+
+// One product's planes, carved from a workspace: a_rows x k and b_rows x k.
+struct Carver {
+  char* base;
+  size_t used;
+  template <typename T>
+  T* take(int64_t count) {
+    char* const at = base + used;
+    used += static_cast<size_t>(round_up(count * static_cast<int64_t>(sizeof(T)), 256));
+    return reinterpret_cast<T*>(at);
+  }
+};
+
+Planes carve_planes(Carver& c, int64_t M, int64_t N, int64_t K) {
+  Planes p{};
+  p.Mp = round_up(M, kRowPad);
+  p.Np = round_up(N, kRowPad);
+  p.Kp = round_up(K, kKPad);
+  p.range = c.take<uint32_t>(kFlagBytes / 4);
+  p.a_hi = c.take<uint16_t>(p.Mp * p.Kp);
+  p.a_lo = c.take<uint16_t>(p.Mp * p.Kp);
+  p.b_hi = c.take<uint16_t>(p.Np * p.Kp);
+  p.b_lo = c.take<uint16_t>(p.Np * p.Kp);
+  return p;
+}
+
+SplitJob job_of(const float* s, int64_t ld, int64_t rows, int64_t cols) {
+  SplitJob j{};
+  j.s = s;
+  j.ld = ld;
+  j.rows = rows;
+  j.cols = cols;
+  return j;
+}
+
+// Adds planes to a job: the A or the B side of p, from its rows or its columns.
+void to_planes(SplitJob& j, const Planes& p, bool side_b, bool columns) {
+  uint16_t* const hi = side_b ? p.b_hi : p.a_hi;
+  uint16_t* const lo = side_b ? p.b_lo : p.a_lo;
+  if (columns) {
+    j.col_hi = hi, j.col_lo = lo;
+    if (side_b) j.col_range = p.range, j.col_stamp = next_stamp();
+  } else {
+    j.row_hi = hi, j.row_lo = lo;
+    if (side_b) j.row_range = p.range, j.row_stamp = next_stamp();
+  }
+}
+
+// Target exponents of a pre-scaled operand (api.hip's range_opts): as A, and as
+// B, where the scaled kernels form s B_hi in FP16.
+int target_a(float scale) { return std::min(14, 26 - std::ilogb(scale)); }
+int target_b(float scale, int variant) {
+  return variant == kTermwise || !scaled_kernel_ok(scale) ? target_a(scale)
+                                                          : 14 - std::ilogb(scale);
+}
+
+}  // namespace
+
+size_t linear_ws(int64_t M, int64_t N, int64_t K) {
+  if (M == 0 || N == 0 || K == 0) return 0;
+  Carver c{nullptr, 0};
+  (void)carve_planes(c, M, N, K);
+  (void)c.take<float>(M * N);
+  return c.used;
+}
+
+hipError_t launch_linear(const LinearArgs& a, void* ws, hipStream_t stream) {
+  if (a.K == 0) return launch_epilogue(a.e, a.M, a.N, nullptr, 0, a.y, a.ldy, stream);
+  Carver c{static_cast<char*>(ws), 0};
+  const Planes p = carve_planes(c, a.M, a.N, a.K);
+  float* const product = c.take<float>(a.M * a.N);
+  SplitJob jobs[2] = {job_of(a.x, a.ldx, a.M, a.K),
+                      a.transpose_w ? job_of(a.w, a.ldw, a.N, a.K)
+                                    : job_of(a.w, a.ldw, a.K, a.N)};
+  to_planes(jobs[0], p, false, false);
+  to_planes(jobs[1], p, true, !a.transpose_w);
+  hipError_t err = launch_split_jobs(jobs, 2, a.scale, stream);
+  if (err == hipSuccess)
+    err = launch_gemm(p, a.M, a.N, product, a.N, a.scale, a.variant, stream);
+  if (err != hipSuccess) return err;
+  return launch_epilogue(a.e, a.M, a.N, product, a.N, a.y, a.ldy, stream);
+}
+
+namespace {
+
+struct GradWorkspace {
+  uint32_t* max_bits;
+  float* partial;
+  Planes dx, dw;
+  size_t bytes;
+};
+
+GradWorkspace carve_grad(void* ws, int64_t M, int64_t N, int64_t K, bool transpose_w) {
+  Carver c{static_cast<char*>(ws), 0};
+  GradWorkspace g{};
+  g.max_bits = c.take<uint32_t>(1);
+  const int64_t strips = (N + kColumnStrip - 1) / kColumnStrip;
+  g.partial = c.take<float>(column_slabs(M, N) * (N + strips));
+  g.dx = carve_planes(c, M, K, N);
+  g.dw = transpose_w ? carve_planes(c, N, K, M) : carve_planes(c, K, N, M);
+  g.bytes = c.used;
+  return g;
+}
+
+}  // namespace
+
+size_t linear_grad_ws(int64_t M, int64_t N, int64_t K) {
+  if (M == 0 || N == 0) return 0;
+  return carve_grad(nullptr, M, N, K, false).bytes;
+}
+
+hipError_t launch_linear_grad(const LinearGradArgs& a, void* ws, hipStream_t stream) {
+  hipError_t err = hipSuccess;
+  const int64_t dw_rows = a.transpose_w ? a.N : a.K, dw_cols = a.transpose_w ? a.K : a.N;
+  if (a.M == 0 || a.N == 0) {
+    // No rows: the sums are empty.  No columns: dX = 0.
+    if (a.dx) err = launch_zero(a.M, a.K, a.dx, a.lddx, stream);
+    if (err == hipSuccess && a.dw) err = launch_zero(dw_rows, dw_cols, a.dw, a.lddw, stream);
+    if (err == hipSuccess && a.dbias) err = launch_zero(1, a.N, a.dbias, a.N, stream);
+    return err;
+  }
+  const GradWorkspace g = carve_grad(ws, a.M, a.N, a.K, a.transpose_w);
+  const ColumnArgs cols{a.M, a.N, a.dy, a.lddy, a.z, a.ldz, a.activation, a.dbias, g.max_bits,
+                        g.partial};
+  err = launch_columns(cols, stream);
+  const bool dx = a.dx && a.K > 0, dw = a.dw && a.K > 0;
+  if (err != hipSuccess || (!dx && !dw)) return err;
+
+  SplitJob jobs[kSplitJobs];
+  int count = 0;
+  SplitJob d = job_of(a.dy, a.lddy, a.M, a.N);
+  d.z = a.z, d.ldz = a.ldz, d.activation = a.activation, d.max_bits = g.max_bits;
+  Epilogue ex{}, ew{};
+  ex.max_bits = ew.max_bits = g.max_bits;
+  if (dx) {
+    // dX = D W^T: D's rows and W's K rows, k over N.
+    d.row_target = ex.target = target_a(a.scale);
+    to_planes(d, g.dx, false, false);
+    jobs[count] = a.transpose_w ? job_of(a.w, a.ldw, a.N, a.K) : job_of(a.w, a.ldw, a.K, a.N);
+    to_planes(jobs[count++], g.dx, true, a.transpose_w);
+  }
+  if (dw) {
+    // dW = X^T D (or D^T X): columns of both, k over M.
+    d.col_target = ew.target =
+        a.transpose_w ? target_a(a.scale) : target_b(a.scale, a.variant);
+    to_planes(d, g.dw, !a.transpose_w, true);
+    jobs[count] = job_of(a.x, a.ldx, a.M, a.K);
+    to_planes(jobs[count++], g.dw, a.transpose_w, true);
+  }
+  jobs[count++] = d;
+  err = launch_split_jobs(jobs, count, a.scale, stream);
+  if (err == hipSuccess && dx) {
+    err = launch_gemm(g.dx, a.M, a.K, a.dx, a.lddx, a.scale, a.variant, stream);
+    if (err == hipSuccess)
+      err = launch_epilogue(ex, a.M, a.K, a.dx, a.lddx, a.dx, a.lddx, stream);
+  }
+  if (err == hipSuccess && dw) {
+    err = launch_gemm(g.dw, dw_rows, dw_cols, a.dw, a.lddw, a.scale, a.variant, stream);
+    if (err == hipSuccess)
+      err = launch_epilogue(ew, dw_rows, dw_cols, a.dw, a.lddw, a.dw, a.lddw, stream);
+  }
+  return err;
+}
+
+}  // namespace sgc

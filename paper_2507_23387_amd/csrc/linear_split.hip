@@ -1,0 +1,263 @@
+// What a linear layer's products need around them (gfx950): the split of its
+// operands into planes in either direction, the gradient D = dY act'(Z) with its
+// column sums and largest magnitude, and the epilogue.
+#include <algorithm>
+
+#include "activation.h"
+#include "layers.h"
+
+namespace sgc {
+namespace {
+
+constexpr int kThreads = 256;
+typedef float floatx4_u __attribute__((ext_vector_type(4), aligned(4)));
+
+// Elements (i, j .. j + 7) of a rows x cols matrix, zeros outside it.
+__device__ __forceinline__ void load8(const float* p, int64_t ld, int64_t i, int64_t j,
+                                      int64_t rows, int64_t cols, float (&v)[8]) {
+  const float* const at = p + i * ld + j;
+  if (i < rows && j + 7 < cols) {
+    const floatx4_u a = *reinterpret_cast<const floatx4_u*>(at);
+    const floatx4_u b = *reinterpret_cast<const floatx4_u*>(at + 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = a[e], v[e + 4] = b[e];
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = i < rows && j + e < cols ? at[e] : 0.0f;
+  }
+}
+
+// The jobs of a launch; job b has blocks first[b] .. first[b + 1].
+struct SplitArgs {
+  SplitJob job[kSplitJobs];
+  uint32_t first[kSplitJobs + 1];
+  int count;
+  float s;
+};
+
+constexpr int kTileRows = 32, kTileCols = 128;
+constexpr int kPitch = kTileRows / 2 + 4;  // words per column in LDS; 16-byte aligned
+
+// A 32 x 128 tile of one matrix: thread t holds rows 2 (t / 16) and the next, 8
+// columns from 8 (t % 16).  As row planes those are two 16-byte chunks of a tile
+// row each.  As column planes the pairs of rows go to LDS as words, a column's
+// side by side, and thread t writes chunk t of each of the tile's two slices.
+__device__ void split_tile(const SplitArgs& a, const SplitJob& g, uint32_t block, uint32_t* ph,
+                           uint32_t* pl) {
+  const int t = threadIdx.x;
+  const uint32_t strips = static_cast<uint32_t>((g.cols + kTileCols - 1) / kTileCols);
+  const int64_t tr = block / strips, tc = block - static_cast<uint32_t>(tr) * strips;
+  const int64_t i = tr * kTileRows + 2 * (t >> 4), j = tc * kTileCols + 8 * (t & 15);
+  float v[2][8];
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    load8(g.s, g.ld, i + u, j, g.rows, g.cols, v[u]);
+    if (g.z) {
+      float z[8];
+      load8(g.z, g.ldz, i + u, j, g.rows, g.cols, z);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[u][e] *= activate_grad(g.activation, z[e]);
+    }
+  }
+  const int64_t kp_row = (g.cols + kKPad - 1) / kKPad * kKPad;
+  const int64_t kp_col = (g.rows + kKPad - 1) / kKPad * kKPad;
+  const uint32_t max_bits = g.max_bits ? *g.max_bits : 0;
+  bool big = false;
+  auto too_big = [&](uint32_t h) {
+    typedef _Float16 half2 __attribute__((ext_vector_type(2)));
+    const half2 x = __builtin_bit_cast(half2, h);
+    big |= __builtin_fabsf(static_cast<float>(x[0])) * a.s > 65504.0f;
+    big |= __builtin_fabsf(static_cast<float>(x[1])) * a.s > 65504.0f;
+  };
+  if (g.row_hi && j < kp_row) {
+    const int shift = g.max_bits ? prescale_shift(max_bits, g.row_target) : 0;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      float w[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e] = shift ? __builtin_ldexpf(v[u][e], shift) : v[u][e];
+      u32x4 hv, lv;
+      split8(w, a.s, hv, lv);
+      if (g.row_range) too_big(hv[0]), too_big(hv[1]), too_big(hv[2]), too_big(hv[3]);
+      const int64_t at = tiled_index(i + u, j, kp_row);
+      store_chunk(g.row_hi + at, hv);
+      store_chunk(g.row_lo + at, lv);
+    }
+  }
+  if (g.row_range) {
+    if (big) g.row_range[kWordBOverflow] = g.row_stamp;
+    if (t == 0) g.row_range[kWordBStamp] = g.row_stamp;
+  }
+  if (!g.col_hi) return;
+  big = false;
+  const int shift = g.max_bits ? prescale_shift(max_bits, g.col_target) : 0;
+  const int cl = 8 * (t & 15), rp = t >> 4;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    uint16_t h0, l0, h1, l1;
+    split_value(shift ? __builtin_ldexpf(v[0][e], shift) : v[0][e], a.s, h0, l0);
+    split_value(shift ? __builtin_ldexpf(v[1][e], shift) : v[1][e], a.s, h1, l1);
+    const uint32_t h = static_cast<uint32_t>(h0) | (static_cast<uint32_t>(h1) << 16);
+    if (g.col_range) too_big(h);
+    ph[(cl + e) * kPitch + rp] = h;
+    pl[(cl + e) * kPitch + rp] = static_cast<uint32_t>(l0) | (static_cast<uint32_t>(l1) << 16);
+  }
+  if (g.col_range) {
+    if (big) g.col_range[kWordBOverflow] = g.col_stamp;
+    if (t == 0) g.col_range[kWordBStamp] = g.col_stamp;
+  }
+  __syncthreads();
+  const int r = t >> 1, c = (t & 1) ^ tile_swizzle(r);
+#pragma unroll
+  for (int sl = 0; sl < kTileRows / kSlice; ++sl) {
+    const int64_t at = (tc * (kp_col / kSlice) + tr * (kTileRows / kSlice) + sl) * kTileHalves + t * 8;
+    store_chunk(g.col_hi + at, *reinterpret_cast<const u32x4*>(ph + r * kPitch + sl * 8 + c * 4));
+    store_chunk(g.col_lo + at, *reinterpret_cast<const u32x4*>(pl + r * kPitch + sl * 8 + c * 4));
+  }
+}
+
+__global__ __launch_bounds__(kThreads) void split_jobs_kernel(SplitArgs a) {
+  __shared__ __align__(16) uint32_t ph[kTileCols * kPitch];
+  __shared__ __align__(16) uint32_t pl[kTileCols * kPitch];
+  for (uint32_t b = blockIdx.x; b < a.first[a.count]; b += gridDim.x) {
+    int n = 0;
+    while (n + 1 < a.count && b >= a.first[n + 1]) ++n;
+    split_tile(a, a.job[n], b - a.first[n], ph, pl);
+    __syncthreads();  // the tile's LDS words are read before the next's are written
+  }
+}
+
+// Sums of 128 columns over a slab of rows: thread t has columns 4 (t % 32) .. + 3
+// of every eighth row.
+__global__ __launch_bounds__(kThreads) void columns_kernel(ColumnArgs a, int64_t slab_rows) {
+  __shared__ float part[kThreads / 32][kColumnStrip];
+  __shared__ float top[kThreads / 64];
+  const int t = threadIdx.x;
+  const int64_t j = static_cast<int64_t>(blockIdx.x) * kColumnStrip + 4 * (t & 31);
+  const int64_t i0 = blockIdx.y * slab_rows, i1 = min(a.M, i0 + slab_rows);
+  float s[4] = {0.0f, 0.0f, 0.0f, 0.0f}, m = 0.0f;
+  for (int64_t i = i0 + (t >> 5); i < i1; i += kThreads / 32) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (j + e >= a.N) continue;
+      float d = a.dy[i * a.lddy + j + e];
+      if (a.z) d *= activate_grad(a.activation, a.z[i * a.ldz + j + e]);
+      s[e] += d;
+      const float b = __builtin_fabsf(d);
+      if (b <= 3.4028235e38f) m = __builtin_fmaxf(m, b);
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) part[t >> 5][4 * (t & 31) + e] = s[e];
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, off));
+  if ((t & 63) == 0) top[t >> 6] = m;
+  __syncthreads();
+  float* const out = a.partial + blockIdx.y * (a.N + gridDim.x);
+  const int64_t col = static_cast<int64_t>(blockIdx.x) * kColumnStrip + t;
+  if (t < kColumnStrip && col < a.N) {
+    float sum = 0.0f;
+#pragma unroll
+    for (int g = 0; g < kThreads / 32; ++g) sum += part[g][t];
+    out[col] = sum;
+  }
+  if (t == 0)
+    out[a.N + blockIdx.x] = __builtin_fmaxf(__builtin_fmaxf(top[0], top[1]),
+                                            __builtin_fmaxf(top[2], top[3]));
+}
+
+// Joins the slabs: blocks 0 .. strips - 1 a strip of columns each, the last the
+// magnitudes.
+__global__ __launch_bounds__(kThreads) void columns_join_kernel(ColumnArgs a, int64_t slabs,
+                                                                int64_t strips) {
+  const int t = threadIdx.x;
+  const int64_t pitch = a.N + strips;
+  if (blockIdx.x < gridDim.x - 1) {
+    const int64_t j = static_cast<int64_t>(blockIdx.x) * kThreads + t;
+    if (j >= a.N || !a.dbias) return;
+    float s = 0.0f;
+    for (int64_t g = 0; g < slabs; ++g) s += a.partial[g * pitch + j];
+    a.dbias[j] = s;
+    return;
+  }
+  __shared__ float top[kThreads / 64];
+  float m = 0.0f;
+  for (int64_t n = t; n < slabs * strips; n += kThreads)
+    m = __builtin_fmaxf(m, a.partial[n / strips * pitch + a.N + n % strips]);
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, off));
+  if ((t & 63) == 0) top[t >> 6] = m;
+  __syncthreads();
+  if (t == 0)
+    *a.max_bits = __builtin_bit_cast(uint32_t, __builtin_fmaxf(__builtin_fmaxf(top[0], top[1]),
+                                                               __builtin_fmaxf(top[2], top[3])));
+}
+
+// Y from the product P (null: zeros), which may be Y.
+__global__ __launch_bounds__(kThreads) void epilogue_kernel(Epilogue e, int64_t M, int64_t N,
+                                                            const float* P, int64_t ldp, float* Y,
+                                                            int64_t ldy) {
+  const int64_t j = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
+  if (j >= N) return;
+  const int shift = e.max_bits ? prescale_shift(*e.max_bits, e.target) : 0;
+  for (int64_t i = blockIdx.y; i < M; i += gridDim.y) {
+    float z = P ? P[i * ldp + j] : 0.0f;
+    if (e.max_bits) z = __builtin_ldexpf(z, -shift);
+    if (e.bias) z += e.bias[j];
+    if (e.z) e.z[i * e.ldz + j] = z;
+    float y = activate(e.activation, z);
+    if (e.r) y += e.r[i * e.ldr + j];
+    Y[i * ldy + j] = y;
+  }
+}
+
+}  // namespace
+
+hipError_t launch_split_jobs(const SplitJob* jobs, int count, float scale, hipStream_t stream) {
+  SplitArgs a{};
+  a.s = scale;
+  a.count = count;
+  int64_t blocks = 0;
+  for (int n = 0; n < count; ++n) {
+    a.job[n] = jobs[n];
+    a.first[n] = static_cast<uint32_t>(blocks);
+    // Rows up to a multiple of 64: the padding of k in column planes.
+    blocks += round_up(jobs[n].rows, kKPad) / kTileRows *
+              ((jobs[n].cols + kTileCols - 1) / kTileCols);
+    if (blocks > UINT32_MAX) return hipErrorInvalidValue;
+  }
+  a.first[count] = static_cast<uint32_t>(blocks);
+  if (blocks == 0) return hipSuccess;
+  const dim3 grid(static_cast<unsigned>(std::min<int64_t>(blocks, int64_t{1} << 22)));
+  hipLaunchKernelGGL(split_jobs_kernel, grid, dim3(kThreads), 0, stream, a);
+  return hipGetLastError();
+}
+
+int64_t column_slabs(int64_t M, int64_t N) {
+  const int64_t strips = (N + kColumnStrip - 1) / kColumnStrip;
+  return std::max<int64_t>(1, std::min<int64_t>((M + 31) / 32, 1024 / strips));
+}
+
+hipError_t launch_columns(const ColumnArgs& a, hipStream_t stream) {
+  const int64_t strips = (a.N + kColumnStrip - 1) / kColumnStrip;
+  const int64_t slabs = column_slabs(a.M, a.N);
+  hipLaunchKernelGGL(columns_kernel, dim3(static_cast<unsigned>(strips), static_cast<unsigned>(slabs)),
+                     dim3(kThreads), 0, stream, a, (a.M + slabs - 1) / slabs);
+  if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  hipLaunchKernelGGL(columns_join_kernel,
+                     dim3(static_cast<unsigned>((a.N + kThreads - 1) / kThreads + 1)),
+                     dim3(kThreads), 0, stream, a, slabs, strips);
+  return hipGetLastError();
+}
+
+hipError_t launch_epilogue(const Epilogue& e, int64_t M, int64_t N, const float* P, int64_t ldp,
+                           float* Y, int64_t ldy, hipStream_t stream) {
+  if (M <= 0 || N <= 0) return hipSuccess;
+  const dim3 grid(static_cast<unsigned>((N + kThreads - 1) / kThreads),
+                  static_cast<unsigned>(std::min<int64_t>(M, 65535)));
+  hipLaunchKernelGGL(epilogue_kernel, grid, dim3(kThreads), 0, stream, e, M, N, P, ldp, Y,
+                     ldy);
+  return hipGetLastError();
+}
+
+}  // namespace sgc

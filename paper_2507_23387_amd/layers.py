@@ -10,7 +10,7 @@ from __future__ import annotations
 import torch
 
 from . import binding
-from .binding import _check, _stream
+from .binding import _check, _order, _stream
 
 _DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
@@ -48,6 +48,81 @@ def _vector(t, name, n):
 
 def _bytes(n, device):
     return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+
+
+def _weight_shape(W, transpose_w):
+    """(K, N) of a weight stored as K x N, or as N x K."""
+    if W.dim() != 2:
+        raise ValueError("W must be 2-D")
+    return (W.size(1), W.size(0)) if transpose_w else (W.size(0), W.size(1))
+
+
+def _activation(name) -> int:
+    if name not in binding.ACTIVATIONS:
+        raise ValueError(f"activation must be one of {', '.join(binding.ACTIVATIONS)}")
+    return binding.ACTIVATIONS[name]
+
+
+def linear(X, W, bias=None, residual=None, activation: str = "none", transpose_w: bool = False,
+           keep_preact: bool = False, scale: float = 2.0**11, order="elementwise", out=None,
+           workspace=None):
+    """act(X W + bias) + residual at the accuracy of an FP32 product, the sums and
+    the epilogue in one pass.  X is M x K, W K x N, or N x K with transpose_w=True.
+    activation: none, relu, gelu, gelu_tanh or silu.  With keep_preact=True returns
+    (Y, Z), Z = X W + bias, which linear_backward needs of a layer with an
+    activation.  residual may be out.  workspace: a byte tensor of
+    sgemm_cube_linear_workspace_size bytes that a program keeps between calls."""
+    px, ldx = _matrix(X, "X")
+    pw, ldw = _matrix(W, "W")
+    M, K = X.shape
+    K2, N = _weight_shape(W, transpose_w)
+    if K != K2:
+        raise ValueError(f"shape mismatch: X has {K} columns, W takes {K2}")
+    pb = _vector(bias, "bias", N)
+    pr, ldr = (None, N) if residual is None else _matrix(residual, "residual", (M, N))
+    Y = out if out is not None else torch.empty((M, N), dtype=torch.float32, device=X.device)
+    py, ldy = _matrix(Y, "out", (M, N))
+    Z = torch.empty((M, N), dtype=torch.float32, device=X.device) if keep_preact else None
+    pz, ldz = _matrix(Z, "Z") if keep_preact else (None, N)
+    ws = workspace if workspace is not None else _bytes(
+        binding.sgemm_cube_linear_workspace_size(M, N, K), X.device)
+    _check(binding.sgemm_cube_linear(
+        M, N, K, px, ldx, pw, ldw, int(transpose_w), pb, _activation(activation), pr, ldr, py, ldy,
+        pz, ldz, scale, _order(order), ws.data_ptr(), ws.numel() * ws.element_size(), _stream()),
+        "sgemm_cube_linear")
+    return (Y, Z) if keep_preact else Y
+
+
+def linear_backward(dY, X, W, preact=None, activation: str = "none", transpose_w: bool = False,
+                    need=("dX", "dW", "db"), scale: float = 2.0**11, order="elementwise",
+                    workspace=None):
+    """(dX, dW, db) of linear at X and W from its output's gradient; preact: the Z
+    that it kept, if it has an activation.  dW has W's layout.  What `need` leaves
+    out is None.  (The residual's gradient is dY.)"""
+    pdy, lddy = _matrix(dY, "dY")
+    px, ldx = _matrix(X, "X")
+    pw, ldw = _matrix(W, "W")
+    M, K = X.shape
+    K2, N = _weight_shape(W, transpose_w)
+    if K != K2 or dY.shape != (M, N):
+        raise ValueError(f"shape mismatch: dY {tuple(dY.shape)}, X {tuple(X.shape)}, "
+                         f"W for {K2} x {N}")
+    if activation != "none" and preact is None:
+        raise ValueError(f"{activation} needs preact, what linear returned with keep_preact=True")
+    if not set(need) <= {"dX", "dW", "db"}:
+        raise ValueError("need may hold dX, dW and db")
+    pz, ldz = (None, N) if activation == "none" else _matrix(preact, "preact", (M, N))
+    new = lambda name, *shape: torch.empty(  # noqa: E731
+        shape, dtype=torch.float32, device=X.device) if name in need else None
+    dX, dW, db = new("dX", M, K), new("dW", *W.shape), new("db", N)
+    at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    ws = workspace if workspace is not None else _bytes(
+        binding.sgemm_cube_linear_backward_workspace_size(M, N, K), X.device)
+    _check(binding.sgemm_cube_linear_backward(
+        M, N, K, pdy, lddy, pz, ldz, px, ldx, pw, ldw, int(transpose_w), _activation(activation),
+        at(dX), max(K, 1), at(dW), max(W.size(1), 1), at(db), scale, _order(order), ws.data_ptr(),
+        ws.numel() * ws.element_size(), _stream()), "sgemm_cube_linear_backward")
+    return dX, dW, db
 
 
 def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, keep_stats: bool = False, out=None):

@@ -118,3 +118,51 @@ def test_adamw_values_validation(lib):
                dict(count=-1), dict(tensors=-1)):
         assert call(**kw) == INVALID, kw
     assert call(count=0) == 0 and call(tensors=0) == 0
+
+
+def test_linear_validation(lib):
+    X, W, B, R, Y, Z, WS = (FAKE + i * GIB for i in range(7))
+    need = lib.sgemm_cube_linear_workspace_size(4, 6, 8)
+    assert need > 0 and need % 256 == 0
+    assert lib.sgemm_cube_linear_workspace_size(0, 6, 8) == 0
+    assert lib.sgemm_cube_linear_workspace_size(4, -6, 8) == 0
+
+    def call(M=4, N=6, K=8, X=X, ldx=8, W=W, ldw=None, t=0, B=B, act=2, R=R, ldr=6, Y=Y, ldy=6,
+             Z=Z, ldz=6, scale=2048.0, order=0, WS=WS, n=need):
+        ldw = max(K if t else N, 1) if ldw is None else ldw
+        return lib.sgemm_cube_linear(M, N, K, X, ldx, W, ldw, t, B, act, R, ldr, Y, ldy, Z, ldz,
+                                     scale, order, WS, n, 0)
+
+    for kw in (dict(M=-1), dict(N=-1), dict(K=-1), dict(ldx=7), dict(ldw=5), dict(t=1, ldw=7),
+               dict(ldr=5), dict(ldy=5), dict(ldz=5), dict(X=None), dict(W=None), dict(Y=None),
+               dict(X=X + 2), dict(B=B + 1), dict(R=R + 2), dict(Z=Z + 2), dict(act=5),
+               dict(act=-1), dict(scale=3.0), dict(order=3), dict(Y=X), dict(Y=W), dict(Y=B),
+               dict(Y=R + 24), dict(R=Y, ldr=7), dict(Z=Y), dict(Z=R), dict(Z=X), dict(WS=None),
+               dict(WS=WS + 8), dict(n=need - 1), dict(WS=X), dict(WS=Y), dict(Z=WS),
+               dict(M=1 << 29, ldx=1 << 40)):
+        assert call(**kw) == INVALID, kw
+    assert call(K=(1 << 30) + 1, ldx=1 << 31, W=FAKE << 3) == NOT_SUPPORTED
+    assert call(M=0) == 0 and call(N=0) == 0 and call(M=0, X=None, Y=None, R=None, Z=None) == 0
+
+
+def test_linear_backward_validation(lib):
+    DY, Z, X, W, DX, DW, DB, WS = (FAKE + i * GIB for i in range(8))
+    need = lib.sgemm_cube_linear_backward_workspace_size(4, 6, 8)
+    assert need > 0 and need % 256 == 0
+    assert lib.sgemm_cube_linear_backward_workspace_size(4, 6, -1) == 0
+
+    def call(M=4, N=6, K=8, DY=DY, lddy=6, Z=Z, ldz=6, X=X, ldx=8, W=W, ldw=None, t=0, act=2,
+             DX=DX, lddx=8, DW=DW, lddw=None, DB=DB, scale=2048.0, order=1, WS=WS, n=need):
+        ldw = max(K if t else N, 1) if ldw is None else ldw
+        lddw = max(K if t else N, 1) if lddw is None else lddw
+        return lib.sgemm_cube_linear_backward(M, N, K, DY, lddy, Z, ldz, X, ldx, W, ldw, t, act,
+                                              DX, lddx, DW, lddw, DB, scale, order, WS, n, 0)
+
+    for kw in (dict(M=-1), dict(lddy=5), dict(ldz=5), dict(ldx=7), dict(ldw=5), dict(t=1, lddw=7),
+               dict(lddx=7), dict(DY=None), dict(Z=None), dict(X=None), dict(W=None),
+               dict(DY=DY + 2), dict(DB=DB + 3), dict(act=5), dict(scale=0.0), dict(order=-1),
+               dict(DX=DY), dict(DX=X), dict(DW=W), dict(DW=DX), dict(DB=DW), dict(DB=Z),
+               dict(WS=None), dict(n=need - 1), dict(WS=WS + 16), dict(WS=DY), dict(DX=WS)):
+        assert call(**kw) == INVALID, kw
+    assert call(M=(1 << 30) + 1, DY=FAKE << 1, Z=FAKE << 2, X=FAKE << 3,
+                DX=FAKE << 4) == NOT_SUPPORTED
