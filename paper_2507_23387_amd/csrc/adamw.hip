@@ -6,6 +6,7 @@
 // blocks of 256 values, a wave to a block: four values a lane, the block's
 // largest by a reduction over the wave.
 #include <algorithm>
+#include <type_traits>
 
 #include "layers.h"
 
@@ -57,10 +58,30 @@ __device__ __forceinline__ int entry_of(const Args& a, uint32_t c) {
   return lo;
 }
 
-__device__ __forceinline__ float grad_of(const void* g, int64_t i, int dtype) {
-  if (dtype == kF32) return static_cast<const float*>(g)[i];
-  if (dtype == kF16) return static_cast<float>(static_cast<const _Float16*>(g)[i]);
-  return static_cast<float>(static_cast<const __bf16*>(g)[i]);
+// A lane's four values of an array, at any address that its elements have.
+template <typename T>
+using Four = T __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+
+template <typename T>
+__device__ __forceinline__ Four<T> load4(const void* p, int64_t i, int64_t count) {
+  const T* const at = static_cast<const T*>(p) + i;
+  if (i + 3 < count) return *reinterpret_cast<const Four<T>*>(at);
+  Four<T> v;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) v[k] = i + k < count ? at[k] : static_cast<T>(0);
+  return v;
+}
+
+template <typename T>
+__device__ __forceinline__ void store4(void* p, int64_t i, int64_t count, Four<T> v) {
+  T* const at = static_cast<T*>(p) + i;
+  if (i + 3 < count) {
+    *reinterpret_cast<Four<T>*>(at) = v;
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (i + k < count) at[k] = v[k];
 }
 
 // Largest of the wave's values, as bits (non-negative floats, infinities and
@@ -105,77 +126,100 @@ __device__ __forceinline__ uint8_t encode_v(float v, float s) {
   return static_cast<uint8_t>(v > 0.0f && c < 1.0f ? 1.0f : c);
 }
 
-template <int kBits>
-__device__ __forceinline__ void adamw_block(const Entry& e, const AdamwHyper& h, int grad_dtype,
-                                            int64_t block) {
-  const int64_t i0 = block * kWaveValues + (threadIdx.x & 63) * 4;
-  float m[4], v[4];
-  float ms = 0.0f, vs = 0.0f;
-  if constexpr (kBits == 8) ms = e.ms[block], vs = e.vs[block];
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const int64_t i = i0 + k;
-    m[k] = v[k] = 0.0f;
-    if (i >= e.count) continue;
-    const float g = grad_of(e.g, i, grad_dtype) * h.grad_scale;
-    float m0, v0;
-    if constexpr (kBits == 8) {
-      m0 = decode_m(static_cast<const int8_t*>(e.m)[i], ms);
-      v0 = decode_v(static_cast<const uint8_t*>(e.v)[i], vs);
-    } else {
-      m0 = static_cast<const float*>(e.m)[i];
-      v0 = static_cast<const float*>(e.v)[i];
-    }
-    m[k] = h.beta1 * m0 + h.rest1 * g;
-    v[k] = h.beta2 * v0 + h.rest2 * (g * g);
-    const float u = m[k] / (__builtin_sqrtf(v[k]) * h.root + h.eps);
-    e.p[i] = e.p[i] * e.keep - h.step_size * u;
-    if constexpr (kBits == 32) {
-      static_cast<float*>(e.m)[i] = m[k];
-      static_cast<float*>(e.v)[i] = v[k];
-    }
+// What a lane reads of a block: four values of each array, states as they lie.
+template <int kBits, typename G>
+struct Loaded {
+  typedef typename std::conditional<kBits == 8, int8_t, float>::type M;
+  typedef typename std::conditional<kBits == 8, uint8_t, float>::type V;
+  Four<float> p;
+  Four<G> g;
+  Four<M> m;
+  Four<V> v;
+  float ms, vs;
+
+  __device__ __forceinline__ void read(const Entry& e, int64_t block) {
+    const int64_t i = block * kWaveValues + (threadIdx.x & 63) * 4;
+    p = load4<float>(e.p, i, e.count);
+    g = load4<G>(e.g, i, e.count);
+    m = load4<M>(e.m, i, e.count);
+    v = load4<V>(e.v, i, e.count);
+    if constexpr (kBits == 8) ms = e.ms[block], vs = e.vs[block];
   }
-  if constexpr (kBits == 8) {
-    ms = wave_max(largest4(m));
-    vs = wave_max(largest4(v));
-    if ((threadIdx.x & 63) == 0) e.ms[block] = ms, e.vs[block] = vs;
+
+  // The step, and what it writes.  Values past the tensor's end read as zeros,
+  // which a block's largest does not see.
+  __device__ __forceinline__ void step(const Entry& e, const AdamwHyper& h, int64_t block) {
+    const int64_t i = block * kWaveValues + (threadIdx.x & 63) * 4;
+    float m1[4], v1[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      if (i0 + k >= e.count) continue;
-      static_cast<int8_t*>(e.m)[i0 + k] = encode_m(m[k], ms);
-      static_cast<uint8_t*>(e.v)[i0 + k] = encode_v(v[k], vs);
+      const float gk = static_cast<float>(g[k]) * h.grad_scale;
+      float m0, v0;
+      if constexpr (kBits == 8) m0 = decode_m(m[k], ms), v0 = decode_v(v[k], vs);
+      else m0 = m[k], v0 = v[k];
+      m1[k] = h.beta1 * m0 + h.rest1 * gk;
+      v1[k] = h.beta2 * v0 + h.rest2 * (gk * gk);
+      const float u = m1[k] / (__builtin_sqrtf(v1[k]) * h.root + h.eps);
+      p[k] = p[k] * e.keep - h.step_size * u;
     }
+    store4<float>(e.p, i, e.count, p);
+    if constexpr (kBits == 8) {
+      ms = wave_max(largest4(m1));
+      vs = wave_max(largest4(v1));
+      if ((threadIdx.x & 63) == 0) e.ms[block] = ms, e.vs[block] = vs;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) m[k] = encode_m(m1[k], ms), v[k] = encode_v(v1[k], vs);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) m[k] = m1[k], v[k] = v1[k];
+    }
+    store4<M>(e.m, i, e.count, m);
+    store4<V>(e.v, i, e.count, v);
   }
+};
+
+// This wave's blocks of its workgroup's chunk: the first, and how many there are.
+__device__ __forceinline__ int wave_blocks(const Entry& e, int64_t& first) {
+  first = (static_cast<int64_t>(blockIdx.x - e.first) * (kThreads / 64) + (threadIdx.x >> 6)) *
+          kWaveBlocks;
+  const int64_t left = (e.count + kWaveValues - 1) / kWaveValues - first;
+  return static_cast<int>(min<int64_t>(max<int64_t>(left, 0), kWaveBlocks));
 }
 
-// f(block) for each block of this wave's part of a workgroup's chunk.
-template <typename F>
-__device__ __forceinline__ void each_block(const Entry& e, F f) {
-  const int64_t b0 = (static_cast<int64_t>(blockIdx.x - e.first) * (kThreads / 64) +
-                      (threadIdx.x >> 6)) * kWaveBlocks;
-  for (int64_t b = b0; b < b0 + kWaveBlocks && b * kWaveValues < e.count; ++b) f(b);
-}
-
-template <int kBits>
-__global__ __launch_bounds__(kThreads) void adamw_kernel(Args a, int grad_dtype) {
+// A wave reads two blocks before it steps either.
+template <int kBits, typename G>
+__global__ __launch_bounds__(kThreads) void adamw_kernel(Args a) {
   const Entry& e = a.e[entry_of(a, blockIdx.x)];
-  each_block(e, [&](int64_t b) { adamw_block<kBits>(e, a.h, grad_dtype, b); });
+  int64_t first;
+  const int blocks = wave_blocks(e, first);
+  for (int b = 0; b < blocks; b += 2) {
+    Loaded<kBits, G> x, y;
+    x.read(e, first + b);
+    if (b + 1 < blocks) y.read(e, first + b + 1);
+    x.step(e, a.h, first + b);
+    if (b + 1 < blocks) y.step(e, a.h, first + b + 1);
+  }
 }
 
 // What 8-bit states stand for, written where an entry's p and g point.
 __global__ __launch_bounds__(kThreads) void values_kernel(Args a) {
   const Entry& e = a.e[entry_of(a, blockIdx.x)];
-  float* const vo = static_cast<float*>(const_cast<void*>(e.g));
-  each_block(e, [&](int64_t b) {
-    const float ms = e.ms[b], vs = e.vs[b];
-    const int64_t i0 = b * kWaveValues + (threadIdx.x & 63) * 4;
+  void* const out = const_cast<void*>(e.g);
+  int64_t first;
+  const int blocks = wave_blocks(e, first);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      if (i0 + k >= e.count) continue;
-      e.p[i0 + k] = decode_m(static_cast<const int8_t*>(e.m)[i0 + k], ms);
-      vo[i0 + k] = decode_v(static_cast<const uint8_t*>(e.v)[i0 + k], vs);
-    }
-  });
+  for (int b = 0; b < kWaveBlocks; ++b) {
+    if (b >= blocks) break;
+    const int64_t i = (first + b) * kWaveValues + (threadIdx.x & 63) * 4;
+    const Four<int8_t> m = load4<int8_t>(e.m, i, e.count);
+    const Four<uint8_t> v = load4<uint8_t>(e.v, i, e.count);
+    const float ms = e.ms[first + b], vs = e.vs[first + b];
+    Four<float> mo, vo;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) mo[k] = decode_m(m[k], ms), vo[k] = decode_v(v[k], vs);
+    store4<float>(e.p, i, e.count, mo);
+    store4<float>(out, i, e.count, vo);
+  }
 }
 
 // Packs the tensors into as few launches as their entries and chunks allow.
@@ -223,10 +267,18 @@ hipError_t launch_adamw(int64_t tensors, const sgemm_cube_adamw_tensor_t* list, 
         e.keep = static_cast<float>(1.0 - lr * list[i].weight_decay);
       },
       [&](dim3 grid) {
-        if (state_bits == 8)
-          hipLaunchKernelGGL(adamw_kernel<8>, grid, dim3(kThreads), 0, stream, a, grad_dtype);
-        else
-          hipLaunchKernelGGL(adamw_kernel<32>, grid, dim3(kThreads), 0, stream, a, grad_dtype);
+        auto launch = [&](auto kernel) {
+          hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, stream, a);
+        };
+        if (state_bits == 8) {
+          if (grad_dtype == kF32) launch(adamw_kernel<8, float>);
+          else if (grad_dtype == kF16) launch(adamw_kernel<8, _Float16>);
+          else launch(adamw_kernel<8, __bf16>);
+        } else {
+          if (grad_dtype == kF32) launch(adamw_kernel<32, float>);
+          else if (grad_dtype == kF16) launch(adamw_kernel<32, _Float16>);
+          else launch(adamw_kernel<32, __bf16>);
+        }
       });
 }
 

@@ -10,44 +10,57 @@ from __future__ import annotations
 import torch
 
 from . import binding
-from .binding import _check, _order, _stream
+from .binding import _check, _order
 
 _DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
 
 
-def _tensor(t, name, dtype, device=None):
+_F32 = (torch.float32,)
+_current_device = torch.cuda.current_device
+# The current stream's handle, without the Stream object that wraps it (2.8 us a
+# call, of the 10 to 17 that a small layer takes).
+_stream = torch._C._cuda_getCurrentRawStream
+
+
+def _refuse(t, name, dtype):
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype not in dtype:
         raise TypeError(f"{name} must be a CUDA/HIP tensor of type "
                         + " or ".join(str(d).removeprefix("torch.") for d in dtype))
-    if t.get_device() != (torch.cuda.current_device() if device is None else device):
-        raise ValueError(f"{name} must be on the current device, with the other operands")
-    return t
+    raise ValueError(f"{name} must be on the current device, with the other operands")
 
 
-def _matrix(t, name, shape=None, dtype=(torch.float32,)):
+def _matrix(t, name, device, shape=None, dtype=_F32):
     """(address, leading dimension) of a 2-D tensor whose columns are adjacent."""
-    _tensor(t, name, dtype)
-    if t.dim() != 2 or (shape is not None and t.shape != shape):
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtype or t.get_device() != device:
+        _refuse(t, name, dtype)
+    got = t.shape
+    if len(got) != 2 or (shape is not None and got != shape):
         raise ValueError(f"{name} must be 2-D" if shape is None else
-                         f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
-    rows, cols = t.shape
-    if (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) < cols):
+                         f"{name} must have the shape {tuple(shape)}, not {tuple(got)}")
+    rows, cols = got
+    ld, step = t.stride()
+    if (cols > 1 and step != 1) or (rows > 1 and ld < cols):
         raise ValueError(f"{name} must be row-major: unit column stride, rows apart")
-    return t.data_ptr(), max(t.stride(0) if rows > 1 else cols, 1)
+    return t.data_ptr(), max(ld if rows > 1 else cols, 1)
 
 
-def _vector(t, name, n):
+def _vector(t, name, device, n):
     """Address of a contiguous FP32 vector of n values, or None."""
     if t is None:
         return None
-    _tensor(t, name, (torch.float32,))
-    if t.dim() != 1 or t.numel() != n or (n > 1 and t.stride(0) != 1):
+    if not isinstance(t, torch.Tensor) or t.dtype not in _F32 or t.get_device() != device:
+        _refuse(t, name, _F32)
+    if t.shape != (n,) or (n > 1 and t.stride(0) != 1):
         raise ValueError(f"{name} must be a contiguous vector of {n} values")
     return t.data_ptr()
 
 
-def _bytes(n, device):
-    return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+def _new(shape, like, dtype=torch.float32):
+    return like.new_empty(shape, dtype=dtype)
+
+
+def _bytes(n, like):
+    return like.new_empty((max(n, 256),), dtype=torch.uint8)
 
 
 def _weight_shape(W, transpose_w):
@@ -72,24 +85,28 @@ def linear(X, W, bias=None, residual=None, activation: str = "none", transpose_w
     (Y, Z), Z = X W + bias, which linear_backward needs of a layer with an
     activation.  residual may be out.  workspace: a byte tensor of
     sgemm_cube_linear_workspace_size bytes that a program keeps between calls."""
-    px, ldx = _matrix(X, "X")
-    pw, ldw = _matrix(W, "W")
+    device = _current_device()
+    px, ldx = _matrix(X, "X", device)
+    pw, ldw = _matrix(W, "W", device)
     M, K = X.shape
     K2, N = _weight_shape(W, transpose_w)
     if K != K2:
         raise ValueError(f"shape mismatch: X has {K} columns, W takes {K2}")
-    pb = _vector(bias, "bias", N)
-    pr, ldr = (None, N) if residual is None else _matrix(residual, "residual", (M, N))
-    Y = out if out is not None else torch.empty((M, N), dtype=torch.float32, device=X.device)
-    py, ldy = _matrix(Y, "out", (M, N))
-    Z = torch.empty((M, N), dtype=torch.float32, device=X.device) if keep_preact else None
-    pz, ldz = _matrix(Z, "Z") if keep_preact else (None, N)
+    pb = _vector(bias, "bias", device, N)
+    pr, ldr = (None, N) if residual is None else _matrix(residual, "residual", device, (M, N))
+    if out is None:
+        Y = _new((M, N), X)
+        py, ldy = Y.data_ptr(), max(N, 1)
+    else:
+        Y = out
+        py, ldy = _matrix(Y, "out", device, (M, N))
+    Z = _new((M, N), X) if keep_preact else None
     ws = workspace if workspace is not None else _bytes(
-        binding.sgemm_cube_linear_workspace_size(M, N, K), X.device)
+        binding.sgemm_cube_linear_workspace_size(M, N, K), X)
     _check(binding.sgemm_cube_linear(
         M, N, K, px, ldx, pw, ldw, int(transpose_w), pb, _activation(activation), pr, ldr, py, ldy,
-        pz, ldz, scale, _order(order), ws.data_ptr(), ws.numel() * ws.element_size(), _stream()),
-        "sgemm_cube_linear")
+        Z.data_ptr() if keep_preact else None, max(N, 1), scale, _order(order), ws.data_ptr(),
+        ws.numel() * ws.element_size(), _stream(device)), "sgemm_cube_linear")
     return (Y, Z) if keep_preact else Y
 
 
@@ -99,9 +116,10 @@ def linear_backward(dY, X, W, preact=None, activation: str = "none", transpose_w
     """(dX, dW, db) of linear at X and W from its output's gradient; preact: the Z
     that it kept, if it has an activation.  dW has W's layout.  What `need` leaves
     out is None.  (The residual's gradient is dY.)"""
-    pdy, lddy = _matrix(dY, "dY")
-    px, ldx = _matrix(X, "X")
-    pw, ldw = _matrix(W, "W")
+    device = _current_device()
+    pdy, lddy = _matrix(dY, "dY", device)
+    px, ldx = _matrix(X, "X", device)
+    pw, ldw = _matrix(W, "W", device)
     M, K = X.shape
     K2, N = _weight_shape(W, transpose_w)
     if K != K2 or dY.shape != (M, N):
@@ -111,17 +129,17 @@ def linear_backward(dY, X, W, preact=None, activation: str = "none", transpose_w
         raise ValueError(f"{activation} needs preact, what linear returned with keep_preact=True")
     if not set(need) <= {"dX", "dW", "db"}:
         raise ValueError("need may hold dX, dW and db")
-    pz, ldz = (None, N) if activation == "none" else _matrix(preact, "preact", (M, N))
-    new = lambda name, *shape: torch.empty(  # noqa: E731
-        shape, dtype=torch.float32, device=X.device) if name in need else None
+    pz, ldz = (None, N) if activation == "none" else _matrix(preact, "preact", device,
+                                                                 (M, N))
+    new = lambda name, *shape: _new(shape, X) if name in need else None  # noqa: E731
     dX, dW, db = new("dX", M, K), new("dW", *W.shape), new("db", N)
     at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
     ws = workspace if workspace is not None else _bytes(
-        binding.sgemm_cube_linear_backward_workspace_size(M, N, K), X.device)
+        binding.sgemm_cube_linear_backward_workspace_size(M, N, K), X)
     _check(binding.sgemm_cube_linear_backward(
         M, N, K, pdy, lddy, pz, ldz, px, ldx, pw, ldw, int(transpose_w), _activation(activation),
         at(dX), max(K, 1), at(dW), max(W.size(1), 1), at(db), scale, _order(order), ws.data_ptr(),
-        ws.numel() * ws.element_size(), _stream()), "sgemm_cube_linear_backward")
+        ws.numel() * ws.element_size(), _stream(device)), "sgemm_cube_linear_backward")
     return dX, dW, db
 
 
@@ -129,42 +147,48 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, keep_stats: bool = 
     """Layer norm of the rows of x (float32, float16 or bfloat16), rounded once to
     x's type; weight and bias are float32.  With keep_stats=True returns
     (y, mean, rstd), what layer_norm_backward needs.  out may be x."""
-    px, ldx = _matrix(x, "x", dtype=_DTYPES)
+    device = _current_device()
+    px, ldx = _matrix(x, "x", device, dtype=_DTYPES)
     rows, cols = x.shape
-    pw, pb = _vector(weight, "weight", cols), _vector(bias, "bias", cols)
-    y = out if out is not None else torch.empty((rows, cols), dtype=x.dtype, device=x.device)
-    py, ldy = _matrix(y, "out", x.shape, (x.dtype,))
-    mean = rstd = None
-    if keep_stats:
-        mean, rstd = torch.empty((2, rows), dtype=torch.float32, device=x.device)
+    pw, pb = _vector(weight, "weight", device, cols), _vector(bias, "bias", device, cols)
+    if out is None:
+        y = _new((rows, cols), x, x.dtype)
+        py, ldy = y.data_ptr(), max(cols, 1)
+    else:
+        y = out
+        py, ldy = _matrix(y, "out", device, x.shape, (x.dtype,))
+    mean, rstd = _new((2, rows), x) if keep_stats else (None, None)
     _check(binding.sgemm_cube_layer_norm(
         rows, cols, _DTYPES[x.dtype], px, ldx, pw, pb, eps, py, ldy,
         mean.data_ptr() if keep_stats else None, rstd.data_ptr() if keep_stats else None,
-        _stream()), "sgemm_cube_layer_norm")
+        _stream(device)), "sgemm_cube_layer_norm")
     return (y, mean, rstd) if keep_stats else y
 
 
 def layer_norm_backward(dy, x, weight, mean, rstd, out=None):
     """(dx, dweight, dbias) of layer_norm at x, with the mean and rstd that it
     kept.  out may be dy; dweight and dbias are float32."""
-    px, ldx = _matrix(x, "x", dtype=_DTYPES)
+    device = _current_device()
+    px, ldx = _matrix(x, "x", device, dtype=_DTYPES)
     rows, cols = x.shape
-    pdy, lddy = _matrix(dy, "dy", x.shape, (x.dtype,))
-    pw = _vector(weight, "weight", cols)
-    pm, pr = _vector(mean, "mean", rows), _vector(rstd, "rstd", rows)
-    dx = out if out is not None else torch.empty((rows, cols), dtype=x.dtype, device=x.device)
-    pdx, lddx = _matrix(dx, "out", x.shape, (x.dtype,))
-    dw, db = torch.empty((2, cols), dtype=torch.float32, device=x.device)
-    ws = _bytes(binding.sgemm_cube_layer_norm_backward_workspace_size(rows, cols), x.device)
+    pdy, lddy = _matrix(dy, "dy", device, x.shape, (x.dtype,))
+    pw = _vector(weight, "weight", device, cols)
+    pm, pr = _vector(mean, "mean", device, rows), _vector(rstd, "rstd", device, rows)
+    dx = out if out is not None else _new((rows, cols), x, x.dtype)
+    pdx, lddx = _matrix(dx, "out", device, x.shape, (x.dtype,))
+    dw, db = _new((2, cols), x)
+    ws = _bytes(binding.sgemm_cube_layer_norm_backward_workspace_size(rows, cols), x)
     _check(binding.sgemm_cube_layer_norm_backward(
         rows, cols, _DTYPES[x.dtype], pdy, lddy, px, ldx, pw, pm, pr, pdx, lddx, dw.data_ptr(),
-        db.data_ptr(), ws.data_ptr(), ws.numel(), _stream()), "sgemm_cube_layer_norm_backward")
+        db.data_ptr(), ws.data_ptr(), ws.numel(), _stream(device)),
+        "sgemm_cube_layer_norm_backward")
     return dx, dw, db
 
 
-def _flat(t, name, n, dtype):
+def _flat(t, name, device, n, dtype):
     """Address of a contiguous tensor of n values."""
-    _tensor(t, name, dtype)
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtype or t.get_device() != device:
+        _refuse(t, name, dtype)
     if t.numel() != n or not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous and hold {n} values")
     return t.data_ptr()
@@ -204,19 +228,18 @@ class AdamW:
         if set(self.states) != set(kinds):
             raise ValueError(f"states must hold {', '.join(kinds)}")
         self._list = (binding.AdamwTensor * n)()
-        self._device = None
+        self._device = device = _current_device()
         for i, p in enumerate(self.params):
             count = p.numel() if isinstance(p, torch.Tensor) else 0
             entry = self._list[i]
             entry.count, entry.weight_decay = count, decay[i]
-            entry.param = _flat(p, f"params[{i}]", count, (torch.float32,))
+            entry.param = _flat(p, f"params[{i}]", device, count, _F32)
             for key, (field, dtype, scale) in kinds.items():
                 if len(self.states[key]) != n:
                     raise ValueError(f"states[{key!r}] must hold {n} tensors")
                 size = -(-count // binding.ADAMW_BLOCK) if scale else count
-                setattr(entry, field, _flat(self.states[key][i], f"states[{key!r}][{i}]", size,
-                                            (dtype,)))
-            self._device = p.get_device()
+                setattr(entry, field, _flat(self.states[key][i], f"states[{key!r}][{i}]", device,
+                                            size, (dtype,)))
         self._counts = [p.numel() for p in self.params]
 
     def _kinds(self):
@@ -246,12 +269,16 @@ class AdamW:
         dtype = grads[0].dtype if grads and isinstance(grads[0], torch.Tensor) else torch.float32
         if dtype not in _DTYPES:
             raise TypeError("grads must be float32, float16 or bfloat16")
-        self._on_device()
+        device = self._on_device()
         for i, (g, n, entry) in enumerate(zip(grads, self._counts, self._list)):
-            entry.grad = _flat(g, f"grads[{i}]", n, (dtype,))
+            # _flat's checks, without a name for each tensor.
+            if (not isinstance(g, torch.Tensor) or g.dtype != dtype or g.get_device() != device
+                    or g.numel() != n or not g.is_contiguous()):
+                _flat(g, f"grads[{i}]", device, n, (dtype,))
+            entry.grad = g.data_ptr()
         _check(binding.sgemm_cube_adamw(
             len(grads), self._list, _DTYPES[dtype], self.state_bits, self.lr, self.betas[0],
-            self.betas[1], self.eps, grad_scale, number, _stream()), "sgemm_cube_adamw")
+            self.betas[1], self.eps, grad_scale, number, _stream(device)), "sgemm_cube_adamw")
         self.steps = number
 
     def state_values(self, out=None):
@@ -265,19 +292,20 @@ class AdamW:
         n = len(self._counts)
         if len(out) != 2 or len(out[0]) != n or len(out[1]) != n:
             raise ValueError(f"out must be a pair of lists of {n} tensors")
-        self._on_device()
+        device = self._on_device()
         addresses = [(binding.ctypes.c_void_p * n)(*(
-            _flat(t, f"out[{k}][{i}]", self._counts[i], (torch.float32,))
+            _flat(t, f"out[{k}][{i}]", device, self._counts[i], _F32)
             for i, t in enumerate(out[k]))) for k in range(2)]
         if self.state_bits == 32:
             for k, key in enumerate(("exp_avgs", "exp_avg_sqs")):
                 for t, s in zip(out[k], self.states[key]):
                     t.view(-1).copy_(s.view(-1))
             return out
-        _check(binding.sgemm_cube_adamw_values(n, self._list, *addresses, _stream()),
+        _check(binding.sgemm_cube_adamw_values(n, self._list, *addresses, _stream(device)),
                "sgemm_cube_adamw_values")
         return out
 
     def _on_device(self):
-        if self._device is not None and torch.cuda.current_device() != self._device:
+        if _current_device() != self._device:
             raise ValueError("the parameters are not on the current device")
+        return self._device
