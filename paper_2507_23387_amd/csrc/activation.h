@@ -21,13 +21,57 @@ __device__ __forceinline__ float gelu_tanh_arg(float z) {
   return z * (kC + (kC * 0.044715f) * z * z);
 }
 
+// The normal distribution Phi(z), and e = exp(-z^2 / 2), by Hastings' formula
+// (Abramowitz and Stegun 7.1.26): erfc(x) = t (a1 + ... + a5 t^4) exp(-x^2),
+// t = 1 / (1 + p x), |error| <= 1.5e-7 in erfc, so 0.75e-7 in Phi, about 1.3 units
+// of 2^-24, and less in the tails, where exp(-x^2) scales it.  16 instructions;
+// the library's erff, both of its branches taken by a wave, is some 80, which cost
+// the epilogue of a 256 x 256 tile more than its stores.
+__device__ __forceinline__ float normal_cdf(float z, float& e) {
+  const float x = 0.707106781f * __builtin_fabsf(z);
+  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, x, 1.0f));
+  float p = __builtin_fmaf(1.061405429f, t, -1.453152027f);
+  p = __builtin_fmaf(p, t, 1.421413741f);
+  p = __builtin_fmaf(p, t, -0.284496736f);
+  p = __builtin_fmaf(p, t, 0.254829592f);
+  e = __builtin_amdgcn_exp2f(-0.721347520f * z * z);
+  const float q = 0.5f * p * t * e;
+  return z < 0.0f ? q : 1.0f - q;
+}
+
 __device__ __forceinline__ float activate(int activation, float z) {
+  float e;
   switch (activation) {
     case SGEMM_CUBE_ACT_RELU: return z < 0.0f ? 0.0f : z;
-    case SGEMM_CUBE_ACT_GELU: return 0.5f * z * (1.0f + erff(0.707106781f * z));
+    case SGEMM_CUBE_ACT_GELU: return z * normal_cdf(z, e);
     case SGEMM_CUBE_ACT_GELU_TANH: return z * sigmoid(gelu_tanh_arg(z));
     case SGEMM_CUBE_ACT_SILU: return z * sigmoid(z);
     default: return z;
+  }
+}
+
+// The same for four values behind one branch.
+template <typename V>
+__device__ __forceinline__ void activate4(int activation, V& v) {
+  float e;
+  switch (activation) {
+    case SGEMM_CUBE_ACT_RELU:
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = activate(SGEMM_CUBE_ACT_RELU, v[k]);
+      break;
+    case SGEMM_CUBE_ACT_GELU:
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = v[k] * normal_cdf(v[k], e);
+      break;
+    case SGEMM_CUBE_ACT_GELU_TANH:
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = activate(SGEMM_CUBE_ACT_GELU_TANH, v[k]);
+      break;
+    case SGEMM_CUBE_ACT_SILU:
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = activate(SGEMM_CUBE_ACT_SILU, v[k]);
+      break;
+    default: break;
   }
 }
 
@@ -35,8 +79,9 @@ __device__ __forceinline__ float activate_grad(int activation, float z) {
   switch (activation) {
     case SGEMM_CUBE_ACT_RELU: return z > 0.0f ? 1.0f : z <= 0.0f ? 0.0f : z;  // NaN stays
     case SGEMM_CUBE_ACT_GELU: {
-      const float density = 0.398942280f * __builtin_amdgcn_exp2f(-0.721347520f * z * z);
-      return 0.5f * (1.0f + erff(0.707106781f * z)) + z * density;
+      float e;
+      const float phi = normal_cdf(z, e);
+      return phi + z * 0.398942280f * e;
     }
     case SGEMM_CUBE_ACT_GELU_TANH: {
       constexpr float kC = 1.59576912f;

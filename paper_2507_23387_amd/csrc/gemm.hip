@@ -35,7 +35,9 @@
 // repeat the last stage.  Each kernel's comment describes its schedule.
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
+#include "epilogue.h"
 #include "gemm_common.h"
 
 namespace sgc {
@@ -156,13 +158,13 @@ __device__ void split_a_planes(const float* __restrict__ A, int64_t lda, int M, 
 // past the end repeat the last stage, so every wait count is a constant.
 // kPrefetch = false (pipeline ablation): the 16 DMAs of a step are issued
 // right before its barrier, so no copy overlaps the MFMAs.
-template <bool kPrefetch, bool kFusedA>
-__global__ __launch_bounds__(kWideThreads, 1) void gemm_el_kernel(
+template <bool kPrefetch, bool kFusedA, class Epi>
+__device__ __forceinline__ void el_tile(
     uint16_t* __restrict__ a_hi, uint16_t* __restrict__ a_lo,
     const uint16_t* __restrict__ b_hi, const uint16_t* __restrict__ b_lo,
     const uint32_t* __restrict__ range, int Kp, int tiles_m, int tiles_n,
-    float* __restrict__ C, int64_t ldc, int M, int N, float s, float inv_s,
-    const float* __restrict__ af, int64_t lda, int K) {
+    float* C, int64_t ldc, int M, int N, float s, float inv_s,
+    const float* __restrict__ af, int64_t lda, int K, const Epi& epi) {
   static_assert(kPrefetch || !kFusedA, "the fused split runs with the overlapped copies only");
   constexpr int kBBase = 2 * kSlotHalves;     // the B slots follow the two A slots
   // The furthest DMA targets: plane tile 3 of the lo plane of B slot 1, and
@@ -178,6 +180,7 @@ __global__ __launch_bounds__(kWideThreads, 1) void gemm_el_kernel(
   int tm, tn;
   if (!tile_of_block(blockIdx.x, tiles_m, tiles_n, tm, tn))
     tile_of<4>(blockIdx.x, tiles_m, tiles_n, tm, tn);
+  scalar_tile<Epi>(tm, tn);
   if (range[0] == range[1]) {
     // s B_hi overflows FP16: gemm_unscaled_kernel runs instead.  Without planes
     // of A (fused split), this kernel first writes them for it.
@@ -424,11 +427,41 @@ __global__ __launch_bounds__(kWideThreads, 1) void gemm_el_kernel(
   wait_vmcnt<0>();
   mfma_drain();
 
+  if constexpr (!std::is_same<Epi, NoEpilogue>::value) {
+    constexpr int kChunk = epilogue_chunk(kWSub, kWSub, 4, kElLdsBytes);
+    lds_barrier();  // every wave is done with the stages
+    epilogue_tile<kWSub, kWSub, kChunk>(
+        epi, reinterpret_cast<float*>(lds) + w * kChunk * kWSub * 256, C, ldc, M, N,
+        tm * kWide + wm * 128, tn * kWide + wn * 128,
+        [&](int i, int j, int r) { return acc[i][j][r] * inv_s; });
+    return;
+  }
   const int col0 = tn * kWide + wn * 128 + (lane & 15);
   const int row0 = tm * kWide + wm * 128 + (lane >> 4) * 4;
   const bool full = (tm + 1) * kWide <= M && (tn + 1) * kWide <= N;
   store_tile16<kWSub, kWSub>(C, ldc, M, N, row0, col0, full,
                              [&](int i, int j, int r) { return acc[i][j][r] * inv_s; });
+}
+
+template <bool kPrefetch, bool kFusedA>
+__global__ __launch_bounds__(kWideThreads, 1) void gemm_el_kernel(
+    uint16_t* __restrict__ a_hi, uint16_t* __restrict__ a_lo, const uint16_t* __restrict__ b_hi,
+    const uint16_t* __restrict__ b_lo, const uint32_t* __restrict__ range, int Kp, int tiles_m,
+    int tiles_n, float* __restrict__ C, int64_t ldc, int M, int N, float s, float inv_s,
+    const float* __restrict__ af, int64_t lda, int K) {
+  el_tile<kPrefetch, kFusedA>(a_hi, a_lo, b_hi, b_lo, range, Kp, tiles_m, tiles_n, C, ldc, M, N, s,
+                              inv_s, af, lda, K, NoEpilogue{});
+}
+
+// The same with a linear layer's epilogue (C and the residual may be one).
+template <bool kFusedA>
+__global__ __launch_bounds__(kWideThreads, 1) void linear_el_kernel(
+    uint16_t* __restrict__ a_hi, uint16_t* __restrict__ a_lo, const uint16_t* __restrict__ b_hi,
+    const uint16_t* __restrict__ b_lo, const uint32_t* __restrict__ range, int Kp, int tiles_m,
+    int tiles_n, float* C, int64_t ldc, int M, int N, float s, float inv_s,
+    const float* __restrict__ af, int64_t lda, int K, Epilogue epi) {
+  el_tile<true, kFusedA>(a_hi, a_lo, b_hi, b_lo, range, Kp, tiles_m, tiles_n, C, ldc, M, N, s,
+                         inv_s, af, lda, K, epi);
 }
 
 // Hi-only kernel: C = A_hi B_hi, the native-FP16 GEMM baseline (Sec. 6.2),
@@ -605,14 +638,14 @@ constexpr int tw_split_slot(int q) {
   return kTwSplitFirst + q * (kTwSplitLast - kTwSplitFirst + 1) / 80;
 }
 
-template <int V, bool kFusedA = false, bool kFusedB = false>
-__global__ __launch_bounds__(kWideThreads, 1) void gemm_n128_kernel(
+template <int V, bool kFusedA, bool kFusedB, class Epi>
+__device__ __forceinline__ void n128_tile(
     const uint16_t* __restrict__ a_hi, const uint16_t* __restrict__ a_lo,
     const uint16_t* __restrict__ b_hi, const uint16_t* __restrict__ b_lo,
     const uint32_t* __restrict__ range, int Kp, int tiles_m, int tiles_n,
-    float* __restrict__ C, int64_t ldc, int M, int N, float inv_s,
+    float* C, int64_t ldc, int M, int N, float inv_s,
     const float* __restrict__ af, int64_t lda, float s, const float* __restrict__ bf,
-    int64_t ldb) {
+    int64_t ldb, const Epi& epi) {
   static_assert(V == kTermwise || V == kCrossScaled, "n128 variants");
   static_assert(!kFusedA || V == kTermwise, "the fused split of A is built for termwise only");
   static_assert(!kFusedB || V == kTermwise, "the fused split of B is built for termwise only");
@@ -640,6 +673,7 @@ __global__ __launch_bounds__(kWideThreads, 1) void gemm_n128_kernel(
   int tm, tn;
   if (!tile_of_block(blockIdx.x, tiles_m, tiles_n, tm, tn))
     tile_of<4>(blockIdx.x, tiles_m, tiles_n, tm, tn);
+  scalar_tile<Epi>(tm, tn);
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t slices = Kp / kSlice;
@@ -1028,16 +1062,46 @@ __global__ __launch_bounds__(kWideThreads, 1) void gemm_n128_kernel(
     fold(kCols - 1, 1, 0, 4 * kRows);
   }
 
-  const int col0 = tn * kTwN + (lane & 15);
-  const int row0 = tm * kTwM + w * 64 + (lane >> 4) * 4;
-  const bool full = (tm + 1) * kTwM <= M && (tn + 1) * kTwN <= N;
-  store_tile16<kRows, kCols>(C, ldc, M, N, row0, col0, full, [&](int i, int j, int r) {
+  auto value = [&](int i, int j, int r) {
     if constexpr (V == kCrossScaled) {
       return hh[i][j][r] * inv_s;
     } else {
       return __builtin_fmaf(xb[i][j][r], inv_s, __builtin_fmaf(xa[i][j][r], inv_s, hh[i][j][r]));
     }
-  });
+  };
+  if constexpr (!std::is_same<Epi, NoEpilogue>::value) {
+    constexpr int kChunk = epilogue_chunk(kRows, kCols, 4, kTwLdsBytes);
+    lds_barrier();  // every wave is done with the stages
+    epilogue_tile<kRows, kCols, kChunk>(epi, reinterpret_cast<float*>(lds) + w * kChunk * kCols * 256,
+                                        C, ldc, M, N, tm * kTwM + w * 64, tn * kTwN, value);
+    return;
+  }
+  const int col0 = tn * kTwN + (lane & 15);
+  const int row0 = tm * kTwM + w * 64 + (lane >> 4) * 4;
+  const bool full = (tm + 1) * kTwM <= M && (tn + 1) * kTwN <= N;
+  store_tile16<kRows, kCols>(C, ldc, M, N, row0, col0, full, value);
+}
+
+template <int V, bool kFusedA = false, bool kFusedB = false>
+__global__ __launch_bounds__(kWideThreads, 1) void gemm_n128_kernel(
+    const uint16_t* __restrict__ a_hi, const uint16_t* __restrict__ a_lo,
+    const uint16_t* __restrict__ b_hi, const uint16_t* __restrict__ b_lo,
+    const uint32_t* __restrict__ range, int Kp, int tiles_m, int tiles_n, float* __restrict__ C,
+    int64_t ldc, int M, int N, float inv_s, const float* __restrict__ af, int64_t lda, float s,
+    const float* __restrict__ bf, int64_t ldb) {
+  n128_tile<V, kFusedA, kFusedB>(a_hi, a_lo, b_hi, b_lo, range, Kp, tiles_m, tiles_n, C, ldc, M, N,
+                                 inv_s, af, lda, s, bf, ldb, NoEpilogue{});
+}
+
+// The same with a linear layer's epilogue (C and the residual may be one).
+template <int V, bool kFusedA>
+__global__ __launch_bounds__(kWideThreads, 1) void linear_n128_kernel(
+    const uint16_t* __restrict__ a_hi, const uint16_t* __restrict__ a_lo,
+    const uint16_t* __restrict__ b_hi, const uint16_t* __restrict__ b_lo,
+    const uint32_t* __restrict__ range, int Kp, int tiles_m, int tiles_n, float* C, int64_t ldc,
+    int M, int N, float inv_s, const float* __restrict__ af, int64_t lda, float s, Epilogue epi) {
+  n128_tile<V, kFusedA, false>(a_hi, a_lo, b_hi, b_lo, range, Kp, tiles_m, tiles_n, C, ldc, M, N,
+                               inv_s, af, lda, s, nullptr, 0, epi);
 }
 
 template <bool kPrefetch, bool kFusedA>
@@ -1090,7 +1154,57 @@ hipError_t launch_n128(const Planes& p, int64_t M, int64_t N, float* C, int64_t 
   return hipGetLastError();
 }
 
+template <bool kFusedA>
+hipError_t launch_linear_el(const Planes& p, int64_t M, int64_t N, float* C, int64_t ldc, float s,
+                            const Epilogue& epi, hipStream_t stream, const float* A = nullptr,
+                            int64_t lda = 0, int64_t K = 0) {
+  static std::atomic<bool> done[kMaxDevices];
+  const hipError_t attr = set_lds(&linear_el_kernel<kFusedA>, kElLdsBytes, done);
+  if (attr != hipSuccess) return attr;
+  const int tiles_m = static_cast<int>(p.Mp / kWide);
+  const int tiles_n = static_cast<int>(p.Np / kWide);
+  hipLaunchKernelGGL((linear_el_kernel<kFusedA>), dim3(tiles_m * tiles_n), dim3(kWideThreads),
+                     kElLdsBytes, stream, p.a_hi, p.a_lo, p.b_hi, p.b_lo, p.range,
+                     static_cast<int>(p.Kp), tiles_m, tiles_n, C, ldc, static_cast<int>(M),
+                     static_cast<int>(N), s, 1.0f / s, A, lda, static_cast<int>(K), epi);
+  return hipGetLastError();
+}
+
+template <int V, bool kFusedA>
+hipError_t launch_linear_n128(const Planes& p, int64_t M, int64_t N, float* C, int64_t ldc,
+                              float s, const Epilogue& epi, hipStream_t stream,
+                              const float* A = nullptr, int64_t lda = 0) {
+  static std::atomic<bool> done[kMaxDevices];
+  const hipError_t attr = set_lds(&linear_n128_kernel<V, kFusedA>, kTwLdsBytes, done);
+  if (attr != hipSuccess) return attr;
+  const int tiles_m = static_cast<int>(p.Mp / kTwM);
+  const int tiles_n = static_cast<int>((N + kTwN - 1) / kTwN);
+  hipLaunchKernelGGL((linear_n128_kernel<V, kFusedA>), dim3(tiles_m * tiles_n), dim3(kWideThreads),
+                     kTwLdsBytes, stream, p.a_hi, p.a_lo, p.b_hi, p.b_lo, p.range,
+                     static_cast<int>(p.Kp), tiles_m, tiles_n, C, ldc, static_cast<int>(M),
+                     static_cast<int>(N), 1.0f / s, A, lda, s, epi);
+  return hipGetLastError();
+}
+
 }  // namespace
+
+hipError_t launch_gemm_epilogue(const Planes& p, int64_t M, int64_t N, float* C, int64_t ldc,
+                                float scale, int variant, const Epilogue& epi,
+                                hipStream_t stream) {
+  if (const int tile = small_gemm_tile(M, N, p.Kp, variant, !scaled_kernel_ok(scale)))
+    return launch_gemm_small_epilogue(tile, p, M, N, C, ldc, scale, variant, epi, stream);
+  if (variant == kTermwise)
+    return launch_linear_n128<kTermwise, false>(p, M, N, C, ldc, scale, epi, stream);
+  const bool scaled = scaled_kernel_ok(scale);
+  if (scaled) {
+    const hipError_t e =
+        variant == kElementwise
+            ? launch_linear_el<false>(p, M, N, C, ldc, scale, epi, stream)
+            : launch_linear_n128<kCrossScaled, false>(p, M, N, C, ldc, scale, epi, stream);
+    if (e != hipSuccess) return e;
+  }
+  return launch_gemm_unscaled_epilogue(p, M, N, C, ldc, scale, variant, !scaled, epi, stream);
+}
 
 hipError_t launch_gemm(const Planes& p, int64_t M, int64_t N, float* C, int64_t ldc,
                        float scale, int variant, hipStream_t stream) {

@@ -27,7 +27,9 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <type_traits>
 
+#include "epilogue.h"
 #include "gemm_common.h"
 
 namespace sgc {
@@ -82,13 +84,14 @@ struct SmallArgs {
   uint32_t* report;  // range report word, or null
 };
 
-template <class S, int kFold>
-__device__ __forceinline__ void small_tile(const SmallArgs& g, uint16_t* lds) {
+template <class S, int kFold, class Epi>
+__device__ __forceinline__ void small_tile(const SmallArgs& g, uint16_t* lds, const Epi& epi) {
   constexpr int kRT = S::kRT, kCT = S::kCT;
   int tm, tn;
   if (S::kBM < 256 || !tile_of_block(blockIdx.x, g.tiles_m, g.tiles_n, tm, tn))
     tile_of<4>(g.by_xcd ? xcd_order(blockIdx.x, g.tiles_m * g.tiles_n) : blockIdx.x, g.tiles_m,
                g.tiles_n, tm, tn);
+  scalar_tile<Epi>(tm, tn);
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = w / S::kWavesN, wn = w % S::kWavesN;
@@ -304,6 +307,16 @@ __device__ __forceinline__ void small_tile(const SmallArgs& g, uint16_t* lds) {
     else
       return acc[i][j][r];
   };
+  if constexpr (!std::is_same<Epi, NoEpilogue>::value) {
+    constexpr int kChunk = epilogue_chunk(kRT, kCT, S::kWaves, S::kLdsBytes);
+    static_assert(static_cast<size_t>(S::kWaves) * kChunk * kCT * 1024 <= S::kLdsBytes,
+                  "the waves' staging fits the ring");
+    lds_barrier();  // every wave is done with the ring
+    epilogue_tile<kRT, kCT, kChunk>(epi, reinterpret_cast<float*>(lds) + w * kChunk * kCT * 256,
+                                    g.C, g.ldc, g.M, g.N, tm * S::kBM + wm * S::kWRows,
+                                    tn * S::kBN + wn * S::kWCols, value);
+    return;
+  }
   if constexpr (kFold != kHiFold) {
     if (g.report && blockIdx.x == 0 && threadIdx.x == 0) *g.report = range_report_bits(g.range);
     if (g.row_max) {
@@ -329,23 +342,36 @@ __device__ __forceinline__ void small_tile(const SmallArgs& g, uint16_t* lds) {
   store_tile16<kRT, kCT>(g.C, g.ldc, g.M, g.N, row0, col0, full, value);
 }
 
-template <int V, int kBM, int kBN, int kWM, int kWN, int kStages>
-__global__ __launch_bounds__(64 * kWM * kWN, 1) void gemm_small_kernel(SmallArgs g,
-                                                                       int unscaled_only) {
-  using S = SmallShape<kBM, kBN, kWM, kWN, kStages, V == kHiOnly>;
+template <int V, class S, class Epi>
+__device__ __forceinline__ void small_body(const SmallArgs& g, int unscaled_only, const Epi& epi) {
   extern __shared__ __align__(16) uint16_t lds[];
   if constexpr (V == kTermwise) {
-    small_tile<S, kTermFold>(g, lds);
+    small_tile<S, kTermFold>(g, lds, epi);
   } else if constexpr (V == kHiOnly) {
-    small_tile<S, kHiFold>(g, lds);
+    small_tile<S, kHiFold>(g, lds, epi);
   } else {
     // The scaled body needs a finite s B_hi (gemm.hip): s <= 2^15 (host) and a
     // clear range flag.
     if (unscaled_only || g.range[0] == g.range[1])
-      small_tile<S, V == kElementwise ? kElUnscaled : kCrUnscaled>(g, lds);
+      small_tile<S, V == kElementwise ? kElUnscaled : kCrUnscaled>(g, lds, epi);
     else
-      small_tile<S, V == kElementwise ? kElScaled : kCrScaled>(g, lds);
+      small_tile<S, V == kElementwise ? kElScaled : kCrScaled>(g, lds, epi);
   }
+}
+
+template <int V, int kBM, int kBN, int kWM, int kWN, int kStages>
+__global__ __launch_bounds__(64 * kWM * kWN, 1) void gemm_small_kernel(SmallArgs g,
+                                                                       int unscaled_only) {
+  small_body<V, SmallShape<kBM, kBN, kWM, kWN, kStages, V == kHiOnly>>(g, unscaled_only,
+                                                                       NoEpilogue{});
+}
+
+// The same with a linear layer's epilogue.
+template <int V, int kBM, int kBN, int kWM, int kWN, int kStages>
+__global__ __launch_bounds__(64 * kWM * kWN, 1) void linear_small_kernel(SmallArgs g,
+                                                                         int unscaled_only,
+                                                                         Epilogue epi) {
+  small_body<V, SmallShape<kBM, kBN, kWM, kWN, kStages, false>>(g, unscaled_only, epi);
 }
 
 // The unscaled body alone, on 256 x 128 tiles: the fallback of the 256-wide
@@ -360,7 +386,14 @@ template <int V>
 __global__ __launch_bounds__(512, 1) void gemm_unscaled_kernel(SmallArgs g, int unscaled_only) {
   extern __shared__ __align__(16) uint16_t lds[];
   if (!unscaled_only && g.range[0] != g.range[1]) return;
-  small_tile<UnscaledShape, V == kElementwise ? kElUnscaled : kCrUnscaled>(g, lds);
+  small_tile<UnscaledShape, V == kElementwise ? kElUnscaled : kCrUnscaled>(g, lds, NoEpilogue{});
+}
+template <int V>
+__global__ __launch_bounds__(512, 1) void linear_unscaled_kernel(SmallArgs g, int unscaled_only,
+                                                                 Epilogue epi) {
+  extern __shared__ __align__(16) uint16_t lds[];
+  if (!unscaled_only && g.range[0] != g.range[1]) return;
+  small_tile<UnscaledShape, V == kElementwise ? kElUnscaled : kCrUnscaled>(g, lds, epi);
 }
 
 template <class S>
@@ -397,6 +430,34 @@ hipError_t launch_unscaled(const Planes& p, int64_t M, int64_t N, float* C, int6
   return hipGetLastError();
 }
 
+template <int V>
+hipError_t launch_unscaled_epilogue(const Planes& p, int64_t M, int64_t N, float* C, int64_t ldc,
+                                    float s, bool only, const Epilogue& epi, hipStream_t stream) {
+  using S = UnscaledShape;
+  static std::atomic<bool> done[kMaxDevices];
+  const hipError_t attr = set_lds(&linear_unscaled_kernel<V>, S::kLdsBytes, done);
+  if (attr != hipSuccess) return attr;
+  const SmallArgs g = small_args<S>(p, M, N, C, ldc, s, RangeOpts{}, nullptr);
+  hipLaunchKernelGGL(linear_unscaled_kernel<V>, dim3(g.tiles_m * g.tiles_n), dim3(S::kThreads),
+                     S::kLdsBytes, stream, g, only ? 1 : 0, epi);
+  return hipGetLastError();
+}
+
+template <int V, int kBM, int kBN, int kWM, int kWN, int kStages>
+hipError_t launch_small_epilogue(const Planes& p, int64_t M, int64_t N, float* C, int64_t ldc,
+                                 float s, const Epilogue& epi, hipStream_t stream) {
+  using S = SmallShape<kBM, kBN, kWM, kWN, kStages, false>;
+  static std::atomic<bool> done[kMaxDevices];
+  const hipError_t attr =
+      set_lds(&linear_small_kernel<V, kBM, kBN, kWM, kWN, kStages>, S::kLdsBytes, done);
+  if (attr != hipSuccess) return attr;
+  const SmallArgs g = small_args<S>(p, M, N, C, ldc, s, RangeOpts{}, nullptr);
+  hipLaunchKernelGGL((linear_small_kernel<V, kBM, kBN, kWM, kWN, kStages>),
+                     dim3(g.tiles_m * g.tiles_n), dim3(S::kThreads), S::kLdsBytes, stream, g,
+                     scaled_kernel_ok(s) ? 0 : 1, epi);
+  return hipGetLastError();
+}
+
 template <int V, int kBM, int kBN, int kWM, int kWN, int kStages>
 hipError_t launch_small(const Planes& p, int64_t M, int64_t N, float* C, int64_t ldc, float s,
                         hipStream_t stream, const RangeOpts& opt, uint32_t* report) {
@@ -413,32 +474,56 @@ hipError_t launch_small(const Planes& p, int64_t M, int64_t N, float* C, int64_t
   return hipGetLastError();
 }
 
-template <int V>
-hipError_t launch_config(int tile, const Planes& p, int64_t M, int64_t N, float* C, int64_t ldc,
-                         float s, hipStream_t stream, const RangeOpts& opt, uint32_t* report) {
+// launch(shape) with the shape of the kernel of a tile.
+template <int kBM_, int kBN_, int kWM_, int kWN_, int kStages_>
+struct Config {
+  static constexpr int kBM = kBM_, kBN = kBN_, kWM = kWM_, kWN = kWN_, kStages = kStages_;
+};
+
+template <int V, typename Launch>
+hipError_t with_config(int tile, Launch launch) {
   switch (tile) {
-    case 32: return launch_small<V, 32, 32, 2, 2, 8>(p, M, N, C, ldc, s, stream, opt, report);
+    case 32: return launch(Config<32, 32, 2, 2, 8>{});
     case 64:
       // Four waves of 32 x 32 read fewer LDS bytes per MFMA than eight of 16 x
       // 32 (1024 x 1024 x 4096: elementwise 32 against 37 us); the cross-first
       // folds keep eight, whose vector adds overlap the other wave's MFMAs (39
       // against 41).
       if constexpr (V == kCrossFirst)
-        return launch_small<V, 64, 64, 4, 2, 4>(p, M, N, C, ldc, s, stream, opt, report);
+        return launch(Config<64, 64, 4, 2, 4>{});
       else
-        return launch_small<V, 64, 64, 2, 2, 4>(p, M, N, C, ldc, s, stream, opt, report);
+        return launch(Config<64, 64, 2, 2, 4>{});
     case 192:
       // Orders of one accumulator set: eight waves of 48 x 96 fit both steps'
       // fragments in VGPRs (four of 96 x 96 move the accumulators of the folds
       // in and out of AGPRs: cross-first 3072 x 3072 x 2048 129 us against 98).
       if constexpr (V == kElementwise || V == kCrossFirst)
-        return launch_small<V, 192, 192, 4, 2, 2>(p, M, N, C, ldc, s, stream, opt, report);
+        return launch(Config<192, 192, 4, 2, 2>{});
       else
         return hipErrorInvalidValue;
     case 128:
-      return launch_small<V, 128, 128, 2, 4, 4>(p, M, N, C, ldc, s, stream, opt, report);
+      return launch(Config<128, 128, 2, 4, 4>{});
     default: return hipErrorInvalidValue;
   }
+}
+
+template <int V>
+hipError_t launch_config(int tile, const Planes& p, int64_t M, int64_t N, float* C, int64_t ldc,
+                         float s, hipStream_t stream, const RangeOpts& opt, uint32_t* report) {
+  return with_config<V>(tile, [&](auto c) {
+    using T = decltype(c);
+    return launch_small<V, T::kBM, T::kBN, T::kWM, T::kWN, T::kStages>(p, M, N, C, ldc, s, stream, opt,
+                                                                     report);
+  });
+}
+
+template <int V>
+hipError_t launch_config_epilogue(int tile, const Planes& p, int64_t M, int64_t N, float* C,
+                                  int64_t ldc, float s, const Epilogue& epi, hipStream_t stream) {
+  return with_config<V>(tile, [&](auto c) {
+    using T = decltype(c);
+    return launch_small_epilogue<V, T::kBM, T::kBN, T::kWM, T::kWN, T::kStages>(p, M, N, C, ldc, s, epi, stream);
+  });
 }
 
 // Time of a grid, in microseconds: `launch`, plus `start` (a tile's prologue and
@@ -571,6 +656,32 @@ hipError_t launch_gemm_small(int tile, const Planes& p, int64_t M, int64_t N, fl
       return launch_config<kCrossFirst>(tile, p, M, N, C, ldc, scale, stream, opt, report);
     case kHiOnly:
       return launch_config<kHiOnly>(tile, p, M, N, C, ldc, scale, stream, opt, report);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+hipError_t launch_gemm_small_epilogue(int tile, const Planes& p, int64_t M, int64_t N, float* C,
+                                      int64_t ldc, float scale, int variant, const Epilogue& epi,
+                                      hipStream_t stream) {
+  switch (variant) {
+    case kElementwise:
+      return launch_config_epilogue<kElementwise>(tile, p, M, N, C, ldc, scale, epi, stream);
+    case kTermwise:
+      return launch_config_epilogue<kTermwise>(tile, p, M, N, C, ldc, scale, epi, stream);
+    case kCrossFirst:
+      return launch_config_epilogue<kCrossFirst>(tile, p, M, N, C, ldc, scale, epi, stream);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+hipError_t launch_gemm_unscaled_epilogue(const Planes& p, int64_t M, int64_t N, float* C,
+                                         int64_t ldc, float scale, int variant, bool only,
+                                         const Epilogue& epi, hipStream_t stream) {
+  switch (variant) {
+    case kElementwise:
+      return launch_unscaled_epilogue<kElementwise>(p, M, N, C, ldc, scale, only, epi, stream);
+    case kCrossFirst:
+      return launch_unscaled_epilogue<kCrossFirst>(p, M, N, C, ldc, scale, only, epi, stream);
     default: return hipErrorInvalidValue;
   }
 }

@@ -69,8 +69,21 @@ struct Epilogue {
   const uint32_t* max_bits;  // shift = prescale_shift(*max_bits, target); null: 0
   int target;
 };
-hipError_t launch_epilogue(const Epilogue& e, int64_t M, int64_t N, const float* P, int64_t ldp,
-                           float* Y, int64_t ldy, hipStream_t stream);
+// The epilogue where K = 0: P = 0.
+hipError_t launch_epilogue(const Epilogue& e, int64_t M, int64_t N, float* Y, int64_t ldy,
+                           hipStream_t stream);
+
+// launch_gemm, launch_gemm_small and launch_gemm_unscaled with an epilogue; the
+// product's bits are theirs.  C may be the residual.
+hipError_t launch_gemm_epilogue(const Planes& p, int64_t M, int64_t N, float* C, int64_t ldc,
+                                float scale, int variant, const Epilogue& epi,
+                                hipStream_t stream);
+hipError_t launch_gemm_small_epilogue(int tile, const Planes& p, int64_t M, int64_t N, float* C,
+                                      int64_t ldc, float scale, int variant, const Epilogue& epi,
+                                      hipStream_t stream);
+hipError_t launch_gemm_unscaled_epilogue(const Planes& p, int64_t M, int64_t N, float* C,
+                                         int64_t ldc, float scale, int variant, bool only,
+                                         const Epilogue& epi, hipStream_t stream);
 
 struct LinearArgs {
   int64_t M, N, K;

@@ -68,25 +68,21 @@ size_t linear_ws(int64_t M, int64_t N, int64_t K) {
   if (M == 0 || N == 0 || K == 0) return 0;
   Carver c{nullptr, 0};
   (void)carve_planes(c, M, N, K);
-  (void)c.take<float>(M * N);
   return c.used;
 }
 
 hipError_t launch_linear(const LinearArgs& a, void* ws, hipStream_t stream) {
-  if (a.K == 0) return launch_epilogue(a.e, a.M, a.N, nullptr, 0, a.y, a.ldy, stream);
+  if (a.K == 0) return launch_epilogue(a.e, a.M, a.N, a.y, a.ldy, stream);
   Carver c{static_cast<char*>(ws), 0};
   const Planes p = carve_planes(c, a.M, a.N, a.K);
-  float* const product = c.take<float>(a.M * a.N);
   SplitJob jobs[2] = {job_of(a.x, a.ldx, a.M, a.K),
                       a.transpose_w ? job_of(a.w, a.ldw, a.N, a.K)
                                     : job_of(a.w, a.ldw, a.K, a.N)};
   to_planes(jobs[0], p, false, false);
   to_planes(jobs[1], p, true, !a.transpose_w);
-  hipError_t err = launch_split_jobs(jobs, 2, a.scale, stream);
-  if (err == hipSuccess)
-    err = launch_gemm(p, a.M, a.N, product, a.N, a.scale, a.variant, stream);
+  const hipError_t err = launch_split_jobs(jobs, 2, a.scale, stream);
   if (err != hipSuccess) return err;
-  return launch_epilogue(a.e, a.M, a.N, product, a.N, a.y, a.ldy, stream);
+  return launch_gemm_epilogue(p, a.M, a.N, a.y, a.ldy, a.scale, a.variant, a.e, stream);
 }
 
 namespace {
@@ -157,16 +153,11 @@ hipError_t launch_linear_grad(const LinearGradArgs& a, void* ws, hipStream_t str
   }
   jobs[count++] = d;
   err = launch_split_jobs(jobs, count, a.scale, stream);
-  if (err == hipSuccess && dx) {
-    err = launch_gemm(g.dx, a.M, a.K, a.dx, a.lddx, a.scale, a.variant, stream);
-    if (err == hipSuccess)
-      err = launch_epilogue(ex, a.M, a.K, a.dx, a.lddx, a.dx, a.lddx, stream);
-  }
-  if (err == hipSuccess && dw) {
-    err = launch_gemm(g.dw, dw_rows, dw_cols, a.dw, a.lddw, a.scale, a.variant, stream);
-    if (err == hipSuccess)
-      err = launch_epilogue(ew, dw_rows, dw_cols, a.dw, a.lddw, a.dw, a.lddw, stream);
-  }
+  if (err == hipSuccess && dx)
+    err = launch_gemm_epilogue(g.dx, a.M, a.K, a.dx, a.lddx, a.scale, a.variant, ex, stream);
+  if (err == hipSuccess && dw)
+    err = launch_gemm_epilogue(g.dw, dw_rows, dw_cols, a.dw, a.lddw, a.scale, a.variant, ew,
+                               stream);
   return err;
 }
 

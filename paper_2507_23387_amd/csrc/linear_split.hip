@@ -193,21 +193,15 @@ __global__ __launch_bounds__(kThreads) void columns_join_kernel(ColumnArgs a, in
                                                                __builtin_fmaxf(top[2], top[3])));
 }
 
-// Y from the product P (null: zeros), which may be Y.
+// The epilogue of a product without terms: Z = bias.
 __global__ __launch_bounds__(kThreads) void epilogue_kernel(Epilogue e, int64_t M, int64_t N,
-                                                            const float* P, int64_t ldp, float* Y,
-                                                            int64_t ldy) {
+                                                            float* Y, int64_t ldy) {
   const int64_t j = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
   if (j >= N) return;
-  const int shift = e.max_bits ? prescale_shift(*e.max_bits, e.target) : 0;
+  const float z = e.bias ? e.bias[j] : 0.0f, y = activate(e.activation, z);
   for (int64_t i = blockIdx.y; i < M; i += gridDim.y) {
-    float z = P ? P[i * ldp + j] : 0.0f;
-    if (e.max_bits) z = __builtin_ldexpf(z, -shift);
-    if (e.bias) z += e.bias[j];
     if (e.z) e.z[i * e.ldz + j] = z;
-    float y = activate(e.activation, z);
-    if (e.r) y += e.r[i * e.ldr + j];
-    Y[i * ldy + j] = y;
+    Y[i * ldy + j] = e.r ? y + e.r[i * e.ldr + j] : y;
   }
 }
 
@@ -250,13 +244,11 @@ hipError_t launch_columns(const ColumnArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-hipError_t launch_epilogue(const Epilogue& e, int64_t M, int64_t N, const float* P, int64_t ldp,
-                           float* Y, int64_t ldy, hipStream_t stream) {
-  if (M <= 0 || N <= 0) return hipSuccess;
+hipError_t launch_epilogue(const Epilogue& e, int64_t M, int64_t N, float* Y, int64_t ldy,
+                           hipStream_t stream) {
   const dim3 grid(static_cast<unsigned>((N + kThreads - 1) / kThreads),
                   static_cast<unsigned>(std::min<int64_t>(M, 65535)));
-  hipLaunchKernelGGL(epilogue_kernel, grid, dim3(kThreads), 0, stream, e, M, N, P, ldp, Y,
-                     ldy);
+  hipLaunchKernelGGL(epilogue_kernel, grid, dim3(kThreads), 0, stream, e, M, N, Y, ldy);
   return hipGetLastError();
 }
 
