@@ -50,26 +50,27 @@ __device__ __forceinline__ float activate(int activation, float z) {
   }
 }
 
-// The same for four values behind one branch.
-template <typename V>
-__device__ __forceinline__ void activate4(int activation, V& v) {
-  float e;
+// The same for kU pieces of four values behind one branch.
+template <typename V, int kU>
+__device__ __forceinline__ void activate_all(int activation, V (&v)[kU]) {
+  auto each = [&](auto f) {
+#pragma unroll
+    for (int u = 0; u < kU; ++u)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[u][k] = f(v[u][k]);
+  };
   switch (activation) {
     case SGEMM_CUBE_ACT_RELU:
-#pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = activate(SGEMM_CUBE_ACT_RELU, v[k]);
+      each([](float z) { return activate(SGEMM_CUBE_ACT_RELU, z); });
       break;
     case SGEMM_CUBE_ACT_GELU:
-#pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = v[k] * normal_cdf(v[k], e);
+      each([](float z) { return activate(SGEMM_CUBE_ACT_GELU, z); });
       break;
     case SGEMM_CUBE_ACT_GELU_TANH:
-#pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = activate(SGEMM_CUBE_ACT_GELU_TANH, v[k]);
+      each([](float z) { return activate(SGEMM_CUBE_ACT_GELU_TANH, z); });
       break;
     case SGEMM_CUBE_ACT_SILU:
-#pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = activate(SGEMM_CUBE_ACT_SILU, v[k]);
+      each([](float z) { return activate(SGEMM_CUBE_ACT_SILU, z); });
       break;
     default: break;
   }
@@ -93,6 +94,32 @@ __device__ __forceinline__ float activate_grad(int activation, float z) {
       return s + z * s * (1.0f - s);
     }
     default: return 1.0f;
+  }
+}
+
+// d *= act'(z) for kU pieces behind one branch.
+template <typename V, int kU>
+__device__ __forceinline__ void multiply_grad(int activation, V (&d)[kU], const V (&z)[kU]) {
+  auto each = [&](auto f) {
+#pragma unroll
+    for (int u = 0; u < kU; ++u)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) d[u][k] *= f(z[u][k]);
+  };
+  switch (activation) {
+    case SGEMM_CUBE_ACT_RELU:
+      each([](float x) { return activate_grad(SGEMM_CUBE_ACT_RELU, x); });
+      break;
+    case SGEMM_CUBE_ACT_GELU:
+      each([](float x) { return activate_grad(SGEMM_CUBE_ACT_GELU, x); });
+      break;
+    case SGEMM_CUBE_ACT_GELU_TANH:
+      each([](float x) { return activate_grad(SGEMM_CUBE_ACT_GELU_TANH, x); });
+      break;
+    case SGEMM_CUBE_ACT_SILU:
+      each([](float x) { return activate_grad(SGEMM_CUBE_ACT_SILU, x); });
+      break;
+    default: break;
   }
 }
 

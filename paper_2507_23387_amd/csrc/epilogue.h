@@ -11,8 +11,22 @@
 namespace sgc {
 namespace {
 
-// In place of an epilogue: C is stored as the product (store_tile16).
+// In place of an epilogue: C is stored as the product (store_tile16), or
+// (Unscale) times 2^-prescale_shift(*max_bits, target).
 struct NoEpilogue {};
+template <class Epi>
+constexpr bool kThroughLds = std::is_same<Epi, Epilogue>::value;
+template <class Epi>
+__device__ __forceinline__ int unscale_shift(const Epi& epi) {
+  if constexpr (std::is_same<Epi, Unscale>::value)
+    return -prescale_shift(*epi.max_bits, epi.target);
+  return 0;
+}
+template <class Epi>
+__device__ __forceinline__ float unscaled(float x, int shift) {
+  if constexpr (std::is_same<Epi, Unscale>::value) return __builtin_ldexpf(x, shift);
+  return x;
+}
 
 // Keeps the tile's indices in scalar registers.  The epilogue uses them lane by
 // lane too, and where the compiler therefore holds them in vector registers it
@@ -27,7 +41,14 @@ __device__ __forceinline__ void scalar_tile(int& tm, int& tn) {
   }
 }
 
+// Four adjacent floats at any address that floats have.
 typedef float floatx4_any __attribute__((ext_vector_type(4), aligned(4)));
+__device__ __forceinline__ floatx4 load_any(const float* p) {
+  return *reinterpret_cast<const floatx4_any*>(p);
+}
+__device__ __forceinline__ void store_any(float* p, floatx4 v) {
+  *reinterpret_cast<floatx4_any*>(p) = v;
+}
 
 // Accumulator blocks (16 rows) that a wave of kWaves stages at a time in
 // `bytes` of LDS, at kCols columns of 16.
@@ -37,22 +58,40 @@ constexpr int epilogue_chunk(int rows, int cols, int waves, size_t bytes) {
   return c;
 }
 
-// Y = act(Z) + R, Z = 2^-shift value(i, j, r) + bias for a wave's kSubM x kSubN
-// accumulators of 16 x 16 (store_tile16's layout; row0, col0: its first row and
-// column).  kChunk rows of blocks at a time go through `stage`, the wave's own
-// LDS, so that lane l then has four adjacent columns: bias, residual, Z and Y move
-// in 16-byte pieces of whole rows, and the activation is one rolled loop and not
-// one copy per accumulator.  Column c of row r is at c ^ 16 ((r / 4) % 4) of the
-// row (as far as its width allows), which spreads the 4 row groups of an
-// accumulator over the banks.
+// One piece of a row at the end of the matrix: entry (gr, gc) and up to three
+// beside it.
+__device__ __forceinline__ void epilogue_edge(const Epilogue& e, float* Y, int64_t ldy, int M,
+                                              int N, int gr, int gc, floatx4 v) {
+  if (gr >= M) return;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    if (gc + k >= N) break;
+    float x = v[k];
+    if (e.bias) x += e.bias[gc + k];
+    if (e.z) e.z[static_cast<int64_t>(gr) * e.ldz + gc + k] = x;
+    x = activate(e.activation, x);
+    if (e.r) x += e.r[static_cast<int64_t>(gr) * e.ldr + gc + k];
+    Y[static_cast<int64_t>(gr) * ldy + gc + k] = x;
+  }
+}
+
+// Y = act(Z) + R, Z = value(i, j, r) + bias for a wave's kSubM x kSubN accumulators
+// of 16 x 16 (store_tile16's layout; row0, col0: its first row and column).  kChunk
+// rows of blocks at a time go through `stage`, the wave's own LDS, so that lane l
+// then has four adjacent columns: bias, residual, Z and Y move in 16-byte pieces of
+// whole rows, and the activation is one rolled loop of four pieces and not one copy
+// per accumulator (one piece at a time, a lone wave per SIMD waited out each step of
+// it: 8192 x 8192 x 4096 with GELU and Z 1289 us in all).  Column c of row r is at
+// c ^ 16 ((r / 4) % 4) of the row (as far as its width allows), which spreads the 4
+// row groups of an accumulator over the banks.
 template <int kSubM, int kSubN, int kChunk, typename F>
 __device__ __forceinline__ void epilogue_tile(const Epilogue& e, float* stage, float* Y,
                                               int64_t ldy, int M, int N, int row0, int col0,
                                               F value) {
-  constexpr int kWidth = 16 * kSubN;
+  constexpr int kWidth = 16 * kSubN, kQuads = kWidth / 4;
   constexpr int kSwap = kSubN % 4 == 0 ? 3 : kSubN % 2 == 0 ? 1 : 0;
   const int lane = threadIdx.x & 63;
-  const int shift = e.max_bits ? -prescale_shift(*e.max_bits, e.target) : 0;
+  const bool full = row0 + 16 * kSubM <= M && col0 + kWidth <= N;
   static_for<(kSubM + kChunk - 1) / kChunk>([&](auto Cc) {
     constexpr int i0 = decltype(Cc)::value * kChunk;
     constexpr int kN = i0 + kChunk <= kSubM ? kChunk : kSubM - i0;
@@ -70,45 +109,54 @@ __device__ __forceinline__ void epilogue_tile(const Epilogue& e, float* stage, f
       }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
+    constexpr int kPieces = kN * kSubN;  // of this lane
+    constexpr int kU = kPieces % 4 == 0 ? 4 : kPieces % 2 == 0 ? 2 : 1;
 #pragma unroll 1
-    for (int q = lane; q < kN * 16 * (kWidth / 4); q += 64) {
-      const int row = q / (kWidth / 4), c = 4 * (q - row * (kWidth / 4));
-      const int gr = row0 + 16 * i0 + row, gc = col0 + c;
-      if (gr >= M || gc >= N) continue;
-      floatx4 v = *reinterpret_cast<const floatx4*>(
-          stage + row * kWidth + (c ^ (((row >> 2) & kSwap) << 4)));
-      if (e.max_bits) {
+    for (int p0 = 0; p0 < kPieces; p0 += kU) {
+      floatx4 v[kU];
+      int gr[kU], gc[kU];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = __builtin_ldexpf(v[k], shift);
+      for (int u = 0; u < kU; ++u) {
+        const int q = lane + 64 * (p0 + u), row = q / kQuads, c = 4 * (q - row * kQuads);
+        gr[u] = row0 + 16 * i0 + row;
+        gc[u] = col0 + c;
+        v[u] = *reinterpret_cast<const floatx4*>(stage + row * kWidth +
+                                                 (c ^ (((row >> 2) & kSwap) << 4)));
       }
-      float* const y = Y + static_cast<int64_t>(gr) * ldy + gc;
-      const float* const res = e.r ? e.r + static_cast<int64_t>(gr) * e.ldr + gc : nullptr;
-      float* const z = e.z ? e.z + static_cast<int64_t>(gr) * e.ldz + gc : nullptr;
-      if (gc + 4 <= N) {
-        floatx4_any b = {0.0f, 0.0f, 0.0f, 0.0f}, rr = b;
-        if (e.bias) b = *reinterpret_cast<const floatx4_any*>(e.bias + gc);
-        if (res) rr = *reinterpret_cast<const floatx4_any*>(res);
-        if (e.bias) {
+      if (!full) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) v[k] += b[k];
-        }
-        if (z) *reinterpret_cast<floatx4_any*>(z) = v;
-        activate4(e.activation, v);
-        if (res) {
+        for (int u = 0; u < kU; ++u) epilogue_edge(e, Y, ldy, M, N, gr[u], gc[u], v[u]);
+        continue;
+      }
+      floatx4 r[kU];
+      if (e.r) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) v[k] += rr[k];
-        }
-        *reinterpret_cast<floatx4_any*>(y) = v;
-      } else {
-        for (int k = 0; k < N - gc; ++k) {
-          float x = k == 0 ? v[0] : k == 1 ? v[1] : v[2];
-          if (e.bias) x += e.bias[gc + k];
-          if (z) z[k] = x;
-          x = activate(e.activation, x);
-          if (res) x += res[k];
-          y[k] = x;
+        for (int u = 0; u < kU; ++u)
+          r[u] = load_any(e.r + static_cast<int64_t>(gr[u]) * e.ldr + gc[u]);
+      }
+      if (e.bias) {
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+          const floatx4 b = load_any(e.bias + gc[u]);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[u][k] += b[k];
         }
       }
+      if (e.z) {
+#pragma unroll
+        for (int u = 0; u < kU; ++u)
+          store_any(e.z + static_cast<int64_t>(gr[u]) * e.ldz + gc[u], v[u]);
+      }
+      activate_all(e.activation, v);
+      if (e.r) {
+#pragma unroll
+        for (int u = 0; u < kU; ++u)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[u][k] += r[u][k];
+      }
+#pragma unroll
+      for (int u = 0; u < kU; ++u)
+        store_any(Y + static_cast<int64_t>(gr[u]) * ldy + gc[u], v[u]);
     }
   });
 }

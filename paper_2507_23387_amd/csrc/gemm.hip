@@ -427,7 +427,7 @@ __device__ __forceinline__ void el_tile(
   wait_vmcnt<0>();
   mfma_drain();
 
-  if constexpr (!std::is_same<Epi, NoEpilogue>::value) {
+  if constexpr (kThroughLds<Epi>) {
     constexpr int kChunk = epilogue_chunk(kWSub, kWSub, 4, kElLdsBytes);
     lds_barrier();  // every wave is done with the stages
     epilogue_tile<kWSub, kWSub, kChunk>(
@@ -439,8 +439,10 @@ __device__ __forceinline__ void el_tile(
   const int col0 = tn * kWide + wn * 128 + (lane & 15);
   const int row0 = tm * kWide + wm * 128 + (lane >> 4) * 4;
   const bool full = (tm + 1) * kWide <= M && (tn + 1) * kWide <= N;
-  store_tile16<kWSub, kWSub>(C, ldc, M, N, row0, col0, full,
-                             [&](int i, int j, int r) { return acc[i][j][r] * inv_s; });
+  const int shift = unscale_shift(epi);
+  store_tile16<kWSub, kWSub>(C, ldc, M, N, row0, col0, full, [&](int i, int j, int r) {
+    return unscaled<Epi>(acc[i][j][r] * inv_s, shift);
+  });
 }
 
 template <bool kPrefetch, bool kFusedA>
@@ -454,14 +456,13 @@ __global__ __launch_bounds__(kWideThreads, 1) void gemm_el_kernel(
 }
 
 // The same with a linear layer's epilogue (C and the residual may be one).
-template <bool kFusedA>
+template <class Epi>
 __global__ __launch_bounds__(kWideThreads, 1) void linear_el_kernel(
     uint16_t* __restrict__ a_hi, uint16_t* __restrict__ a_lo, const uint16_t* __restrict__ b_hi,
     const uint16_t* __restrict__ b_lo, const uint32_t* __restrict__ range, int Kp, int tiles_m,
-    int tiles_n, float* C, int64_t ldc, int M, int N, float s, float inv_s,
-    const float* __restrict__ af, int64_t lda, int K, Epilogue epi) {
-  el_tile<true, kFusedA>(a_hi, a_lo, b_hi, b_lo, range, Kp, tiles_m, tiles_n, C, ldc, M, N, s,
-                         inv_s, af, lda, K, epi);
+    int tiles_n, float* C, int64_t ldc, int M, int N, float s, float inv_s, Epi epi) {
+  el_tile<true, false>(a_hi, a_lo, b_hi, b_lo, range, Kp, tiles_m, tiles_n, C, ldc, M, N, s, inv_s,
+                       nullptr, 0, 0, epi);
 }
 
 // Hi-only kernel: C = A_hi B_hi, the native-FP16 GEMM baseline (Sec. 6.2),
@@ -1069,7 +1070,7 @@ __device__ __forceinline__ void n128_tile(
       return __builtin_fmaf(xb[i][j][r], inv_s, __builtin_fmaf(xa[i][j][r], inv_s, hh[i][j][r]));
     }
   };
-  if constexpr (!std::is_same<Epi, NoEpilogue>::value) {
+  if constexpr (kThroughLds<Epi>) {
     constexpr int kChunk = epilogue_chunk(kRows, kCols, 4, kTwLdsBytes);
     lds_barrier();  // every wave is done with the stages
     epilogue_tile<kRows, kCols, kChunk>(epi, reinterpret_cast<float*>(lds) + w * kChunk * kCols * 256,
@@ -1079,7 +1080,10 @@ __device__ __forceinline__ void n128_tile(
   const int col0 = tn * kTwN + (lane & 15);
   const int row0 = tm * kTwM + w * 64 + (lane >> 4) * 4;
   const bool full = (tm + 1) * kTwM <= M && (tn + 1) * kTwN <= N;
-  store_tile16<kRows, kCols>(C, ldc, M, N, row0, col0, full, value);
+  const int shift = unscale_shift(epi);
+  store_tile16<kRows, kCols>(C, ldc, M, N, row0, col0, full, [&](int i, int j, int r) {
+    return unscaled<Epi>(value(i, j, r), shift);
+  });
 }
 
 template <int V, bool kFusedA = false, bool kFusedB = false>
@@ -1094,14 +1098,14 @@ __global__ __launch_bounds__(kWideThreads, 1) void gemm_n128_kernel(
 }
 
 // The same with a linear layer's epilogue (C and the residual may be one).
-template <int V, bool kFusedA>
+template <int V, class Epi>
 __global__ __launch_bounds__(kWideThreads, 1) void linear_n128_kernel(
     const uint16_t* __restrict__ a_hi, const uint16_t* __restrict__ a_lo,
     const uint16_t* __restrict__ b_hi, const uint16_t* __restrict__ b_lo,
     const uint32_t* __restrict__ range, int Kp, int tiles_m, int tiles_n, float* C, int64_t ldc,
-    int M, int N, float inv_s, const float* __restrict__ af, int64_t lda, float s, Epilogue epi) {
-  n128_tile<V, kFusedA, false>(a_hi, a_lo, b_hi, b_lo, range, Kp, tiles_m, tiles_n, C, ldc, M, N,
-                               inv_s, af, lda, s, nullptr, 0, epi);
+    int M, int N, float inv_s, float s, Epi epi) {
+  n128_tile<V, false, false>(a_hi, a_lo, b_hi, b_lo, range, Kp, tiles_m, tiles_n, C, ldc, M, N,
+                             inv_s, nullptr, 0, s, nullptr, 0, epi);
 }
 
 template <bool kPrefetch, bool kFusedA>
@@ -1154,57 +1158,61 @@ hipError_t launch_n128(const Planes& p, int64_t M, int64_t N, float* C, int64_t 
   return hipGetLastError();
 }
 
-template <bool kFusedA>
+template <class Epi>
 hipError_t launch_linear_el(const Planes& p, int64_t M, int64_t N, float* C, int64_t ldc, float s,
-                            const Epilogue& epi, hipStream_t stream, const float* A = nullptr,
-                            int64_t lda = 0, int64_t K = 0) {
+                            const Epi& epi, hipStream_t stream) {
   static std::atomic<bool> done[kMaxDevices];
-  const hipError_t attr = set_lds(&linear_el_kernel<kFusedA>, kElLdsBytes, done);
+  const hipError_t attr = set_lds(&linear_el_kernel<Epi>, kElLdsBytes, done);
   if (attr != hipSuccess) return attr;
   const int tiles_m = static_cast<int>(p.Mp / kWide);
   const int tiles_n = static_cast<int>(p.Np / kWide);
-  hipLaunchKernelGGL((linear_el_kernel<kFusedA>), dim3(tiles_m * tiles_n), dim3(kWideThreads),
+  hipLaunchKernelGGL(linear_el_kernel<Epi>, dim3(tiles_m * tiles_n), dim3(kWideThreads),
                      kElLdsBytes, stream, p.a_hi, p.a_lo, p.b_hi, p.b_lo, p.range,
                      static_cast<int>(p.Kp), tiles_m, tiles_n, C, ldc, static_cast<int>(M),
-                     static_cast<int>(N), s, 1.0f / s, A, lda, static_cast<int>(K), epi);
+                     static_cast<int>(N), s, 1.0f / s, epi);
   return hipGetLastError();
 }
 
-template <int V, bool kFusedA>
+template <int V, class Epi>
 hipError_t launch_linear_n128(const Planes& p, int64_t M, int64_t N, float* C, int64_t ldc,
-                              float s, const Epilogue& epi, hipStream_t stream,
-                              const float* A = nullptr, int64_t lda = 0) {
+                              float s, const Epi& epi, hipStream_t stream) {
   static std::atomic<bool> done[kMaxDevices];
-  const hipError_t attr = set_lds(&linear_n128_kernel<V, kFusedA>, kTwLdsBytes, done);
+  const hipError_t attr = set_lds(&linear_n128_kernel<V, Epi>, kTwLdsBytes, done);
   if (attr != hipSuccess) return attr;
   const int tiles_m = static_cast<int>(p.Mp / kTwM);
   const int tiles_n = static_cast<int>((N + kTwN - 1) / kTwN);
-  hipLaunchKernelGGL((linear_n128_kernel<V, kFusedA>), dim3(tiles_m * tiles_n), dim3(kWideThreads),
+  hipLaunchKernelGGL((linear_n128_kernel<V, Epi>), dim3(tiles_m * tiles_n), dim3(kWideThreads),
                      kTwLdsBytes, stream, p.a_hi, p.a_lo, p.b_hi, p.b_lo, p.range,
                      static_cast<int>(p.Kp), tiles_m, tiles_n, C, ldc, static_cast<int>(M),
-                     static_cast<int>(N), 1.0f / s, A, lda, s, epi);
+                     static_cast<int>(N), 1.0f / s, s, epi);
   return hipGetLastError();
 }
 
 }  // namespace
 
+template <class Epi>
 hipError_t launch_gemm_epilogue(const Planes& p, int64_t M, int64_t N, float* C, int64_t ldc,
-                                float scale, int variant, const Epilogue& epi,
+                                float scale, int variant, const Epi& epi, bool no_overflow,
                                 hipStream_t stream) {
   if (const int tile = small_gemm_tile(M, N, p.Kp, variant, !scaled_kernel_ok(scale)))
     return launch_gemm_small_epilogue(tile, p, M, N, C, ldc, scale, variant, epi, stream);
   if (variant == kTermwise)
-    return launch_linear_n128<kTermwise, false>(p, M, N, C, ldc, scale, epi, stream);
+    return launch_linear_n128<kTermwise>(p, M, N, C, ldc, scale, epi, stream);
   const bool scaled = scaled_kernel_ok(scale);
   if (scaled) {
     const hipError_t e =
         variant == kElementwise
-            ? launch_linear_el<false>(p, M, N, C, ldc, scale, epi, stream)
-            : launch_linear_n128<kCrossScaled, false>(p, M, N, C, ldc, scale, epi, stream);
-    if (e != hipSuccess) return e;
+            ? launch_linear_el(p, M, N, C, ldc, scale, epi, stream)
+            : launch_linear_n128<kCrossScaled>(p, M, N, C, ldc, scale, epi, stream);
+    if (e != hipSuccess || no_overflow) return e;
   }
   return launch_gemm_unscaled_epilogue(p, M, N, C, ldc, scale, variant, !scaled, epi, stream);
 }
+template hipError_t launch_gemm_epilogue<Epilogue>(const Planes&, int64_t, int64_t, float*,
+                                                   int64_t, float, int, const Epilogue&, bool,
+                                                   hipStream_t);
+template hipError_t launch_gemm_epilogue<Unscale>(const Planes&, int64_t, int64_t, float*, int64_t,
+                                                  float, int, const Unscale&, bool, hipStream_t);
 
 hipError_t launch_gemm(const Planes& p, int64_t M, int64_t N, float* C, int64_t ldc,
                        float scale, int variant, hipStream_t stream) {

@@ -307,7 +307,7 @@ __device__ __forceinline__ void small_tile(const SmallArgs& g, uint16_t* lds, co
     else
       return acc[i][j][r];
   };
-  if constexpr (!std::is_same<Epi, NoEpilogue>::value) {
+  if constexpr (kThroughLds<Epi>) {
     constexpr int kChunk = epilogue_chunk(kRT, kCT, S::kWaves, S::kLdsBytes);
     static_assert(static_cast<size_t>(S::kWaves) * kChunk * kCT * 1024 <= S::kLdsBytes,
                   "the waves' staging fits the ring");
@@ -339,7 +339,10 @@ __device__ __forceinline__ void small_tile(const SmallArgs& g, uint16_t* lds, co
       return;
     }
   }
-  store_tile16<kRT, kCT>(g.C, g.ldc, g.M, g.N, row0, col0, full, value);
+  const int shift = unscale_shift(epi);
+  store_tile16<kRT, kCT>(g.C, g.ldc, g.M, g.N, row0, col0, full, [&](int i, int j, int r) {
+    return unscaled<Epi>(value(i, j, r), shift);
+  });
 }
 
 template <int V, class S, class Epi>
@@ -367,10 +370,10 @@ __global__ __launch_bounds__(64 * kWM * kWN, 1) void gemm_small_kernel(SmallArgs
 }
 
 // The same with a linear layer's epilogue.
-template <int V, int kBM, int kBN, int kWM, int kWN, int kStages>
+template <int V, int kBM, int kBN, int kWM, int kWN, int kStages, class Epi>
 __global__ __launch_bounds__(64 * kWM * kWN, 1) void linear_small_kernel(SmallArgs g,
                                                                          int unscaled_only,
-                                                                         Epilogue epi) {
+                                                                         Epi epi) {
   small_body<V, SmallShape<kBM, kBN, kWM, kWN, kStages, false>>(g, unscaled_only, epi);
 }
 
@@ -388,9 +391,9 @@ __global__ __launch_bounds__(512, 1) void gemm_unscaled_kernel(SmallArgs g, int 
   if (!unscaled_only && g.range[0] != g.range[1]) return;
   small_tile<UnscaledShape, V == kElementwise ? kElUnscaled : kCrUnscaled>(g, lds, NoEpilogue{});
 }
-template <int V>
+template <int V, class Epi>
 __global__ __launch_bounds__(512, 1) void linear_unscaled_kernel(SmallArgs g, int unscaled_only,
-                                                                 Epilogue epi) {
+                                                                 Epi epi) {
   extern __shared__ __align__(16) uint16_t lds[];
   if (!unscaled_only && g.range[0] != g.range[1]) return;
   small_tile<UnscaledShape, V == kElementwise ? kElUnscaled : kCrUnscaled>(g, lds, epi);
@@ -430,29 +433,29 @@ hipError_t launch_unscaled(const Planes& p, int64_t M, int64_t N, float* C, int6
   return hipGetLastError();
 }
 
-template <int V>
+template <int V, class Epi>
 hipError_t launch_unscaled_epilogue(const Planes& p, int64_t M, int64_t N, float* C, int64_t ldc,
-                                    float s, bool only, const Epilogue& epi, hipStream_t stream) {
+                                    float s, bool only, const Epi& epi, hipStream_t stream) {
   using S = UnscaledShape;
   static std::atomic<bool> done[kMaxDevices];
-  const hipError_t attr = set_lds(&linear_unscaled_kernel<V>, S::kLdsBytes, done);
+  const hipError_t attr = set_lds(&linear_unscaled_kernel<V, Epi>, S::kLdsBytes, done);
   if (attr != hipSuccess) return attr;
   const SmallArgs g = small_args<S>(p, M, N, C, ldc, s, RangeOpts{}, nullptr);
-  hipLaunchKernelGGL(linear_unscaled_kernel<V>, dim3(g.tiles_m * g.tiles_n), dim3(S::kThreads),
+  hipLaunchKernelGGL((linear_unscaled_kernel<V, Epi>), dim3(g.tiles_m * g.tiles_n), dim3(S::kThreads),
                      S::kLdsBytes, stream, g, only ? 1 : 0, epi);
   return hipGetLastError();
 }
 
-template <int V, int kBM, int kBN, int kWM, int kWN, int kStages>
+template <int V, int kBM, int kBN, int kWM, int kWN, int kStages, class Epi>
 hipError_t launch_small_epilogue(const Planes& p, int64_t M, int64_t N, float* C, int64_t ldc,
-                                 float s, const Epilogue& epi, hipStream_t stream) {
+                                 float s, const Epi& epi, hipStream_t stream) {
   using S = SmallShape<kBM, kBN, kWM, kWN, kStages, false>;
   static std::atomic<bool> done[kMaxDevices];
   const hipError_t attr =
-      set_lds(&linear_small_kernel<V, kBM, kBN, kWM, kWN, kStages>, S::kLdsBytes, done);
+      set_lds(&linear_small_kernel<V, kBM, kBN, kWM, kWN, kStages, Epi>, S::kLdsBytes, done);
   if (attr != hipSuccess) return attr;
   const SmallArgs g = small_args<S>(p, M, N, C, ldc, s, RangeOpts{}, nullptr);
-  hipLaunchKernelGGL((linear_small_kernel<V, kBM, kBN, kWM, kWN, kStages>),
+  hipLaunchKernelGGL((linear_small_kernel<V, kBM, kBN, kWM, kWN, kStages, Epi>),
                      dim3(g.tiles_m * g.tiles_n), dim3(S::kThreads), S::kLdsBytes, stream, g,
                      scaled_kernel_ok(s) ? 0 : 1, epi);
   return hipGetLastError();
@@ -517,9 +520,9 @@ hipError_t launch_config(int tile, const Planes& p, int64_t M, int64_t N, float*
   });
 }
 
-template <int V>
+template <int V, class Epi>
 hipError_t launch_config_epilogue(int tile, const Planes& p, int64_t M, int64_t N, float* C,
-                                  int64_t ldc, float s, const Epilogue& epi, hipStream_t stream) {
+                                  int64_t ldc, float s, const Epi& epi, hipStream_t stream) {
   return with_config<V>(tile, [&](auto c) {
     using T = decltype(c);
     return launch_small_epilogue<V, T::kBM, T::kBN, T::kWM, T::kWN, T::kStages>(p, M, N, C, ldc, s, epi, stream);
@@ -660,8 +663,9 @@ hipError_t launch_gemm_small(int tile, const Planes& p, int64_t M, int64_t N, fl
   }
 }
 
+template <class Epi>
 hipError_t launch_gemm_small_epilogue(int tile, const Planes& p, int64_t M, int64_t N, float* C,
-                                      int64_t ldc, float scale, int variant, const Epilogue& epi,
+                                      int64_t ldc, float scale, int variant, const Epi& epi,
                                       hipStream_t stream) {
   switch (variant) {
     case kElementwise:
@@ -674,9 +678,10 @@ hipError_t launch_gemm_small_epilogue(int tile, const Planes& p, int64_t M, int6
   }
 }
 
+template <class Epi>
 hipError_t launch_gemm_unscaled_epilogue(const Planes& p, int64_t M, int64_t N, float* C,
                                          int64_t ldc, float scale, int variant, bool only,
-                                         const Epilogue& epi, hipStream_t stream) {
+                                         const Epi& epi, hipStream_t stream) {
   switch (variant) {
     case kElementwise:
       return launch_unscaled_epilogue<kElementwise>(p, M, N, C, ldc, scale, only, epi, stream);
@@ -685,5 +690,18 @@ hipError_t launch_gemm_unscaled_epilogue(const Planes& p, int64_t M, int64_t N, 
     default: return hipErrorInvalidValue;
   }
 }
+
+template hipError_t launch_gemm_small_epilogue<Epilogue>(int, const Planes&, int64_t, int64_t,
+                                                         float*, int64_t, float, int,
+                                                         const Epilogue&, hipStream_t);
+template hipError_t launch_gemm_small_epilogue<Unscale>(int, const Planes&, int64_t, int64_t,
+                                                        float*, int64_t, float, int,
+                                                        const Unscale&, hipStream_t);
+template hipError_t launch_gemm_unscaled_epilogue<Epilogue>(const Planes&, int64_t, int64_t, float*,
+                                                            int64_t, float, int, bool,
+                                                            const Epilogue&, hipStream_t);
+template hipError_t launch_gemm_unscaled_epilogue<Unscale>(const Planes&, int64_t, int64_t, float*,
+                                                           int64_t, float, int, bool,
+                                                           const Unscale&, hipStream_t);
 
 }  // namespace sgc

@@ -58,7 +58,7 @@ struct ColumnArgs {
 };
 hipError_t launch_columns(const ColumnArgs& a, hipStream_t stream);
 
-// What follows a product P: Y = act(Z) + R, Z = 2^-shift P + bias.
+// What follows a product P: Y = act(Z) + R, Z = P + bias.
 struct Epilogue {
   const float* bias;  // null: none
   int activation;
@@ -66,24 +66,32 @@ struct Epilogue {
   int64_t ldr;
   float* z;           // null: not kept
   int64_t ldz;
-  const uint32_t* max_bits;  // shift = prescale_shift(*max_bits, target); null: 0
+};
+// A gradient's product: 2^-prescale_shift(*max_bits, target) P.
+struct Unscale {
+  const uint32_t* max_bits;
   int target;
 };
 // The epilogue where K = 0: P = 0.
 hipError_t launch_epilogue(const Epilogue& e, int64_t M, int64_t N, float* Y, int64_t ldy,
                            hipStream_t stream);
 
-// launch_gemm, launch_gemm_small and launch_gemm_unscaled with an epilogue; the
-// product's bits are theirs.  C may be the residual.
+// launch_gemm, launch_gemm_small and launch_gemm_unscaled with an epilogue (Epi:
+// Epilogue or Unscale); the product's bits are theirs.  C may be the residual.
+// no_overflow: s B_hi is known to be finite, so that the scaled kernels need no
+// fallback.
+template <class Epi>
 hipError_t launch_gemm_epilogue(const Planes& p, int64_t M, int64_t N, float* C, int64_t ldc,
-                                float scale, int variant, const Epilogue& epi,
+                                float scale, int variant, const Epi& epi, bool no_overflow,
                                 hipStream_t stream);
+template <class Epi>
 hipError_t launch_gemm_small_epilogue(int tile, const Planes& p, int64_t M, int64_t N, float* C,
-                                      int64_t ldc, float scale, int variant, const Epilogue& epi,
+                                      int64_t ldc, float scale, int variant, const Epi& epi,
                                       hipStream_t stream);
+template <class Epi>
 hipError_t launch_gemm_unscaled_epilogue(const Planes& p, int64_t M, int64_t N, float* C,
                                          int64_t ldc, float scale, int variant, bool only,
-                                         const Epilogue& epi, hipStream_t stream);
+                                         const Epi& epi, hipStream_t stream);
 
 struct LinearArgs {
   int64_t M, N, K;
@@ -98,6 +106,13 @@ struct LinearArgs {
   float scale;
   int variant;
 };
+
+// The linear layer for few rows (linear_rows.hip), its sums termwise whatever the
+// variant.  linear_by_rows: the rule that chooses it.
+bool linear_by_rows(int64_t M, int64_t N);
+size_t linear_rows_ws(int64_t M, int64_t N, int64_t K);
+hipError_t launch_linear_rows(const LinearArgs& a, void* ws, hipStream_t stream);
+
 size_t linear_ws(int64_t M, int64_t N, int64_t K);
 hipError_t launch_linear(const LinearArgs& a, void* ws, hipStream_t stream);
 

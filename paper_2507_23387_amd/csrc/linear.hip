@@ -64,8 +64,19 @@ int target_b(float scale, int variant) {
 
 }  // namespace
 
+// Few rows: every 64 rows read W once more, as FP32, where the tiles read it,
+// write its planes and read those for every 32 to 256 rows.  On N, K = 256 .. 8192,
+// rows against tiles, us: 64 x 4096 x 4096 27 and 42, 128 x 4096 x 4096 38 and 51, 128
+// x 8192 x 8192 120 and 185, 256 x 512 x 4096 17 and 26; 192 x 4096 x 4096 49 and 54,
+// 256 x 2048 x 2048 23 and 28, but 256 x 4096 x 4096 59 and 58, 192 x 8192 x 4096 89 to
+// 106 and 96, 384 x 2048 x 4096 45 to 52 and 45.
+bool linear_by_rows(int64_t M, int64_t N) {
+  return M <= 128 || (M <= 256 && M * N <= 800000);
+}
+
 size_t linear_ws(int64_t M, int64_t N, int64_t K) {
   if (M == 0 || N == 0 || K == 0) return 0;
+  if (linear_by_rows(M, N)) return linear_rows_ws(M, N, K);
   Carver c{nullptr, 0};
   (void)carve_planes(c, M, N, K);
   return c.used;
@@ -73,6 +84,7 @@ size_t linear_ws(int64_t M, int64_t N, int64_t K) {
 
 hipError_t launch_linear(const LinearArgs& a, void* ws, hipStream_t stream) {
   if (a.K == 0) return launch_epilogue(a.e, a.M, a.N, a.y, a.ldy, stream);
+  if (linear_by_rows(a.M, a.N)) return launch_linear_rows(a, ws, stream);
   Carver c{static_cast<char*>(ws), 0};
   const Planes p = carve_planes(c, a.M, a.N, a.K);
   SplitJob jobs[2] = {job_of(a.x, a.ldx, a.M, a.K),
@@ -82,7 +94,8 @@ hipError_t launch_linear(const LinearArgs& a, void* ws, hipStream_t stream) {
   to_planes(jobs[1], p, true, !a.transpose_w);
   const hipError_t err = launch_split_jobs(jobs, 2, a.scale, stream);
   if (err != hipSuccess) return err;
-  return launch_gemm_epilogue(p, a.M, a.N, a.y, a.ldy, a.scale, a.variant, a.e, stream);
+  return launch_gemm_epilogue(p, a.M, a.N, a.y, a.ldy, a.scale, a.variant, a.e, false,
+                              stream);
 }
 
 namespace {
@@ -134,7 +147,7 @@ hipError_t launch_linear_grad(const LinearGradArgs& a, void* ws, hipStream_t str
   int count = 0;
   SplitJob d = job_of(a.dy, a.lddy, a.M, a.N);
   d.z = a.z, d.ldz = a.ldz, d.activation = a.activation, d.max_bits = g.max_bits;
-  Epilogue ex{}, ew{};
+  Unscale ex{}, ew{};
   ex.max_bits = ew.max_bits = g.max_bits;
   if (dx) {
     // dX = D W^T: D's rows and W's K rows, k over N.
@@ -154,10 +167,12 @@ hipError_t launch_linear_grad(const LinearGradArgs& a, void* ws, hipStream_t str
   jobs[count++] = d;
   err = launch_split_jobs(jobs, count, a.scale, stream);
   if (err == hipSuccess && dx)
-    err = launch_gemm_epilogue(g.dx, a.M, a.K, a.dx, a.lddx, a.scale, a.variant, ex, stream);
+    err = launch_gemm_epilogue(g.dx, a.M, a.K, a.dx, a.lddx, a.scale, a.variant, ex, false,
+                               stream);
+  // As B, D is scaled so that s B_hi is finite.
   if (err == hipSuccess && dw)
     err = launch_gemm_epilogue(g.dw, dw_rows, dw_cols, a.dw, a.lddw, a.scale, a.variant, ew,
-                               stream);
+                               !a.transpose_w, stream);
   return err;
 }
 

@@ -10,7 +10,8 @@ namespace sgc {
 namespace {
 
 constexpr int kThreads = 256;
-typedef float floatx4_u __attribute__((ext_vector_type(4), aligned(4)));
+typedef float floatx4v __attribute__((ext_vector_type(4)));
+typedef float floatx4_u __attribute__((ext_vector_type(4), aligned(4)));  // at any address
 
 // Elements (i, j .. j + 7) of a rows x cols matrix, zeros outside it.
 __device__ __forceinline__ void load8(const float* p, int64_t ld, int64_t i, int64_t j,
@@ -127,6 +128,9 @@ __global__ __launch_bounds__(kThreads) void split_jobs_kernel(SplitArgs a) {
   }
 }
 
+// Rows that a thread has in flight.
+constexpr int kColumnRows = 4;
+
 // Sums of 128 columns over a slab of rows: thread t has columns 4 (t % 32) .. + 3
 // of every eighth row.
 __global__ __launch_bounds__(kThreads) void columns_kernel(ColumnArgs a, int64_t slab_rows) {
@@ -136,16 +140,40 @@ __global__ __launch_bounds__(kThreads) void columns_kernel(ColumnArgs a, int64_t
   const int64_t j = static_cast<int64_t>(blockIdx.x) * kColumnStrip + 4 * (t & 31);
   const int64_t i0 = blockIdx.y * slab_rows, i1 = min(a.M, i0 + slab_rows);
   float s[4] = {0.0f, 0.0f, 0.0f, 0.0f}, m = 0.0f;
-  for (int64_t i = i0 + (t >> 5); i < i1; i += kThreads / 32) {
+  auto add = [&](const float (&d)[4]) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      if (j + e >= a.N) continue;
-      float d = a.dy[i * a.lddy + j + e];
-      if (a.z) d *= activate_grad(a.activation, a.z[i * a.ldz + j + e]);
-      s[e] += d;
-      const float b = __builtin_fabsf(d);
+      s[e] += d[e];
+      const float b = __builtin_fabsf(d[e]);
       if (b <= 3.4028235e38f) m = __builtin_fmaxf(m, b);
     }
+  };
+  constexpr int kStride = kThreads / 32;
+  int64_t i = i0 + (t >> 5);
+  if (j + 3 < a.N) {
+    for (; i + (kColumnRows - 1) * kStride < i1; i += kColumnRows * kStride) {
+      floatx4v d[kColumnRows], z[kColumnRows];
+#pragma unroll
+      for (int u = 0; u < kColumnRows; ++u)
+        d[u] = *reinterpret_cast<const floatx4_u*>(a.dy + (i + u * kStride) * a.lddy + j);
+      if (a.z) {
+#pragma unroll
+        for (int u = 0; u < kColumnRows; ++u)
+          z[u] = *reinterpret_cast<const floatx4_u*>(a.z + (i + u * kStride) * a.ldz + j);
+        multiply_grad(a.activation, d, z);
+      }
+#pragma unroll
+      for (int u = 0; u < kColumnRows; ++u) add({d[u][0], d[u][1], d[u][2], d[u][3]});
+    }
+  }
+  for (; i < i1; i += kStride) {
+    float d[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      d[e] = j + e < a.N ? a.dy[i * a.lddy + j + e] : 0.0f;
+      if (a.z && j + e < a.N) d[e] *= activate_grad(a.activation, a.z[i * a.ldz + j + e]);
+    }
+    add(d);
   }
 #pragma unroll
   for (int e = 0; e < 4; ++e) part[t >> 5][4 * (t & 31) + e] = s[e];
@@ -166,31 +194,43 @@ __global__ __launch_bounds__(kThreads) void columns_kernel(ColumnArgs a, int64_t
                                             __builtin_fmaxf(top[2], top[3]));
 }
 
-// Joins the slabs: blocks 0 .. strips - 1 a strip of columns each, the last the
-// magnitudes.
+// Joins the slabs: every workgroup but the last has 32 columns, every eighth slab a
+// thread; the last the magnitudes.
+constexpr int kJoinCols = 32, kJoinGroups = kThreads / kJoinCols;
 __global__ __launch_bounds__(kThreads) void columns_join_kernel(ColumnArgs a, int64_t slabs,
                                                                 int64_t strips) {
+  __shared__ float part[kJoinGroups][kJoinCols];
   const int t = threadIdx.x;
   const int64_t pitch = a.N + strips;
   if (blockIdx.x < gridDim.x - 1) {
-    const int64_t j = static_cast<int64_t>(blockIdx.x) * kThreads + t;
-    if (j >= a.N || !a.dbias) return;
+    if (!a.dbias) return;
+    const int c = t % kJoinCols, g = t / kJoinCols;
+    const int64_t j = static_cast<int64_t>(blockIdx.x) * kJoinCols + c;
     float s = 0.0f;
-    for (int64_t g = 0; g < slabs; ++g) s += a.partial[g * pitch + j];
+    if (j < a.N) {
+#pragma unroll 4
+      for (int64_t n = g; n < slabs; n += kJoinGroups) s += a.partial[n * pitch + j];
+    }
+    part[g][c] = s;
+    __syncthreads();
+    if (g != 0 || j >= a.N) return;
+#pragma unroll
+    for (int q = 1; q < kJoinGroups; ++q) s += part[q][c];
     a.dbias[j] = s;
     return;
   }
-  __shared__ float top[kThreads / 64];
   float m = 0.0f;
+#pragma unroll 4
   for (int64_t n = t; n < slabs * strips; n += kThreads)
     m = __builtin_fmaxf(m, a.partial[n / strips * pitch + a.N + n % strips]);
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, off));
-  if ((t & 63) == 0) top[t >> 6] = m;
+  if ((t & 63) == 0) part[0][t >> 6] = m;
   __syncthreads();
   if (t == 0)
-    *a.max_bits = __builtin_bit_cast(uint32_t, __builtin_fmaxf(__builtin_fmaxf(top[0], top[1]),
-                                                               __builtin_fmaxf(top[2], top[3])));
+    *a.max_bits = __builtin_bit_cast(
+        uint32_t, __builtin_fmaxf(__builtin_fmaxf(part[0][0], part[0][1]),
+                                  __builtin_fmaxf(part[0][2], part[0][3])));
 }
 
 // The epilogue of a product without terms: Z = bias.
@@ -239,7 +279,7 @@ hipError_t launch_columns(const ColumnArgs& a, hipStream_t stream) {
                      dim3(kThreads), 0, stream, a, (a.M + slabs - 1) / slabs);
   if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   hipLaunchKernelGGL(columns_join_kernel,
-                     dim3(static_cast<unsigned>((a.N + kThreads - 1) / kThreads + 1)),
+                     dim3(static_cast<unsigned>((a.N + kJoinCols - 1) / kJoinCols + 1)),
                      dim3(kThreads), 0, stream, a, slabs, strips);
   return hipGetLastError();
 }
