@@ -38,11 +38,28 @@ struct SplitJob {
   uint32_t row_stamp, col_stamp;
 };
 constexpr int kSplitJobs = 3;
-hipError_t launch_split_jobs(const SplitJob* jobs, int count, float scale, hipStream_t stream);
+// The join of launch_columns' slabs, for a split launch to do on the way: `tops`
+// magnitudes, of which each workgroup of a job with max_bits takes the largest, the
+// first also writing it to *max_bits, and slabs x N sums that workgroups of their
+// own add up to dbias (null: none).
+struct ColumnJoin {
+  const float* top;
+  int tops;
+  uint32_t* max_bits;
+  const float* sums;
+  int slabs;
+  int64_t N;
+  float* dbias;
+};
+hipError_t launch_split_jobs(const SplitJob* jobs, int count, float scale, hipStream_t stream,
+                             const ColumnJoin* join = nullptr);
+// Workgroups of such a launch without the join's own.
+int64_t split_jobs_blocks(const SplitJob* jobs, int count);
 
-// The sums of D = dY act'(Z)'s columns in `dbias` (null: none) and the bits of
-// its largest finite magnitude in *max_bits.  `partial` holds
-// column_slabs(M, N) x (N + ceil(N / kColumnStrip)) floats.
+// The sums of D = dY act'(Z)'s columns and its largest finite magnitude, per slab of
+// rows and strip of columns, in `partial`: column_slabs(M, N) x N sums, then
+// column_slabs(M, N) x ceil(N / kColumnStrip) magnitudes.  launch_columns_join forms
+// dbias (null: none) and the bits of the largest magnitude in *max_bits.
 constexpr int kColumnStrip = 128;
 int64_t column_slabs(int64_t M, int64_t N);
 struct ColumnArgs {
@@ -55,8 +72,11 @@ struct ColumnArgs {
   float* dbias;
   uint32_t* max_bits;
   float* partial;
+  float* d;  // null, or M x N that receives D
 };
 hipError_t launch_columns(const ColumnArgs& a, hipStream_t stream);
+ColumnJoin column_join(const ColumnArgs& a);
+hipError_t launch_columns_join(const ColumnJoin& j, hipStream_t stream);
 
 // What follows a product P: Y = act(Z) + R, Z = P + bias.
 struct Epilogue {
@@ -108,10 +128,13 @@ struct LinearArgs {
 };
 
 // The linear layer for few rows (linear_rows.hip), its sums termwise whatever the
-// variant.  linear_by_rows: the rule that chooses it.
+// variant.  linear_by_rows: the rule that chooses it.  With `grad`, x is a gradient
+// that is multiplied by the power of two of grad's Unscale as it is split, and the
+// result is freed of it again.
 bool linear_by_rows(int64_t M, int64_t N);
 size_t linear_rows_ws(int64_t M, int64_t N, int64_t K);
-hipError_t launch_linear_rows(const LinearArgs& a, void* ws, hipStream_t stream);
+hipError_t launch_linear_rows(const LinearArgs& a, const Unscale* grad, void* ws,
+                              hipStream_t stream);
 
 size_t linear_ws(int64_t M, int64_t N, int64_t K);
 hipError_t launch_linear(const LinearArgs& a, void* ws, hipStream_t stream);

@@ -54,6 +54,9 @@ void to_planes(SplitJob& j, const Planes& p, bool side_b, bool columns) {
   }
 }
 
+// Most tiles of a split that also joins the column sums.
+constexpr int64_t kSplitJoinBlocks = 2048;
+
 // Target exponents of a pre-scaled operand (api.hip's range_opts): as A, and as
 // B, where the scaled kernels form s B_hi in FP16.
 int target_a(float scale) { return std::min(14, 26 - std::ilogb(scale)); }
@@ -84,7 +87,7 @@ size_t linear_ws(int64_t M, int64_t N, int64_t K) {
 
 hipError_t launch_linear(const LinearArgs& a, void* ws, hipStream_t stream) {
   if (a.K == 0) return launch_epilogue(a.e, a.M, a.N, a.y, a.ldy, stream);
-  if (linear_by_rows(a.M, a.N)) return launch_linear_rows(a, ws, stream);
+  if (linear_by_rows(a.M, a.N)) return launch_linear_rows(a, nullptr, ws, stream);
   Carver c{static_cast<char*>(ws), 0};
   const Planes p = carve_planes(c, a.M, a.N, a.K);
   SplitJob jobs[2] = {job_of(a.x, a.ldx, a.M, a.K),
@@ -100,9 +103,15 @@ hipError_t launch_linear(const LinearArgs& a, void* ws, hipStream_t stream) {
 
 namespace {
 
+// Whether dX = D W^T (M x K, k over N) goes by rows.  D is then written as FP32 by
+// the kernel that sums its columns, where an activation makes it other than dY.
+bool grad_by_rows(int64_t M, int64_t K) { return linear_by_rows(M, K); }
+
 struct GradWorkspace {
   uint32_t* max_bits;
   float* partial;
+  void* rows;  // launch_linear_rows' workspace
+  float* d;    // M x N, by rows
   Planes dx, dw;
   size_t bytes;
 };
@@ -113,8 +122,15 @@ GradWorkspace carve_grad(void* ws, int64_t M, int64_t N, int64_t K, bool transpo
   g.max_bits = c.take<uint32_t>(1);
   const int64_t strips = (N + kColumnStrip - 1) / kColumnStrip;
   g.partial = c.take<float>(column_slabs(M, N) * (N + strips));
-  g.dx = carve_planes(c, M, K, N);
-  g.dw = transpose_w ? carve_planes(c, N, K, M) : carve_planes(c, K, N, M);
+  if (K > 0) {
+    if (grad_by_rows(M, K)) {
+      g.rows = c.take<char>(static_cast<int64_t>(linear_rows_ws(M, K, N)));
+      g.d = c.take<float>(M * N);
+    } else {
+      g.dx = carve_planes(c, M, K, N);
+    }
+    g.dw = transpose_w ? carve_planes(c, N, K, M) : carve_planes(c, K, N, M);
+  }
   g.bytes = c.used;
   return g;
 }
@@ -137,21 +153,23 @@ hipError_t launch_linear_grad(const LinearGradArgs& a, void* ws, hipStream_t str
     return err;
   }
   const GradWorkspace g = carve_grad(ws, a.M, a.N, a.K, a.transpose_w);
-  const ColumnArgs cols{a.M, a.N, a.dy, a.lddy, a.z, a.ldz, a.activation, a.dbias, g.max_bits,
-                        g.partial};
-  err = launch_columns(cols, stream);
   const bool dx = a.dx && a.K > 0, dw = a.dw && a.K > 0;
-  if (err != hipSuccess || (!dx && !dw)) return err;
+  const bool dx_rows = dx && grad_by_rows(a.M, a.K);
+  const ColumnArgs cols{a.M, a.N, a.dy, a.lddy, a.z, a.ldz, a.activation, a.dbias, g.max_bits,
+                        g.partial, dx_rows && a.z ? g.d : nullptr};
+  const ColumnJoin join = column_join(cols);
 
   SplitJob jobs[kSplitJobs];
   int count = 0;
-  SplitJob d = job_of(a.dy, a.lddy, a.M, a.N);
-  d.z = a.z, d.ldz = a.ldz, d.activation = a.activation, d.max_bits = g.max_bits;
+  SplitJob d = cols.d ? job_of(cols.d, a.N, a.M, a.N) : job_of(a.dy, a.lddy, a.M, a.N);
+  if (!cols.d) d.z = a.z, d.ldz = a.ldz, d.activation = a.activation;
+  d.max_bits = g.max_bits;
   Unscale ex{}, ew{};
   ex.max_bits = ew.max_bits = g.max_bits;
-  if (dx) {
+  ex.target = target_a(a.scale);
+  if (dx && !dx_rows) {
     // dX = D W^T: D's rows and W's K rows, k over N.
-    d.row_target = ex.target = target_a(a.scale);
+    d.row_target = ex.target;
     to_planes(d, g.dx, false, false);
     jobs[count] = a.transpose_w ? job_of(a.w, a.ldw, a.N, a.K) : job_of(a.w, a.ldw, a.K, a.N);
     to_planes(jobs[count++], g.dx, true, a.transpose_w);
@@ -164,11 +182,28 @@ hipError_t launch_linear_grad(const LinearGradArgs& a, void* ws, hipStream_t str
     jobs[count] = job_of(a.x, a.ldx, a.M, a.K);
     to_planes(jobs[count++], g.dw, a.transpose_w, true);
   }
-  jobs[count++] = d;
-  err = launch_split_jobs(jobs, count, a.scale, stream);
-  if (err == hipSuccess && dx)
+  if (count > 0) jobs[count++] = d;
+
+  // A split of few tiles joins the column sums itself: every one of its workgroups
+  // reads the magnitudes, 2 us, instead of a launch between (777 x 1003 x 530: 39
+  // us with it).
+  const bool split_joins = count > 0 && split_jobs_blocks(jobs, count) <= kSplitJoinBlocks;
+  err = launch_columns(cols, stream);
+  if (err == hipSuccess && !split_joins) err = launch_columns_join(join, stream);
+  if (err == hipSuccess && count > 0)
+    err = launch_split_jobs(jobs, count, a.scale, stream, split_joins ? &join : nullptr);
+  if (err == hipSuccess && dx_rows) {
+    LinearArgs r{};
+    r.M = a.M, r.N = a.K, r.K = a.N;
+    r.x = d.s, r.ldx = d.ld;
+    r.w = a.w, r.ldw = a.ldw, r.transpose_w = !a.transpose_w;
+    r.y = a.dx, r.ldy = a.lddx;
+    r.scale = a.scale, r.variant = a.variant;
+    err = launch_linear_rows(r, &ex, g.rows, stream);
+  } else if (err == hipSuccess && dx) {
     err = launch_gemm_epilogue(g.dx, a.M, a.K, a.dx, a.lddx, a.scale, a.variant, ex, false,
                                stream);
+  }
   // As B, D is scaled so that s B_hi is finite.
   if (err == hipSuccess && dw)
     err = launch_gemm_epilogue(g.dw, dw_rows, dw_cols, a.dw, a.lddw, a.scale, a.variant, ew,

@@ -32,6 +32,16 @@ typedef _Float16 half2 __attribute__((ext_vector_type(2)));
 // Eight values and their split (Sec. 3.3): hi = fl16(v), lo = fl16((v - hi) s).
 struct Values {
   float v[8];
+  // Times 2^shift, for a gradient.
+  template <bool kGrad>
+  __device__ __forceinline__ Values shifted(int shift) const {
+    Values x = *this;
+    if constexpr (kGrad) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x.v[e] = __builtin_ldexpf(x.v[e], shift);
+    }
+    return x;
+  }
   __device__ __forceinline__ void split(float s, half8& hi, half8& lo) const {
 #pragma unroll
     for (int e = 0; e < 8; e += 2) {
@@ -83,13 +93,18 @@ __device__ __forceinline__ void load_across(const float* col, int64_t ldw, int64
 
 struct RowsArgs {
   LinearArgs a;
+  bool grad;
+  Unscale unscale;
   float inv_s;
   int groups;      // of columns
   int splits;      // workgroups that share a group's k
   float* partial;  // splits x M x N, where splits > 1
 };
 
-__device__ __forceinline__ float finish(const Epilogue& e, int64_t i, int64_t j, float z) {
+__device__ __forceinline__ float finish(const RowsArgs& g, int64_t i, int64_t j, float z) {
+  const Epilogue& e = g.a.e;
+  if (g.grad)
+    return __builtin_ldexpf(z, -prescale_shift(*g.unscale.max_bits, g.unscale.target));
   if (e.bias) z += e.bias[j];
   if (e.z) e.z[i * e.ldz + j] = z;
   const float y = activate(e.activation, z);
@@ -99,7 +114,7 @@ __device__ __forceinline__ float finish(const Epilogue& e, int64_t i, int64_t j,
 // Sum v of this split for entry (i, j): the result, or a partial sum.
 __device__ __forceinline__ void store(const RowsArgs& g, int split, int64_t i, int64_t j, float v) {
   if (g.splits == 1)
-    g.a.y[i * g.a.ldy + j] = finish(g.a.e, i, j, v);
+    g.a.y[i * g.a.ldy + j] = finish(g, i, j, v);
   else
     g.partial[(split * g.a.M + i) * g.a.N + j] = v;
 }
@@ -110,7 +125,7 @@ __device__ __forceinline__ void store(const RowsArgs& g, int split, int64_t i, i
 // TB/s (64 columns a workgroup as below 30; 8 waves 28.6; one column block 30).
 constexpr int kLineWaves = 16;
 
-template <int kC>
+template <int kC, bool kGrad>
 __global__ __launch_bounds__(64 * kLineWaves) void linear_line_kernel(RowsArgs g) {
   const LinearArgs& a = g.a;
   __shared__ float tile[kLineWaves][256 * kC];
@@ -121,6 +136,7 @@ __global__ __launch_bounds__(64 * kLineWaves) void linear_line_kernel(RowsArgs g
   const int64_t col0 = static_cast<int64_t>(col_group) * (16 * kC);
   // Rows and columns past the end repeat the last; they are not stored.
   const float* const xrow = a.x + min<int64_t>(l16, a.M - 1) * a.ldx;
+  const int shift = kGrad ? prescale_shift(*g.unscale.max_bits, g.unscale.target) : 0;
   const float* wrow[kC];
 #pragma unroll
   for (int c = 0; c < kC; ++c) wrow[c] = a.w + min<int64_t>(col0 + 16 * c + l16, a.N - 1) * a.ldw;
@@ -139,7 +155,7 @@ __global__ __launch_bounds__(64 * kLineWaves) void linear_line_kernel(RowsArgs g
   for (int c = 0; c < kC; ++c) hh[c] = cross[c] = floatx4{};
   auto multiply = [&](const Step& s) {
     half8 xh, xl;
-    s.x.split(a.scale, xh, xl);
+    s.x.template shifted<kGrad>(shift).split(a.scale, xh, xl);
 #pragma unroll
     for (int c = 0; c < kC; ++c) {
       half8 wh, wl;
@@ -206,7 +222,7 @@ __global__ __launch_bounds__(64 * kLineWaves) void linear_line_kernel(RowsArgs g
 constexpr int kTileWaves = 4, kTileCols = 16 * kTileWaves;
 constexpr int kChunkSteps = 2, kChunkK = kChunkSteps * kStep;
 
-template <bool kNk, int kR>
+template <bool kNk, int kR, bool kGrad>
 __global__ __launch_bounds__(64 * kTileWaves, 3) void linear_rows_tile_kernel(RowsArgs g) {
   const LinearArgs& a = g.a;
   constexpr int kUnits = kChunkSteps * kR;  // fragments of a chunk of X, of each plane
@@ -230,9 +246,10 @@ __global__ __launch_bounds__(64 * kTileWaves, 3) void linear_rows_tile_kernel(Ro
 #pragma unroll
   for (int n = 0; n < kPer; ++n) {
     unit[n] = min(wave + kTileWaves * n, kUnits - 1);
-    xrow[n] = a.x + min<int64_t>(row0 + 16 * (unit[n] % kR) + l16, a.M - 1) * a.ldx +
-              unit[n] / kR * kStep;
+    xrow[n] = a.x + min<int64_t>(row0 + 16 * (unit[n] % kR) + l16, a.M - 1) * a.ldx;
   }
+
+  const int shift = kGrad ? prescale_shift(*g.unscale.max_bits, g.unscale.target) : 0;
 
   Values w[2][kChunkSteps], x[kPer];
   auto load_w = [&](int64_t c, int st, Values& to, auto tail) {
@@ -245,13 +262,13 @@ __global__ __launch_bounds__(64 * kTileWaves, 3) void linear_rows_tile_kernel(Ro
   auto load_x = [&](int64_t c, auto tail) {
 #pragma unroll
     for (int n = 0; n < kPer; ++n)
-      load_along<kNk, tail.value>(xrow[n], c * kChunkK, a.K - unit[n] / kR * kStep, group, x[n]);
+      load_along<kNk, tail.value>(xrow[n], c * kChunkK + unit[n] / kR * kStep, a.K, group, x[n]);
   };
   auto store_x = [&](int slot) {
 #pragma unroll
     for (int n = 0; n < kPer; ++n) {
       half8 hi, lo;
-      x[n].split(a.scale, hi, lo);
+      x[n].template shifted<kGrad>(shift).split(a.scale, hi, lo);
       half8* const at = frags + ((slot * kUnits + unit[n]) * 2) * 64 + lane;
       at[0] = hi;
       at[64] = lo;
@@ -343,7 +360,7 @@ __global__ __launch_bounds__(256) void linear_join_kernel(RowsArgs g) {
   float v = 0.0f;
 #pragma unroll 4
   for (int s = 0; s < g.splits; ++s) v += g.partial[s * a.M * a.N + q];
-  a.y[i * a.ldy + j] = finish(a.e, i, j, v);
+  a.y[i * a.ldy + j] = finish(g, i, j, v);
 }
 
 struct RowsPlan {
@@ -375,30 +392,40 @@ RowsPlan plan_rows(int64_t M, int64_t N, int64_t K, bool transpose_w) {
   return p;
 }
 
-template <int kC>
+template <int kC, bool kGrad>
 hipError_t launch_line(const RowsArgs& g, const RowsPlan& p, hipStream_t stream) {
-  hipLaunchKernelGGL(linear_line_kernel<kC>, dim3(p.groups * p.splits), dim3(64 * kLineWaves), 0,
-                     stream, g);
+  hipLaunchKernelGGL((linear_line_kernel<kC, kGrad>), dim3(p.groups * p.splits),
+                     dim3(64 * kLineWaves), 0, stream, g);
   return hipGetLastError();
 }
 
-template <bool kNk, int kR>
+template <bool kNk, int kR, bool kGrad>
 hipError_t launch_tile(const RowsArgs& g, const RowsPlan& p, hipStream_t stream) {
   constexpr size_t kLds = static_cast<size_t>(2) * kChunkSteps * kR * 2 * 1024;
   static_assert(kLds <= 64 * 1024, "both chunks fit LDS without asking for more");
-  hipLaunchKernelGGL((linear_rows_tile_kernel<kNk, kR>), dim3(p.groups * p.splits, p.row_groups),
-                     dim3(64 * kTileWaves), kLds, stream, g);
+  hipLaunchKernelGGL((linear_rows_tile_kernel<kNk, kR, kGrad>),
+                     dim3(p.groups * p.splits, p.row_groups), dim3(64 * kTileWaves), kLds, stream,
+                     g);
   return hipGetLastError();
 }
 
-template <bool kNk>
+template <bool kNk, bool kGrad>
 hipError_t launch_tiles(const RowsArgs& g, const RowsPlan& p, hipStream_t stream) {
   switch (p.blocks) {
-    case 1: return launch_tile<kNk, 1>(g, p, stream);
-    case 2: return launch_tile<kNk, 2>(g, p, stream);
-    case 3: return launch_tile<kNk, 3>(g, p, stream);
-    default: return launch_tile<kNk, 4>(g, p, stream);
+    case 1: return launch_tile<kNk, 1, kGrad>(g, p, stream);
+    case 2: return launch_tile<kNk, 2, kGrad>(g, p, stream);
+    case 3: return launch_tile<kNk, 3, kGrad>(g, p, stream);
+    default: return launch_tile<kNk, 4, kGrad>(g, p, stream);
   }
+}
+
+template <bool kGrad>
+hipError_t launch_plan(const RowsArgs& g, const RowsPlan& p, hipStream_t stream) {
+  if (p.line)
+    return p.blocks == 1 ? launch_line<1, kGrad>(g, p, stream)
+                         : launch_line<2, kGrad>(g, p, stream);
+  return g.a.transpose_w ? launch_tiles<true, kGrad>(g, p, stream)
+                         : launch_tiles<false, kGrad>(g, p, stream);
 }
 
 }  // namespace
@@ -409,13 +436,12 @@ size_t linear_rows_ws(int64_t M, int64_t N, int64_t K) {
   return static_cast<size_t>(round_up(splits > 1 ? splits * M * N * 4 : 1, 256));
 }
 
-hipError_t launch_linear_rows(const LinearArgs& a, void* ws, hipStream_t stream) {
+hipError_t launch_linear_rows(const LinearArgs& a, const Unscale* grad, void* ws,
+                              hipStream_t stream) {
   const RowsPlan p = plan_rows(a.M, a.N, a.K, a.transpose_w);
-  const RowsArgs g{a, 1.0f / a.scale, p.groups, p.splits, static_cast<float*>(ws)};
-  const hipError_t e = p.line ? p.blocks == 1 ? launch_line<1>(g, p, stream)
-                                              : launch_line<2>(g, p, stream)
-                       : a.transpose_w ? launch_tiles<true>(g, p, stream)
-                                       : launch_tiles<false>(g, p, stream);
+  const RowsArgs g{a, grad != nullptr, grad ? *grad : Unscale{}, 1.0f / a.scale, p.groups,
+                   p.splits, static_cast<float*>(ws)};
+  const hipError_t e = grad ? launch_plan<true>(g, p, stream) : launch_plan<false>(g, p, stream);
   if (e != hipSuccess || p.splits == 1) return e;
   hipLaunchKernelGGL(linear_join_kernel, dim3(static_cast<unsigned>((a.M * a.N + 255) / 256)),
                      dim3(256), 0, stream, g);

@@ -34,7 +34,41 @@ struct SplitArgs {
   uint32_t first[kSplitJobs + 1];
   int count;
   float s;
+  ColumnJoin join;
 };
+
+constexpr int kJoinCols = 32, kJoinGroups = kThreads / kJoinCols;
+
+// The largest of the slabs' magnitudes, in every thread.  `lds`: a word per wave.
+__device__ uint32_t join_top(const ColumnJoin& g, float* lds) {
+  const int t = threadIdx.x;
+  float m = 0.0f;
+#pragma unroll 4
+  for (int n = t; n < g.tops; n += kThreads) m = __builtin_fmaxf(m, g.top[n]);
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, off));
+  if ((t & 63) == 0) lds[t >> 6] = m;
+  __syncthreads();
+  m = __builtin_fmaxf(__builtin_fmaxf(lds[0], lds[1]), __builtin_fmaxf(lds[2], lds[3]));
+  return __builtin_bit_cast(uint32_t, m);
+}
+
+// dbias of 32 columns, every eighth slab a thread.  `part`: a word per thread.
+__device__ void join_columns(const ColumnJoin& g, uint32_t block, float* part) {
+  const int c = threadIdx.x % kJoinCols, q = threadIdx.x / kJoinCols;
+  const int64_t j = static_cast<int64_t>(block) * kJoinCols + c;
+  float s = 0.0f;
+  if (j < g.N) {
+#pragma unroll 4
+    for (int n = q; n < g.slabs; n += kJoinGroups) s += g.sums[n * g.N + j];
+  }
+  part[q * kJoinCols + c] = s;
+  __syncthreads();
+  if (q != 0 || j >= g.N) return;
+#pragma unroll
+  for (int n = 1; n < kJoinGroups; ++n) s += part[n * kJoinCols + c];
+  g.dbias[j] = s;
+}
 
 constexpr int kTileRows = 32, kTileCols = 128;
 constexpr int kPitch = kTileRows / 2 + 4;  // words per column in LDS; 16-byte aligned
@@ -43,8 +77,8 @@ constexpr int kPitch = kTileRows / 2 + 4;  // words per column in LDS; 16-byte a
 // columns from 8 (t % 16).  As row planes those are two 16-byte chunks of a tile
 // row each.  As column planes the pairs of rows go to LDS as words, a column's
 // side by side, and thread t writes chunk t of each of the tile's two slices.
-__device__ void split_tile(const SplitArgs& a, const SplitJob& g, uint32_t block, uint32_t* ph,
-                           uint32_t* pl) {
+__device__ void split_tile(const SplitArgs& a, const SplitJob& g, uint32_t block,
+                           uint32_t max_bits, uint32_t* ph, uint32_t* pl) {
   const int t = threadIdx.x;
   const uint32_t strips = static_cast<uint32_t>((g.cols + kTileCols - 1) / kTileCols);
   const int64_t tr = block / strips, tc = block - static_cast<uint32_t>(tr) * strips;
@@ -62,7 +96,6 @@ __device__ void split_tile(const SplitArgs& a, const SplitJob& g, uint32_t block
   }
   const int64_t kp_row = (g.cols + kKPad - 1) / kKPad * kKPad;
   const int64_t kp_col = (g.rows + kKPad - 1) / kKPad * kKPad;
-  const uint32_t max_bits = g.max_bits ? *g.max_bits : 0;
   bool big = false;
   auto too_big = [&](uint32_t h) {
     typedef _Float16 half2 __attribute__((ext_vector_type(2)));
@@ -123,9 +156,31 @@ __global__ __launch_bounds__(kThreads) void split_jobs_kernel(SplitArgs a) {
   for (uint32_t b = blockIdx.x; b < a.first[a.count]; b += gridDim.x) {
     int n = 0;
     while (n + 1 < a.count && b >= a.first[n + 1]) ++n;
-    split_tile(a, a.job[n], b - a.first[n], ph, pl);
+    const SplitJob& g = a.job[n];
+    split_tile(a, g, b - a.first[n], g.max_bits ? *g.max_bits : 0, ph, pl);
     __syncthreads();  // the tile's LDS words are read before the next's are written
   }
+}
+
+// With the join: a tile a workgroup, then the join's workgroups.
+__global__ __launch_bounds__(kThreads) void split_join_kernel(SplitArgs a) {
+  __shared__ __align__(16) uint32_t ph[kTileCols * kPitch];
+  __shared__ __align__(16) uint32_t pl[kTileCols * kPitch];
+  const uint32_t b = blockIdx.x;
+  if (b >= a.first[a.count]) {
+    join_columns(a.join, b - a.first[a.count], reinterpret_cast<float*>(ph));
+    return;
+  }
+  int n = 0;
+  while (n + 1 < a.count && b >= a.first[n + 1]) ++n;
+  const SplitJob& g = a.job[n];
+  uint32_t max_bits = 0;
+  if (g.max_bits) {
+    max_bits = join_top(a.join, reinterpret_cast<float*>(pl));
+    if (b == a.first[n] && threadIdx.x == 0) *a.join.max_bits = max_bits;
+    __syncthreads();  // pl is read before the tile is written
+  }
+  split_tile(a, g, b - a.first[n], max_bits, ph, pl);
 }
 
 // Rows that a thread has in flight.
@@ -162,6 +217,11 @@ __global__ __launch_bounds__(kThreads) void columns_kernel(ColumnArgs a, int64_t
           z[u] = *reinterpret_cast<const floatx4_u*>(a.z + (i + u * kStride) * a.ldz + j);
         multiply_grad(a.activation, d, z);
       }
+      if (a.d) {
+#pragma unroll
+        for (int u = 0; u < kColumnRows; ++u)
+          *reinterpret_cast<floatx4_u*>(a.d + (i + u * kStride) * a.N + j) = d[u];
+      }
 #pragma unroll
       for (int u = 0; u < kColumnRows; ++u) add({d[u][0], d[u][1], d[u][2], d[u][3]});
     }
@@ -172,6 +232,7 @@ __global__ __launch_bounds__(kThreads) void columns_kernel(ColumnArgs a, int64_t
     for (int e = 0; e < 4; ++e) {
       d[e] = j + e < a.N ? a.dy[i * a.lddy + j + e] : 0.0f;
       if (a.z && j + e < a.N) d[e] *= activate_grad(a.activation, a.z[i * a.ldz + j + e]);
+      if (a.d && j + e < a.N) a.d[i * a.N + j + e] = d[e];
     }
     add(d);
   }
@@ -181,56 +242,27 @@ __global__ __launch_bounds__(kThreads) void columns_kernel(ColumnArgs a, int64_t
   for (int off = 32; off > 0; off >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, off));
   if ((t & 63) == 0) top[t >> 6] = m;
   __syncthreads();
-  float* const out = a.partial + blockIdx.y * (a.N + gridDim.x);
   const int64_t col = static_cast<int64_t>(blockIdx.x) * kColumnStrip + t;
   if (t < kColumnStrip && col < a.N) {
     float sum = 0.0f;
 #pragma unroll
     for (int g = 0; g < kThreads / 32; ++g) sum += part[g][t];
-    out[col] = sum;
+    a.partial[blockIdx.y * a.N + col] = sum;
   }
   if (t == 0)
-    out[a.N + blockIdx.x] = __builtin_fmaxf(__builtin_fmaxf(top[0], top[1]),
+    a.partial[gridDim.y * a.N + blockIdx.y * gridDim.x + blockIdx.x] = __builtin_fmaxf(__builtin_fmaxf(top[0], top[1]),
                                             __builtin_fmaxf(top[2], top[3]));
 }
 
-// Joins the slabs: every workgroup but the last has 32 columns, every eighth slab a
-// thread; the last the magnitudes.
-constexpr int kJoinCols = 32, kJoinGroups = kThreads / kJoinCols;
-__global__ __launch_bounds__(kThreads) void columns_join_kernel(ColumnArgs a, int64_t slabs,
-                                                                int64_t strips) {
-  __shared__ float part[kJoinGroups][kJoinCols];
-  const int t = threadIdx.x;
-  const int64_t pitch = a.N + strips;
+// The join alone: every workgroup but the last has 32 columns.
+__global__ __launch_bounds__(kThreads) void columns_join_kernel(ColumnJoin g) {
+  __shared__ float part[kThreads];
   if (blockIdx.x < gridDim.x - 1) {
-    if (!a.dbias) return;
-    const int c = t % kJoinCols, g = t / kJoinCols;
-    const int64_t j = static_cast<int64_t>(blockIdx.x) * kJoinCols + c;
-    float s = 0.0f;
-    if (j < a.N) {
-#pragma unroll 4
-      for (int64_t n = g; n < slabs; n += kJoinGroups) s += a.partial[n * pitch + j];
-    }
-    part[g][c] = s;
-    __syncthreads();
-    if (g != 0 || j >= a.N) return;
-#pragma unroll
-    for (int q = 1; q < kJoinGroups; ++q) s += part[q][c];
-    a.dbias[j] = s;
-    return;
+    join_columns(g, blockIdx.x, part);
+  } else {
+    const uint32_t bits = join_top(g, part);
+    if (threadIdx.x == 0) *g.max_bits = bits;
   }
-  float m = 0.0f;
-#pragma unroll 4
-  for (int64_t n = t; n < slabs * strips; n += kThreads)
-    m = __builtin_fmaxf(m, a.partial[n / strips * pitch + a.N + n % strips]);
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, off));
-  if ((t & 63) == 0) part[0][t >> 6] = m;
-  __syncthreads();
-  if (t == 0)
-    *a.max_bits = __builtin_bit_cast(
-        uint32_t, __builtin_fmaxf(__builtin_fmaxf(part[0][0], part[0][1]),
-                                  __builtin_fmaxf(part[0][2], part[0][3])));
 }
 
 // The epilogue of a product without terms: Z = bias.
@@ -247,7 +279,27 @@ __global__ __launch_bounds__(kThreads) void epilogue_kernel(Epilogue e, int64_t 
 
 }  // namespace
 
-hipError_t launch_split_jobs(const SplitJob* jobs, int count, float scale, hipStream_t stream) {
+namespace {
+
+// Tiles of a job.  Rows up to a multiple of 64: the padding of k in column planes.
+int64_t job_blocks(const SplitJob& j) {
+  return round_up(j.rows, kKPad) / kTileRows * ((j.cols + kTileCols - 1) / kTileCols);
+}
+
+unsigned join_blocks(const ColumnJoin& j) {
+  return j.dbias ? static_cast<unsigned>((j.N + kJoinCols - 1) / kJoinCols) : 0u;
+}
+
+}  // namespace
+
+int64_t split_jobs_blocks(const SplitJob* jobs, int count) {
+  int64_t blocks = 0;
+  for (int n = 0; n < count; ++n) blocks += job_blocks(jobs[n]);
+  return blocks;
+}
+
+hipError_t launch_split_jobs(const SplitJob* jobs, int count, float scale, hipStream_t stream,
+                             const ColumnJoin* join) {
   SplitArgs a{};
   a.s = scale;
   a.count = count;
@@ -255,13 +307,17 @@ hipError_t launch_split_jobs(const SplitJob* jobs, int count, float scale, hipSt
   for (int n = 0; n < count; ++n) {
     a.job[n] = jobs[n];
     a.first[n] = static_cast<uint32_t>(blocks);
-    // Rows up to a multiple of 64: the padding of k in column planes.
-    blocks += round_up(jobs[n].rows, kKPad) / kTileRows *
-              ((jobs[n].cols + kTileCols - 1) / kTileCols);
+    blocks += job_blocks(jobs[n]);
     if (blocks > UINT32_MAX) return hipErrorInvalidValue;
   }
   a.first[count] = static_cast<uint32_t>(blocks);
   if (blocks == 0) return hipSuccess;
+  if (join) {
+    a.join = *join;
+    hipLaunchKernelGGL(split_join_kernel, dim3(a.first[count] + join_blocks(*join)),
+                       dim3(kThreads), 0, stream, a);
+    return hipGetLastError();
+  }
   const dim3 grid(static_cast<unsigned>(std::min<int64_t>(blocks, int64_t{1} << 22)));
   hipLaunchKernelGGL(split_jobs_kernel, grid, dim3(kThreads), 0, stream, a);
   return hipGetLastError();
@@ -277,10 +333,17 @@ hipError_t launch_columns(const ColumnArgs& a, hipStream_t stream) {
   const int64_t slabs = column_slabs(a.M, a.N);
   hipLaunchKernelGGL(columns_kernel, dim3(static_cast<unsigned>(strips), static_cast<unsigned>(slabs)),
                      dim3(kThreads), 0, stream, a, (a.M + slabs - 1) / slabs);
-  if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-  hipLaunchKernelGGL(columns_join_kernel,
-                     dim3(static_cast<unsigned>((a.N + kJoinCols - 1) / kJoinCols + 1)),
-                     dim3(kThreads), 0, stream, a, slabs, strips);
+  return hipGetLastError();
+}
+
+ColumnJoin column_join(const ColumnArgs& a) {
+  const int64_t slabs = column_slabs(a.M, a.N), strips = (a.N + kColumnStrip - 1) / kColumnStrip;
+  return ColumnJoin{a.partial + slabs * a.N, static_cast<int>(slabs * strips), a.max_bits,
+                    a.partial, static_cast<int>(slabs), a.N, a.dbias};
+}
+
+hipError_t launch_columns_join(const ColumnJoin& j, hipStream_t stream) {
+  hipLaunchKernelGGL(columns_join_kernel, dim3(join_blocks(j) + 1), dim3(kThreads), 0, stream, j);
   return hipGetLastError();
 }
 
