@@ -32,7 +32,7 @@ __device__ __forceinline__ float unscaled(float x, int shift) {
 // lane too, and where the compiler therefore holds them in vector registers it
 // moves the copies' base addresses to scalar ones right before each dma16s, whose
 // inline asm it gives none of the 5 wait states that a VMEM instruction needs
-// after a vector instruction wrote its scalar base (tests/test_sgpr_hazard.py).
+// after a vector instruction wrote its scalar base (tests/test_asm_hazards.py).
 template <class Epi>
 __device__ __forceinline__ void scalar_tile(int& tm, int& tn) {
   if constexpr (!std::is_same<Epi, NoEpilogue>::value) {
@@ -106,6 +106,9 @@ __device__ __forceinline__ void epilogue_tile(const Epilogue& e, float* stage, f
 #pragma unroll
         for (int j = 0; j < kSubN; ++j)
           stage[row * kWidth + ((16 * j + (lane & 15)) ^ swap)] = value(i0 + i, j, r);
+        // Row by row, so that no more accumulators are read ahead than there are
+        // registers for.
+        SCHED_FENCE();
       }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();

@@ -427,6 +427,7 @@ __device__ __forceinline__ void el_tile(
   wait_vmcnt<0>();
   mfma_drain();
 
+  if constexpr (!std::is_same<Epi, NoEpilogue>::value) SCHED_FENCE();
   if constexpr (kThroughLds<Epi>) {
     constexpr int kChunk = epilogue_chunk(kWSub, kWSub, 4, kElLdsBytes);
     lds_barrier();  // every wave is done with the stages
@@ -1063,6 +1064,7 @@ __device__ __forceinline__ void n128_tile(
     fold(kCols - 1, 1, 0, 4 * kRows);
   }
 
+  if constexpr (!std::is_same<Epi, NoEpilogue>::value) SCHED_FENCE();
   auto value = [&](int i, int j, int r) {
     if constexpr (V == kCrossScaled) {
       return hh[i][j][r] * inv_s;
