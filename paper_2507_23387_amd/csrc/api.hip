@@ -88,6 +88,8 @@ RangeOpts range_opts(unsigned options, bool report, float scale) {
   return o;
 }
 
+}  // namespace
+
 // The in-kernel split of A redoes the split of an A tile once per tile
 // column of C, on the vector ALU between the matrix instructions, while the
 // split pass costs one read of A and one write of its planes through HBM.
@@ -100,11 +102,11 @@ RangeOpts range_opts(unsigned options, bool report, float scale) {
 // used up to N = 3072.  Termwise (128-column tiles, so twice the repeats per
 // column of C): 10 % faster at 16384 x 1024 x 8192, even at 4096^3 and 4 %
 // slower at 4096 x 4096 x 16384, so it is used up to N = 2048.
-constexpr int64_t kElementwiseFusedMaxN = 3072;
-constexpr int64_t kTermwiseFusedMaxN = 2048;
+static constexpr int64_t kElementwiseFusedMaxN = 3072;
+static constexpr int64_t kTermwiseFusedMaxN = 2048;
 
 // Whether the 256-wide kernels, where they run, split this A in registers.
-bool wide_kernel_splits_a(int64_t N, const float* A, int64_t lda, int64_t K, float scale,
+static bool wide_kernel_splits_a(int64_t N, const float* A, int64_t lda, int64_t K, float scale,
                           int variant) {
   const int64_t max_n = variant == kElementwise ? kElementwiseFusedMaxN
                         : variant == kTermwise  ? kTermwiseFusedMaxN
@@ -122,6 +124,8 @@ bool splits_a_in_gemm(int64_t M, int64_t N, const float* A, int64_t lda, int64_t
   return wide_kernel_splits_a(N, A, lda, K, scale, variant) &&
          small_gemm_tile(M, N, K, variant, !scaled_kernel_ok(scale), split_a_us(M, K)) == 0;
 }
+
+namespace {
 
 // GEMM from FP32 A and a workspace whose B planes are prepared: the 256-wide
 // kernel splits A in registers when splits_a_in_gemm says so, else A is split

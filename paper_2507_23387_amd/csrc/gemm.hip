@@ -86,9 +86,9 @@ __device__ __forceinline__ void wide_frag_offsets(int lane, int panel, int (&off
 // compute unit, so each pass of the loop loads four blocks before it splits
 // and stores them, to keep enough reads in flight.  A is 16-byte aligned with
 // lda a multiple of 4 here; rows past M and k past K are written as zeros.
-__device__ void split_a_planes(const float* __restrict__ A, int64_t lda, int M, int K, int Mp,
-                               int Kp, uint16_t* __restrict__ a_hi, uint16_t* __restrict__ a_lo,
-                               float s) {
+__device__ __forceinline__ void split_a_planes(const float* __restrict__ A, int64_t lda, int M,
+                                               int K, int Mp, int Kp, uint16_t* __restrict__ a_hi,
+                                               uint16_t* __restrict__ a_lo, float s) {
   constexpr int kUnroll = 4;
   const int lane = threadIdx.x & 63;
   const int kblocks = (Kp + 127) / 128;
@@ -457,13 +457,14 @@ __global__ __launch_bounds__(kWideThreads, 1) void gemm_el_kernel(
 }
 
 // The same with a linear layer's epilogue (C and the residual may be one).
-template <class Epi>
+template <class Epi, bool kFusedA>
 __global__ __launch_bounds__(kWideThreads, 1) void linear_el_kernel(
     uint16_t* __restrict__ a_hi, uint16_t* __restrict__ a_lo, const uint16_t* __restrict__ b_hi,
     const uint16_t* __restrict__ b_lo, const uint32_t* __restrict__ range, int Kp, int tiles_m,
-    int tiles_n, float* C, int64_t ldc, int M, int N, float s, float inv_s, Epi epi) {
-  el_tile<true, false>(a_hi, a_lo, b_hi, b_lo, range, Kp, tiles_m, tiles_n, C, ldc, M, N, s, inv_s,
-                       nullptr, 0, 0, epi);
+    int tiles_n, float* C, int64_t ldc, int M, int N, float s, float inv_s,
+    const float* __restrict__ af, int64_t lda, int K, Epi epi) {
+  el_tile<true, kFusedA>(a_hi, a_lo, b_hi, b_lo, range, Kp, tiles_m, tiles_n, C, ldc, M, N, s,
+                         inv_s, af, lda, K, epi);
 }
 
 // Hi-only kernel: C = A_hi B_hi, the native-FP16 GEMM baseline (Sec. 6.2),
@@ -1100,14 +1101,14 @@ __global__ __launch_bounds__(kWideThreads, 1) void gemm_n128_kernel(
 }
 
 // The same with a linear layer's epilogue (C and the residual may be one).
-template <int V, class Epi>
+template <int V, class Epi, bool kFusedA>
 __global__ __launch_bounds__(kWideThreads, 1) void linear_n128_kernel(
     const uint16_t* __restrict__ a_hi, const uint16_t* __restrict__ a_lo,
     const uint16_t* __restrict__ b_hi, const uint16_t* __restrict__ b_lo,
     const uint32_t* __restrict__ range, int Kp, int tiles_m, int tiles_n, float* C, int64_t ldc,
-    int M, int N, float inv_s, float s, Epi epi) {
-  n128_tile<V, false, false>(a_hi, a_lo, b_hi, b_lo, range, Kp, tiles_m, tiles_n, C, ldc, M, N,
-                             inv_s, nullptr, 0, s, nullptr, 0, epi);
+    int M, int N, float inv_s, const float* __restrict__ af, int64_t lda, float s, Epi epi) {
+  n128_tile<V, kFusedA, false>(a_hi, a_lo, b_hi, b_lo, range, Kp, tiles_m, tiles_n, C, ldc, M, N,
+                               inv_s, af, lda, s, nullptr, 0, epi);
 }
 
 template <bool kPrefetch, bool kFusedA>
@@ -1160,33 +1161,36 @@ hipError_t launch_n128(const Planes& p, int64_t M, int64_t N, float* C, int64_t 
   return hipGetLastError();
 }
 
-template <class Epi>
+template <bool kFusedA = false, class Epi>
 hipError_t launch_linear_el(const Planes& p, int64_t M, int64_t N, float* C, int64_t ldc, float s,
-                            const Epi& epi, hipStream_t stream) {
+                            const Epi& epi, hipStream_t stream, const float* A = nullptr,
+                            int64_t lda = 0, int64_t K = 0) {
   static std::atomic<bool> done[kMaxDevices];
-  const hipError_t attr = set_lds(&linear_el_kernel<Epi>, kElLdsBytes, done);
+  const hipError_t attr = set_lds(&linear_el_kernel<Epi, kFusedA>, kElLdsBytes, done);
   if (attr != hipSuccess) return attr;
   const int tiles_m = static_cast<int>(p.Mp / kWide);
   const int tiles_n = static_cast<int>(p.Np / kWide);
-  hipLaunchKernelGGL(linear_el_kernel<Epi>, dim3(tiles_m * tiles_n), dim3(kWideThreads),
-                     kElLdsBytes, stream, p.a_hi, p.a_lo, p.b_hi, p.b_lo, p.range,
-                     static_cast<int>(p.Kp), tiles_m, tiles_n, C, ldc, static_cast<int>(M),
-                     static_cast<int>(N), s, 1.0f / s, epi);
+  hipLaunchKernelGGL((linear_el_kernel<Epi, kFusedA>), dim3(tiles_m * tiles_n),
+                     dim3(kWideThreads), kElLdsBytes, stream, p.a_hi, p.a_lo, p.b_hi, p.b_lo,
+                     p.range, static_cast<int>(p.Kp), tiles_m, tiles_n, C, ldc,
+                     static_cast<int>(M), static_cast<int>(N), s, 1.0f / s, A, lda,
+                     static_cast<int>(K), epi);
   return hipGetLastError();
 }
 
-template <int V, class Epi>
+template <int V, bool kFusedA = false, class Epi>
 hipError_t launch_linear_n128(const Planes& p, int64_t M, int64_t N, float* C, int64_t ldc,
-                              float s, const Epi& epi, hipStream_t stream) {
+                              float s, const Epi& epi, hipStream_t stream,
+                              const float* A = nullptr, int64_t lda = 0) {
   static std::atomic<bool> done[kMaxDevices];
-  const hipError_t attr = set_lds(&linear_n128_kernel<V, Epi>, kTwLdsBytes, done);
+  const hipError_t attr = set_lds(&linear_n128_kernel<V, Epi, kFusedA>, kTwLdsBytes, done);
   if (attr != hipSuccess) return attr;
   const int tiles_m = static_cast<int>(p.Mp / kTwM);
   const int tiles_n = static_cast<int>((N + kTwN - 1) / kTwN);
-  hipLaunchKernelGGL((linear_n128_kernel<V, Epi>), dim3(tiles_m * tiles_n), dim3(kWideThreads),
-                     kTwLdsBytes, stream, p.a_hi, p.a_lo, p.b_hi, p.b_lo, p.range,
-                     static_cast<int>(p.Kp), tiles_m, tiles_n, C, ldc, static_cast<int>(M),
-                     static_cast<int>(N), 1.0f / s, s, epi);
+  hipLaunchKernelGGL((linear_n128_kernel<V, Epi, kFusedA>), dim3(tiles_m * tiles_n),
+                     dim3(kWideThreads), kTwLdsBytes, stream, p.a_hi, p.a_lo, p.b_hi, p.b_lo,
+                     p.range, static_cast<int>(p.Kp), tiles_m, tiles_n, C, ldc,
+                     static_cast<int>(M), static_cast<int>(N), 1.0f / s, A, lda, s, epi);
   return hipGetLastError();
 }
 
@@ -1210,6 +1214,18 @@ hipError_t launch_gemm_epilogue(const Planes& p, int64_t M, int64_t N, float* C,
   }
   return launch_gemm_unscaled_epilogue(p, M, N, C, ldc, scale, variant, !scaled, epi, stream);
 }
+hipError_t launch_gemm_fused_a_epilogue(const Planes& p, int64_t M, int64_t N, int64_t K,
+                                        const float* A, int64_t lda, float* C, int64_t ldc,
+                                        float scale, int variant, const Epilogue& epi,
+                                        hipStream_t stream) {
+  if (!fused_split_ok(A, lda, K, scale, variant)) return hipErrorInvalidValue;
+  if (variant == kTermwise)
+    return launch_linear_n128<kTermwise, true>(p, M, N, C, ldc, scale, epi, stream, A, lda);
+  const hipError_t e = launch_linear_el<true>(p, M, N, C, ldc, scale, epi, stream, A, lda, K);
+  if (e != hipSuccess) return e;
+  return launch_gemm_unscaled_epilogue(p, M, N, C, ldc, scale, variant, false, epi, stream);
+}
+
 template hipError_t launch_gemm_epilogue<Epilogue>(const Planes&, int64_t, int64_t, float*,
                                                    int64_t, float, int, const Epilogue&, bool,
                                                    hipStream_t);

@@ -84,12 +84,14 @@ struct SmallArgs {
   uint32_t* report;  // range report word, or null
 };
 
+// `index`: the workgroup's place in the grid of this product.
 template <class S, int kFold, class Epi>
-__device__ __forceinline__ void small_tile(const SmallArgs& g, uint16_t* lds, const Epi& epi) {
+__device__ __forceinline__ void small_tile(const SmallArgs& g, uint16_t* lds, const Epi& epi,
+                                           int index) {
   constexpr int kRT = S::kRT, kCT = S::kCT;
   int tm, tn;
-  if (S::kBM < 256 || !tile_of_block(blockIdx.x, g.tiles_m, g.tiles_n, tm, tn))
-    tile_of<4>(g.by_xcd ? xcd_order(blockIdx.x, g.tiles_m * g.tiles_n) : blockIdx.x, g.tiles_m,
+  if (S::kBM < 256 || !tile_of_block(index, g.tiles_m, g.tiles_n, tm, tn))
+    tile_of<4>(g.by_xcd ? xcd_order(index, g.tiles_m * g.tiles_n) : index, g.tiles_m,
                g.tiles_n, tm, tn);
   scalar_tile<Epi>(tm, tn);
   const int lane = threadIdx.x & 63;
@@ -318,7 +320,7 @@ __device__ __forceinline__ void small_tile(const SmallArgs& g, uint16_t* lds, co
     return;
   }
   if constexpr (kFold != kHiFold) {
-    if (g.report && blockIdx.x == 0 && threadIdx.x == 0) *g.report = range_report_bits(g.range);
+    if (g.report && index == 0 && threadIdx.x == 0) *g.report = range_report_bits(g.range);
     if (g.row_max) {
       int p[kRT][4], q[kCT];
 #pragma unroll
@@ -346,19 +348,20 @@ __device__ __forceinline__ void small_tile(const SmallArgs& g, uint16_t* lds, co
 }
 
 template <int V, class S, class Epi>
-__device__ __forceinline__ void small_body(const SmallArgs& g, int unscaled_only, const Epi& epi) {
+__device__ __forceinline__ void small_body(const SmallArgs& g, int unscaled_only, const Epi& epi,
+                                           int index) {
   extern __shared__ __align__(16) uint16_t lds[];
   if constexpr (V == kTermwise) {
-    small_tile<S, kTermFold>(g, lds, epi);
+    small_tile<S, kTermFold>(g, lds, epi, index);
   } else if constexpr (V == kHiOnly) {
-    small_tile<S, kHiFold>(g, lds, epi);
+    small_tile<S, kHiFold>(g, lds, epi, index);
   } else {
     // The scaled body needs a finite s B_hi (gemm.hip): s <= 2^15 (host) and a
     // clear range flag.
     if (unscaled_only || g.range[0] == g.range[1])
-      small_tile<S, V == kElementwise ? kElUnscaled : kCrUnscaled>(g, lds, epi);
+      small_tile<S, V == kElementwise ? kElUnscaled : kCrUnscaled>(g, lds, epi, index);
     else
-      small_tile<S, V == kElementwise ? kElScaled : kCrScaled>(g, lds, epi);
+      small_tile<S, V == kElementwise ? kElScaled : kCrScaled>(g, lds, epi, index);
   }
 }
 
@@ -366,7 +369,7 @@ template <int V, int kBM, int kBN, int kWM, int kWN, int kStages>
 __global__ __launch_bounds__(64 * kWM * kWN, 1) void gemm_small_kernel(SmallArgs g,
                                                                        int unscaled_only) {
   small_body<V, SmallShape<kBM, kBN, kWM, kWN, kStages, V == kHiOnly>>(g, unscaled_only,
-                                                                       NoEpilogue{});
+                                                                       NoEpilogue{}, blockIdx.x);
 }
 
 // The same with a linear layer's epilogue.
@@ -374,7 +377,23 @@ template <int V, int kBM, int kBN, int kWM, int kWN, int kStages, class Epi>
 __global__ __launch_bounds__(64 * kWM * kWN, 1) void linear_small_kernel(SmallArgs g,
                                                                          int unscaled_only,
                                                                          Epi epi) {
-  small_body<V, SmallShape<kBM, kBN, kWM, kWN, kStages, false>>(g, unscaled_only, epi);
+  small_body<V, SmallShape<kBM, kBN, kWM, kWN, kStages, false>>(g, unscaled_only, epi, blockIdx.x);
+}
+
+// Two products in one launch (a layer's two gradients), the first `first`
+// workgroups on the one.  Alone, neither fills the GPU for long: 777 x 530 x 1003 and
+// 1003 x 530 x 777 took 11 and 14 us, and a launch between.  The arguments are an
+// array, so that a scalar index into it keeps them in scalar registers.
+struct PairArgs {
+  SmallArgs g[2];
+  Unscale e[2];
+  int first, unscaled_only;
+};
+template <int V, int kBM, int kBN, int kWM, int kWN, int kStages>
+__global__ __launch_bounds__(64 * kWM * kWN, 1) void linear_pair_kernel(PairArgs a) {
+  using S = SmallShape<kBM, kBN, kWM, kWN, kStages, false>;
+  const int i = static_cast<int>(blockIdx.x) >= a.first ? 1 : 0;
+  small_body<V, S>(a.g[i], a.unscaled_only, a.e[i], blockIdx.x - (i ? a.first : 0));
 }
 
 // The unscaled body alone, on 256 x 128 tiles: the fallback of the 256-wide
@@ -389,14 +408,15 @@ template <int V>
 __global__ __launch_bounds__(512, 1) void gemm_unscaled_kernel(SmallArgs g, int unscaled_only) {
   extern __shared__ __align__(16) uint16_t lds[];
   if (!unscaled_only && g.range[0] != g.range[1]) return;
-  small_tile<UnscaledShape, V == kElementwise ? kElUnscaled : kCrUnscaled>(g, lds, NoEpilogue{});
+  small_tile<UnscaledShape, V == kElementwise ? kElUnscaled : kCrUnscaled>(g, lds, NoEpilogue{},
+                                                                     blockIdx.x);
 }
 template <int V, class Epi>
 __global__ __launch_bounds__(512, 1) void linear_unscaled_kernel(SmallArgs g, int unscaled_only,
                                                                  Epi epi) {
   extern __shared__ __align__(16) uint16_t lds[];
   if (!unscaled_only && g.range[0] != g.range[1]) return;
-  small_tile<UnscaledShape, V == kElementwise ? kElUnscaled : kCrUnscaled>(g, lds, epi);
+  small_tile<UnscaledShape, V == kElementwise ? kElUnscaled : kCrUnscaled>(g, lds, epi, blockIdx.x);
 }
 
 template <class S>
@@ -529,6 +549,35 @@ hipError_t launch_config_epilogue(int tile, const Planes& p, int64_t M, int64_t 
   });
 }
 
+template <int V>
+hipError_t launch_config_pair(int tile, const Planes (&p)[2], const int64_t (&M)[2],
+                              const int64_t (&N)[2], float* const (&C)[2],
+                              const int64_t (&ldc)[2], float s, const Unscale (&epi)[2],
+                              hipStream_t stream) {
+  return with_config<V>(tile, [&](auto c) {
+    using T = decltype(c);
+    if constexpr (T::kBM > 128) {
+      return hipErrorInvalidValue;  // pair_gemm_tile offers none
+    } else {
+      using S = SmallShape<T::kBM, T::kBN, T::kWM, T::kWN, T::kStages, false>;
+      static std::atomic<bool> done[kMaxDevices];
+      constexpr auto kernel = &linear_pair_kernel<V, T::kBM, T::kBN, T::kWM, T::kWN, T::kStages>;
+      const hipError_t attr = set_lds(kernel, S::kLdsBytes, done);
+      if (attr != hipSuccess) return attr;
+      PairArgs a;
+      for (int i = 0; i < 2; ++i) {
+        a.g[i] = small_args<S>(p[i], M[i], N[i], C[i], ldc[i], s, RangeOpts{}, nullptr);
+        a.e[i] = epi[i];
+      }
+      a.first = a.g[0].tiles_m * a.g[0].tiles_n;
+      a.unscaled_only = scaled_kernel_ok(s) ? 0 : 1;
+      hipLaunchKernelGGL(kernel, dim3(a.first + a.g[1].tiles_m * a.g[1].tiles_n),
+                         dim3(S::kThreads), S::kLdsBytes, stream, a);
+      return hipGetLastError();
+    }
+  });
+}
+
 // Time of a grid, in microseconds: `launch`, plus `start` (a tile's prologue and
 // its stores) per round of workgroups that run together, plus for each 32-wide
 // k-step `round` per round and `tile` per workgroup of each compute unit
@@ -540,6 +589,34 @@ double grid_time(const GridCost& c, int64_t tiles, int64_t together, int64_t kst
   const int64_t rounds = (tiles + together - 1) / together;
   return c.launch + rounds * (c.start + ksteps * c.round) + ksteps * c.tile * tiles / 256;
 }
+
+// The constants of each kernel, in the order of Variant, then the unscaled
+// elementwise body's (small_gemm_tile says how they were found).
+constexpr GridCost k32[5] = {{2.0, 1.56, 0.083, 0.050},
+                                    {2.2, 1.31, 0.067, 0.050},
+                                    {3.1, 0.32, 0.053, 0.014},
+                                    {2.3, 1.37, 0.100, 0.043},
+                                    {2.1, 1.44, 0.124, 0.036}};
+constexpr GridCost k64[5] = {{2.0, 2.70, 0.124, 0.141},
+                                    {1.6, 2.79, 0.113, 0.137},
+                                    {2.5, 1.22, 0.089, 0.049},
+                                    {1.8, 2.45, 0.149, 0.149},
+                                    {1.7, 2.37, 0.256, 0.154}};
+constexpr GridCost k128[5] = {{2.2, 4.38, 0.356, 0.258},
+                                     {1.7, 4.61, 0.327, 0.274},
+                                     {2.2, 2.37, 0.156, 0.072},
+                                     {2.2, 4.30, 0.394, 0.281},
+                                     {1.8, 3.86, 0.459, 0.281}};
+constexpr GridCost k192[5] = {{2.5, 7.53, 0.772, 0.479},
+                                     {},
+                                     {},
+                                     {2.7, 7.55, 0.867, 0.503},
+                                     {1.9, 7.05, 0.859, 0.575}};
+constexpr GridCost kWide[5] = {{4.2, 13.14, 1.306, 0.618},
+                                      {2.9, 9.05, 0.660, 0.397},
+                                      {1.6, 11.56, 0.601, 0.199},
+                                      {4.4, 6.95, 0.790, 0.435},
+                                      {2.1, 6.92, 0.809, 0.496}};
 
 }  // namespace
 
@@ -571,31 +648,6 @@ double grid_time(const GridCost& c, int64_t tiles, int64_t together, int64_t kst
 // 712).
 int small_gemm_tile(int64_t M, int64_t N, int64_t K, int variant, bool unscaled,
                     double split_us) {
-  static constexpr GridCost k32[5] = {{2.0, 1.56, 0.083, 0.050},
-                                      {2.2, 1.31, 0.067, 0.050},
-                                      {3.1, 0.32, 0.053, 0.014},
-                                      {2.3, 1.37, 0.100, 0.043},
-                                      {2.1, 1.44, 0.124, 0.036}};
-  static constexpr GridCost k64[5] = {{2.0, 2.70, 0.124, 0.141},
-                                      {1.6, 2.79, 0.113, 0.137},
-                                      {2.5, 1.22, 0.089, 0.049},
-                                      {1.8, 2.45, 0.149, 0.149},
-                                      {1.7, 2.37, 0.256, 0.154}};
-  static constexpr GridCost k128[5] = {{2.2, 4.38, 0.356, 0.258},
-                                       {1.7, 4.61, 0.327, 0.274},
-                                       {2.2, 2.37, 0.156, 0.072},
-                                       {2.2, 4.30, 0.394, 0.281},
-                                       {1.8, 3.86, 0.459, 0.281}};
-  static constexpr GridCost k192[5] = {{2.5, 7.53, 0.772, 0.479},
-                                       {},
-                                       {},
-                                       {2.7, 7.55, 0.867, 0.503},
-                                       {1.9, 7.05, 0.859, 0.575}};
-  static constexpr GridCost kWide[5] = {{4.2, 13.14, 1.306, 0.618},
-                                        {2.9, 9.05, 0.660, 0.397},
-                                        {1.6, 11.56, 0.601, 0.199},
-                                        {4.4, 6.95, 0.790, 0.435},
-                                        {2.1, 6.92, 0.809, 0.496}};
   const int row = unscaled && variant == kElementwise ? 4 : variant;
   auto time = [&](const GridCost& c, int64_t bm, int64_t bn, int64_t together) {
     const int64_t tiles = ((M + bm - 1) / bm) * ((N + bn - 1) / bn);
@@ -635,6 +687,52 @@ int small_gemm_tile(int64_t M, int64_t N, int64_t K, int variant, bool unscaled,
   if (variant == kElementwise || variant == kCrossFirst)
     consider(192, time(k192[row], 192, 192, 256));
   return tile;
+}
+
+int pair_gemm_tile(const int64_t (&M)[2], const int64_t (&N)[2], const int64_t (&K)[2],
+                   int variant, bool unscaled) {
+  const int row = unscaled && variant == kElementwise ? 4 : variant;
+  auto side_cost = [&](int side) -> const GridCost& {
+    return side == 32 ? k32[row] : side == 64 ? k64[row] : side == 128 ? k128[row] : k192[row];
+  };
+  auto together = [](int side) { return side <= 64 ? 512 : 256; };
+  auto tiles = [&](int i, int side) {
+    return ((M[i] + side - 1) / side) * ((N[i] + side - 1) / side);
+  };
+  int64_t steps[2];
+  double apart = 0.0;
+  for (int i = 0; i < 2; ++i) {
+    steps[i] = round_up(K[i], kKPad) / kSmallStep;
+    const int side = small_gemm_tile(M[i], N[i], K[i], variant, unscaled);
+    if (side == 0) return 0;
+    apart += grid_time(side_cost(side), tiles(i, side), together(side), steps[i]);
+  }
+  int best = 0;
+  for (int side : {32, 64, 128}) {
+    const GridCost& c = side_cost(side);
+    const int64_t t0 = tiles(0, side), t1 = tiles(1, side);
+    if ((t0 + t1) * small_tile_threads(side, variant) > UINT32_MAX) continue;
+    const int64_t rounds = (t0 + t1 + together(side) - 1) / together(side);
+    const double us = c.launch + rounds * (c.start + std::max(steps[0], steps[1]) * c.round) +
+                      c.tile * (t0 * steps[0] + t1 * steps[1]) / 256;
+    if (us < apart) apart = us, best = side;
+  }
+  return best;
+}
+
+hipError_t launch_gemm_pair(int tile, const Planes (&p)[2], const int64_t (&M)[2],
+                            const int64_t (&N)[2], float* const (&C)[2], const int64_t (&ldc)[2],
+                            float scale, int variant, const Unscale (&epi)[2],
+                            hipStream_t stream) {
+  switch (variant) {
+    case kElementwise:
+      return launch_config_pair<kElementwise>(tile, p, M, N, C, ldc, scale, epi, stream);
+    case kTermwise:
+      return launch_config_pair<kTermwise>(tile, p, M, N, C, ldc, scale, epi, stream);
+    case kCrossFirst:
+      return launch_config_pair<kCrossFirst>(tile, p, M, N, C, ldc, scale, epi, stream);
+    default: return hipErrorInvalidValue;
+  }
 }
 
 hipError_t launch_gemm_unscaled(const Planes& p, int64_t M, int64_t N, float* C, int64_t ldc,

@@ -260,6 +260,10 @@ hipError_t launch_gemm_tile(const Planes& p, int64_t M, int64_t N, float* C, int
 // also s <= 2^15 (its kernel keeps the s-scaled accumulator).
 bool fused_split_ok(const float* A, int64_t lda, int64_t K, float scale, int variant);
 
+// Whether the GEMM of this problem runs on FP32 A (api.hip has the rule).
+bool splits_a_in_gemm(int64_t M, int64_t N, const float* A, int64_t lda, int64_t K, float scale,
+                      int variant);
+
 // GEMM that reads A as FP32 and splits it in registers, on a workspace whose B
 // planes (and range flag) were written by launch_split; requires
 // fused_split_ok.  Elementwise: the 256 x 256 kernel; when the range flag is

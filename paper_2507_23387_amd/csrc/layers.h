@@ -113,6 +113,21 @@ hipError_t launch_gemm_unscaled_epilogue(const Planes& p, int64_t M, int64_t N, 
                                          int64_t ldc, float scale, int variant, bool only,
                                          const Epi& epi, hipStream_t stream);
 
+// launch_gemm_fused_a with an epilogue (requires splits_a_in_gemm).
+hipError_t launch_gemm_fused_a_epilogue(const Planes& p, int64_t M, int64_t N, int64_t K,
+                                        const float* A, int64_t lda, float* C, int64_t ldc,
+                                        float scale, int variant, const Epilogue& epi,
+                                        hipStream_t stream);
+
+// Two gradients' products in one launch, on tiles of 32, 64 or 128.
+// pair_gemm_tile: the tile where that takes less time than two launches, or 0.
+int pair_gemm_tile(const int64_t (&M)[2], const int64_t (&N)[2], const int64_t (&K)[2],
+                   int variant, bool unscaled);
+hipError_t launch_gemm_pair(int tile, const Planes (&p)[2], const int64_t (&M)[2],
+                            const int64_t (&N)[2], float* const (&C)[2], const int64_t (&ldc)[2],
+                            float scale, int variant, const Unscale (&epi)[2],
+                            hipStream_t stream);
+
 struct LinearArgs {
   int64_t M, N, K;
   const float* x;

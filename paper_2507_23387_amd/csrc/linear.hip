@@ -90,13 +90,17 @@ hipError_t launch_linear(const LinearArgs& a, void* ws, hipStream_t stream) {
   if (linear_by_rows(a.M, a.N)) return launch_linear_rows(a, nullptr, ws, stream);
   Carver c{static_cast<char*>(ws), 0};
   const Planes p = carve_planes(c, a.M, a.N, a.K);
-  SplitJob jobs[2] = {job_of(a.x, a.ldx, a.M, a.K),
-                      a.transpose_w ? job_of(a.w, a.ldw, a.N, a.K)
-                                    : job_of(a.w, a.ldw, a.K, a.N)};
-  to_planes(jobs[0], p, false, false);
-  to_planes(jobs[1], p, true, !a.transpose_w);
-  const hipError_t err = launch_split_jobs(jobs, 2, a.scale, stream);
+  SplitJob jobs[2] = {a.transpose_w ? job_of(a.w, a.ldw, a.N, a.K)
+                                    : job_of(a.w, a.ldw, a.K, a.N),
+                      job_of(a.x, a.ldx, a.M, a.K)};
+  to_planes(jobs[0], p, true, !a.transpose_w);
+  to_planes(jobs[1], p, false, false);
+  const bool x_in_gemm = splits_a_in_gemm(a.M, a.N, a.x, a.ldx, a.K, a.scale, a.variant);
+  const hipError_t err = launch_split_jobs(jobs, x_in_gemm ? 1 : 2, a.scale, stream);
   if (err != hipSuccess) return err;
+  if (x_in_gemm)
+    return launch_gemm_fused_a_epilogue(p, a.M, a.N, a.K, a.x, a.ldx, a.y, a.ldy, a.scale,
+                                        a.variant, a.e, stream);
   return launch_gemm_epilogue(p, a.M, a.N, a.y, a.ldy, a.scale, a.variant, a.e, false,
                               stream);
 }
@@ -104,8 +108,11 @@ hipError_t launch_linear(const LinearArgs& a, void* ws, hipStream_t stream) {
 namespace {
 
 // Whether dX = D W^T (M x K, k over N) goes by rows.  D is then written as FP32 by
-// the kernel that sums its columns, where an activation makes it other than dY.
-bool grad_by_rows(int64_t M, int64_t K) { return linear_by_rows(M, K); }
+// the kernel that sums its columns, where an activation makes it other than dY.  A
+// small W is split with the rest instead, and both products take one launch (us,
+// rows against that: 64 rows, 1024 x 1024 30 and 25, 1024 x 2048 30 and 30, 2048 x
+// 2048 32 and 39, 4096 x 4096 58 and 75; 256 rows 4096 x 4096 122 and 104).
+bool grad_by_rows(int64_t M, int64_t N, int64_t K) { return M <= 128 && N * K >= 1500000; }
 
 struct GradWorkspace {
   uint32_t* max_bits;
@@ -123,7 +130,7 @@ GradWorkspace carve_grad(void* ws, int64_t M, int64_t N, int64_t K, bool transpo
   const int64_t strips = (N + kColumnStrip - 1) / kColumnStrip;
   g.partial = c.take<float>(column_slabs(M, N) * (N + strips));
   if (K > 0) {
-    if (grad_by_rows(M, K)) {
+    if (grad_by_rows(M, N, K)) {
       g.rows = c.take<char>(static_cast<int64_t>(linear_rows_ws(M, K, N)));
       g.d = c.take<float>(M * N);
     } else {
@@ -154,7 +161,7 @@ hipError_t launch_linear_grad(const LinearGradArgs& a, void* ws, hipStream_t str
   }
   const GradWorkspace g = carve_grad(ws, a.M, a.N, a.K, a.transpose_w);
   const bool dx = a.dx && a.K > 0, dw = a.dw && a.K > 0;
-  const bool dx_rows = dx && grad_by_rows(a.M, a.K);
+  const bool dx_rows = dx && grad_by_rows(a.M, a.N, a.K);
   const ColumnArgs cols{a.M, a.N, a.dy, a.lddy, a.z, a.ldz, a.activation, a.dbias, g.max_bits,
                         g.partial, dx_rows && a.z ? g.d : nullptr};
   const ColumnJoin join = column_join(cols);
@@ -201,6 +208,16 @@ hipError_t launch_linear_grad(const LinearGradArgs& a, void* ws, hipStream_t str
     r.scale = a.scale, r.variant = a.variant;
     err = launch_linear_rows(r, &ex, g.rows, stream);
   } else if (err == hipSuccess && dx) {
+    if (dw) {
+      const int64_t M[2] = {a.M, dw_rows}, N[2] = {a.K, dw_cols}, K[2] = {a.N, a.M};
+      if (const int tile = pair_gemm_tile(M, N, K, a.variant, !scaled_kernel_ok(a.scale))) {
+        const Planes p[2] = {g.dx, g.dw};
+        float* const C[2] = {a.dx, a.dw};
+        const int64_t ldc[2] = {a.lddx, a.lddw};
+        const Unscale epi[2] = {ex, ew};
+        return launch_gemm_pair(tile, p, M, N, C, ldc, a.scale, a.variant, epi, stream);
+      }
+    }
     err = launch_gemm_epilogue(g.dx, a.M, a.K, a.dx, a.lddx, a.scale, a.variant, ex, false,
                                stream);
   }

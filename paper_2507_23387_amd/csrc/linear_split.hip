@@ -77,22 +77,28 @@ constexpr int kPitch = kTileRows / 2 + 4;  // words per column in LDS; 16-byte a
 // columns from 8 (t % 16).  As row planes those are two 16-byte chunks of a tile
 // row each.  As column planes the pairs of rows go to LDS as words, a column's
 // side by side, and thread t writes chunk t of each of the tile's two slices.
-__device__ void split_tile(const SplitArgs& a, const SplitJob& g, uint32_t block,
-                           uint32_t max_bits, uint32_t* ph, uint32_t* pl) {
+// max_bits(): the bits of the magnitude that a job is scaled by, asked for once the
+// tile's loads are on their way.
+template <typename F>
+__device__ __forceinline__ void split_tile(const SplitArgs& a, const SplitJob& g, uint32_t block,
+                                           uint32_t* ph, uint32_t* pl, F max_bits_of) {
   const int t = threadIdx.x;
   const uint32_t strips = static_cast<uint32_t>((g.cols + kTileCols - 1) / kTileCols);
   const int64_t tr = block / strips, tc = block - static_cast<uint32_t>(tr) * strips;
   const int64_t i = tr * kTileRows + 2 * (t >> 4), j = tc * kTileCols + 8 * (t & 15);
-  float v[2][8];
+  float v[2][8], z[2][8];
 #pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    load8(g.s, g.ld, i + u, j, g.rows, g.cols, v[u]);
-    if (g.z) {
-      float z[8];
-      load8(g.z, g.ldz, i + u, j, g.rows, g.cols, z);
+  for (int u = 0; u < 2; ++u) load8(g.s, g.ld, i + u, j, g.rows, g.cols, v[u]);
+  if (g.z) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[u][e] *= activate_grad(g.activation, z[e]);
-    }
+    for (int u = 0; u < 2; ++u) load8(g.z, g.ldz, i + u, j, g.rows, g.cols, z[u]);
+  }
+  const uint32_t max_bits = g.max_bits ? max_bits_of() : 0;
+  if (g.z) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[u][e] *= activate_grad(g.activation, z[u][e]);
   }
   const int64_t kp_row = (g.cols + kKPad - 1) / kKPad * kKPad;
   const int64_t kp_col = (g.rows + kKPad - 1) / kKPad * kKPad;
@@ -157,7 +163,7 @@ __global__ __launch_bounds__(kThreads) void split_jobs_kernel(SplitArgs a) {
     int n = 0;
     while (n + 1 < a.count && b >= a.first[n + 1]) ++n;
     const SplitJob& g = a.job[n];
-    split_tile(a, g, b - a.first[n], g.max_bits ? *g.max_bits : 0, ph, pl);
+    split_tile(a, g, b - a.first[n], ph, pl, [&] { return *g.max_bits; });
     __syncthreads();  // the tile's LDS words are read before the next's are written
   }
 }
@@ -174,13 +180,12 @@ __global__ __launch_bounds__(kThreads) void split_join_kernel(SplitArgs a) {
   int n = 0;
   while (n + 1 < a.count && b >= a.first[n + 1]) ++n;
   const SplitJob& g = a.job[n];
-  uint32_t max_bits = 0;
-  if (g.max_bits) {
-    max_bits = join_top(a.join, reinterpret_cast<float*>(pl));
-    if (b == a.first[n] && threadIdx.x == 0) *a.join.max_bits = max_bits;
+  split_tile(a, g, b - a.first[n], ph, pl, [&] {
+    const uint32_t bits = join_top(a.join, reinterpret_cast<float*>(pl));
+    if (b == a.first[n] && threadIdx.x == 0) *a.join.max_bits = bits;
     __syncthreads();  // pl is read before the tile is written
-  }
-  split_tile(a, g, b - a.first[n], max_bits, ph, pl);
+    return bits;
+  });
 }
 
 // Rows that a thread has in flight.

@@ -95,12 +95,12 @@ def linear(X, W, bias=None, residual=None, activation: str = "none", transpose_w
     pb = _vector(bias, "bias", device, N)
     pr, ldr = (None, N) if residual is None else _matrix(residual, "residual", device, (M, N))
     if out is None:
-        Y = _new((M, N), X)
+        Y = X.new_empty((M, N))
         py, ldy = Y.data_ptr(), max(N, 1)
     else:
         Y = out
         py, ldy = _matrix(Y, "out", device, (M, N))
-    Z = _new((M, N), X) if keep_preact else None
+    Z = X.new_empty((M, N)) if keep_preact else None
     ws = workspace if workspace is not None else _bytes(
         binding.sgemm_cube_linear_workspace_size(M, N, K), X)
     _check(binding.sgemm_cube_linear(
@@ -110,8 +110,11 @@ def linear(X, W, bias=None, residual=None, activation: str = "none", transpose_w
     return (Y, Z) if keep_preact else Y
 
 
+_GRADIENTS = ("dX", "dW", "db")
+
+
 def linear_backward(dY, X, W, preact=None, activation: str = "none", transpose_w: bool = False,
-                    need=("dX", "dW", "db"), scale: float = 2.0**11, order="elementwise",
+                    need=_GRADIENTS, scale: float = 2.0**11, order="elementwise",
                     workspace=None):
     """(dX, dW, db) of linear at X and W from its output's gradient; preact: the Z
     that it kept, if it has an activation.  dW has W's layout.  What `need` leaves
@@ -127,18 +130,20 @@ def linear_backward(dY, X, W, preact=None, activation: str = "none", transpose_w
                          f"W for {K2} x {N}")
     if activation != "none" and preact is None:
         raise ValueError(f"{activation} needs preact, what linear returned with keep_preact=True")
-    if not set(need) <= {"dX", "dW", "db"}:
+    if need is not _GRADIENTS and not set(need) <= set(_GRADIENTS):
         raise ValueError("need may hold dX, dW and db")
     pz, ldz = (None, N) if activation == "none" else _matrix(preact, "preact", device,
                                                                  (M, N))
-    new = lambda name, *shape: _new(shape, X) if name in need else None  # noqa: E731
-    dX, dW, db = new("dX", M, K), new("dW", *W.shape), new("db", N)
-    at = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    dX = X.new_empty((M, K)) if "dX" in need else None
+    dW = X.new_empty(W.shape) if "dW" in need else None
+    db = X.new_empty((N,)) if "db" in need else None
     ws = workspace if workspace is not None else _bytes(
         binding.sgemm_cube_linear_backward_workspace_size(M, N, K), X)
     _check(binding.sgemm_cube_linear_backward(
         M, N, K, pdy, lddy, pz, ldz, px, ldx, pw, ldw, int(transpose_w), _activation(activation),
-        at(dX), max(K, 1), at(dW), max(W.size(1), 1), at(db), scale, _order(order), ws.data_ptr(),
+        None if dX is None else dX.data_ptr(), max(K, 1),
+        None if dW is None else dW.data_ptr(), max(W.shape[1], 1),
+        None if db is None else db.data_ptr(), scale, _order(order), ws.data_ptr(),
         ws.numel() * ws.element_size(), _stream(device)), "sgemm_cube_linear_backward")
     return dX, dW, db
 
