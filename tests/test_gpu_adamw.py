@@ -263,6 +263,21 @@ def test_empty_and_refused(gpu):
         sgc.AdamW(p, states={"exp_avgs": [shared[:8]], "exp_avg_sqs": [shared[4:]]}).step([f(8)])
 
 
+def test_exchanged_memory_is_refused(gpu):
+    import paper_2507_23387_amd as sgc
+
+    p, g = [torch.zeros(8, device="cuda") for _ in range(2)], [torch.ones(8, device="cuda")] * 2
+    opt = sgc.AdamW(p)
+    opt.step(g)
+    before = p[0].clone()
+    p[1].data = torch.zeros(8, device="cuda")
+    with pytest.raises(ValueError, match="memory"):
+        opt.step(g)
+    assert torch.equal(p[0], before) and opt.steps == 1
+    with pytest.raises(TypeError):
+        opt.states["exp_avgs"] = []
+
+
 def test_graph(gpu):
     import paper_2507_23387_amd as sgc
 

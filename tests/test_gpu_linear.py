@@ -357,3 +357,17 @@ def test_refused(gpu):
                 lambda: sgc.linear_backward(dY, X, W, scale=0.5)):
         with pytest.raises(sgc.SgemmCubeError):
             bad()
+
+
+def test_workspaces_the_device_cannot_reach_are_refused(gpu):
+    import paper_2507_23387_amd as sgc
+    from paper_2507_23387_amd import binding
+
+    X, W, dY = (torch.zeros(s, device="cuda") for s in ((4, 8), (8, 6), (4, 6)))
+    size = binding.sgemm_cube_linear_backward_workspace_size(4, 6, 8)
+    for ws in (torch.zeros(size, dtype=torch.uint8),
+               torch.zeros(2 * size, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(ValueError):
+            sgc.linear(X, W, workspace=ws)
+        with pytest.raises(ValueError):
+            sgc.linear_backward(dY, X, W, workspace=ws)
