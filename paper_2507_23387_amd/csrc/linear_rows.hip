@@ -119,13 +119,13 @@ __device__ __forceinline__ void store(const RowsArgs& g, int split, int64_t i, i
     g.partial[(split * g.a.M + i) * g.a.N + j] = v;
 }
 
-// Up to 16 rows and W's rows along k: the waves of a workgroup share 16 C columns
-// and take the steps of k in turn, so that together they read 2 KiB of each of
-// those rows of W in line, and add their sums in LDS.  1 x 8192 x 4096: 25.7 us, 5.2
+// Up to 16 rows (plan_rows): the waves of a workgroup share 16 C columns and take the
+// steps of k in turn, and add their sums in LDS.  Where W's rows are along k they
+// read 2 KiB of each of those rows in line together.  1 x 8192 x 4096: 25.7 us, 5.2
 // TB/s (64 columns a workgroup as below 30; 8 waves 28.6; one column block 30).
 constexpr int kLineWaves = 16;
 
-template <int kC, bool kGrad>
+template <bool kNk, int kC, bool kGrad>
 __global__ __launch_bounds__(64 * kLineWaves) void linear_line_kernel(RowsArgs g) {
   const LinearArgs& a = g.a;
   __shared__ float tile[kLineWaves][256 * kC];
@@ -137,9 +137,10 @@ __global__ __launch_bounds__(64 * kLineWaves) void linear_line_kernel(RowsArgs g
   // Rows and columns past the end repeat the last; they are not stored.
   const float* const xrow = a.x + min<int64_t>(l16, a.M - 1) * a.ldx;
   const int shift = kGrad ? prescale_shift(*g.unscale.max_bits, g.unscale.target) : 0;
-  const float* wrow[kC];
+  const float* wcol[kC];
 #pragma unroll
-  for (int c = 0; c < kC; ++c) wrow[c] = a.w + min<int64_t>(col0 + 16 * c + l16, a.N - 1) * a.ldw;
+  for (int c = 0; c < kC; ++c)
+    wcol[c] = a.w + min<int64_t>(col0 + 16 * c + l16, a.N - 1) * (kNk ? a.ldw : 1);
 
   struct Step {
     Values x, w[kC];
@@ -147,8 +148,11 @@ __global__ __launch_bounds__(64 * kLineWaves) void linear_line_kernel(RowsArgs g
   auto load = [&](int64_t step, Step& s, auto tail) {
 #pragma unroll
     for (int c = 0; c < kC; ++c)
-      load_along<true, tail.value>(wrow[c], step * kStep, a.K, group, s.w[c]);
-    load_along<true, tail.value>(xrow, step * kStep, a.K, group, s.x);
+      if constexpr (kNk)
+        load_along<true, tail.value>(wcol[c], step * kStep, a.K, group, s.w[c]);
+      else
+        load_across<tail.value>(wcol[c], a.ldw, step * kStep, a.K, group, s.w[c]);
+    load_along<kNk, tail.value>(xrow, step * kStep, a.K, group, s.x);
   };
   floatx4 hh[kC], cross[kC];
 #pragma unroll
@@ -371,10 +375,14 @@ struct RowsPlan {
 
 RowsPlan plan_rows(int64_t M, int64_t N, int64_t K, bool transpose_w) {
   RowsPlan p{};
-  p.line = transpose_w && M <= kBlockRows;
+  // Rows of W along n: 16 columns are half a cache line, which costs large weights
+  // more than the tiles' join (1 x 8192 x 8192 73 us, tiles 51; 16 x 4096 x 4096 22.6
+  // and 20.3) and small ones less (1 x 2048 x 2048 8.9 and 11.7, 512 x 512 9.0 and
+  // 11.6, 1024 x 4096 11.8 and 11.6).
+  p.line = M <= kBlockRows && (transpose_w || N * K <= (int64_t{1} << 22));
   int64_t most, fill;
   if (p.line) {
-    p.blocks = N >= 256 * 32 ? 2 : 1;
+    p.blocks = transpose_w && N >= 256 * 32 ? 2 : 1;
     p.groups = static_cast<int>((N + 16 * p.blocks - 1) / (16 * p.blocks));
     p.row_groups = 1;
     most = K / kStep / (4 * kLineWaves);  // four steps a wave at least
@@ -392,9 +400,9 @@ RowsPlan plan_rows(int64_t M, int64_t N, int64_t K, bool transpose_w) {
   return p;
 }
 
-template <int kC, bool kGrad>
+template <bool kNk, int kC, bool kGrad>
 hipError_t launch_line(const RowsArgs& g, const RowsPlan& p, hipStream_t stream) {
-  hipLaunchKernelGGL((linear_line_kernel<kC, kGrad>), dim3(p.groups * p.splits),
+  hipLaunchKernelGGL((linear_line_kernel<kNk, kC, kGrad>), dim3(p.groups * p.splits),
                      dim3(64 * kLineWaves), 0, stream, g);
   return hipGetLastError();
 }
@@ -422,8 +430,9 @@ hipError_t launch_tiles(const RowsArgs& g, const RowsPlan& p, hipStream_t stream
 template <bool kGrad>
 hipError_t launch_plan(const RowsArgs& g, const RowsPlan& p, hipStream_t stream) {
   if (p.line)
-    return p.blocks == 1 ? launch_line<1, kGrad>(g, p, stream)
-                         : launch_line<2, kGrad>(g, p, stream);
+    return !g.a.transpose_w ? launch_line<false, 1, kGrad>(g, p, stream)
+           : p.blocks == 1  ? launch_line<true, 1, kGrad>(g, p, stream)
+                            : launch_line<true, 2, kGrad>(g, p, stream);
   return g.a.transpose_w ? launch_tiles<true, kGrad>(g, p, stream)
                          : launch_tiles<false, kGrad>(g, p, stream);
 }
