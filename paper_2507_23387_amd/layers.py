@@ -242,7 +242,9 @@ class AdamW:
         kinds = self._kinds()
         if set(self.states) != set(kinds):
             raise ValueError(f"states must hold {', '.join(kinds)}")
-        self.states = MappingProxyType({key: tuple(self.states[key]) for key in kinds})
+        # Aliases of the given states: their memory stays as long as the optimizer.
+        self.states = MappingProxyType({key: tuple(t.detach() if isinstance(t, torch.Tensor) else t
+                                                   for t in self.states[key]) for key in kinds})
         self._list = (binding.AdamwTensor * n)()
         self._entries = list(self._list)
         self._device = device = _current_device()
@@ -258,8 +260,7 @@ class AdamW:
                 setattr(entry, field, _flat(self.states[key][i], f"states[{key!r}][{i}]", device,
                                             size, (dtype,)))
         self._counts = [p.numel() for p in self.params]
-        self._held = [t for ts in (self.params, *self.states.values()) for t in ts]
-        self._addresses = list(map(_address, self._held))
+        self._addresses = list(map(_address, self.params))
 
     def _kinds(self):
         """states' keys: (field of the list's entries, type, one value per block)."""
@@ -289,9 +290,9 @@ class AdamW:
         if dtype not in _DTYPES:
             raise TypeError("grads must be float32, float16 or bfloat16")
         device = self._check_held()
-        # _flat's checks over the whole list at a time, 20 us instead of 32 for 48
-        # gradients; where one fails, _flat finds which.
-        if (any(type(g) is not torch.Tensor for g in grads) or {g.dtype for g in grads} != {dtype}
+        # _flat's checks over the whole list at a time, two thirds of the time of one
+        # tensor after the other; where one fails, _flat finds which.
+        if (set(map(type, grads)) != {torch.Tensor} or {g.dtype for g in grads} != {dtype}
                 or set(map(_device_of, grads)) != {device} or not all(map(_contiguous, grads))
                 or list(map(_count, grads)) != self._counts):
             for i, (g, n) in enumerate(zip(grads, self._counts)):
@@ -328,9 +329,10 @@ class AdamW:
         return out
 
     def _check_held(self):
-        """The device; refuses what has moved since the addresses were taken."""
+        """The device; refuses parameters that have moved since their addresses were
+        taken."""
         if _current_device() != self._device:
             raise ValueError("the parameters are not on the current device")
-        if list(map(_address, self._held)) != self._addresses:
-            raise ValueError("a parameter or state is no longer in the memory it had")
+        if list(map(_address, self.params)) != self._addresses:
+            raise ValueError("a parameter is no longer in the memory it had")
         return self._device
