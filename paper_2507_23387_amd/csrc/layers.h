@@ -142,14 +142,17 @@ struct LinearArgs {
   int variant;
 };
 
-// The linear layer for few rows (linear_rows.hip), its sums termwise whatever the
-// variant.  linear_by_rows: the rule that chooses it.  With `grad`, x is a gradient
-// that is multiplied by the power of two of grad's Unscale as it is split, and the
-// result is freed of it again.
+// The linear layer for few rows or few columns (linear_rows.hip), its sums termwise
+// whatever the variant.  linear_by_rows, linear_by_columns: the rules that choose
+// them.  With `grad`, x is a gradient that is multiplied by the power of two of
+// grad's Unscale as it is split, and the result is freed of it again.  The
+// workspace of N columns is that of as many rows, linear_rows_ws(N, M, K).
 bool linear_by_rows(int64_t M, int64_t N);
+bool linear_by_columns(int64_t M, int64_t N);
 size_t linear_rows_ws(int64_t M, int64_t N, int64_t K);
 hipError_t launch_linear_rows(const LinearArgs& a, const Unscale* grad, void* ws,
                               hipStream_t stream);
+hipError_t launch_linear_columns(const LinearArgs& a, void* ws, hipStream_t stream);
 
 size_t linear_ws(int64_t M, int64_t N, int64_t K);
 hipError_t launch_linear(const LinearArgs& a, void* ws, hipStream_t stream);

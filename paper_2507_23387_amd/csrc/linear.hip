@@ -77,9 +77,19 @@ bool linear_by_rows(int64_t M, int64_t N) {
   return M <= 128 || (M <= 256 && M * N <= 800000);
 }
 
+// Few columns: the same with the sides exchanged, X read once as FP32 instead of
+// its planes written and read too.  Against tiles, us: 16384 x 1 x 8192 94 and 304,
+// 16384 x 64 x 2048 51 and 71, 300 x 128 x 8192 19 and 40, 16384 x 128 x 2048 76 and 82,
+// 4000 x 128 x 512 19 and 18, 1000 x 256 x 2048 21 and 21, but 4000 x 192 x 2048 38 and
+// 33.  (The bound on M keeps the grid below 2^32 threads.)
+bool linear_by_columns(int64_t M, int64_t N) {
+  return M <= (int64_t{1} << 25) && (N <= 128 || (N <= 256 && M * N <= 300000));
+}
+
 size_t linear_ws(int64_t M, int64_t N, int64_t K) {
   if (M == 0 || N == 0 || K == 0) return 0;
   if (linear_by_rows(M, N)) return linear_rows_ws(M, N, K);
+  if (linear_by_columns(M, N)) return linear_rows_ws(N, M, K);
   Carver c{nullptr, 0};
   (void)carve_planes(c, M, N, K);
   return c.used;
@@ -88,6 +98,7 @@ size_t linear_ws(int64_t M, int64_t N, int64_t K) {
 hipError_t launch_linear(const LinearArgs& a, void* ws, hipStream_t stream) {
   if (a.K == 0) return launch_epilogue(a.e, a.M, a.N, a.y, a.ldy, stream);
   if (linear_by_rows(a.M, a.N)) return launch_linear_rows(a, nullptr, ws, stream);
+  if (linear_by_columns(a.M, a.N)) return launch_linear_columns(a, ws, stream);
   Carver c{static_cast<char*>(ws), 0};
   const Planes p = carve_planes(c, a.M, a.N, a.K);
   SplitJob jobs[2] = {a.transpose_w ? job_of(a.w, a.ldw, a.N, a.K)

@@ -1,6 +1,8 @@
 // A linear layer for few rows (gfx950): what a token, or a serving step's tokens,
 // cost is reading W once, so W is read as FP32 and split in registers, and nothing
-// but the result is written.
+// but the result is written.  Few columns are the same with the sides exchanged,
+// Y^T = W^T X^T: "X" is then W^T, whose rows may lie along k or (kAcross) across it,
+// and "W" is X.
 //
 // Both kernels multiply 16-row blocks of X with 16 columns of W a wave, a 32-wide
 // step of k at a time: three v_mfma_f32_16x16x32_f16 per block, A_hi B_hi into one
@@ -91,9 +93,24 @@ __device__ __forceinline__ void load_across(const float* col, int64_t ldw, int64
   }
 }
 
+// Rows along n: eight values of step k0 of one column, each `ld` apart, at the k
+// that kNk gives them.
+template <bool kNk, bool kTail>
+__device__ __forceinline__ void load_strided(const float* col, int64_t ld, int64_t k0,
+                                             int64_t k_end, int g, Values& out) {
+#pragma unroll
+  for (int q = 0; q < 2; ++q)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int64_t k = k0 + quad_k<kNk>(g, q) + e;
+      out.v[4 * q + e] = !kTail || k < k_end ? col[k * ld] : 0.0f;
+    }
+}
+
 struct RowsArgs {
   LinearArgs a;
   bool grad;
+  bool swapped;  // Y^T = W^T X^T: entry (i, j) is row j, column i of Y
   Unscale unscale;
   float inv_s;
   int groups;      // of columns
@@ -101,20 +118,24 @@ struct RowsArgs {
   float* partial;  // splits x M x N, where splits > 1
 };
 
-__device__ __forceinline__ float finish(const RowsArgs& g, int64_t i, int64_t j, float z) {
+// Stores the result of row i, column j of Y.
+__device__ __forceinline__ void finish(const RowsArgs& g, int64_t i, int64_t j, float z) {
+  float* const y = g.a.y + i * g.a.ldy + j;
   const Epilogue& e = g.a.e;
-  if (g.grad)
-    return __builtin_ldexpf(z, -prescale_shift(*g.unscale.max_bits, g.unscale.target));
+  if (g.grad) {
+    *y = __builtin_ldexpf(z, -prescale_shift(*g.unscale.max_bits, g.unscale.target));
+    return;
+  }
   if (e.bias) z += e.bias[j];
   if (e.z) e.z[i * e.ldz + j] = z;
-  const float y = activate(e.activation, z);
-  return e.r ? y + e.r[i * e.ldr + j] : y;
+  const float v = activate(e.activation, z);
+  *y = e.r ? v + e.r[i * e.ldr + j] : v;
 }
 
 // Sum v of this split for entry (i, j): the result, or a partial sum.
 __device__ __forceinline__ void store(const RowsArgs& g, int split, int64_t i, int64_t j, float v) {
   if (g.splits == 1)
-    g.a.y[i * g.a.ldy + j] = finish(g, i, j, v);
+    finish(g, g.swapped ? j : i, g.swapped ? i : j, v);
   else
     g.partial[(split * g.a.M + i) * g.a.N + j] = v;
 }
@@ -125,7 +146,7 @@ __device__ __forceinline__ void store(const RowsArgs& g, int split, int64_t i, i
 // TB/s (64 columns a workgroup as below 30; 8 waves 28.6; one column block 30).
 constexpr int kLineWaves = 16;
 
-template <bool kNk, int kC, bool kGrad>
+template <bool kNk, int kC, bool kGrad, bool kAcross>
 __global__ __launch_bounds__(64 * kLineWaves) void linear_line_kernel(RowsArgs g) {
   const LinearArgs& a = g.a;
   __shared__ float tile[kLineWaves][256 * kC];
@@ -135,7 +156,7 @@ __global__ __launch_bounds__(64 * kLineWaves) void linear_line_kernel(RowsArgs g
   const int col_group = index / g.splits, split = index - col_group * g.splits;
   const int64_t col0 = static_cast<int64_t>(col_group) * (16 * kC);
   // Rows and columns past the end repeat the last; they are not stored.
-  const float* const xrow = a.x + min<int64_t>(l16, a.M - 1) * a.ldx;
+  const float* const xrow = a.x + min<int64_t>(l16, a.M - 1) * (kAcross ? 1 : a.ldx);
   const int shift = kGrad ? prescale_shift(*g.unscale.max_bits, g.unscale.target) : 0;
   const float* wcol[kC];
 #pragma unroll
@@ -152,7 +173,10 @@ __global__ __launch_bounds__(64 * kLineWaves) void linear_line_kernel(RowsArgs g
         load_along<true, tail.value>(wcol[c], step * kStep, a.K, group, s.w[c]);
       else
         load_across<tail.value>(wcol[c], a.ldw, step * kStep, a.K, group, s.w[c]);
-    load_along<kNk, tail.value>(xrow, step * kStep, a.K, group, s.x);
+    if constexpr (kAcross)
+      load_strided<kNk, tail.value>(xrow, a.ldx, step * kStep, a.K, group, s.x);
+    else
+      load_along<kNk, tail.value>(xrow, step * kStep, a.K, group, s.x);
   };
   floatx4 hh[kC], cross[kC];
 #pragma unroll
@@ -226,7 +250,7 @@ __global__ __launch_bounds__(64 * kLineWaves) void linear_line_kernel(RowsArgs g
 constexpr int kTileWaves = 4, kTileCols = 16 * kTileWaves;
 constexpr int kChunkSteps = 2, kChunkK = kChunkSteps * kStep;
 
-template <bool kNk, int kR, bool kGrad>
+template <bool kNk, int kR, bool kGrad, bool kAcross>
 __global__ __launch_bounds__(64 * kTileWaves, 3) void linear_rows_tile_kernel(RowsArgs g) {
   const LinearArgs& a = g.a;
   constexpr int kUnits = kChunkSteps * kR;  // fragments of a chunk of X, of each plane
@@ -250,7 +274,8 @@ __global__ __launch_bounds__(64 * kTileWaves, 3) void linear_rows_tile_kernel(Ro
 #pragma unroll
   for (int n = 0; n < kPer; ++n) {
     unit[n] = min(wave + kTileWaves * n, kUnits - 1);
-    xrow[n] = a.x + min<int64_t>(row0 + 16 * (unit[n] % kR) + l16, a.M - 1) * a.ldx;
+    xrow[n] = a.x + min<int64_t>(row0 + 16 * (unit[n] % kR) + l16, a.M - 1) *
+                        (kAcross ? 1 : a.ldx);
   }
 
   const int shift = kGrad ? prescale_shift(*g.unscale.max_bits, g.unscale.target) : 0;
@@ -265,8 +290,13 @@ __global__ __launch_bounds__(64 * kTileWaves, 3) void linear_rows_tile_kernel(Ro
   };
   auto load_x = [&](int64_t c, auto tail) {
 #pragma unroll
-    for (int n = 0; n < kPer; ++n)
-      load_along<kNk, tail.value>(xrow[n], c * kChunkK + unit[n] / kR * kStep, a.K, group, x[n]);
+    for (int n = 0; n < kPer; ++n) {
+      const int64_t k0 = c * kChunkK + unit[n] / kR * kStep;
+      if constexpr (kAcross)
+        load_strided<kNk, tail.value>(xrow[n], a.ldx, k0, a.K, group, x[n]);
+      else
+        load_along<kNk, tail.value>(xrow[n], k0, a.K, group, x[n]);
+    }
   };
   auto store_x = [&](int slot) {
 #pragma unroll
@@ -364,7 +394,7 @@ __global__ __launch_bounds__(256) void linear_join_kernel(RowsArgs g) {
   float v = 0.0f;
 #pragma unroll 4
   for (int s = 0; s < g.splits; ++s) v += g.partial[s * a.M * a.N + q];
-  a.y[i * a.ldy + j] = finish(g, i, j, v);
+  finish(g, g.swapped ? j : i, g.swapped ? i : j, v);
 }
 
 struct RowsPlan {
@@ -390,6 +420,9 @@ RowsPlan plan_rows(int64_t M, int64_t N, int64_t K, bool transpose_w) {
   } else {
     p.blocks = static_cast<int>(std::min<int64_t>((M + kBlockRows - 1) / kBlockRows, 4));
     p.row_groups = static_cast<int>((M + kBlockRows * p.blocks - 1) / (kBlockRows * p.blocks));
+    // The groups even: 65 to 96 rows are two groups of three blocks.
+    const int64_t even = kBlockRows * static_cast<int64_t>(p.row_groups);
+    p.blocks = static_cast<int>((M + even - 1) / even);
     p.groups = static_cast<int>((N + kTileCols - 1) / kTileCols);
     // The join costs 4 us, as much as four chunks of a lone workgroup.
     most = K / kChunkK > 5 ? K / kChunkK / 2 : 1;
@@ -400,30 +433,30 @@ RowsPlan plan_rows(int64_t M, int64_t N, int64_t K, bool transpose_w) {
   return p;
 }
 
-template <bool kNk, int kC, bool kGrad>
+template <bool kNk, int kC, bool kGrad, bool kAcross = false>
 hipError_t launch_line(const RowsArgs& g, const RowsPlan& p, hipStream_t stream) {
-  hipLaunchKernelGGL((linear_line_kernel<kNk, kC, kGrad>), dim3(p.groups * p.splits),
+  hipLaunchKernelGGL((linear_line_kernel<kNk, kC, kGrad, kAcross>), dim3(p.groups * p.splits),
                      dim3(64 * kLineWaves), 0, stream, g);
   return hipGetLastError();
 }
 
-template <bool kNk, int kR, bool kGrad>
+template <bool kNk, int kR, bool kGrad, bool kAcross>
 hipError_t launch_tile(const RowsArgs& g, const RowsPlan& p, hipStream_t stream) {
   constexpr size_t kLds = static_cast<size_t>(2) * kChunkSteps * kR * 2 * 1024;
   static_assert(kLds <= 64 * 1024, "both chunks fit LDS without asking for more");
-  hipLaunchKernelGGL((linear_rows_tile_kernel<kNk, kR, kGrad>),
+  hipLaunchKernelGGL((linear_rows_tile_kernel<kNk, kR, kGrad, kAcross>),
                      dim3(p.groups * p.splits, p.row_groups), dim3(64 * kTileWaves), kLds, stream,
                      g);
   return hipGetLastError();
 }
 
-template <bool kNk, bool kGrad>
+template <bool kNk, bool kGrad, bool kAcross = false>
 hipError_t launch_tiles(const RowsArgs& g, const RowsPlan& p, hipStream_t stream) {
   switch (p.blocks) {
-    case 1: return launch_tile<kNk, 1, kGrad>(g, p, stream);
-    case 2: return launch_tile<kNk, 2, kGrad>(g, p, stream);
-    case 3: return launch_tile<kNk, 3, kGrad>(g, p, stream);
-    default: return launch_tile<kNk, 4, kGrad>(g, p, stream);
+    case 1: return launch_tile<kNk, 1, kGrad, kAcross>(g, p, stream);
+    case 2: return launch_tile<kNk, 2, kGrad, kAcross>(g, p, stream);
+    case 3: return launch_tile<kNk, 3, kGrad, kAcross>(g, p, stream);
+    default: return launch_tile<kNk, 4, kGrad, kAcross>(g, p, stream);
   }
 }
 
@@ -437,6 +470,15 @@ hipError_t launch_plan(const RowsArgs& g, const RowsPlan& p, hipStream_t stream)
                          : launch_tiles<false, kGrad>(g, p, stream);
 }
 
+// The join, where sums were left for one.
+hipError_t launch_join(const RowsArgs& g, hipStream_t stream) {
+  if (g.splits == 1) return hipSuccess;
+  hipLaunchKernelGGL(linear_join_kernel,
+                     dim3(static_cast<unsigned>((g.a.M * g.a.N + 255) / 256)), dim3(256), 0,
+                     stream, g);
+  return hipGetLastError();
+}
+
 }  // namespace
 
 size_t linear_rows_ws(int64_t M, int64_t N, int64_t K) {
@@ -448,13 +490,26 @@ size_t linear_rows_ws(int64_t M, int64_t N, int64_t K) {
 hipError_t launch_linear_rows(const LinearArgs& a, const Unscale* grad, void* ws,
                               hipStream_t stream) {
   const RowsPlan p = plan_rows(a.M, a.N, a.K, a.transpose_w);
-  const RowsArgs g{a, grad != nullptr, grad ? *grad : Unscale{}, 1.0f / a.scale, p.groups,
-                   p.splits, static_cast<float*>(ws)};
+  const RowsArgs g{a, grad != nullptr, false, grad ? *grad : Unscale{}, 1.0f / a.scale,
+                   p.groups, p.splits, static_cast<float*>(ws)};
   const hipError_t e = grad ? launch_plan<true>(g, p, stream) : launch_plan<false>(g, p, stream);
-  if (e != hipSuccess || p.splits == 1) return e;
-  hipLaunchKernelGGL(linear_join_kernel, dim3(static_cast<unsigned>((a.M * a.N + 255) / 256)),
-                     dim3(256), 0, stream, g);
-  return hipGetLastError();
+  return e == hipSuccess ? launch_join(g, stream) : e;
+}
+
+hipError_t launch_linear_columns(const LinearArgs& a, void* ws, hipStream_t stream) {
+  LinearArgs t = a;
+  t.M = a.N, t.N = a.M;
+  t.x = a.w, t.ldx = a.ldw;
+  t.w = a.x, t.ldw = a.ldx, t.transpose_w = true;
+  const RowsPlan p = plan_rows(t.M, t.N, t.K, true);
+  const RowsArgs g{t, false, true, Unscale{}, 1.0f / a.scale, p.groups, p.splits,
+                   static_cast<float*>(ws)};
+  const hipError_t e =
+      a.transpose_w ? launch_plan<false>(g, p, stream)
+      : !p.line     ? launch_tiles<true, false, true>(g, p, stream)
+      : p.blocks == 1 ? launch_line<true, 1, false, true>(g, p, stream)
+                      : launch_line<true, 2, false, true>(g, p, stream);
+  return e == hipSuccess ? launch_join(g, stream) : e;
 }
 
 }  // namespace sgc
