@@ -38,16 +38,6 @@ struct Elem<kBF16> {
 
 constexpr int kThreads = 256;
 
-// Sum over the workgroup's threads, the same bits in each.
-__device__ __forceinline__ float block_sum(float v, float* lds) {
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return (lds[0] + lds[1]) + (lds[2] + lds[3]);
-}
-
 // Elements j .. j + kE - 1 of a row of n, zeros past its end.
 template <int kDtype>
 __device__ __forceinline__ void load_piece(const typename Elem<kDtype>::T* row, int j, int n,
@@ -88,23 +78,27 @@ __device__ __forceinline__ void load_row(const typename Elem<kDtype>::T* row, in
   for (int c = 0; c < kP / kE; ++c) load_piece<kDtype>(row, (c * kT + t) * kE, n, v + c * kE);
 }
 
-// The same values of an FP32 vector, `fill` where there is no vector.
+// Values j .. j + kE - 1 of an FP32 vector, `fill` where there is no vector.
+template <int kE>
+__device__ __forceinline__ void vector_piece(const float* p, int j, int n, float fill, float* v) {
+#pragma unroll
+  for (int e = 0; e < kE; e += 4) {
+    if (p) {
+      load_piece<kF32>(p, j + e, n, v + e);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[e + i] = fill;
+    }
+  }
+}
+
+// A thread's kP values of an FP32 vector (load_row).
 template <int kDtype, int kT, int kP>
 __device__ __forceinline__ void load_vector(const float* p, int t, int n, float fill,
                                             float (&v)[kP]) {
   constexpr int kE = Elem<kDtype>::kE;
 #pragma unroll
-  for (int c = 0; c < kP / kE; ++c)
-#pragma unroll
-    for (int e = 0; e < kE; e += 4) {
-      const int j = (c * kT + t) * kE + e;
-      if (p) {
-        load_piece<kF32>(p, j, n, v + c * kE + e);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[c * kE + e + i] = fill;
-      }
-    }
+  for (int c = 0; c < kP / kE; ++c) vector_piece<kE>(p, (c * kT + t) * kE, n, fill, v + c * kE);
 }
 
 __device__ __forceinline__ float wave_sum(float v) {
@@ -192,27 +186,57 @@ __global__ __launch_bounds__(kT < kThreads ? kThreads : kT, kP <= 8 ? 8 : 4) voi
   }
 }
 
-// Rows of any length: a workgroup per row, three passes over it.
+// Rows of any length: a workgroup of 1024 threads per row, three passes over it, the
+// last two from the caches.  A thread at a value and 256 to a row, it was the wait for
+// one load after the other: 64 x 33000 53 us.
+constexpr int kLongThreads = 1024;
+
+// f(j, piece of x at j) over a row's pieces.
+template <int kDtype, typename F>
+__device__ __forceinline__ void each_piece(const typename Elem<kDtype>::T* row, int n, F f) {
+  constexpr int kE = Elem<kDtype>::kE;
+#pragma unroll 2
+  for (int64_t j = threadIdx.x * kE; j < n; j += kLongThreads * kE) {
+    float v[kE];
+    load_piece<kDtype>(row, static_cast<int>(j), n, v);
+    f(static_cast<int>(j), v);
+  }
+}
+
 template <int kDtype>
-__global__ __launch_bounds__(kThreads) void norm_kernel(NormArgs a) {
+__global__ __launch_bounds__(kLongThreads) void norm_kernel(NormArgs a) {
   typedef typename Elem<kDtype>::T T;
-  __shared__ float lds[kThreads / 64];
+  constexpr int kE = Elem<kDtype>::kE;
+  __shared__ float lds[2][kLongThreads / 64];
+  const int n = static_cast<int>(a.cols);
   for (int64_t i = blockIdx.x; i < a.rows; i += gridDim.x) {
     const T* x = static_cast<const T*>(a.x) + i * a.ldx;
     T* y = static_cast<T*>(a.y) + i * a.ldy;
-    float s = 0.0f;
-    for (int64_t j = threadIdx.x; j < a.cols; j += kThreads) s += static_cast<float>(x[j]);
-    const float mu = block_sum(s, lds) / static_cast<float>(a.cols);
-    s = 0.0f;
-    for (int64_t j = threadIdx.x; j < a.cols; j += kThreads) {
-      const float d = static_cast<float>(x[j]) - mu;
-      s += d * d;
-    }
-    const float r = 1.0f / __builtin_sqrtf(block_sum(s, lds) / static_cast<float>(a.cols) + a.eps);
-    for (int64_t j = threadIdx.x; j < a.cols; j += kThreads) {
-      const float h = (static_cast<float>(x[j]) - mu) * r;
-      y[j] = static_cast<T>(h * (a.weight ? a.weight[j] : 1.0f) + (a.bias ? a.bias[j] : 0.0f));
-    }
+    float s[1] = {0.0f};
+    each_piece<kDtype>(x, n, [&](int, const float (&v)[kE]) {
+#pragma unroll
+      for (int e = 0; e < kE; ++e) s[0] += v[e];
+    });
+    row_sums<kLongThreads, 1>(s, lds[0]);
+    const float mu = s[0] / static_cast<float>(a.cols);
+    s[0] = 0.0f;
+    each_piece<kDtype>(x, n, [&](int j, const float (&v)[kE]) {
+#pragma unroll
+      for (int e = 0; e < kE; ++e) {
+        const float d = j + e < n ? v[e] - mu : 0.0f;
+        s[0] += d * d;
+      }
+    });
+    row_sums<kLongThreads, 1>(s, lds[1]);
+    const float r = 1.0f / __builtin_sqrtf(s[0] / static_cast<float>(a.cols) + a.eps);
+    each_piece<kDtype>(x, n, [&](int j, const float (&v)[kE]) {
+      float w[kE], b[kE], o[kE];
+      vector_piece<kE>(a.weight, j, n, 1.0f, w);
+      vector_piece<kE>(a.bias, j, n, 0.0f, b);
+#pragma unroll
+      for (int e = 0; e < kE; ++e) o[e] = (v[e] - mu) * r * w[e] + b[e];
+      store_piece<kDtype>(y, j, n, o);
+    });
     if (threadIdx.x == 0) {
       if (a.mean) a.mean[i] = mu;
       if (a.rstd) a.rstd[i] = r;
@@ -304,29 +328,46 @@ __global__ __launch_bounds__(kGradThreads) void norm_grad_rows_kernel(NormGradAr
   }
 }
 
-// dX, a workgroup per row.
+// dX of rows of any length, a workgroup per row.
 template <int kDtype>
-__global__ __launch_bounds__(kThreads) void norm_dx_kernel(NormGradArgs a) {
+__global__ __launch_bounds__(kLongThreads) void norm_dx_kernel(NormGradArgs a) {
   typedef typename Elem<kDtype>::T T;
-  __shared__ float lds[kThreads / 64];
-  for (int64_t i = blockIdx.x; i < a.rows; i += gridDim.x) {
+  constexpr int kE = Elem<kDtype>::kE;
+  __shared__ float lds[2][2 * kLongThreads / 64];
+  const int n = static_cast<int>(a.cols);
+  int turn = 0;
+  for (int64_t i = blockIdx.x; i < a.rows; i += gridDim.x, turn ^= 1) {
     const T* x = static_cast<const T*>(a.x) + i * a.ldx;
     const T* dy = static_cast<const T*>(a.dy) + i * a.lddy;
     T* dx = static_cast<T*>(a.dx) + i * a.lddx;
     const float mu = a.mean[i], r = a.rstd[i];
-    float s1 = 0.0f, s2 = 0.0f;
-    for (int64_t j = threadIdx.x; j < a.cols; j += kThreads) {
-      const float g = static_cast<float>(dy[j]) * (a.weight ? a.weight[j] : 1.0f);
-      s1 += g;
-      s2 += g * ((static_cast<float>(x[j]) - mu) * r);
-    }
-    s1 = block_sum(s1, lds) / static_cast<float>(a.cols);
-    s2 = block_sum(s2, lds) / static_cast<float>(a.cols);
-    for (int64_t j = threadIdx.x; j < a.cols; j += kThreads) {
-      const float g = static_cast<float>(dy[j]) * (a.weight ? a.weight[j] : 1.0f);
-      const float h = (static_cast<float>(x[j]) - mu) * r;
-      dx[j] = static_cast<T>(r * (g - s1 - h * s2));
-    }
+    // g = dY weight and h of a piece; zeros past the row's end.
+    auto both = [&](int j, const float (&v)[kE], float (&g)[kE], float (&h)[kE]) {
+      float w[kE];
+      vector_piece<kE>(a.weight, j, n, 1.0f, w);
+      load_piece<kDtype>(dy, j, n, g);
+#pragma unroll
+      for (int e = 0; e < kE; ++e) {
+        g[e] *= w[e];
+        h[e] = j + e < n ? (v[e] - mu) * r : 0.0f;
+      }
+    };
+    float s[2] = {0.0f, 0.0f};
+    each_piece<kDtype>(x, n, [&](int j, const float (&v)[kE]) {
+      float g[kE], h[kE];
+      both(j, v, g, h);
+#pragma unroll
+      for (int e = 0; e < kE; ++e) s[0] += g[e], s[1] += g[e] * h[e];
+    });
+    row_sums<kLongThreads, 2>(s, lds[turn]);
+    const float m1 = s[0] / static_cast<float>(a.cols), m2 = s[1] / static_cast<float>(a.cols);
+    each_piece<kDtype>(x, n, [&](int j, const float (&v)[kE]) {
+      float g[kE], h[kE], o[kE];
+      both(j, v, g, h);
+#pragma unroll
+      for (int e = 0; e < kE; ++e) o[e] = r * (g[e] - m1 - h[e] * m2);
+      store_piece<kDtype>(dx, j, n, o);
+    });
   }
 }
 
@@ -399,7 +440,7 @@ hipError_t forward(const NormArgs& a, hipStream_t stream) {
   if (n > 0 && n <= 256 * 16) return forward_rows<kDtype, 256, 16>(a, stream);
   if (n > 0 && n <= 1024 * 8) return forward_rows<kDtype, 1024, 8>(a, stream);
   if (n > 0 && n <= 1024 * 16) return forward_rows<kDtype, 1024, 16>(a, stream);
-  hipLaunchKernelGGL(norm_kernel<kDtype>, dim3(row_grid(a.rows)), dim3(kThreads), 0, stream, a);
+  hipLaunchKernelGGL(norm_kernel<kDtype>, dim3(row_grid(a.rows)), dim3(kLongThreads), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -449,7 +490,7 @@ hipError_t grad(const NormGradArgs& a, hipStream_t stream) {
     if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     if (const hipError_t e = join(a, slabs, stream); e != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(norm_dx_kernel<kDtype>, dim3(row_grid(a.rows)), dim3(kThreads), 0, stream, a);
+  hipLaunchKernelGGL(norm_dx_kernel<kDtype>, dim3(row_grid(a.rows)), dim3(kLongThreads), 0, stream, a);
   return hipGetLastError();
 }
 
