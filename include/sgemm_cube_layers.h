@@ -44,7 +44,9 @@ typedef enum {
  *   Y, ldy       row-major M x N, ldy >= max(1, N).
  *   Z, ldz       NULL, or row-major M x N that receives Z, what the backward
  *                pass needs of a layer with an activation.
- *   scale, accum_order  as for sgemm_cube.
+ *   scale, accum_order  as for sgemm_cube.  Results of few rows or columns (up to
+ *                128, or 256 where there are few entries) are computed from FP32
+ *                operands directly, the sums termwise whatever the order.
  *   ws, ws_bytes at least sgemm_cube_linear_workspace_size(M, N, K) bytes,
  *                256-byte aligned, as for sgemm_cube_ws.
  * Outputs must not overlap each other, an input or the workspace, but for R.

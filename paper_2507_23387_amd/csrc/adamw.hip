@@ -262,7 +262,9 @@ __device__ __forceinline__ int wave_blocks(const Entry& e, int64_t& first) {
   return static_cast<int>(min<int64_t>(max<int64_t>(left, 0), kWaveBlocks));
 }
 
-// Where the wave has all its blocks whole it reads two before it steps either.
+// Where the wave has all its blocks whole it reads two before it steps either.  HBM
+// bounds it: 201 M values with 32-bit states and bfloat16 gradients 968 us (5.24 GB,
+// 5.4 TB/s), one value a lane and access 2190; 8 bits: above.
 template <int kBits, typename G>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(Args a) {
   const Entry& e = a.e[entry_of(a, blockIdx.x)];

@@ -78,6 +78,24 @@ __device__ __forceinline__ void load_row(const typename Elem<kDtype>::T* row, in
   for (int c = 0; c < kP / kE; ++c) load_piece<kDtype>(row, (c * kT + t) * kE, n, v + c * kE);
 }
 
+// The same pieces as they lie.
+template <int kDtype, int kT, int kP>
+__device__ __forceinline__ void load_raw(const typename Elem<kDtype>::T* row, int t, int n,
+                                         typename Elem<kDtype>::Piece (&p)[kP / Elem<kDtype>::kE]) {
+  using L = Elem<kDtype>;
+#pragma unroll
+  for (int c = 0; c < kP / L::kE; ++c) {
+    const int j = (c * kT + t) * L::kE;
+    if (j + L::kE <= n) {
+      p[c] = *reinterpret_cast<const typename L::Piece*>(row + j);
+    } else {
+#pragma unroll
+      for (int e = 0; e < L::kE; ++e)
+        p[c][e] = j + e < n ? row[j + e] : static_cast<typename L::T>(0.0f);
+    }
+  }
+}
+
 // Values j .. j + kE - 1 of an FP32 vector, `fill` where there is no vector.
 template <int kE>
 __device__ __forceinline__ void vector_piece(const float* p, int j, int n, float fill, float* v) {
@@ -132,7 +150,8 @@ __device__ __forceinline__ void row_sums(float (&v)[kN], float* lds) {
 
 // Rows whose values fit the registers of kT threads, kP each: one pass over HBM.
 // A workgroup walks the rows with a stride, so that weight and bias are read once
-// and the next row is on its way while this one is reduced.
+// and the next row is on its way while this one is reduced.  HBM bounds it: 16384 x
+// 4096 98 us in FP32 (5.5 TB/s), 46 in bfloat16 (5.8); three passes took 209.
 template <int kDtype, int kT, int kP>
 __global__ __launch_bounds__(kT < kThreads ? kThreads : kT, kP <= 8 ? 8 : 4) void norm_rows_kernel(
     NormArgs a) {
@@ -188,7 +207,7 @@ __global__ __launch_bounds__(kT < kThreads ? kThreads : kT, kP <= 8 ? 8 : 4) voi
 
 // Rows of any length: a workgroup of 1024 threads per row, three passes over it, the
 // last two from the caches.  A thread at a value and 256 to a row, it was the wait for
-// one load after the other: 64 x 33000 53 us.
+// one load after the other: 64 x 33000 53 us, so 11; 4096 x 33000 530 and 280 (3.9 TB/s).
 constexpr int kLongThreads = 1024;
 
 // f(j, piece of x at j) over a row's pieces.
@@ -248,56 +267,62 @@ __global__ __launch_bounds__(kLongThreads) void norm_kernel(NormArgs a) {
 // the column sums of the workgroup's rows, in one pass over HBM.  1024 threads
 // work on 1024 / kT rows at a time, each with the columns of its values; at the
 // end those threads' sums are added in LDS, row by row of threads, and the
-// workgroup writes one slab of partial sums.
+// workgroup writes one slab of partial sums.  16384 x 4096: 152 us in FP32 (5.3 TB/s),
+// 88 in bfloat16 (4.6 TB/s); dX and the sums in passes of their own took 315 there.
 constexpr int kGradThreads = 1024;
 
 template <int kDtype, int kT, int kP>
 __global__ __launch_bounds__(kGradThreads) void norm_grad_rows_kernel(NormGradArgs a) {
   typedef typename Elem<kDtype>::T T;
   constexpr int kE = Elem<kDtype>::kE, kRows = kGradThreads / kT;
-  // The next row is on its way while this one is reduced; at 16 values a thread
-  // there are no registers for it.
-  constexpr bool kAhead = kP <= 8;
+  // Rows on their way while one is reduced, as they lie: two of 16-bit values, one of
+  // FP32 (a second one's registers spill: 16384 x 4096 156 us, so 152), none at 16
+  // values a thread.  16384 x 4096 bfloat16 100 us with one, 88 with two.
+  constexpr int kDepth = kP > 8 ? 0 : kE == 4 ? 1 : 2;
   __shared__ float lds[2][2 * kGradThreads / 64];
   extern __shared__ float sums[];  // 2 x kT x kP
   static_assert(2 * kT * kP * sizeof(float) <= 128 * 1024, "the sums fit LDS");
   const int t = threadIdx.x % kT, group = threadIdx.x / kT, n = static_cast<int>(a.cols);
-  float w[kP], dw[kP], db[kP], nx[kP], ng[kP];
+  float w[kP], dw[kP], db[kP];
   load_vector<kDtype, kT, kP>(a.weight, t, n, 1.0f, w);
 #pragma unroll
   for (int e = 0; e < kP; ++e) dw[e] = db[e] = 0.0f;
   const float rn = 1.0f / static_cast<float>(n);
   const int64_t stride = static_cast<int64_t>(gridDim.x) * kRows;
   int64_t first = static_cast<int64_t>(blockIdx.x) * kRows;
-  auto fetch = [&](int64_t row) {
-    row = min(row, a.rows - 1);
-    load_row<kDtype, kT, kP>(static_cast<const T*>(a.x) + row * a.ldx, t, n, nx);
-    load_row<kDtype, kT, kP>(static_cast<const T*>(a.dy) + row * a.lddy, t, n, ng);
+  struct Ahead {
+    typename Elem<kDtype>::Piece x[kP / kE], g[kP / kE];
+    float mu, r;
   };
-  if (kAhead) fetch(first + group);
+  auto fetch = [&](int64_t row, Ahead& to) {
+    row = min(row + group, a.rows - 1);
+    load_raw<kDtype, kT, kP>(static_cast<const T*>(a.x) + row * a.ldx, t, n, to.x);
+    load_raw<kDtype, kT, kP>(static_cast<const T*>(a.dy) + row * a.lddy, t, n, to.g);
+    to.mu = a.mean[row];
+    to.r = a.rstd[row];
+  };
   // The whole workgroup takes every step (the sums wait at barriers); threads past
   // the last row repeat it and keep nothing.
-  for (int turn = 0; first < a.rows; first += stride, turn ^= 1) {
-    const int64_t i = min(first + group, a.rows - 1);
+  auto step = [&](Ahead& in, float* slot) {
     const bool mine = first + group < a.rows;
-    const float mu = a.mean[i], r = a.rstd[i];
-    if (!kAhead) fetch(first + group);
+    const float mu = in.mu, r = in.r;
     float h[kP], g[kP], s[2] = {0.0f, 0.0f};
 #pragma unroll
     for (int e = 0; e < kP; ++e) {
-      const bool in = (e / kE * kT + t) * kE + e % kE < n;
-      h[e] = in ? (nx[e] - mu) * r : 0.0f;
-      dw[e] += mine ? ng[e] * h[e] : 0.0f;
-      db[e] += mine ? ng[e] : 0.0f;
-      g[e] = ng[e] * w[e];
+      const bool inside = (e / kE * kT + t) * kE + e % kE < n;
+      const float dy = static_cast<float>(in.g[e / kE][e % kE]);
+      h[e] = inside ? (static_cast<float>(in.x[e / kE][e % kE]) - mu) * r : 0.0f;
+      dw[e] += mine ? dy * h[e] : 0.0f;
+      db[e] += mine ? dy : 0.0f;
+      g[e] = dy * w[e];
       s[0] += g[e];
       s[1] += g[e] * h[e];
     }
-    if (kAhead && first + stride < a.rows) fetch(first + stride + group);
-    row_sums<kT, 2>(s, lds[turn]);
+    if (kDepth && first + kDepth * stride < a.rows) fetch(first + kDepth * stride, in);
+    row_sums<kT, 2>(s, slot);
     if (mine) {
       const float m1 = s[0] * rn, m2 = s[1] * rn;
-      T* const dx = static_cast<T*>(a.dx) + i * a.lddx;
+      T* const dx = static_cast<T*>(a.dx) + (first + group) * a.lddx;
 #pragma unroll
       for (int c = 0; c < kP / kE; ++c) {
         float o[kE];
@@ -305,6 +330,22 @@ __global__ __launch_bounds__(kGradThreads) void norm_grad_rows_kernel(NormGradAr
         for (int e = 0; e < kE; ++e) o[e] = r * (g[c * kE + e] - m1 - h[c * kE + e] * m2);
         store_piece<kDtype>(dx, (c * kT + t) * kE, n, o);
       }
+    }
+    first += stride;
+  };
+  Ahead in[kDepth ? kDepth : 1];
+#pragma unroll
+  for (int d = 0; d < kDepth; ++d) fetch(first + d * stride, in[d]);
+  if constexpr (kDepth == 2) {
+    while (first < a.rows) {
+      step(in[0], lds[0]);
+      if (first >= a.rows) break;
+      step(in[1], lds[1]);
+    }
+  } else {
+    for (int turn = 0; first < a.rows; turn ^= 1) {
+      if (kDepth == 0) fetch(first, in[0]);
+      step(in[0], lds[turn]);
     }
   }
   if (!a.dweight && !a.dbias) return;
