@@ -1,7 +1,7 @@
 """The LDS copies and the MFMAs of the GEMM kernels are inline asm, so the compiler's
 hazard recognizer does not see them.  A VMEM instruction may read a scalar register
 that a vector instruction wrote only after 5 wait states, and a vector instruction
-an MFMA's result only after 16 (more than the 11 of an 8-pass MFMA; each later MFMA
+read or write an MFMA's result only after 16 (more than the 11 of an 8-pass MFMA; each later MFMA
 counts as four), and nothing inserts them there.  These tests check the distances
 in the assembly of every source with such copies, in program order: a loop's exit
 is the code after it."""
@@ -57,8 +57,9 @@ def _vector_registers(operand):
     return {(one.group(1), int(one.group(2)))} if one else set()
 
 
-def read_early(assembly):
-    """(function, line number, instruction) that read an inline-asm MFMA's result too soon."""
+def touched_early(assembly):
+    """(function, line number, instruction) that read an inline-asm MFMA's result, or
+    write to it, too soon."""
     found, mfmas, function, written, clock, inline = [], 0, "", {}, 0, False
     for number, line in enumerate(assembly.splitlines(), 1):
         if "#ASMSTART" in line or "#ASMEND" in line:
@@ -78,9 +79,8 @@ def read_early(assembly):
                 written.update((r, clock) for r in _vector_registers(operands[0]))
             continue
         if name.startswith(("v_", "ds_", "global_", "scratch_")):
-            stores = name.startswith(("ds_", "global_store", "scratch_store"))
-            read = set().union(*map(_vector_registers, operands if stores else operands[1:]), set())
-            if any(clock - written.get(r, -100) < MFMA_WAIT for r in read):
+            touched = set().union(*map(_vector_registers, operands))
+            if any(clock - written.get(r, -100) < MFMA_WAIT for r in touched):
                 found.append((function, number, code))
             if name.startswith("v_"):
                 for r in _vector_registers(operands[0]):
@@ -93,10 +93,11 @@ def read_early(assembly):
 def test_the_checks_themselves():
     loop = ("_Zk:\n;;#ASMSTART\n v_mfma_f32_16x16x32_f16 a[252:255], v[0:3], v[4:7], a[252:255]\n"
             ";;#ASMEND\n s_cbranch_scc0 .L1\n.L2:\n v_accvgpr_read_b32 v2, a254\n")
-    assert len(read_early(loop)[0]) == 1
-    assert not read_early(loop.replace(".L2:\n", ".L2:\n s_nop 7\n s_nop 7\n"))[0]
-    assert not read_early(loop.replace("a254", "a251"))[0]
-    assert not read_early(loop.replace("#ASMSTART", ""))[0]  # the compiler's own MFMA
+    assert len(touched_early(loop)[0]) == 1
+    assert not touched_early(loop.replace(".L2:\n", ".L2:\n s_nop 7\n s_nop 7\n"))[0]
+    assert not touched_early(loop.replace("a254", "a251"))[0]
+    assert len(touched_early(loop.replace("read_b32 v2, a254", "write_b32 a254, v2"))[0]) == 1
+    assert not touched_early(loop.replace("#ASMSTART", ""))[0]  # the compiler's own MFMA
     bad = "_Zk:\n v_readfirstlane_b32 s10, v6\n global_load_lds_dwordx4 v1, s[10:11]\n"
     assert len(too_close(bad)[0]) == 1
     assert len(too_close(bad.replace("v6\n", "v6\n s_nop 3\n"))[0]) == 1
@@ -121,6 +122,6 @@ def test_copies_and_results_keep_their_distances(tmp_path):
             found, copies = too_close(text)
             assert copies > 0, src
             assert not found, (os.path.basename(src), found[:5])
-            found, mfmas = read_early(text)
+            found, mfmas = touched_early(text)
             assert mfmas > 0 or os.path.basename(src) != "gemm.hip"  # the others use builtins
             assert not found, (os.path.basename(src), found[:5])
