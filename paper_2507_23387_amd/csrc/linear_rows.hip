@@ -412,7 +412,11 @@ RowsPlan plan_rows(int64_t M, int64_t N, int64_t K, bool transpose_w) {
   p.line = M <= kBlockRows && (transpose_w || N * K <= (int64_t{1} << 22));
   int64_t most, fill;
   if (p.line) {
-    p.blocks = transpose_w && N >= 256 * 32 ? 2 : 1;
+    // A compute unit holds one workgroup, and a round of them takes 12 us with one
+    // block of columns and 21 with two (K = 4096): 1 x 6144 25.0 and 21.3 us, 8192 29.2
+    // and 25.8, 11008 37.5 and 42.4, 14336 48.4 and 44.0.
+    const int64_t one = (N + 4095) / 4096, two = (N + 8191) / 8192;
+    p.blocks = transpose_w && 7 * two <= 4 * one ? 2 : 1;
     p.groups = static_cast<int>((N + 16 * p.blocks - 1) / (16 * p.blocks));
     p.row_groups = 1;
     most = K / kStep / (4 * kLineWaves);  // four steps a wave at least
