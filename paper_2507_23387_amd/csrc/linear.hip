@@ -122,8 +122,13 @@ namespace {
 // the kernel that sums its columns, where an activation makes it other than dY.  A
 // small W is split with the rest instead, and both products take one launch (us,
 // rows against that: 64 rows, 1024 x 1024 30 and 25, 1024 x 2048 30 and 30, 2048 x
-// 2048 32 and 39, 4096 x 4096 58 and 75; 256 rows 4096 x 4096 122 and 104).
-bool grad_by_rows(int64_t M, int64_t N, int64_t K) { return M <= 128 && N * K >= 1500000; }
+// 2048 32 and 39, 4096 x 4096 58 and 75; 256 rows 4096 x 4096 122 and 104).  A long k
+// for few tiles takes longer still, while rows share it (N x K, 1 and 128 rows: 2048 x
+// 512 25 and 27 against 27 and 29, 3000 x 128 25 and 27 against 23 and 25, 4096 x 128 28
+// against 32, 8192 x 64 28 and 31 against 45 and 48).
+bool grad_by_rows(int64_t M, int64_t N, int64_t K) {
+  return M <= 128 && (N * K >= 1500000 || static_cast<double>(N) * N * K >= 1.6e9);
+}
 
 struct GradWorkspace {
   uint32_t* max_bits;
