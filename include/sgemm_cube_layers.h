@@ -66,7 +66,8 @@ size_t sgemm_cube_linear_workspace_size(int64_t M, int64_t N, int64_t K);
  * (the residual's gradient is dY itself).  Gradients are often far below what
  * FP16 holds, so D is multiplied by a power of two, found from its largest
  * finite magnitude, before it is split, and dX and dW are scaled back; X and W
- * are taken as they are, as in the forward pass.
+ * are taken as they are, as in the forward pass.  (dW of few rows is summed in FP32
+ * without a split.)
  *   dY, lddy     row-major M x N.
  *   Z, ldz       row-major M x N; NULL (and ldz ignored) without an activation.
  *   X, W         as in the forward pass.

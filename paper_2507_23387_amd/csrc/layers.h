@@ -154,6 +154,23 @@ hipError_t launch_linear_rows(const LinearArgs& a, const Unscale* grad, void* ws
                               hipStream_t stream);
 hipError_t launch_linear_columns(const LinearArgs& a, void* ws, hipStream_t stream);
 
+// out = L^T R in FP32, L and R of M <= kOuterRows rows; a side with z is p times
+// act'(z).
+constexpr int kOuterRows = 24;
+struct OuterSide {
+  const float* p;
+  int64_t ld, cols;
+  const float* z;  // null: p
+  int64_t ldz;
+};
+struct OuterArgs {
+  int M, activation;
+  OuterSide left, right;
+  float* out;  // left.cols x right.cols
+  int64_t ldo;
+};
+hipError_t launch_linear_outer(const OuterArgs& g, hipStream_t stream);
+
 size_t linear_ws(int64_t M, int64_t N, int64_t K);
 hipError_t launch_linear(const LinearArgs& a, void* ws, hipStream_t stream);
 

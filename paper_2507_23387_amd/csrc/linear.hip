@@ -130,6 +130,12 @@ bool grad_by_rows(int64_t M, int64_t N, int64_t K) {
   return M <= 128 && (N * K >= 1500000 || static_cast<double>(N) * N * K >= 1.6e9);
 }
 
+// Whether dW = X^T D is formed in FP32 from few rows, where dX needs no planes of D
+// either.
+bool grad_outer(int64_t M, int64_t N, int64_t K) {
+  return M <= kOuterRows && grad_by_rows(M, N, K);
+}
+
 struct GradWorkspace {
   uint32_t* max_bits;
   float* partial;
@@ -152,7 +158,8 @@ GradWorkspace carve_grad(void* ws, int64_t M, int64_t N, int64_t K, bool transpo
     } else {
       g.dx = carve_planes(c, M, K, N);
     }
-    g.dw = transpose_w ? carve_planes(c, N, K, M) : carve_planes(c, K, N, M);
+    if (!grad_outer(M, N, K))
+      g.dw = transpose_w ? carve_planes(c, N, K, M) : carve_planes(c, K, N, M);
   }
   g.bytes = c.used;
   return g;
@@ -176,7 +183,8 @@ hipError_t launch_linear_grad(const LinearGradArgs& a, void* ws, hipStream_t str
     return err;
   }
   const GradWorkspace g = carve_grad(ws, a.M, a.N, a.K, a.transpose_w);
-  const bool dx = a.dx && a.K > 0, dw = a.dw && a.K > 0;
+  const bool dx = a.dx && a.K > 0, outer = a.dw && a.K > 0 && grad_outer(a.M, a.N, a.K);
+  const bool dw = a.dw && a.K > 0 && !outer;
   const bool dx_rows = dx && grad_by_rows(a.M, a.N, a.K);
   const ColumnArgs cols{a.M, a.N, a.dy, a.lddy, a.z, a.ldz, a.activation, a.dbias, g.max_bits,
                         g.partial, dx_rows && a.z ? g.d : nullptr};
@@ -215,6 +223,12 @@ hipError_t launch_linear_grad(const LinearGradArgs& a, void* ws, hipStream_t str
   if (err == hipSuccess && !split_joins) err = launch_columns_join(join, stream);
   if (err == hipSuccess && count > 0)
     err = launch_split_jobs(jobs, count, a.scale, stream, split_joins ? &join : nullptr);
+  if (err == hipSuccess && outer) {
+    const OuterSide x{a.x, a.ldx, a.K, nullptr, 0}, dd{d.s, d.ld, a.N, d.z, d.ldz};
+    const OuterArgs o{static_cast<int>(a.M), a.activation, a.transpose_w ? dd : x,
+                      a.transpose_w ? x : dd, a.dw, a.lddw};
+    err = launch_linear_outer(o, stream);
+  }
   if (err == hipSuccess && dx_rows) {
     LinearArgs r{};
     r.M = a.M, r.N = a.K, r.K = a.N;

@@ -29,7 +29,8 @@ SHAPES = [(1, 1, 1), (1, 7, 3), (1, 300, 1000), (2, 129, 64), (3, 64, 65), (5, 1
           (4090, 4091, 70), (4096, 4096, 64), (16300, 1000, 128), (16384, 2048, 64),
           (3, 2100, 2049), (16, 4096, 1030), (300, 1, 65), (1000, 16, 130), (4097, 17, 64),
           (700, 100, 2050), (3001, 128, 70), (1500, 200, 40), (270, 256, 1001), (5000, 3, 33),
-          (1, 5003, 65), (20, 4100, 130), (128, 3001, 190)]
+          (1, 5003, 65), (20, 4100, 130), (128, 3001, 190),
+          (24, 1301, 1303), (25, 1301, 1303), (2, 2050, 1030)]
 
 
 def _act64(name, z, grad=False):
