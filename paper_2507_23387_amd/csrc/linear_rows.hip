@@ -238,7 +238,7 @@ __global__ __launch_bounds__(64 * kLineWaves) void linear_line_kernel(RowsArgs g
   }
 }
 
-// Other layouts and more rows: 64 columns a workgroup, 16 a wave, up to 64 rows, a
+// Other layouts and more rows: 64 columns a workgroup, 16 a wave, up to 96 rows, a
 // stretch of k per workgroup.  X is split once per workgroup, 64 k at a time, into
 // LDS in the order of the fragments (a wave reads 1 KiB in line), W in the
 // registers of the wave that multiplies it; the next two stretches of W and the
@@ -251,7 +251,8 @@ constexpr int kTileWaves = 4, kTileCols = 16 * kTileWaves;
 constexpr int kChunkSteps = 2, kChunkK = kChunkSteps * kStep;
 
 template <bool kNk, int kR, bool kGrad, bool kAcross>
-__global__ __launch_bounds__(64 * kTileWaves, 3) void linear_rows_tile_kernel(RowsArgs g) {
+__global__ __launch_bounds__(64 * kTileWaves, kR > (kAcross ? 4 : 5) ? 2 : 3)
+void linear_rows_tile_kernel(RowsArgs g) {
   const LinearArgs& a = g.a;
   constexpr int kUnits = kChunkSteps * kR;  // fragments of a chunk of X, of each plane
   extern __shared__ __align__(16) half8 frags[];  // 2 x kUnits x 2 x 64
@@ -481,15 +482,20 @@ RowsPlan plan_rows(int64_t M, int64_t N, int64_t K, bool transpose_w) {
     most = K / kStep / (4 * kLineWaves);  // four steps a wave at least
     fill = 256;
   } else {
-    p.blocks = static_cast<int>(std::min<int64_t>((M + kBlockRows - 1) / kBlockRows, 4));
+    // 65 to 96 rows in one group read W once and not twice: 65 x 8192 x 8192 kn 108 us in
+    // two, 83 so; 96 x 4096 x 4096 nk 39 and 32; few columns 10265 x 84 x 6848 137 and 88.
+    // Small kn weights lose a little (80 x 2048 x 2048 12.6 and 13.3), 128 rows in one
+    // group (registers) more.
+    const bool six = M > 64 && M <= 96 && (transpose_w || N >= 4096);
+    p.blocks = static_cast<int>(std::min<int64_t>((M + kBlockRows - 1) / kBlockRows, six ? 6 : 4));
     p.row_groups = static_cast<int>((M + kBlockRows * p.blocks - 1) / (kBlockRows * p.blocks));
-    // The groups even: 65 to 96 rows are two groups of three blocks.
+    // The groups even.
     const int64_t even = kBlockRows * static_cast<int64_t>(p.row_groups);
     p.blocks = static_cast<int>((M + even - 1) / even);
     p.groups = static_cast<int>((N + kTileCols - 1) / kTileCols);
     // The join costs 4 us, as much as four chunks of a lone workgroup.
     most = K / kChunkK > 5 ? K / kChunkK / 2 : 1;
-    fill = 768;
+    fill = p.blocks > 5 ? 512 : 768;  // what the registers of a compute unit hold
   }
   const int64_t want = fill / (static_cast<int64_t>(p.groups) * p.row_groups);
   p.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({want, most, 16})));
@@ -519,7 +525,9 @@ hipError_t launch_tiles(const RowsArgs& g, const RowsPlan& p, hipStream_t stream
     case 1: return launch_tile<kNk, 1, kGrad, kAcross>(g, p, stream);
     case 2: return launch_tile<kNk, 2, kGrad, kAcross>(g, p, stream);
     case 3: return launch_tile<kNk, 3, kGrad, kAcross>(g, p, stream);
-    default: return launch_tile<kNk, 4, kGrad, kAcross>(g, p, stream);
+    case 4: return launch_tile<kNk, 4, kGrad, kAcross>(g, p, stream);
+    case 5: return launch_tile<kNk, 5, kGrad, kAcross>(g, p, stream);
+    default: return launch_tile<kNk, 6, kGrad, kAcross>(g, p, stream);
   }
 }
 

@@ -30,7 +30,8 @@ SHAPES = [(1, 1, 1), (1, 7, 3), (1, 300, 1000), (2, 129, 64), (3, 64, 65), (5, 1
           (3, 2100, 2049), (16, 4096, 1030), (300, 1, 65), (1000, 16, 130), (4097, 17, 64),
           (700, 100, 2050), (3001, 128, 70), (1500, 200, 40), (270, 256, 1001), (5000, 3, 33),
           (1, 5003, 65), (20, 4100, 130), (128, 3001, 190),
-          (24, 1301, 1303), (25, 1301, 1303), (2, 2050, 1030)]
+          (24, 1301, 1303), (25, 1301, 1303), (2, 2050, 1030),
+          (65, 4101, 200), (96, 4096, 999), (81, 4100, 1030), (2001, 70, 777), (1990, 96, 333)]
 
 
 def _act64(name, z, grad=False):
