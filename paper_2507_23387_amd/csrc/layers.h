@@ -19,7 +19,8 @@ inline int dtype_bytes(int dtype) { return dtype == kF32 ? 4 : 2; }
 // cols and kp_col = rows rounded up to 64.  With max_bits the values are first
 // multiplied by the power of two that brings the magnitude of those bits to
 // 2^target (one target for each kind of planes).  `range`: the header of B-side
-// planes, whose flag words get `stamp` as launch_split's do (null: none).
+// planes, whose flag words get `stamp` as launch_split's do (null: none), but with
+// max_bits never say that s B_hi overflows.
 struct SplitJob {
   const float* s;
   int64_t ld;
@@ -98,8 +99,8 @@ hipError_t launch_epilogue(const Epilogue& e, int64_t M, int64_t N, float* Y, in
 
 // launch_gemm, launch_gemm_small and launch_gemm_unscaled with an epilogue (Epi:
 // Epilogue or Unscale); the product's bits are theirs.  C may be the residual.
-// no_overflow: s B_hi is known to be finite, so that the scaled kernels need no
-// fallback.
+// no_overflow: the range words say that s B_hi is finite, whatever its values, so
+// that the scaled kernels need no fallback.
 template <class Epi>
 hipError_t launch_gemm_epilogue(const Planes& p, int64_t M, int64_t N, float* C, int64_t ldc,
                                 float scale, int variant, const Epi& epi, bool no_overflow,

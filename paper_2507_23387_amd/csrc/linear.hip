@@ -251,7 +251,8 @@ hipError_t launch_linear_grad(const LinearGradArgs& a, void* ws, hipStream_t str
     err = launch_gemm_epilogue(g.dx, a.M, a.K, a.dx, a.lddx, a.scale, a.variant, ex, false,
                                stream);
   }
-  // As B, D is scaled so that s B_hi is finite.
+  // As B, D is scaled so that s B_hi is finite where D is, and its words never ask
+  // for the fallback (split_tile).
   if (err == hipSuccess && dw)
     err = launch_gemm_epilogue(g.dw, dw_rows, dw_cols, a.dw, a.lddw, a.scale, a.variant, ew,
                                !a.transpose_w, stream);

@@ -110,6 +110,14 @@ __device__ __forceinline__ void split_tile(const SplitArgs& a, const SplitJob& g
     big |= __builtin_fabsf(static_cast<float>(x[0])) * a.s > 65504.0f;
     big |= __builtin_fabsf(static_cast<float>(x[1])) * a.s > 65504.0f;
   };
+  // A pre-scaled operand's finite entries stay below the limit, and its infinities
+  // belong in the result: no flag, whatever its words held (an earlier replay of a
+  // captured call has the same stamp), as the GEMM has no fallback to run for it.
+  auto flag = [&](uint32_t* range, uint32_t stamp) {
+    if (big && !g.max_bits) range[kWordBOverflow] = stamp;
+    if (t == 0 && g.max_bits) range[kWordBOverflow] = 0;  // no stamp is 0
+    if (t == 0) range[kWordBStamp] = stamp;
+  };
   if (g.row_hi && j < kp_row) {
     const int shift = g.max_bits ? prescale_shift(max_bits, g.row_target) : 0;
 #pragma unroll
@@ -125,10 +133,7 @@ __device__ __forceinline__ void split_tile(const SplitArgs& a, const SplitJob& g
       store_chunk(g.row_lo + at, lv);
     }
   }
-  if (g.row_range) {
-    if (big) g.row_range[kWordBOverflow] = g.row_stamp;
-    if (t == 0) g.row_range[kWordBStamp] = g.row_stamp;
-  }
+  if (g.row_range) flag(g.row_range, g.row_stamp);
   if (!g.col_hi) return;
   big = false;
   const int shift = g.max_bits ? prescale_shift(max_bits, g.col_target) : 0;
@@ -143,10 +148,7 @@ __device__ __forceinline__ void split_tile(const SplitArgs& a, const SplitJob& g
     ph[(cl + e) * kPitch + rp] = h;
     pl[(cl + e) * kPitch + rp] = static_cast<uint32_t>(l0) | (static_cast<uint32_t>(l1) << 16);
   }
-  if (g.col_range) {
-    if (big) g.col_range[kWordBOverflow] = g.col_stamp;
-    if (t == 0) g.col_range[kWordBStamp] = g.col_stamp;
-  }
+  if (g.col_range) flag(g.col_range, g.col_stamp);
   __syncthreads();
   const int r = t >> 1, c = (t & 1) ^ tile_swizzle(r);
 #pragma unroll
