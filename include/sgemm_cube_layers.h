@@ -64,10 +64,12 @@ size_t sgemm_cube_linear_workspace_size(int64_t M, int64_t N, int64_t K);
  * Gradients of the linear layer: with D = dY act'(Z), entry by entry,
  *   dX = D W^T,   dW = X^T D,   dbias_j = sum_i D_ij
  * (the residual's gradient is dY itself).  Gradients are often far below what
- * FP16 holds, so D is multiplied by a power of two, found from its largest
- * finite magnitude, before it is split, and dX and dW are scaled back; X and W
- * are taken as they are, as in the forward pass.  (dW of few rows is summed in FP32
- * without a split.)
+ * FP16 holds, so before it is split D is multiplied by powers of two, for dX one
+ * for each row and for dW one for each column, found from the line's largest finite
+ * magnitude, and dX and dW are scaled back: a line far below the others keeps its
+ * digits, and within one an entry is off by at most 2^-38 of the line's largest (or
+ * 2^-22 of itself).  X and W are taken as they are, as in the forward pass.  (dW of
+ * few rows is summed in FP32 without a split.)
  *   dY, lddy     row-major M x N.
  *   Z, ldz       row-major M x N; NULL (and ldz ignored) without an activation.
  *   X, W         as in the forward pass.

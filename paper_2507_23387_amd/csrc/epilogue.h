@@ -11,21 +11,53 @@
 namespace sgc {
 namespace {
 
-// In place of an epilogue: C is stored as the product (store_tile16), or
-// (Unscale) times 2^-prescale_shift(*max_bits, target).
+// In place of an epilogue: C is stored as the product (store_tile16).
 struct NoEpilogue {};
 template <class Epi>
 constexpr bool kThroughLds = std::is_same<Epi, Epilogue>::value;
-template <class Epi>
-__device__ __forceinline__ int unscale_shift(const Epi& epi) {
-  if constexpr (std::is_same<Epi, Unscale>::value)
-    return -prescale_shift(*epi.max_bits, epi.target);
-  return 0;
-}
-template <class Epi>
-__device__ __forceinline__ float unscaled(float x, int shift) {
-  if constexpr (std::is_same<Epi, Unscale>::value) return __builtin_ldexpf(x, shift);
-  return x;
+
+// store_tile16, for Unscale each entry times the power of two of its row or column.
+// The rows and columns past the end take the last one's; they are not stored.
+template <int kSubM, int kSubN, class Epi, typename F>
+__device__ __forceinline__ void store_product(const Epi& epi, float* __restrict__ C, int64_t ldc,
+                                              int M, int N, int row0, int col0, bool full,
+                                              F value) {
+  if constexpr (!std::is_same<Epi, Unscale>::value) {
+    store_tile16<kSubM, kSubN>(C, ldc, M, N, row0, col0, full, value);
+  } else if (epi.columns) {
+    int q[kSubN];
+#pragma unroll
+    for (int j = 0; j < kSubN; ++j) q[j] = -epi.shift[min(col0 + 16 * j, N - 1)];
+    store_tile16<kSubM, kSubN>(C, ldc, M, N, row0, col0, full, [&](int i, int j, int r) {
+      return __builtin_ldexpf(value(i, j, r), q[j]);
+    });
+  } else {
+    // The wave's lanes hold the shifts of 64 of its rows at a time and hand them out: 32
+    // in every lane are more than the wide kernels' accumulators leave registers for.
+    const int lane = threadIdx.x & 63, first = row0 - 4 * (lane >> 4);
+    constexpr int kHeld = (kSubM + 3) / 4;
+    int held[kHeld];
+#pragma unroll
+    for (int h = 0; h < kHeld; ++h) held[h] = -epi.shift[min(first + 64 * h + lane, M - 1)];
+    float* const base = C + static_cast<int64_t>(row0) * ldc + col0;
+#pragma unroll
+    for (int i = 0; i < kSubM; ++i) {
+      int p[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        p[r] = __shfl(held[i / 4], (i % 4) * 16 + 4 * (lane >> 4) + r);
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int rr = i * 16 + r;
+        float* const at = base + static_cast<int64_t>(rr) * ldc;
+#pragma unroll
+        for (int j = 0; j < kSubN; ++j)
+          if (full || (row0 + rr < M && col0 + j * 16 < N))
+            at[j * 16] = __builtin_ldexpf(value(i, j, r), p[r]);
+      }
+      SCHED_FENCE();
+    }
+  }
 }
 
 // Keeps the tile's indices in scalar registers.  The epilogue uses them lane by

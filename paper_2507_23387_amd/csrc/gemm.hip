@@ -440,10 +440,8 @@ __device__ __forceinline__ void el_tile(
   const int col0 = tn * kWide + wn * 128 + (lane & 15);
   const int row0 = tm * kWide + wm * 128 + (lane >> 4) * 4;
   const bool full = (tm + 1) * kWide <= M && (tn + 1) * kWide <= N;
-  const int shift = unscale_shift(epi);
-  store_tile16<kWSub, kWSub>(C, ldc, M, N, row0, col0, full, [&](int i, int j, int r) {
-    return unscaled<Epi>(acc[i][j][r] * inv_s, shift);
-  });
+  store_product<kWSub, kWSub>(epi, C, ldc, M, N, row0, col0, full,
+                              [&](int i, int j, int r) { return acc[i][j][r] * inv_s; });
 }
 
 template <bool kPrefetch, bool kFusedA>
@@ -1083,10 +1081,7 @@ __device__ __forceinline__ void n128_tile(
   const int col0 = tn * kTwN + (lane & 15);
   const int row0 = tm * kTwM + w * 64 + (lane >> 4) * 4;
   const bool full = (tm + 1) * kTwM <= M && (tn + 1) * kTwN <= N;
-  const int shift = unscale_shift(epi);
-  store_tile16<kRows, kCols>(C, ldc, M, N, row0, col0, full, [&](int i, int j, int r) {
-    return unscaled<Epi>(value(i, j, r), shift);
-  });
+  store_product<kRows, kCols>(epi, C, ldc, M, N, row0, col0, full, value);
 }
 
 template <int V, bool kFusedA = false, bool kFusedB = false>

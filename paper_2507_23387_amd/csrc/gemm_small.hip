@@ -341,10 +341,7 @@ __device__ __forceinline__ void small_tile(const SmallArgs& g, uint16_t* lds, co
       return;
     }
   }
-  const int shift = unscale_shift(epi);
-  store_tile16<kRT, kCT>(g.C, g.ldc, g.M, g.N, row0, col0, full, [&](int i, int j, int r) {
-    return unscaled<Epi>(value(i, j, r), shift);
-  });
+  store_product<kRT, kCT>(epi, g.C, g.ldc, g.M, g.N, row0, col0, full, value);
 }
 
 template <int V, class S, class Epi>

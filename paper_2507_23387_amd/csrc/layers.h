@@ -16,11 +16,10 @@ inline int dtype_bytes(int dtype) { return dtype == kF32 ? 4 : 2; }
 // One matrix of a split launch: S is rows x cols row-major, times act'(Z) where z
 // is not null.  Its planes with S's rows as rows (k = cols) go to row_*, those
 // with its columns as rows (k = rows) to col_*; either may be null.  kp_row =
-// cols and kp_col = rows rounded up to 64.  With max_bits the values are first
-// multiplied by the power of two that brings the magnitude of those bits to
-// 2^target (one target for each kind of planes).  `range`: the header of B-side
-// planes, whose flag words get `stamp` as launch_split's do (null: none), but with
-// max_bits never say that s B_hi overflows.
+// cols and kp_col = rows rounded up to 64.  Where the planes have shifts, one for
+// each of S's rows (columns), the values are first multiplied by 2^shift.
+// `range`: the header of B-side planes, whose flag words get `stamp` as
+// launch_split's do (null: none), but with shifts never say that s B_hi overflows.
 struct SplitJob {
   const float* s;
   int64_t ld;
@@ -32,24 +31,27 @@ struct SplitJob {
   uint16_t* row_lo;
   uint16_t* col_hi;
   uint16_t* col_lo;
-  const uint32_t* max_bits;
-  int row_target, col_target;
+  const int* row_shift;
+  const int* col_shift;
   uint32_t* row_range;
   uint32_t* col_range;
   uint32_t row_stamp, col_stamp;
 };
 constexpr int kSplitJobs = 3;
-// The join of launch_columns' slabs, for a split launch to do on the way: `tops`
-// magnitudes, of which each workgroup of a job with max_bits takes the largest, the
-// first also writing it to *max_bits, and slabs x N sums that workgroups of their
-// own add up to dbias (null: none).
+// The join of what launch_columns left: for each of D's M rows and N columns the
+// shift that brings its largest finite magnitude to 2^target (prescale_shift), and
+// the sums of the columns.  Null: not wanted.  A split launch can do it on the way:
+// each workgroup of the job with shifts finds those of its tile, the first of a line
+// also writing them, and workgroups of their own add up dbias.
 struct ColumnJoin {
-  const float* top;
-  int tops;
-  uint32_t* max_bits;
-  const float* sums;
-  int slabs;
-  int64_t N;
+  int64_t M, N;
+  int strips, slabs;
+  const float* row_top;  // strips x M
+  const float* col_top;  // slabs x N
+  const float* sums;     // slabs x N
+  int row_target, col_target;
+  int* row_shift;
+  int* col_shift;
   float* dbias;
 };
 hipError_t launch_split_jobs(const SplitJob* jobs, int count, float scale, hipStream_t stream,
@@ -57,12 +59,12 @@ hipError_t launch_split_jobs(const SplitJob* jobs, int count, float scale, hipSt
 // Workgroups of such a launch without the join's own.
 int64_t split_jobs_blocks(const SplitJob* jobs, int count);
 
-// The sums of D = dY act'(Z)'s columns and its largest finite magnitude, per slab of
-// rows and strip of columns, in `partial`: column_slabs(M, N) x N sums, then
-// column_slabs(M, N) x ceil(N / kColumnStrip) magnitudes.  launch_columns_join forms
-// dbias (null: none) and the bits of the largest magnitude in *max_bits.
+// One pass over D = dY act'(Z): for each slab of rows the sums and the largest finite
+// magnitudes of D's columns, and for each strip of columns the largest finite
+// magnitudes of its rows (ColumnJoin's arrays; null: not wanted).
 constexpr int kColumnStrip = 128;
 int64_t column_slabs(int64_t M, int64_t N);
+int64_t column_strips(int64_t N);
 struct ColumnArgs {
   int64_t M, N;
   const float* dy;
@@ -70,13 +72,12 @@ struct ColumnArgs {
   const float* z;  // null: D = dY
   int64_t ldz;
   int activation;
-  float* dbias;
-  uint32_t* max_bits;
-  float* partial;
+  float* row_top;
+  float* col_top;
+  float* sums;
   float* d;  // null, or M x N that receives D
 };
 hipError_t launch_columns(const ColumnArgs& a, hipStream_t stream);
-ColumnJoin column_join(const ColumnArgs& a);
 hipError_t launch_columns_join(const ColumnJoin& j, hipStream_t stream);
 
 // What follows a product P: Y = act(Z) + R, Z = P + bias.
@@ -88,10 +89,10 @@ struct Epilogue {
   float* z;           // null: not kept
   int64_t ldz;
 };
-// A gradient's product: 2^-prescale_shift(*max_bits, target) P.
+// A gradient's product: row i (or column i) of P times 2^-shift[i].
 struct Unscale {
-  const uint32_t* max_bits;
-  int target;
+  const int* shift;
+  bool columns;
 };
 // The epilogue where K = 0: P = 0.
 hipError_t launch_epilogue(const Epilogue& e, int64_t M, int64_t N, float* Y, int64_t ldy,
@@ -145,13 +146,13 @@ struct LinearArgs {
 
 // The linear layer for few rows or few columns (linear_rows.hip), its sums termwise
 // whatever the variant.  linear_by_rows, linear_by_columns: the rules that choose
-// them.  With `grad`, x is a gradient that is multiplied by the power of two of
-// grad's Unscale as it is split, and the result is freed of it again.  The
-// workspace of N columns is that of as many rows, linear_rows_ws(N, M, K).
+// them.  With `row_shift`, row i of x, a gradient, is multiplied by 2^row_shift[i] as
+// it is split, and the result is freed of it again.  The workspace of N columns is
+// that of as many rows, linear_rows_ws(N, M, K).
 bool linear_by_rows(int64_t M, int64_t N);
 bool linear_by_columns(int64_t M, int64_t N);
 size_t linear_rows_ws(int64_t M, int64_t N, int64_t K);
-hipError_t launch_linear_rows(const LinearArgs& a, const Unscale* grad, void* ws,
+hipError_t launch_linear_rows(const LinearArgs& a, const int* row_shift, void* ws,
                               hipStream_t stream);
 hipError_t launch_linear_columns(const LinearArgs& a, void* ws, hipStream_t stream);
 

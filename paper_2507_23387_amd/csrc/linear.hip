@@ -137,8 +137,8 @@ bool grad_outer(int64_t M, int64_t N, int64_t K) {
 }
 
 struct GradWorkspace {
-  uint32_t* max_bits;
-  float* partial;
+  float *row_top, *col_top, *sums;  // launch_columns' arrays
+  int *row_shift, *col_shift;
   void* rows;  // launch_linear_rows' workspace
   float* d;    // M x N, by rows
   Planes dx, dw;
@@ -148,9 +148,12 @@ struct GradWorkspace {
 GradWorkspace carve_grad(void* ws, int64_t M, int64_t N, int64_t K, bool transpose_w) {
   Carver c{static_cast<char*>(ws), 0};
   GradWorkspace g{};
-  g.max_bits = c.take<uint32_t>(1);
-  const int64_t strips = (N + kColumnStrip - 1) / kColumnStrip;
-  g.partial = c.take<float>(column_slabs(M, N) * (N + strips));
+  const int64_t slabs = column_slabs(M, N);
+  g.row_top = c.take<float>(column_strips(N) * M);
+  g.col_top = c.take<float>(slabs * N);
+  g.sums = c.take<float>(slabs * N);
+  g.row_shift = c.take<int>(M);
+  g.col_shift = c.take<int>(N);
   if (K > 0) {
     if (grad_by_rows(M, N, K)) {
       g.rows = c.take<char>(static_cast<int64_t>(linear_rows_ws(M, K, N)));
@@ -186,38 +189,47 @@ hipError_t launch_linear_grad(const LinearGradArgs& a, void* ws, hipStream_t str
   const bool dx = a.dx && a.K > 0, outer = a.dw && a.K > 0 && grad_outer(a.M, a.N, a.K);
   const bool dw = a.dw && a.K > 0 && !outer;
   const bool dx_rows = dx && grad_by_rows(a.M, a.N, a.K);
-  const ColumnArgs cols{a.M, a.N, a.dy, a.lddy, a.z, a.ldz, a.activation, a.dbias, g.max_bits,
-                        g.partial, dx_rows && a.z ? g.d : nullptr};
-  const ColumnJoin join = column_join(cols);
+  // dX is scaled by rows, dW by columns: each of their entries sums one line of D, so
+  // that a line far below the others keeps its digits.
+  const ColumnArgs cols{a.M, a.N, a.dy, a.lddy, a.z, a.ldz, a.activation,
+                        dx ? g.row_top : nullptr, dw ? g.col_top : nullptr, g.sums,
+                        dx_rows && a.z ? g.d : nullptr};
+  ColumnJoin join{};
+  join.M = a.M, join.N = a.N;
+  join.strips = static_cast<int>(column_strips(a.N));
+  join.slabs = static_cast<int>(column_slabs(a.M, a.N));
+  join.row_top = g.row_top, join.col_top = g.col_top, join.sums = g.sums;
+  join.row_target = target_a(a.scale);
+  join.col_target = a.transpose_w ? target_a(a.scale) : target_b(a.scale, a.variant);
+  join.row_shift = dx ? g.row_shift : nullptr;
+  join.col_shift = dw ? g.col_shift : nullptr;
+  join.dbias = a.dbias;
 
   SplitJob jobs[kSplitJobs];
   int count = 0;
   SplitJob d = cols.d ? job_of(cols.d, a.N, a.M, a.N) : job_of(a.dy, a.lddy, a.M, a.N);
   if (!cols.d) d.z = a.z, d.ldz = a.ldz, d.activation = a.activation;
-  d.max_bits = g.max_bits;
-  Unscale ex{}, ew{};
-  ex.max_bits = ew.max_bits = g.max_bits;
-  ex.target = target_a(a.scale);
+  // In dW, D's columns are the result's columns, or with N x K weights its rows.
+  const Unscale ex{g.row_shift, false}, ew{g.col_shift, !a.transpose_w};
   if (dx && !dx_rows) {
     // dX = D W^T: D's rows and W's K rows, k over N.
-    d.row_target = ex.target;
+    d.row_shift = g.row_shift;
     to_planes(d, g.dx, false, false);
     jobs[count] = a.transpose_w ? job_of(a.w, a.ldw, a.N, a.K) : job_of(a.w, a.ldw, a.K, a.N);
     to_planes(jobs[count++], g.dx, true, a.transpose_w);
   }
   if (dw) {
     // dW = X^T D (or D^T X): columns of both, k over M.
-    d.col_target = ew.target =
-        a.transpose_w ? target_a(a.scale) : target_b(a.scale, a.variant);
+    d.col_shift = g.col_shift;
     to_planes(d, g.dw, !a.transpose_w, true);
     jobs[count] = job_of(a.x, a.ldx, a.M, a.K);
     to_planes(jobs[count++], g.dw, a.transpose_w, true);
   }
   if (count > 0) jobs[count++] = d;
 
-  // A split of few tiles joins the column sums itself: every one of its workgroups
-  // reads the magnitudes, 2 us, instead of a launch between (777 x 1003 x 530: 39
-  // us with it).
+  // A split of few tiles joins the column sums itself: every one of D's workgroups
+  // reads its lines' magnitudes, 2 us, instead of a launch between (777 x 1003 x 530:
+  // 39 us with it).
   const bool split_joins = count > 0 && split_jobs_blocks(jobs, count) <= kSplitJoinBlocks;
   err = launch_columns(cols, stream);
   if (err == hipSuccess && !split_joins) err = launch_columns_join(join, stream);
@@ -236,7 +248,7 @@ hipError_t launch_linear_grad(const LinearGradArgs& a, void* ws, hipStream_t str
     r.w = a.w, r.ldw = a.ldw, r.transpose_w = !a.transpose_w;
     r.y = a.dx, r.ldy = a.lddx;
     r.scale = a.scale, r.variant = a.variant;
-    err = launch_linear_rows(r, &ex, g.rows, stream);
+    err = launch_linear_rows(r, g.row_shift, g.rows, stream);
   } else if (err == hipSuccess && dx) {
     if (dw) {
       const int64_t M[2] = {a.M, dw_rows}, N[2] = {a.K, dw_cols}, K[2] = {a.N, a.M};

@@ -109,9 +109,8 @@ __device__ __forceinline__ void load_strided(const float* col, int64_t ld, int64
 
 struct RowsArgs {
   LinearArgs a;
-  bool grad;
+  const int* row_shift;  // of a gradient's rows, or null
   bool swapped;  // Y^T = W^T X^T: entry (i, j) is row j, column i of Y
-  Unscale unscale;
   float inv_s;
   int groups;      // of columns
   int splits;      // workgroups that share a group's k
@@ -122,8 +121,8 @@ struct RowsArgs {
 __device__ __forceinline__ void finish(const RowsArgs& g, int64_t i, int64_t j, float z) {
   float* const y = g.a.y + i * g.a.ldy + j;
   const Epilogue& e = g.a.e;
-  if (g.grad) {
-    *y = __builtin_ldexpf(z, -prescale_shift(*g.unscale.max_bits, g.unscale.target));
+  if (g.row_shift) {
+    *y = __builtin_ldexpf(z, -g.row_shift[i]);
     return;
   }
   if (e.bias) z += e.bias[j];
@@ -156,8 +155,9 @@ __global__ __launch_bounds__(64 * kLineWaves) void linear_line_kernel(RowsArgs g
   const int col_group = index / g.splits, split = index - col_group * g.splits;
   const int64_t col0 = static_cast<int64_t>(col_group) * (16 * kC);
   // Rows and columns past the end repeat the last; they are not stored.
-  const float* const xrow = a.x + min<int64_t>(l16, a.M - 1) * (kAcross ? 1 : a.ldx);
-  const int shift = kGrad ? prescale_shift(*g.unscale.max_bits, g.unscale.target) : 0;
+  const int64_t row = min<int64_t>(l16, a.M - 1);
+  const float* const xrow = a.x + row * (kAcross ? 1 : a.ldx);
+  const int shift = kGrad ? g.row_shift[row] : 0;
   const float* wcol[kC];
 #pragma unroll
   for (int c = 0; c < kC; ++c)
@@ -270,16 +270,15 @@ void linear_rows_tile_kernel(RowsArgs g) {
   // Units of X's chunk: step u / kR, row block u % kR.  The waves take them in turn,
   // the last one again where there are fewer.
   constexpr int kPer = (kUnits + kTileWaves - 1) / kTileWaves;
-  int unit[kPer];
+  int unit[kPer], shift[kPer];
   const float* xrow[kPer];
 #pragma unroll
   for (int n = 0; n < kPer; ++n) {
     unit[n] = min(wave + kTileWaves * n, kUnits - 1);
-    xrow[n] = a.x + min<int64_t>(row0 + 16 * (unit[n] % kR) + l16, a.M - 1) *
-                        (kAcross ? 1 : a.ldx);
+    const int64_t row = min<int64_t>(row0 + 16 * (unit[n] % kR) + l16, a.M - 1);
+    xrow[n] = a.x + row * (kAcross ? 1 : a.ldx);
+    shift[n] = kGrad ? g.row_shift[row] : 0;
   }
-
-  const int shift = kGrad ? prescale_shift(*g.unscale.max_bits, g.unscale.target) : 0;
 
   Values w[2][kChunkSteps], x[kPer];
   auto load_w = [&](int64_t c, int st, Values& to, auto tail) {
@@ -303,7 +302,7 @@ void linear_rows_tile_kernel(RowsArgs g) {
 #pragma unroll
     for (int n = 0; n < kPer; ++n) {
       half8 hi, lo;
-      x[n].template shifted<kGrad>(shift).split(a.scale, hi, lo);
+      x[n].template shifted<kGrad>(shift[n]).split(a.scale, hi, lo);
       half8* const at = frags + ((slot * kUnits + unit[n]) * 2) * 64 + lane;
       at[0] = hi;
       at[64] = lo;
@@ -567,12 +566,13 @@ size_t linear_rows_ws(int64_t M, int64_t N, int64_t K) {
   return static_cast<size_t>(round_up(splits > 1 ? splits * M * N * 4 : 1, 256));
 }
 
-hipError_t launch_linear_rows(const LinearArgs& a, const Unscale* grad, void* ws,
+hipError_t launch_linear_rows(const LinearArgs& a, const int* row_shift, void* ws,
                               hipStream_t stream) {
   const RowsPlan p = plan_rows(a.M, a.N, a.K, a.transpose_w);
-  const RowsArgs g{a, grad != nullptr, false, grad ? *grad : Unscale{}, 1.0f / a.scale,
-                   p.groups, p.splits, static_cast<float*>(ws)};
-  const hipError_t e = grad ? launch_plan<true>(g, p, stream) : launch_plan<false>(g, p, stream);
+  const RowsArgs g{a, row_shift, false, 1.0f / a.scale, p.groups, p.splits,
+                   static_cast<float*>(ws)};
+  const hipError_t e =
+      row_shift ? launch_plan<true>(g, p, stream) : launch_plan<false>(g, p, stream);
   return e == hipSuccess ? launch_join(g, stream) : e;
 }
 
@@ -582,7 +582,7 @@ hipError_t launch_linear_columns(const LinearArgs& a, void* ws, hipStream_t stre
   t.x = a.w, t.ldx = a.ldw;
   t.w = a.x, t.ldw = a.ldx, t.transpose_w = true;
   const RowsPlan p = plan_rows(t.M, t.N, t.K, true);
-  const RowsArgs g{t, false, true, Unscale{}, 1.0f / a.scale, p.groups, p.splits,
+  const RowsArgs g{t, nullptr, true, 1.0f / a.scale, p.groups, p.splits,
                    static_cast<float*>(ws)};
   const hipError_t e =
       a.transpose_w ? launch_plan<false>(g, p, stream)

@@ -1,7 +1,8 @@
 // What a linear layer's products need around them (gfx950): the split of its
 // operands into planes in either direction, the gradient D = dY act'(Z) with its
-// column sums and largest magnitude, and the epilogue.
+// column sums and its lines' largest magnitudes, and the epilogue.
 #include <algorithm>
+#include <type_traits>
 
 #include "activation.h"
 #include "layers.h"
@@ -28,6 +29,15 @@ __device__ __forceinline__ void load8(const float* p, int64_t ld, int64_t i, int
   }
 }
 
+// Four values from column j of a row of n, zeros past its end.
+__device__ __forceinline__ floatx4v load4(const float* row, int64_t j, int64_t n) {
+  if (j + 3 < n) return *reinterpret_cast<const floatx4_u*>(row + j);
+  floatx4v v;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = j + e < n ? row[j + e] : 0.0f;
+  return v;
+}
+
 // The jobs of a launch; job b has blocks first[b] .. first[b + 1].
 struct SplitArgs {
   SplitJob job[kSplitJobs];
@@ -37,37 +47,46 @@ struct SplitArgs {
   ColumnJoin join;
 };
 
-constexpr int kJoinCols = 32, kJoinGroups = kThreads / kJoinCols;
+constexpr int kJoinLines = 32, kJoinGroups = kThreads / kJoinLines;
 
-// The largest of the slabs' magnitudes, in every thread.  `lds`: a word per wave.
-__device__ uint32_t join_top(const ColumnJoin& g, float* lds) {
-  const int t = threadIdx.x;
-  float m = 0.0f;
+// Line j's sum or largest of `count` values, `lines` apart, in the threads of the
+// first 32 (j < lines), every eighth value a thread.  `part`: a word per thread.
+template <bool kMax>
+__device__ __forceinline__ float join_line(const float* p, int count, int64_t lines, int64_t j,
+                                           float* part) {
+  const int c = threadIdx.x % kJoinLines, q = threadIdx.x / kJoinLines;
+  auto add = [](float x, float y) { return kMax ? __builtin_fmaxf(x, y) : x + y; };
+  float s = 0.0f;
+  if (j < lines) {
 #pragma unroll 4
-  for (int n = t; n < g.tops; n += kThreads) m = __builtin_fmaxf(m, g.top[n]);
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, off));
-  if ((t & 63) == 0) lds[t >> 6] = m;
+    for (int n = q; n < count; n += kJoinGroups) s = add(s, p[n * lines + j]);
+  }
+  part[q * kJoinLines + c] = s;
   __syncthreads();
-  m = __builtin_fmaxf(__builtin_fmaxf(lds[0], lds[1]), __builtin_fmaxf(lds[2], lds[3]));
-  return __builtin_bit_cast(uint32_t, m);
+  if (q == 0) {
+#pragma unroll
+    for (int n = 1; n < kJoinGroups; ++n) s = add(s, part[n * kJoinLines + c]);
+  }
+  return s;
 }
 
-// dbias of 32 columns, every eighth slab a thread.  `part`: a word per thread.
-__device__ void join_columns(const ColumnJoin& g, uint32_t block, float* part) {
-  const int c = threadIdx.x % kJoinCols, q = threadIdx.x / kJoinCols;
-  const int64_t j = static_cast<int64_t>(block) * kJoinCols + c;
-  float s = 0.0f;
-  if (j < g.N) {
-#pragma unroll 4
-    for (int n = q; n < g.slabs; n += kJoinGroups) s += g.sums[n * g.N + j];
-  }
-  part[q * kJoinCols + c] = s;
-  __syncthreads();
-  if (q != 0 || j >= g.N) return;
-#pragma unroll
-  for (int n = 1; n < kJoinGroups; ++n) s += part[n * kJoinCols + c];
-  g.dbias[j] = s;
+__device__ __forceinline__ int shift_of(float top, int target) {
+  return prescale_shift(__builtin_bit_cast(uint32_t, top), target);
+}
+
+// dbias of 32 columns.
+__device__ void join_sums(const ColumnJoin& g, uint32_t block, float* part) {
+  const int64_t j = static_cast<int64_t>(block) * kJoinLines + threadIdx.x % kJoinLines;
+  const float s = join_line<false>(g.sums, g.slabs, g.N, j, part);
+  if (threadIdx.x < kJoinLines && j < g.N) g.dbias[j] = s;
+}
+
+// The shifts of 32 rows or columns.
+__device__ void join_shifts(const float* top, int count, int64_t lines, int target, int* shift,
+                            uint32_t block, float* part) {
+  const int64_t j = static_cast<int64_t>(block) * kJoinLines + threadIdx.x % kJoinLines;
+  const float m = join_line<true>(top, count, lines, j, part);
+  if (threadIdx.x < kJoinLines && j < lines) shift[j] = shift_of(m, target);
 }
 
 constexpr int kTileRows = 32, kTileCols = 128;
@@ -77,12 +96,15 @@ constexpr int kPitch = kTileRows / 2 + 4;  // words per column in LDS; 16-byte a
 // columns from 8 (t % 16).  As row planes those are two 16-byte chunks of a tile
 // row each.  As column planes the pairs of rows go to LDS as words, a column's
 // side by side, and thread t writes chunk t of each of the tile's two slices.
-// max_bits(): the bits of the magnitude that a job is scaled by, asked for once the
-// tile's loads are on their way.  HBM bounds it: the gradient of 8192 x 4096 x 4096 (dY
-// times act'(Z) both ways, X and W) 150 us, 0.94 GB.
+// lines_of(): the shifts of this thread's two rows and eight columns, asked for once
+// the tile's loads are on their way.  HBM bounds it: the gradient of 8192 x 4096 x 4096
+// (dY times act'(Z) both ways, X and W) 150 us, 0.94 GB.
+struct Shifts {
+  int row[2], col[8];
+};
 template <typename F>
 __device__ __forceinline__ void split_tile(const SplitArgs& a, const SplitJob& g, uint32_t block,
-                                           uint32_t* ph, uint32_t* pl, F max_bits_of) {
+                                           uint32_t* ph, uint32_t* pl, F lines_of) {
   const int t = threadIdx.x;
   const uint32_t strips = static_cast<uint32_t>((g.cols + kTileCols - 1) / kTileCols);
   const int64_t tr = block / strips, tc = block - static_cast<uint32_t>(tr) * strips;
@@ -94,7 +116,9 @@ __device__ __forceinline__ void split_tile(const SplitArgs& a, const SplitJob& g
 #pragma unroll
     for (int u = 0; u < 2; ++u) load8(g.z, g.ldz, i + u, j, g.rows, g.cols, z[u]);
   }
-  const uint32_t max_bits = g.max_bits ? max_bits_of() : 0;
+  const bool scaled = g.row_shift || g.col_shift;
+  Shifts lines;
+  if (scaled) lines = lines_of(tr, tc);
   if (g.z) {
 #pragma unroll
     for (int u = 0; u < 2; ++u)
@@ -114,17 +138,17 @@ __device__ __forceinline__ void split_tile(const SplitArgs& a, const SplitJob& g
   // belong in the result: no flag, whatever its words held (an earlier replay of a
   // captured call has the same stamp), as the GEMM has no fallback to run for it.
   auto flag = [&](uint32_t* range, uint32_t stamp) {
-    if (big && !g.max_bits) range[kWordBOverflow] = stamp;
-    if (t == 0 && g.max_bits) range[kWordBOverflow] = 0;  // no stamp is 0
+    if (big && !scaled) range[kWordBOverflow] = stamp;
+    if (t == 0 && scaled) range[kWordBOverflow] = 0;  // no stamp is 0
     if (t == 0) range[kWordBStamp] = stamp;
   };
   if (g.row_hi && j < kp_row) {
-    const int shift = g.max_bits ? prescale_shift(max_bits, g.row_target) : 0;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       float w[8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) w[e] = shift ? __builtin_ldexpf(v[u][e], shift) : v[u][e];
+      for (int e = 0; e < 8; ++e)
+        w[e] = g.row_shift ? __builtin_ldexpf(v[u][e], lines.row[u]) : v[u][e];
       u32x4 hv, lv;
       split8(w, a.s, hv, lv);
       if (g.row_range) too_big(hv[0]), too_big(hv[1]), too_big(hv[2]), too_big(hv[3]);
@@ -136,13 +160,16 @@ __device__ __forceinline__ void split_tile(const SplitArgs& a, const SplitJob& g
   if (g.row_range) flag(g.row_range, g.row_stamp);
   if (!g.col_hi) return;
   big = false;
-  const int shift = g.max_bits ? prescale_shift(max_bits, g.col_target) : 0;
   const int cl = 8 * (t & 15), rp = t >> 4;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
+    if (g.col_shift) {
+      v[0][e] = __builtin_ldexpf(v[0][e], lines.col[e]);
+      v[1][e] = __builtin_ldexpf(v[1][e], lines.col[e]);
+    }
     uint16_t h0, l0, h1, l1;
-    split_value(shift ? __builtin_ldexpf(v[0][e], shift) : v[0][e], a.s, h0, l0);
-    split_value(shift ? __builtin_ldexpf(v[1][e], shift) : v[1][e], a.s, h1, l1);
+    split_value(v[0][e], a.s, h0, l0);
+    split_value(v[1][e], a.s, h1, l1);
     const uint32_t h = static_cast<uint32_t>(h0) | (static_cast<uint32_t>(h1) << 16);
     if (g.col_range) too_big(h);
     ph[(cl + e) * kPitch + rp] = h;
@@ -166,111 +193,192 @@ __global__ __launch_bounds__(kThreads) void split_jobs_kernel(SplitArgs a) {
     int n = 0;
     while (n + 1 < a.count && b >= a.first[n + 1]) ++n;
     const SplitJob& g = a.job[n];
-    split_tile(a, g, b - a.first[n], ph, pl, [&] { return *g.max_bits; });
+    split_tile(a, g, b - a.first[n], ph, pl, [&](int64_t tr, int64_t tc) {
+      const int64_t i = tr * kTileRows + 2 * (threadIdx.x >> 4);
+      const int64_t j = tc * kTileCols + 8 * (threadIdx.x & 15);
+      Shifts s{};
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        if (g.row_shift && i + u < g.rows) s.row[u] = g.row_shift[i + u];
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (g.col_shift && j + e < g.cols) s.col[e] = g.col_shift[j + e];
+      return s;
+    });
     __syncthreads();  // the tile's LDS words are read before the next's are written
   }
 }
 
-// With the join: a tile a workgroup, then the join's workgroups.
+// A tile's shifts from what launch_columns left.  Both lines' largest magnitudes are
+// joined in LDS: 32 rows by eight threads each over the strips, 128 columns by eight
+// threads to four of them over the slabs.
+__device__ __forceinline__ Shifts join_tile(const ColumnJoin& g, int64_t tr, int64_t tc,
+                                            float* col_part, float* row_part) {
+  __shared__ int rows[kTileRows], cols[kTileCols];
+  static_assert(kTileRows == kJoinLines && kTileCols == 4 * kJoinLines &&
+                kTileRows + kTileCols <= kThreads, "threads to a line");
+  const int t = threadIdx.x, l = t % kJoinLines, q = t / kJoinLines;
+  const int64_t i0 = tr * kTileRows, j0 = tc * kTileCols;
+  float m[4] = {0.0f, 0.0f, 0.0f, 0.0f}, top = 0.0f;
+  if (g.col_shift) {
+    const int64_t j = j0 + 4 * l;
+#pragma unroll 4
+    for (int n = q; n < g.slabs; n += kJoinGroups) {
+      const floatx4v x = load4(g.col_top + n * g.N, j, g.N);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) m[e] = __builtin_fmaxf(m[e], x[e]);
+    }
+  }
+  if (g.row_shift && i0 + l < g.M) {
+#pragma unroll 4
+    for (int n = q; n < g.strips; n += kJoinGroups)
+      top = __builtin_fmaxf(top, g.row_top[n * g.M + i0 + l]);
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) col_part[q * kTileCols + 4 * l + e] = m[e];
+  row_part[q * kTileRows + l] = top;
+  __syncthreads();
+  if (t < kTileCols) {
+    float c = col_part[t];
+#pragma unroll
+    for (int n = 1; n < kJoinGroups; ++n) c = __builtin_fmaxf(c, col_part[n * kTileCols + t]);
+    cols[t] = shift_of(c, g.col_target);
+    if (g.col_shift && tr == 0 && j0 + t < g.N) g.col_shift[j0 + t] = cols[t];
+  } else if (t < kTileCols + kTileRows) {
+    const int k = t - kTileCols;
+    float r = row_part[k];
+#pragma unroll
+    for (int n = 1; n < kJoinGroups; ++n) r = __builtin_fmaxf(r, row_part[n * kTileRows + k]);
+    rows[k] = shift_of(r, g.row_target);
+    if (g.row_shift && tc == 0 && i0 + k < g.M) g.row_shift[i0 + k] = rows[k];
+  }
+  __syncthreads();
+  Shifts s;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) s.row[u] = rows[2 * (t >> 4) + u];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) s.col[e] = cols[8 * (t & 15) + e];
+  return s;
+}
+
+// With the join: a tile a workgroup, then the workgroups of dbias.
 __global__ __launch_bounds__(kThreads) void split_join_kernel(SplitArgs a) {
   __shared__ __align__(16) uint32_t ph[kTileCols * kPitch];
   __shared__ __align__(16) uint32_t pl[kTileCols * kPitch];
   const uint32_t b = blockIdx.x;
   if (b >= a.first[a.count]) {
-    join_columns(a.join, b - a.first[a.count], reinterpret_cast<float*>(ph));
+    join_sums(a.join, b - a.first[a.count], reinterpret_cast<float*>(ph));
     return;
   }
   int n = 0;
   while (n + 1 < a.count && b >= a.first[n + 1]) ++n;
-  const SplitJob& g = a.job[n];
-  split_tile(a, g, b - a.first[n], ph, pl, [&] {
-    const uint32_t bits = join_top(a.join, reinterpret_cast<float*>(pl));
-    if (b == a.first[n] && threadIdx.x == 0) *a.join.max_bits = bits;
-    __syncthreads();  // pl is read before the tile is written
-    return bits;
+  split_tile(a, a.job[n], b - a.first[n], ph, pl, [&](int64_t tr, int64_t tc) {
+    return join_tile(a.join, tr, tc, reinterpret_cast<float*>(ph), reinterpret_cast<float*>(pl));
   });
 }
 
 // Rows that a thread has in flight.
 constexpr int kColumnRows = 4;
 
-// Sums of 128 columns over a slab of rows: thread t has columns 4 (t % 32) .. + 3
-// of every eighth row.  8192 x 4096 with Z: 44 us, 6.1 TB/s.
+// Largest of the 32 lanes that have a row: by rotations within rows of 16 lanes, then
+// between two of those.
+__device__ __forceinline__ float half_max(float v) {
+  auto step = [&](auto control) {
+    const int o = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v),
+                                              decltype(control)::value, 0xf, 0xf, true);
+    v = __builtin_fmaxf(v, __builtin_bit_cast(float, o));
+  };
+  step(std::integral_constant<int, 0x121>{});  // row_ror:1
+  step(std::integral_constant<int, 0x122>{});
+  step(std::integral_constant<int, 0x124>{});
+  step(std::integral_constant<int, 0x128>{});
+  return __builtin_fmaxf(v, __shfl_xor(v, 16));
+}
+
+// 128 columns of a slab of rows: thread t has columns 4 (t % 32) .. + 3 of every
+// eighth row, so that the half of a wave that has a row also finds its largest
+// magnitude.  8192 x 4096 with Z: 44 us, 6.1 TB/s.
 __global__ __launch_bounds__(kThreads) void columns_kernel(ColumnArgs a, int64_t slab_rows) {
-  __shared__ float part[kThreads / 32][kColumnStrip];
-  __shared__ float top[kThreads / 64];
+  __shared__ float sums[kThreads / 32][kColumnStrip], tops[kThreads / 32][kColumnStrip];
   const int t = threadIdx.x;
   const int64_t j = static_cast<int64_t>(blockIdx.x) * kColumnStrip + 4 * (t & 31);
   const int64_t i0 = blockIdx.y * slab_rows, i1 = min(a.M, i0 + slab_rows);
-  float s[4] = {0.0f, 0.0f, 0.0f, 0.0f}, m = 0.0f;
-  auto add = [&](const float (&d)[4]) {
+  float s[4] = {0.0f, 0.0f, 0.0f, 0.0f}, top[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  constexpr int kStride = kThreads / 32;
+  // Rows i, i + 8, ... (kU): all lanes of a row take every step together.
+  auto rows = [&](int64_t i, auto count) {
+    constexpr int kU = decltype(count)::value;
+    floatx4v d[kU], z[kU];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      s[e] += d[e];
-      const float b = __builtin_fabsf(d[e]);
-      if (b <= 3.4028235e38f) m = __builtin_fmaxf(m, b);
+    for (int u = 0; u < kU; ++u) d[u] = load4(a.dy + (i + u * kStride) * a.lddy, j, a.N);
+    if (a.z) {
+#pragma unroll
+      for (int u = 0; u < kU; ++u) z[u] = load4(a.z + (i + u * kStride) * a.ldz, j, a.N);
+      multiply_grad(a.activation, d, z);
+    }
+    if (a.d) {
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        float* const at = a.d + (i + u * kStride) * a.N + j;
+        if (j + 3 < a.N) {
+          *reinterpret_cast<floatx4_u*>(at) = d[u];
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (j + e < a.N) at[e] = d[u][e];
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      float b[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s[e] += d[u][e];
+        b[e] = __builtin_fabsf(d[u][e]);
+        b[e] = b[e] <= 3.4028235e38f ? b[e] : 0.0f;
+        top[e] = __builtin_fmaxf(top[e], b[e]);
+      }
+      if (a.row_top) {
+        const float m = half_max(__builtin_fmaxf(__builtin_fmaxf(b[0], b[1]),
+                                                 __builtin_fmaxf(b[2], b[3])));
+        if ((t & 31) == 0) a.row_top[blockIdx.x * a.M + i + u * kStride] = m;
+      }
     }
   };
-  constexpr int kStride = kThreads / 32;
   int64_t i = i0 + (t >> 5);
-  if (j + 3 < a.N) {
-    for (; i + (kColumnRows - 1) * kStride < i1; i += kColumnRows * kStride) {
-      floatx4v d[kColumnRows], z[kColumnRows];
+  for (; i + (kColumnRows - 1) * kStride < i1; i += kColumnRows * kStride)
+    rows(i, std::integral_constant<int, kColumnRows>{});
+  for (; i < i1; i += kStride) rows(i, std::integral_constant<int, 1>{});
 #pragma unroll
-      for (int u = 0; u < kColumnRows; ++u)
-        d[u] = *reinterpret_cast<const floatx4_u*>(a.dy + (i + u * kStride) * a.lddy + j);
-      if (a.z) {
-#pragma unroll
-        for (int u = 0; u < kColumnRows; ++u)
-          z[u] = *reinterpret_cast<const floatx4_u*>(a.z + (i + u * kStride) * a.ldz + j);
-        multiply_grad(a.activation, d, z);
-      }
-      if (a.d) {
-#pragma unroll
-        for (int u = 0; u < kColumnRows; ++u)
-          *reinterpret_cast<floatx4_u*>(a.d + (i + u * kStride) * a.N + j) = d[u];
-      }
-#pragma unroll
-      for (int u = 0; u < kColumnRows; ++u) add({d[u][0], d[u][1], d[u][2], d[u][3]});
-    }
+  for (int e = 0; e < 4; ++e) {
+    sums[t >> 5][4 * (t & 31) + e] = s[e];
+    tops[t >> 5][4 * (t & 31) + e] = top[e];
   }
-  for (; i < i1; i += kStride) {
-    float d[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      d[e] = j + e < a.N ? a.dy[i * a.lddy + j + e] : 0.0f;
-      if (a.z && j + e < a.N) d[e] *= activate_grad(a.activation, a.z[i * a.ldz + j + e]);
-      if (a.d && j + e < a.N) a.d[i * a.N + j + e] = d[e];
-    }
-    add(d);
-  }
-#pragma unroll
-  for (int e = 0; e < 4; ++e) part[t >> 5][4 * (t & 31) + e] = s[e];
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) m = __builtin_fmaxf(m, __shfl_xor(m, off));
-  if ((t & 63) == 0) top[t >> 6] = m;
   __syncthreads();
   const int64_t col = static_cast<int64_t>(blockIdx.x) * kColumnStrip + t;
-  if (t < kColumnStrip && col < a.N) {
-    float sum = 0.0f;
+  if (t >= kColumnStrip || col >= a.N) return;
+  float sum = 0.0f, most = 0.0f;
 #pragma unroll
-    for (int g = 0; g < kThreads / 32; ++g) sum += part[g][t];
-    a.partial[blockIdx.y * a.N + col] = sum;
+  for (int g = 0; g < kThreads / 32; ++g) {
+    sum += sums[g][t];
+    most = __builtin_fmaxf(most, tops[g][t]);
   }
-  if (t == 0)
-    a.partial[gridDim.y * a.N + blockIdx.y * gridDim.x + blockIdx.x] = __builtin_fmaxf(__builtin_fmaxf(top[0], top[1]),
-                                            __builtin_fmaxf(top[2], top[3]));
+  a.sums[blockIdx.y * a.N + col] = sum;
+  if (a.col_top) a.col_top[blockIdx.y * a.N + col] = most;
 }
 
-// The join alone: every workgroup but the last has 32 columns.
-__global__ __launch_bounds__(kThreads) void columns_join_kernel(ColumnJoin g) {
+// The join alone, 32 columns or rows a workgroup: dbias, the columns' shifts, the rows'.
+__global__ __launch_bounds__(kThreads) void columns_join_kernel(ColumnJoin g, uint32_t sums,
+                                                                uint32_t cols) {
   __shared__ float part[kThreads];
-  if (blockIdx.x < gridDim.x - 1) {
-    join_columns(g, blockIdx.x, part);
-  } else {
-    const uint32_t bits = join_top(g, part);
-    if (threadIdx.x == 0) *g.max_bits = bits;
-  }
+  if (blockIdx.x < sums)
+    join_sums(g, blockIdx.x, part);
+  else if (blockIdx.x < sums + cols)
+    join_shifts(g.col_top, g.slabs, g.N, g.col_target, g.col_shift, blockIdx.x - sums, part);
+  else
+    join_shifts(g.row_top, g.strips, g.M, g.row_target, g.row_shift, blockIdx.x - sums - cols,
+                part);
 }
 
 // The epilogue of a product without terms: Z = bias.
@@ -294,8 +402,8 @@ int64_t job_blocks(const SplitJob& j) {
   return round_up(j.rows, kKPad) / kTileRows * ((j.cols + kTileCols - 1) / kTileCols);
 }
 
-unsigned join_blocks(const ColumnJoin& j) {
-  return j.dbias ? static_cast<unsigned>((j.N + kJoinCols - 1) / kJoinCols) : 0u;
+unsigned join_blocks(const void* wanted, int64_t lines) {
+  return wanted ? static_cast<unsigned>((lines + kJoinLines - 1) / kJoinLines) : 0u;
 }
 
 }  // namespace
@@ -322,7 +430,7 @@ hipError_t launch_split_jobs(const SplitJob* jobs, int count, float scale, hipSt
   if (blocks == 0) return hipSuccess;
   if (join) {
     a.join = *join;
-    hipLaunchKernelGGL(split_join_kernel, dim3(a.first[count] + join_blocks(*join)),
+    hipLaunchKernelGGL(split_join_kernel, dim3(a.first[count] + join_blocks(join->dbias, join->N)),
                        dim3(kThreads), 0, stream, a);
     return hipGetLastError();
   }
@@ -331,27 +439,26 @@ hipError_t launch_split_jobs(const SplitJob* jobs, int count, float scale, hipSt
   return hipGetLastError();
 }
 
+int64_t column_strips(int64_t N) { return (N + kColumnStrip - 1) / kColumnStrip; }
+
 int64_t column_slabs(int64_t M, int64_t N) {
-  const int64_t strips = (N + kColumnStrip - 1) / kColumnStrip;
-  return std::max<int64_t>(1, std::min<int64_t>((M + 31) / 32, 1024 / strips));
+  return std::max<int64_t>(1, std::min<int64_t>((M + 31) / 32, 1024 / column_strips(N)));
 }
 
 hipError_t launch_columns(const ColumnArgs& a, hipStream_t stream) {
-  const int64_t strips = (a.N + kColumnStrip - 1) / kColumnStrip;
   const int64_t slabs = column_slabs(a.M, a.N);
-  hipLaunchKernelGGL(columns_kernel, dim3(static_cast<unsigned>(strips), static_cast<unsigned>(slabs)),
+  hipLaunchKernelGGL(columns_kernel, dim3(static_cast<unsigned>(column_strips(a.N)),
+                                          static_cast<unsigned>(slabs)),
                      dim3(kThreads), 0, stream, a, (a.M + slabs - 1) / slabs);
   return hipGetLastError();
 }
 
-ColumnJoin column_join(const ColumnArgs& a) {
-  const int64_t slabs = column_slabs(a.M, a.N), strips = (a.N + kColumnStrip - 1) / kColumnStrip;
-  return ColumnJoin{a.partial + slabs * a.N, static_cast<int>(slabs * strips), a.max_bits,
-                    a.partial, static_cast<int>(slabs), a.N, a.dbias};
-}
-
 hipError_t launch_columns_join(const ColumnJoin& j, hipStream_t stream) {
-  hipLaunchKernelGGL(columns_join_kernel, dim3(join_blocks(j) + 1), dim3(kThreads), 0, stream, j);
+  const unsigned sums = join_blocks(j.dbias, j.N), cols = join_blocks(j.col_shift, j.N);
+  const unsigned rows = join_blocks(j.row_shift, j.M);
+  if (sums + cols + rows == 0) return hipSuccess;
+  hipLaunchKernelGGL(columns_join_kernel, dim3(sums + cols + rows), dim3(kThreads), 0, stream, j,
+                     sums, cols);
   return hipGetLastError();
 }
 
