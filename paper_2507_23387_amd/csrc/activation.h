@@ -94,7 +94,9 @@ __device__ __forceinline__ float activate_grad(int activation, float z) {
     case SGEMM_CUBE_ACT_GELU_TANH: {
       constexpr float kC = 1.59576912f;
       const float s = sigmoid(gelu_tanh_arg(z));
-      return s + z * s * (1.0f - s) * (kC + (3.0f * kC * 0.044715f) * z * z);
+      // z^2 stays finite where s (1 - s) is 0.
+      const float zz = __builtin_fminf(z * z, 1e30f);
+      return s + z * s * (1.0f - s) * (kC + (3.0f * kC * 0.044715f) * zz);
     }
     case SGEMM_CUBE_ACT_SILU: {
       const float s = sigmoid(z);

@@ -64,3 +64,16 @@ def test_gelu_derivative(gpu):
     want = _phi(z64) + z64 * density
     worst = ((_derivative(z, "gelu").double() - want).abs() / (5 * U)).max().item()
     assert worst <= 1, f"{worst:.3f} of the bound"
+
+
+@pytest.mark.parametrize("activation", ["relu", "gelu", "gelu_tanh", "silu"])
+def test_far_from_zero(gpu, activation):
+    """z itself and 1 above, 0 below, up to the largest float."""
+    z = torch.tensor([50.0, 1e4, 1e13, 1e19, 2e19, 1e30, 3.4e38], device="cuda")
+    z = torch.cat([z, -z])
+    positive = z > 0
+    # exp(50) is 5e21: sigmoid and Phi are 1 to the last bit above zero, and below 50 exp(-50)
+    # is under 1e-19.
+    y = _forward(z, activation)
+    assert torch.equal(y[positive], z[positive]) and torch.all(y[~positive].abs() <= 1e-19)
+    assert torch.all((_derivative(z, activation) - positive.float()).abs() <= 1e-19)
