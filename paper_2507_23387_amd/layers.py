@@ -223,8 +223,9 @@ class AdamW:
                   states start at zero.  The attribute `states` holds them.
 
     The object holds the parameters and states themselves; new values are copied
-    into them.  A parameter whose memory was exchanged since (p.data = ...) is
-    refused; gradients are given to each step.
+    into them.  Two entries that share memory are refused, and so is a parameter whose
+    memory was exchanged since (p.data = ...).  Gradients are given to each step; they
+    must not lie in the parameters or states.
     """
 
     def __init__(self, params, lr: float = 1e-3, betas=(0.9, 0.999), eps: float = 1e-8,
@@ -259,6 +260,7 @@ class AdamW:
                 size = -(-count // binding.ADAMW_BLOCK) if scale else count
                 setattr(entry, field, _flat(self.states[key][i], f"states[{key!r}][{i}]", device,
                                             size, (dtype,)))
+        self._check_apart()
         self._counts = [p.numel() for p in self.params]
         self._addresses = list(map(_address, self.params))
 
@@ -327,6 +329,27 @@ class AdamW:
         _check(binding.sgemm_cube_adamw_values(n, self._list, *addresses, _stream(device)),
                "sgemm_cube_adamw_values")
         return out
+
+    def _check_apart(self):
+        """Refuses memory that two entries share (a tied weight given twice, say): one
+        launch writes both, in no order.  (An entry's own operands are the library's to
+        check.)"""
+        held = {"params": self.params, **self.states}
+        spans = sorted((t.data_ptr(), t.data_ptr() + t.numel() * t.element_size(), i, key)
+                       for key, tensors in held.items() for i, t in enumerate(tensors)
+                       if t.numel())
+        # The furthest end so far of any entry, and of any other than that one.
+        first, second = (0, -1, ""), (0, -1, "")
+        for begin, end, i, key in spans:
+            other = first if first[1] != i else second
+            if other[0] > begin:
+                raise ValueError(f"{key}[{i}] shares memory with {other[2]}[{other[1]}]")
+            if end > first[0]:
+                if first[1] != i:
+                    second = first
+                first = (end, i, key)
+            elif first[1] != i and end > second[0]:
+                second = (end, i, key)
 
     def _check_held(self):
         """The device; refuses parameters that have moved since their addresses were
