@@ -309,9 +309,10 @@ class AdamW:
     def state_values(self, out=None):
         """(exp_avgs, exp_avg_sqs) as lists of float32 tensors in the parameters'
         shapes, as a checkpoint holds them; out: a pair of lists to write to.
-        With 32-bit states, the states themselves (or copies in out)."""
+        With 32-bit states, views of the states themselves (or copies in out)."""
         if out is None and self.state_bits == 32:
-            return self.states["exp_avgs"], self.states["exp_avg_sqs"]
+            return tuple([state.view(p.shape) for state, p in zip(self.states[key], self.params)]
+                         for key in ("exp_avgs", "exp_avg_sqs"))
         if out is None:
             out = tuple([torch.empty_like(p) for p in self.params] for _ in range(2))
         n = len(self._counts)
