@@ -22,6 +22,9 @@ _contiguous, _device_of = torch.Tensor.is_contiguous, torch.Tensor.get_device
 # The current stream's handle, without the Stream object that wraps it (2.8 us a
 # call, of the 10 to 17 that a small layer takes).
 _stream = torch._C._cuda_getCurrentRawStream
+# Tells autograd of tensors that the library has written to, as torch's own in-place
+# operations do, so that a graph which has saved one refuses its old values.
+_written = torch.autograd.graph.increment_version
 
 
 def _refuse(t, name, dtype):
@@ -115,6 +118,8 @@ def linear(X, W, bias=None, residual=None, activation: str = "none", transpose_w
         M, N, K, px, ldx, pw, ldw, int(transpose_w), pb, _activation(activation), pr, ldr, py, ldy,
         Z.data_ptr() if keep_preact else None, max(N, 1), scale, _order(order), ws, size,
         _stream(device)), "sgemm_cube_linear")
+    if out is not None:
+        _written(out)
     return (Y, Z) if keep_preact else Y
 
 
@@ -175,6 +180,8 @@ def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, keep_stats: bool = 
         rows, cols, _DTYPES[x.dtype], px, ldx, pw, pb, eps, py, ldy,
         mean.data_ptr() if keep_stats else None, rstd.data_ptr() if keep_stats else None,
         _stream(device)), "sgemm_cube_layer_norm")
+    if out is not None:
+        _written(out)
     return (y, mean, rstd) if keep_stats else y
 
 
@@ -196,6 +203,8 @@ def layer_norm_backward(dy, x, weight, mean, rstd, out=None):
         rows, cols, _DTYPES[x.dtype], pdy, lddy, px, ldx, pw, pm, pr, pdx, lddx, dw.data_ptr(),
         db.data_ptr(), ws, size, _stream(device)),
         "sgemm_cube_layer_norm_backward")
+    if out is not None:
+        _written(out)
     return dx, dw, db
 
 
@@ -304,6 +313,7 @@ class AdamW:
         _check(binding.sgemm_cube_adamw(
             len(grads), self._list, _DTYPES[dtype], self.state_bits, self.lr, self.betas[0],
             self.betas[1], self.eps, grad_scale, number, _stream(device)), "sgemm_cube_adamw")
+        _written(self.params)
         self.steps = number
 
     def state_values(self, out=None):
@@ -329,6 +339,7 @@ class AdamW:
             return out
         _check(binding.sgemm_cube_adamw_values(n, self._list, *addresses, _stream(device)),
                "sgemm_cube_adamw_values")
+        _written([*out[0], *out[1]])
         return out
 
     def _check_apart(self):
