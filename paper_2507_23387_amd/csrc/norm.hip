@@ -7,7 +7,9 @@
 // dx = r (g - mean(g) - h mean(g h)); over the rows: dw = sum dy h, db = sum dy.
 // All sums are FP32 and have an order that the sizes alone fix.
 #include <algorithm>
+#include <atomic>
 
+#include "gemm_common.h"
 #include "layers.h"
 
 namespace sgc {
@@ -502,9 +504,13 @@ hipError_t join(const NormGradArgs& a, int64_t slabs, hipStream_t stream) {
 
 template <int kDtype, int kT, int kP>
 hipError_t grad_rows(const NormGradArgs& a, hipStream_t stream) {
+  constexpr size_t kLds = 2 * kT * kP * sizeof(float);
+  static std::atomic<bool> done[kMaxDevices];
+  const hipError_t attr = set_lds(&norm_grad_rows_kernel<kDtype, kT, kP>, kLds, done);
+  if (attr != hipSuccess) return attr;
   const int64_t slabs = norm_slabs(a.rows, a.cols);
   hipLaunchKernelGGL((norm_grad_rows_kernel<kDtype, kT, kP>), dim3(static_cast<unsigned>(slabs)),
-                     dim3(kGradThreads), 2 * kT * kP * sizeof(float), stream, a);
+                     dim3(kGradThreads), kLds, stream, a);
   if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
   return join(a, slabs, stream);
 }
