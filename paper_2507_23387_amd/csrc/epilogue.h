@@ -16,8 +16,25 @@ struct NoEpilogue {};
 template <class Epi>
 constexpr bool kThroughLds = std::is_same<Epi, Epilogue>::value;
 
-// store_tile16, for Unscale each entry times the power of two of its row or column.
-// The rows and columns past the end take the last one's; they are not stored.
+// The shifts of a wave's kBlocks x 16 rows (or columns) from `first` on, 64 lines at a
+// time, one a lane, which hand them out: all of a lane's own are more than the wide
+// kernels' accumulators leave registers for.  Lines past the end take the last one's;
+// they are not stored.
+template <int kBlocks>
+struct LineShifts {
+  int held[(kBlocks + 3) / 4];
+  __device__ __forceinline__ LineShifts(const int* shift, int first, int lines) {
+#pragma unroll
+    for (int h = 0; h < (kBlocks + 3) / 4; ++h)
+      held[h] = shift[min(first + 64 * h + static_cast<int>(threadIdx.x & 63), lines - 1)];
+  }
+  // That of line i of block b.
+  __device__ __forceinline__ int of(int b, int i) const {
+    return __shfl(held[b / 4], b % 4 * 16 + i);
+  }
+};
+
+// store_tile16, for Unscale each entry times 2^-shift of its row or column.
 template <int kSubM, int kSubN, class Epi, typename F>
 __device__ __forceinline__ void store_product(const Epi& epi, float* __restrict__ C, int64_t ldc,
                                               int M, int N, int row0, int col0, bool full,
@@ -25,27 +42,23 @@ __device__ __forceinline__ void store_product(const Epi& epi, float* __restrict_
   if constexpr (!std::is_same<Epi, Unscale>::value) {
     store_tile16<kSubM, kSubN>(C, ldc, M, N, row0, col0, full, value);
   } else if (epi.columns) {
+    const int i0 = threadIdx.x & 15;
+    const LineShifts<kSubN> lines(epi.shift, col0 - i0, N);
     int q[kSubN];
 #pragma unroll
-    for (int j = 0; j < kSubN; ++j) q[j] = -epi.shift[min(col0 + 16 * j, N - 1)];
+    for (int j = 0; j < kSubN; ++j) q[j] = -lines.of(j, i0);
     store_tile16<kSubM, kSubN>(C, ldc, M, N, row0, col0, full, [&](int i, int j, int r) {
       return __builtin_ldexpf(value(i, j, r), q[j]);
     });
   } else {
-    // The wave's lanes hold the shifts of 64 of its rows at a time and hand them out: 32
-    // in every lane are more than the wide kernels' accumulators leave registers for.
-    const int lane = threadIdx.x & 63, first = row0 - 4 * (lane >> 4);
-    constexpr int kHeld = (kSubM + 3) / 4;
-    int held[kHeld];
-#pragma unroll
-    for (int h = 0; h < kHeld; ++h) held[h] = -epi.shift[min(first + 64 * h + lane, M - 1)];
+    const int i0 = 4 * ((threadIdx.x & 63) >> 4);
+    const LineShifts<kSubM> lines(epi.shift, row0 - i0, M);
     float* const base = C + static_cast<int64_t>(row0) * ldc + col0;
 #pragma unroll
     for (int i = 0; i < kSubM; ++i) {
       int p[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-        p[r] = __shfl(held[i / 4], (i % 4) * 16 + 4 * (lane >> 4) + r);
+      for (int r = 0; r < 4; ++r) p[r] = -lines.of(i, i0 + r);
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int rr = i * 16 + r;

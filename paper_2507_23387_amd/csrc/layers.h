@@ -17,7 +17,8 @@ inline int dtype_bytes(int dtype) { return dtype == kF32 ? 4 : 2; }
 // is not null.  Its planes with S's rows as rows (k = cols) go to row_*, those
 // with its columns as rows (k = rows) to col_*; either may be null.  kp_row =
 // cols and kp_col = rows rounded up to 64.  Where the planes have shifts, one for
-// each of S's rows (columns), the values are first multiplied by 2^shift.
+// each of S's rows (columns; read up to a multiple of 64, of 128, whatever is there),
+// the values are first multiplied by 2^shift.
 // `range`: the header of B-side planes, whose flag words get `stamp` as
 // launch_split's do (null: none), but with shifts never say that s B_hi overflows.
 struct SplitJob {
@@ -45,9 +46,9 @@ constexpr int kSplitJobs = 3;
 // also writing them, and workgroups of their own add up dbias.
 struct ColumnJoin {
   int64_t M, N;
-  int strips, slabs;
-  const float* row_top;  // strips x M
-  const float* col_top;  // slabs x N
+  int pieces, slabs;
+  const float* row_top;  // pieces x M
+  const float* col_top;  // slabs x N rounded up to kColumnStrip
   const float* sums;     // slabs x N
   int row_target, col_target;
   int* row_shift;
@@ -60,11 +61,12 @@ hipError_t launch_split_jobs(const SplitJob* jobs, int count, float scale, hipSt
 int64_t split_jobs_blocks(const SplitJob* jobs, int count);
 
 // One pass over D = dY act'(Z): for each slab of rows the sums and the largest finite
-// magnitudes of D's columns, and for each strip of columns the largest finite
+// magnitudes of D's columns, and for each half of a strip of columns the largest finite
 // magnitudes of its rows (ColumnJoin's arrays; null: not wanted).
 constexpr int kColumnStrip = 128;
 int64_t column_slabs(int64_t M, int64_t N);
 int64_t column_strips(int64_t N);
+inline int64_t row_pieces(int64_t N) { return 2 * column_strips(N); }
 struct ColumnArgs {
   int64_t M, N;
   const float* dy;

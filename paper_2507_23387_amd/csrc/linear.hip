@@ -149,11 +149,11 @@ GradWorkspace carve_grad(void* ws, int64_t M, int64_t N, int64_t K, bool transpo
   Carver c{static_cast<char*>(ws), 0};
   GradWorkspace g{};
   const int64_t slabs = column_slabs(M, N);
-  g.row_top = c.take<float>(column_strips(N) * M);
-  g.col_top = c.take<float>(slabs * N);
+  g.row_top = c.take<float>(row_pieces(N) * M);
+  g.col_top = c.take<float>(slabs * round_up(N, kColumnStrip));
   g.sums = c.take<float>(slabs * N);
-  g.row_shift = c.take<int>(M);
-  g.col_shift = c.take<int>(N);
+  g.row_shift = c.take<int>(round_up(M, kKPad));
+  g.col_shift = c.take<int>(round_up(N, kColumnStrip));
   if (K > 0) {
     if (grad_by_rows(M, N, K)) {
       g.rows = c.take<char>(static_cast<int64_t>(linear_rows_ws(M, K, N)));
@@ -196,7 +196,7 @@ hipError_t launch_linear_grad(const LinearGradArgs& a, void* ws, hipStream_t str
                         dx_rows && a.z ? g.d : nullptr};
   ColumnJoin join{};
   join.M = a.M, join.N = a.N;
-  join.strips = static_cast<int>(column_strips(a.N));
+  join.pieces = static_cast<int>(row_pieces(a.N));
   join.slabs = static_cast<int>(column_slabs(a.M, a.N));
   join.row_top = g.row_top, join.col_top = g.col_top, join.sums = g.sums;
   join.row_target = target_a(a.scale);

@@ -49,17 +49,17 @@ struct SplitArgs {
 
 constexpr int kJoinLines = 32, kJoinGroups = kThreads / kJoinLines;
 
-// Line j's sum or largest of `count` values, `lines` apart, in the threads of the
-// first 32 (j < lines), every eighth value a thread.  `part`: a word per thread.
+// Line j's sum or largest of `count` values, `stride` apart, in the first 32 threads
+// (j < lines), every eighth value a thread.  `part`: a word per thread.
 template <bool kMax>
-__device__ __forceinline__ float join_line(const float* p, int count, int64_t lines, int64_t j,
-                                           float* part) {
+__device__ __forceinline__ float join_line(const float* p, int count, int64_t stride,
+                                           int64_t lines, int64_t j, float* part) {
   const int c = threadIdx.x % kJoinLines, q = threadIdx.x / kJoinLines;
   auto add = [](float x, float y) { return kMax ? __builtin_fmaxf(x, y) : x + y; };
   float s = 0.0f;
   if (j < lines) {
 #pragma unroll 4
-    for (int n = q; n < count; n += kJoinGroups) s = add(s, p[n * lines + j]);
+    for (int n = q; n < count; n += kJoinGroups) s = add(s, p[n * stride + j]);
   }
   part[q * kJoinLines + c] = s;
   __syncthreads();
@@ -77,15 +77,15 @@ __device__ __forceinline__ int shift_of(float top, int target) {
 // dbias of 32 columns.
 __device__ void join_sums(const ColumnJoin& g, uint32_t block, float* part) {
   const int64_t j = static_cast<int64_t>(block) * kJoinLines + threadIdx.x % kJoinLines;
-  const float s = join_line<false>(g.sums, g.slabs, g.N, j, part);
+  const float s = join_line<false>(g.sums, g.slabs, g.N, g.N, j, part);
   if (threadIdx.x < kJoinLines && j < g.N) g.dbias[j] = s;
 }
 
 // The shifts of 32 rows or columns.
-__device__ void join_shifts(const float* top, int count, int64_t lines, int target, int* shift,
-                            uint32_t block, float* part) {
+__device__ void join_shifts(const float* top, int count, int64_t stride, int64_t lines,
+                            int target, int* shift, uint32_t block, float* part) {
   const int64_t j = static_cast<int64_t>(block) * kJoinLines + threadIdx.x % kJoinLines;
-  const float m = join_line<true>(top, count, lines, j, part);
+  const float m = join_line<true>(top, count, stride, lines, j, part);
   if (threadIdx.x < kJoinLines && j < lines) shift[j] = shift_of(m, target);
 }
 
@@ -99,8 +99,11 @@ constexpr int kPitch = kTileRows / 2 + 4;  // words per column in LDS; 16-byte a
 // lines_of(): the shifts of this thread's two rows and eight columns, asked for once
 // the tile's loads are on their way.  HBM bounds it: the gradient of 8192 x 4096 x 4096
 // (dY times act'(Z) both ways, X and W) 150 us, 0.94 GB.
+typedef int intx2 __attribute__((ext_vector_type(2)));
+typedef int intx8 __attribute__((ext_vector_type(8)));
 struct Shifts {
-  int row[2], col[8];
+  intx2 row;
+  intx8 col;
 };
 template <typename F>
 __device__ __forceinline__ void split_tile(const SplitArgs& a, const SplitJob& g, uint32_t block,
@@ -194,15 +197,14 @@ __global__ __launch_bounds__(kThreads) void split_jobs_kernel(SplitArgs a) {
     while (n + 1 < a.count && b >= a.first[n + 1]) ++n;
     const SplitJob& g = a.job[n];
     split_tile(a, g, b - a.first[n], ph, pl, [&](int64_t tr, int64_t tc) {
-      const int64_t i = tr * kTileRows + 2 * (threadIdx.x >> 4);
-      const int64_t j = tc * kTileCols + 8 * (threadIdx.x & 15);
+      // Past the end the shifts are anything, and the values that take them 0.
       Shifts s{};
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-        if (g.row_shift && i + u < g.rows) s.row[u] = g.row_shift[i + u];
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (g.col_shift && j + e < g.cols) s.col[e] = g.col_shift[j + e];
+      if (g.row_shift)
+        s.row = *reinterpret_cast<const intx2*>(g.row_shift + tr * kTileRows +
+                                                2 * (threadIdx.x >> 4));
+      if (g.col_shift)
+        s.col = *reinterpret_cast<const intx8*>(g.col_shift + tc * kTileCols +
+                                                8 * (threadIdx.x & 15));
       return s;
     });
     __syncthreads();  // the tile's LDS words are read before the next's are written
@@ -214,24 +216,24 @@ __global__ __launch_bounds__(kThreads) void split_jobs_kernel(SplitArgs a) {
 // threads to four of them over the slabs.
 __device__ __forceinline__ Shifts join_tile(const ColumnJoin& g, int64_t tr, int64_t tc,
                                             float* col_part, float* row_part) {
-  __shared__ int rows[kTileRows], cols[kTileCols];
+  __shared__ __align__(32) int rows[kTileRows], cols[kTileCols];
   static_assert(kTileRows == kJoinLines && kTileCols == 4 * kJoinLines &&
                 kTileRows + kTileCols <= kThreads, "threads to a line");
   const int t = threadIdx.x, l = t % kJoinLines, q = t / kJoinLines;
   const int64_t i0 = tr * kTileRows, j0 = tc * kTileCols;
   float m[4] = {0.0f, 0.0f, 0.0f, 0.0f}, top = 0.0f;
   if (g.col_shift) {
-    const int64_t j = j0 + 4 * l;
-#pragma unroll 4
+    const int64_t stride = (g.N + kColumnStrip - 1) / kColumnStrip * kColumnStrip;
+#pragma unroll 8
     for (int n = q; n < g.slabs; n += kJoinGroups) {
-      const floatx4v x = load4(g.col_top + n * g.N, j, g.N);
+      const floatx4v x = *reinterpret_cast<const floatx4v*>(g.col_top + n * stride + j0 + 4 * l);
 #pragma unroll
       for (int e = 0; e < 4; ++e) m[e] = __builtin_fmaxf(m[e], x[e]);
     }
   }
   if (g.row_shift && i0 + l < g.M) {
-#pragma unroll 4
-    for (int n = q; n < g.strips; n += kJoinGroups)
+#pragma unroll 8
+    for (int n = q; n < g.pieces; n += kJoinGroups)
       top = __builtin_fmaxf(top, g.row_top[n * g.M + i0 + l]);
   }
 #pragma unroll
@@ -253,12 +255,8 @@ __device__ __forceinline__ Shifts join_tile(const ColumnJoin& g, int64_t tr, int
     if (g.row_shift && tc == 0 && i0 + k < g.M) g.row_shift[i0 + k] = rows[k];
   }
   __syncthreads();
-  Shifts s;
-#pragma unroll
-  for (int u = 0; u < 2; ++u) s.row[u] = rows[2 * (t >> 4) + u];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) s.col[e] = cols[8 * (t & 15) + e];
-  return s;
+  return {*reinterpret_cast<const intx2*>(rows + 2 * (t >> 4)),
+          *reinterpret_cast<const intx8*>(cols + 8 * (t & 15))};
 }
 
 // With the join: a tile a workgroup, then the workgroups of dbias.
@@ -280,9 +278,8 @@ __global__ __launch_bounds__(kThreads) void split_join_kernel(SplitArgs a) {
 // Rows that a thread has in flight.
 constexpr int kColumnRows = 4;
 
-// Largest of the 32 lanes that have a row: by rotations within rows of 16 lanes, then
-// between two of those.
-__device__ __forceinline__ float half_max(float v) {
+// Largest of 16 lanes, by rotations.
+__device__ __forceinline__ float quarter_max(float v) {
   auto step = [&](auto control) {
     const int o = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v),
                                               decltype(control)::value, 0xf, 0xf, true);
@@ -292,12 +289,12 @@ __device__ __forceinline__ float half_max(float v) {
   step(std::integral_constant<int, 0x122>{});
   step(std::integral_constant<int, 0x124>{});
   step(std::integral_constant<int, 0x128>{});
-  return __builtin_fmaxf(v, __shfl_xor(v, 16));
+  return v;
 }
 
 // 128 columns of a slab of rows: thread t has columns 4 (t % 32) .. + 3 of every
-// eighth row, so that the half of a wave that has a row also finds its largest
-// magnitude.  8192 x 4096 with Z: 44 us, 6.1 TB/s.
+// eighth row, so that 16 lanes also find the largest magnitude of half of its strip.
+// 8192 x 4096 with Z: 44 us, 6.1 TB/s.
 __global__ __launch_bounds__(kThreads) void columns_kernel(ColumnArgs a, int64_t slab_rows) {
   __shared__ float sums[kThreads / 32][kColumnStrip], tops[kThreads / 32][kColumnStrip];
   const int t = threadIdx.x;
@@ -305,22 +302,28 @@ __global__ __launch_bounds__(kThreads) void columns_kernel(ColumnArgs a, int64_t
   const int64_t i0 = blockIdx.y * slab_rows, i1 = min(a.M, i0 + slab_rows);
   float s[4] = {0.0f, 0.0f, 0.0f, 0.0f}, top[4] = {0.0f, 0.0f, 0.0f, 0.0f};
   constexpr int kStride = kThreads / 32;
-  // Rows i, i + 8, ... (kU): all lanes of a row take every step together.
-  auto rows = [&](int64_t i, auto count) {
+  // Rows i, i + 8, ... (kU) of a whole strip or (not kFull) of the last: all lanes of a
+  // row take every step together.
+  auto rows = [&](int64_t i, auto count, auto whole) {
     constexpr int kU = decltype(count)::value;
+    constexpr bool kFull = decltype(whole)::value;
+    auto load = [&](const float* row) {
+      if constexpr (kFull) return floatx4v(*reinterpret_cast<const floatx4_u*>(row + j));
+      else return load4(row, j, a.N);
+    };
     floatx4v d[kU], z[kU];
 #pragma unroll
-    for (int u = 0; u < kU; ++u) d[u] = load4(a.dy + (i + u * kStride) * a.lddy, j, a.N);
+    for (int u = 0; u < kU; ++u) d[u] = load(a.dy + (i + u * kStride) * a.lddy);
     if (a.z) {
 #pragma unroll
-      for (int u = 0; u < kU; ++u) z[u] = load4(a.z + (i + u * kStride) * a.ldz, j, a.N);
+      for (int u = 0; u < kU; ++u) z[u] = load(a.z + (i + u * kStride) * a.ldz);
       multiply_grad(a.activation, d, z);
     }
     if (a.d) {
 #pragma unroll
       for (int u = 0; u < kU; ++u) {
         float* const at = a.d + (i + u * kStride) * a.N + j;
-        if (j + 3 < a.N) {
+        if (kFull || j + 3 < a.N) {
           *reinterpret_cast<floatx4_u*>(at) = d[u];
         } else {
 #pragma unroll
@@ -340,16 +343,23 @@ __global__ __launch_bounds__(kThreads) void columns_kernel(ColumnArgs a, int64_t
         top[e] = __builtin_fmaxf(top[e], b[e]);
       }
       if (a.row_top) {
-        const float m = half_max(__builtin_fmaxf(__builtin_fmaxf(b[0], b[1]),
-                                                 __builtin_fmaxf(b[2], b[3])));
-        if ((t & 31) == 0) a.row_top[blockIdx.x * a.M + i + u * kStride] = m;
+        const float m = quarter_max(__builtin_fmaxf(__builtin_fmaxf(b[0], b[1]),
+                                                    __builtin_fmaxf(b[2], b[3])));
+        if ((t & 15) == 0)
+          a.row_top[(2 * blockIdx.x + (t >> 4 & 1)) * a.M + i + u * kStride] = m;
       }
     }
   };
-  int64_t i = i0 + (t >> 5);
-  for (; i + (kColumnRows - 1) * kStride < i1; i += kColumnRows * kStride)
-    rows(i, std::integral_constant<int, kColumnRows>{});
-  for (; i < i1; i += kStride) rows(i, std::integral_constant<int, 1>{});
+  auto slab = [&](auto whole) {
+    int64_t i = i0 + (t >> 5);
+    for (; i + (kColumnRows - 1) * kStride < i1; i += kColumnRows * kStride)
+      rows(i, std::integral_constant<int, kColumnRows>{}, whole);
+    for (; i < i1; i += kStride) rows(i, std::integral_constant<int, 1>{}, whole);
+  };
+  if ((blockIdx.x + 1) * static_cast<int64_t>(kColumnStrip) <= a.N)
+    slab(std::true_type{});
+  else
+    slab(std::false_type{});
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     sums[t >> 5][4 * (t & 31) + e] = s[e];
@@ -357,15 +367,16 @@ __global__ __launch_bounds__(kThreads) void columns_kernel(ColumnArgs a, int64_t
   }
   __syncthreads();
   const int64_t col = static_cast<int64_t>(blockIdx.x) * kColumnStrip + t;
-  if (t >= kColumnStrip || col >= a.N) return;
+  if (t >= kColumnStrip) return;
   float sum = 0.0f, most = 0.0f;
 #pragma unroll
   for (int g = 0; g < kThreads / 32; ++g) {
     sum += sums[g][t];
     most = __builtin_fmaxf(most, tops[g][t]);
   }
-  a.sums[blockIdx.y * a.N + col] = sum;
-  if (a.col_top) a.col_top[blockIdx.y * a.N + col] = most;
+  if (col < a.N) a.sums[blockIdx.y * a.N + col] = sum;
+  if (a.col_top)
+    a.col_top[blockIdx.y * (static_cast<int64_t>(gridDim.x) * kColumnStrip) + col] = most;
 }
 
 // The join alone, 32 columns or rows a workgroup: dbias, the columns' shifts, the rows'.
@@ -375,10 +386,11 @@ __global__ __launch_bounds__(kThreads) void columns_join_kernel(ColumnJoin g, ui
   if (blockIdx.x < sums)
     join_sums(g, blockIdx.x, part);
   else if (blockIdx.x < sums + cols)
-    join_shifts(g.col_top, g.slabs, g.N, g.col_target, g.col_shift, blockIdx.x - sums, part);
+    join_shifts(g.col_top, g.slabs, (g.N + kColumnStrip - 1) / kColumnStrip * kColumnStrip, g.N,
+                g.col_target, g.col_shift, blockIdx.x - sums, part);
   else
-    join_shifts(g.row_top, g.strips, g.M, g.row_target, g.row_shift, blockIdx.x - sums - cols,
-                part);
+    join_shifts(g.row_top, g.pieces, g.M, g.M, g.row_target, g.row_shift,
+                blockIdx.x - sums - cols, part);
 }
 
 // The epilogue of a product without terms: Z = bias.
