@@ -182,7 +182,7 @@ __global__ __launch_bounds__(kT < kThreads ? kThreads : kT, kP <= 8 ? 8 : 4) voi
 #pragma unroll
     for (int e = 0; e < kP; ++e) s[0] += x[e];
     row_sums<kT, 1>(s, lds[0]);
-    // A division, so that a constant row is centred to zeros.
+    // A division, so that a row of equal values whose sum is exact is centred to zeros.
     const float mu = s[0] / static_cast<float>(n);
     s[0] = 0.0f;
 #pragma unroll
@@ -270,17 +270,17 @@ __global__ __launch_bounds__(kLongThreads) void norm_kernel(NormArgs a) {
 // work on 1024 / kT rows at a time, each with the columns of its values; at the
 // end those threads' sums are added in LDS, row by row of threads, and the
 // workgroup writes one slab of partial sums.  16384 x 4096: 152 us in FP32 (5.3 TB/s),
-// 88 in bfloat16 (4.6 TB/s); dX and the sums in passes of their own took 315 there.
+// 78 in bfloat16 (5.2 TB/s); dX and the sums in passes of their own took 315 there.
 constexpr int kGradThreads = 1024;
 
 template <int kDtype, int kT, int kP>
 __global__ __launch_bounds__(kGradThreads) void norm_grad_rows_kernel(NormGradArgs a) {
   typedef typename Elem<kDtype>::T T;
   constexpr int kE = Elem<kDtype>::kE, kRows = kGradThreads / kT;
-  // Rows on their way while one is reduced, as they lie: two of 16-bit values, one of
-  // FP32 (a second one's registers spill: 16384 x 4096 156 us, so 152), none at 16
-  // values a thread.  16384 x 4096 bfloat16 100 us with one, 88 with two.
-  constexpr int kDepth = kP > 8 ? 0 : kE == 4 ? 1 : 2;
+  // The next row is on its way, as it lies, while one is reduced, but not at 16 values
+  // a thread, where its registers spill.  A second one gives nothing: 16384 x 4096 in FP32
+  // 156 us, so 152; calls in bfloat16 87.4, so 86.5, of 32000 x 500 31.5 and 31.4.
+  constexpr bool kAhead = kP <= 8;
   __shared__ float lds[2][2 * kGradThreads / 64];
   extern __shared__ float sums[];  // 2 x kT x kP
   static_assert(2 * kT * kP * sizeof(float) <= 128 * 1024, "the sums fit LDS");
@@ -320,7 +320,7 @@ __global__ __launch_bounds__(kGradThreads) void norm_grad_rows_kernel(NormGradAr
       s[0] += g[e];
       s[1] += g[e] * h[e];
     }
-    if (kDepth && first + kDepth * stride < a.rows) fetch(first + kDepth * stride, in);
+    if (kAhead && first + stride < a.rows) fetch(first + stride, in);
     row_sums<kT, 2>(s, slot);
     if (mine) {
       const float m1 = s[0] * rn, m2 = s[1] * rn;
@@ -335,20 +335,11 @@ __global__ __launch_bounds__(kGradThreads) void norm_grad_rows_kernel(NormGradAr
     }
     first += stride;
   };
-  Ahead in[kDepth ? kDepth : 1];
-#pragma unroll
-  for (int d = 0; d < kDepth; ++d) fetch(first + d * stride, in[d]);
-  if constexpr (kDepth == 2) {
-    while (first < a.rows) {
-      step(in[0], lds[0]);
-      if (first >= a.rows) break;
-      step(in[1], lds[1]);
-    }
-  } else {
-    for (int turn = 0; first < a.rows; turn ^= 1) {
-      if (kDepth == 0) fetch(first, in[0]);
-      step(in[0], lds[turn]);
-    }
+  Ahead in;
+  if (kAhead) fetch(first, in);
+  for (int turn = 0; first < a.rows; turn ^= 1) {
+    if (!kAhead) fetch(first, in);
+    step(in, lds[turn]);
   }
   if (!a.dweight && !a.dbias) return;
   // Value e of thread t at e * kT + t: neighbours in neighbouring banks.
