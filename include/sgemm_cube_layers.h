@@ -5,9 +5,13 @@
  * Conventions of sgemm_cube.h hold: row-major matrices with leading
  * dimensions in elements, device pointers owned by the caller, asynchronous
  * calls on `stream` whose argument errors are reported before any device work,
- * its status codes, no allocation and no state kept between calls.  Sums and
- * statistics are held in 32 bits, in an order that depends on the sizes alone,
- * so a call repeated on the same operands gives the same bits.
+ * its status codes, no allocation and no state kept between calls.  Operands
+ * overlap where the memory from their first to their last entry does, so also
+ * as columns side by side in one buffer.  Sums and statistics are held in 32
+ * bits, in an order that depends on the sizes alone, so a call repeated on the
+ * same operands gives the same bits.  (One exception: a replay of a captured
+ * linear or linear_backward, after an earlier one whose W or X had entries past
+ * 65504 / scale, stays with the kernels that those need, which round differently.)
  */
 #ifndef SGEMM_CUBE_LAYERS_H_
 #define SGEMM_CUBE_LAYERS_H_
@@ -22,7 +26,8 @@ extern "C" {
 typedef enum {
   SGEMM_CUBE_ACT_NONE = 0,
   SGEMM_CUBE_ACT_RELU = 1,      /* max(z, 0), derivative 0 at 0 */
-  SGEMM_CUBE_ACT_GELU = 2,      /* z Phi(z), Phi the normal distribution */
+  SGEMM_CUBE_ACT_GELU = 2,      /* z Phi(z), Phi the normal distribution to 3 units of
+                                   2^-24, and to 1e-5 of itself from -8 on */
   SGEMM_CUBE_ACT_GELU_TANH = 3, /* z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2 */
   SGEMM_CUBE_ACT_SILU = 4       /* z / (1 + exp(-z)) */
 } sgemm_cube_activation_t;
@@ -51,7 +56,9 @@ typedef enum {
  *                256-byte aligned, as for sgemm_cube_ws.
  * Outputs must not overlap each other, an input or the workspace, but for R.
  * As for sgemm_cube there is no range guard: entries of X and W with a
- * magnitude of 65520 or more give infinities or NaN in their rows and columns.
+ * magnitude of 65520 or more give infinities or NaN in their rows and columns,
+ * and entries below 2^-14 are off by up to 2^-36 and not by 2^-22 of themselves.
+ * There is no pre-scaling or range report here (sgemm_cube_ex has both).
  */
 int sgemm_cube_linear(int64_t M, int64_t N, int64_t K, const float* X, int64_t ldx,
                       const float* W, int64_t ldw, int transpose_w, const float* bias,
@@ -106,7 +113,8 @@ typedef enum {
  *   dtype        sgemm_cube_dtype_t of X and Y.
  *   X, ldx       row-major rows x cols, ldx >= max(1, cols).
  *   weight, bias FP32, cols values each; NULL: all ones, all zeros.
- *   eps          finite, >= 0.  (With eps = 0 a constant row gives NaN.)
+ *   eps          finite, >= 0.  (With eps = 0 a row of equal values has no result:
+ *                it gives NaN, or its mean's rounding error over itself.)
  *   Y, ldy       row-major rows x cols; may be X itself (same pointer and
  *                leading dimension), otherwise must not overlap X.
  *   mean, rstd   NULL, or rows FP32 values each that receive mu and r.
@@ -180,7 +188,8 @@ typedef struct {
  *                   of different entries (only the former is checked).
  *   grad_dtype      sgemm_cube_dtype_t of every gradient.
  *   state_bits      8 or 32.
- *   step            >= 1, the number of this step.
+ *   step            >= 1, the number of this step.  A captured call keeps it, and so
+ *                   both powers of beta, on every replay.
  */
 int sgemm_cube_adamw(int64_t tensors, const sgemm_cube_adamw_tensor_t* list, int grad_dtype,
                      int state_bits, double lr, double beta1, double beta2, double eps,

@@ -126,8 +126,8 @@ __device__ __forceinline__ void epilogue_edge(const Epilogue& e, float* Y, int64
 // then has four adjacent columns: bias, residual, Z and Y move in 16-byte pieces of
 // whole rows, and the activation is one rolled loop of four pieces and not one copy
 // per accumulator (one piece at a time, a lone wave per SIMD waited out each step of
-// it: 8192 x 8192 x 4096 with GELU and Z 1289 us in all, so 1220 to 1258, of which
-// the split is 98; the product alone 1170 to 1198).  Column c of row r is at
+// it: 8192 x 8192 x 4096 with GELU and Z 1289 us in all, so 1199 to 1269, of which
+// the split is 94 to 98; the product alone 1170 to 1198).  Column c of row r is at
 // c ^ 16 ((r / 4) % 4) of the row (as far as its width allows), which spreads the 4
 // row groups of an accumulator over the banks.
 template <int kSubM, int kSubN, int kChunk, typename F>

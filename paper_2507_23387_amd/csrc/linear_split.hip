@@ -294,7 +294,7 @@ __device__ __forceinline__ float quarter_max(float v) {
 
 // 128 columns of a slab of rows: thread t has columns 4 (t % 32) .. + 3 of every
 // eighth row, so that 16 lanes also find the largest magnitude of half of its strip.
-// 8192 x 4096 with Z: 44 us, 6.1 TB/s.
+// 8192 x 4096 with Z: 46 us, 5.8 TB/s.
 __global__ __launch_bounds__(kThreads) void columns_kernel(ColumnArgs a, int64_t slab_rows) {
   __shared__ float sums[kThreads / 32][kColumnStrip], tops[kThreads / 32][kColumnStrip];
   const int t = threadIdx.x;

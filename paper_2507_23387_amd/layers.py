@@ -3,7 +3,8 @@ torch tensors: marshalling only, like binding.py.  Every call checks its
 tensors, takes its results and workspace from torch's allocator, enqueues the
 library's kernels on the current torch stream and returns; nothing is kept
 between calls, and a non-zero status raises SgemmCubeError.  There is no
-autograd here: the backward functions are called by the program.
+autograd here: results require no gradient, whatever the operands do, and the
+backward functions are called by the program.
 """
 from __future__ import annotations
 
@@ -94,8 +95,11 @@ def linear(X, W, bias=None, residual=None, activation: str = "none", transpose_w
     the epilogue in one pass.  X is M x K, W K x N, or N x K with transpose_w=True.
     activation: none, relu, gelu, gelu_tanh or silu.  With keep_preact=True returns
     (Y, Z), Z = X W + bias, which linear_backward needs of a layer with an
-    activation.  residual may be out.  workspace: a byte tensor of
-    sgemm_cube_linear_workspace_size bytes that a program keeps between calls."""
+    activation.  residual may be out.  order: of the three products' sums, as for
+    matmul, but for few rows or columns, which are summed termwise (up to 128, or 256
+    where there are few entries: a row's last bits can change with the batch there).
+    workspace: a byte tensor of sgemm_cube_linear_workspace_size bytes that a program
+    keeps between calls.  The results are not part of an autograd graph."""
     device = _current_device()
     px, ldx = _matrix(X, "X", device)
     pw, ldw = _matrix(W, "W", device)
@@ -131,7 +135,8 @@ def linear_backward(dY, X, W, preact=None, activation: str = "none", transpose_w
                     workspace=None):
     """(dX, dW, db) of linear at X and W from its output's gradient; preact: the Z
     that it kept, if it has an activation.  dW has W's layout.  What `need` leaves
-    out is None.  (The residual's gradient is dY.)"""
+    out is None.  (The residual's gradient is dY.)  order, workspace: as for linear,
+    sgemm_cube_linear_backward_workspace_size bytes."""
     device = _current_device()
     pdy, lddy = _matrix(dY, "dY", device)
     px, ldx = _matrix(X, "X", device)
@@ -164,7 +169,8 @@ def linear_backward(dY, X, W, preact=None, activation: str = "none", transpose_w
 def layer_norm(x, weight=None, bias=None, eps: float = 1e-5, keep_stats: bool = False, out=None):
     """Layer norm of the rows of x (float32, float16 or bfloat16), rounded once to
     x's type; weight and bias are float32.  With keep_stats=True returns
-    (y, mean, rstd), what layer_norm_backward needs.  out may be x."""
+    (y, mean, rstd), what layer_norm_backward needs.  out may be x.  The results are
+    not part of an autograd graph."""
     device = _current_device()
     px, ldx = _matrix(x, "x", device, dtype=_DTYPES)
     rows, cols = x.shape
@@ -292,7 +298,8 @@ class AdamW:
     def step(self, grads, step: int | None = None, grad_scale: float = 1.0):
         """One step from grads (contiguous tensors of one type: float32, float16 or
         bfloat16), multiplied by grad_scale first.  step: its number, by default
-        one more than the last."""
+        one more than the last.  A captured step keeps its number, and with it the bias
+        corrections, on every replay."""
         grads = list(grads)
         if len(grads) != len(self._counts):
             raise ValueError(f"grads must hold {len(self._counts)} tensors")
