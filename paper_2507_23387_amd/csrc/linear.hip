@@ -54,8 +54,12 @@ void to_planes(SplitJob& j, const Planes& p, bool side_b, bool columns) {
   }
 }
 
-// Most tiles of a split that also joins the column sums.
-constexpr int64_t kSplitJoinBlocks = 2048;
+// Most tiles of a split that also joins what the pass over D left: each of D's tiles
+// then joins its own lines' magnitudes, 2 us and more where they are many, instead of
+// a launch between (us, so and with it: 256 x 1024 x 1024 27.9 and 28.9, 777 x 1003 x 530
+// 30.8 and 32.7, 4096 x 256 x 256 39.8 and 41.6, 1024 x 1024 x 512 30.3 and 30.6; of more
+// tiles 2048 x 1024 x 1024 56.1 and 55.4, 2048 x 2560 x 512 79.5 and 73.0).
+constexpr int64_t kSplitJoinBlocks = 1024;
 
 // Target exponents of a pre-scaled operand (api.hip's range_opts): as A, and as
 // B, where the scaled kernels form s B_hi in FP16.
@@ -227,9 +231,6 @@ hipError_t launch_linear_grad(const LinearGradArgs& a, void* ws, hipStream_t str
   }
   if (count > 0) jobs[count++] = d;
 
-  // A split of few tiles joins the column sums itself: every one of D's workgroups
-  // reads its lines' magnitudes, 2 us, instead of a launch between (777 x 1003 x 530:
-  // 39 us with it).
   const bool split_joins = count > 0 && split_jobs_blocks(jobs, count) <= kSplitJoinBlocks;
   err = launch_columns(cols, stream);
   if (err == hipSuccess && !split_joins) err = launch_columns_join(join, stream);
