@@ -95,7 +95,7 @@ int sgemm_cube_linear_backward(int64_t M, int64_t N, int64_t K, const float* dY,
                                hipStream_t stream);
 size_t sgemm_cube_linear_backward_workspace_size(int64_t M, int64_t N, int64_t K);
 
-/* Element types of a layer norm's rows. */
+/* Element types of a layer norm's rows, an embedding's table and AdamW's gradients. */
 typedef enum {
   SGEMM_CUBE_F32 = 0,
   SGEMM_CUBE_F16 = 1,
@@ -146,6 +146,141 @@ int sgemm_cube_layer_norm_backward(int64_t rows, int64_t cols, int dtype, const 
                                    float* dweight, float* dbias, void* ws, size_t ws_bytes,
                                    hipStream_t stream);
 size_t sgemm_cube_layer_norm_backward_workspace_size(int64_t rows, int64_t cols);
+
+/*
+ * Rows of an embedding table: Y_i = scale W[id_i], computed in 32 bits and rounded
+ * once to the table's type.
+ *   n            >= 0 ids, of 32 or 64 bits each (id_bits; int32_t, int64_t).  A
+ *                negative id is a place without a token: its row is zeros.  An id
+ *                of vocab or more gives a row of NaN.
+ *   vocab, cols  >= 0, the table's size.  n, vocab, cols <= 2^28.
+ *   dtype        sgemm_cube_dtype_t of W and Y.
+ *   W, ldw       row-major vocab x cols, ldw >= max(1, cols).
+ *   scale        finite.
+ *   Y, ldy       row-major n x cols; must not overlap an input.
+ */
+int sgemm_cube_embedding(int64_t n, int64_t vocab, int64_t cols, int dtype, const void* ids,
+                         int id_bits, const void* W, int64_t ldw, float scale, void* Y,
+                         int64_t ldy, hipStream_t stream);
+
+/*
+ * Its gradient: dW_v = scale sum of dY_i over the i with id_i = v, the sums in 32 bits
+ * in an order that the sizes and ids alone fix.
+ *   dtype        sgemm_cube_dtype_t of dY.
+ *   dY, lddy     row-major n x cols.  Rows whose id is no row of the table (negative,
+ *                or vocab or more) are not read.
+ *   accumulate   0: dW is overwritten, zeros where no id is.  Otherwise the sums are
+ *                added to what dW holds, and only the rows of the ids are touched (the
+ *                gradient of a table that an output layer shares).
+ *   dW, lddw     FP32, row-major vocab x cols; must not overlap an input or ws.
+ *   ws, ws_bytes at least sgemm_cube_embedding_backward_workspace_size(n, cols) bytes,
+ *                256-byte aligned, as for sgemm_cube_ws.
+ */
+int sgemm_cube_embedding_backward(int64_t n, int64_t vocab, int64_t cols, int dtype,
+                                  const void* dY, int64_t lddy, const void* ids, int id_bits,
+                                  float scale, int accumulate, float* dW, int64_t lddw, void* ws,
+                                  size_t ws_bytes, hipStream_t stream);
+size_t sgemm_cube_embedding_backward_workspace_size(int64_t n, int64_t cols);
+
+/*
+ * Cross entropy of a linear layer's rows over a vocabulary, the logits
+ * z = X W + bias taken in pieces of the vocabulary and never kept:
+ *   lse_i = log(sum_j exp(z_ij)),   loss_i = lse_i - z_i,target.
+ *   M, V, K      >= 0: rows, entries of the vocabulary, features.
+ *   X, ldx       row-major M x K, ldx >= max(1, K).
+ *   W, ldw       transpose_w == 0: row-major K x V, ldw >= max(1, V); otherwise
+ *                row-major V x K (as an embedding table lies), ldw >= max(1, K).
+ *   bias         NULL, or V values; -inf leaves an entry out.
+ *   targets      M ids of 32 or 64 bits (target_bits).  A negative target leaves the
+ *                row out: its loss is 0 (lse is computed).  A target of V or more gives
+ *                a loss of NaN.
+ *   loss, lse    M values each.
+ *   scale, accum_order  as for sgemm_cube_linear, its ranges too.
+ *   ws, ws_bytes at least sgemm_cube_linear_cross_entropy_workspace_size(M, V, K)
+ *                bytes, 256-byte aligned, as for sgemm_cube_ws.
+ * Outputs must not overlap each other, an input or the workspace.  Logits may be -inf
+ * (lse is -inf where a row has nothing else); NaN or +inf gives NaN in its row.
+ */
+int sgemm_cube_linear_cross_entropy(int64_t M, int64_t V, int64_t K, const float* X, int64_t ldx,
+                                    const float* W, int64_t ldw, int transpose_w,
+                                    const float* bias, const void* targets, int target_bits,
+                                    float* loss, float* lse, float scale, int accum_order,
+                                    void* ws, size_t ws_bytes, hipStream_t stream);
+size_t sgemm_cube_linear_cross_entropy_workspace_size(int64_t M, int64_t V, int64_t K);
+
+/*
+ * Its gradients: with the rows' dloss and dlse (of a penalty on lse),
+ *   D_ij = exp(z_ij - lse_i) (dloss_i + dlse_i) - [j = target_i] dloss_i,
+ *   dX = D W^T,   dW = X^T D,   dbias_j = sum_i D_ij,
+ * dloss_i taken as 0 where the target is negative.  The logits are computed again, a
+ * piece of the vocabulary at a time, and D is multiplied by powers of two for each row
+ * and column of a piece as in sgemm_cube_linear_backward.  A row whose dloss + dlse is 0
+ * has p = 0 whatever its logits (its X must be finite, as it enters dW times 0); a
+ * target of V or more gives a D of NaN.
+ *   dloss        M values; dlse: NULL (zeros), or M values.
+ *   lse          what the forward call gave for the same operands.
+ *   dX, lddx     NULL, or row-major M x K, overwritten.
+ *   dW, lddw     NULL, or of W's shape and layout, overwritten (zeros for M == 0).
+ *   dbias        NULL, or V values, overwritten (zeros for M == 0).
+ *   ws, ws_bytes at least sgemm_cube_linear_cross_entropy_backward_workspace_size(M,
+ *                V, K) bytes, 256-byte aligned, as for sgemm_cube_ws.
+ * Outputs must not overlap each other, an input or the workspace.
+ */
+int sgemm_cube_linear_cross_entropy_backward(
+    int64_t M, int64_t V, int64_t K, const float* dloss, const float* dlse, const float* X,
+    int64_t ldx, const float* W, int64_t ldw, int transpose_w, const float* bias,
+    const void* targets, int target_bits, const float* lse, float* dX, int64_t lddx, float* dW,
+    int64_t lddw, float* dbias, float scale, int accum_order, void* ws, size_t ws_bytes,
+    hipStream_t stream);
+size_t sgemm_cube_linear_cross_entropy_backward_workspace_size(int64_t M, int64_t V, int64_t K);
+
+/*
+ * The first half of a gated feed-forward block:
+ *   G = X Wg + bias_g,   U = X Wu + bias_u,   Y = act(G) U.
+ *   M, N, K      >= 0, as for sgemm_cube_linear.
+ *   Wg, Wu       both K x N, or with transpose_w both N x K, each with a leading
+ *                dimension of its own (the halves of one matrix, say).
+ *   bias_g, bias_u  NULL, or N values each.
+ *   activation   sgemm_cube_activation_t.
+ *   Y, ldy       row-major M x N, ldy >= max(1, N).
+ *   G, ldg, U, ldu  both NULL, or row-major M x N matrices that receive G and U,
+ *                what the backward pass needs.
+ *   scale, accum_order  as for sgemm_cube_linear, its ranges too.
+ *   ws, ws_bytes at least sgemm_cube_gated_linear_workspace_size(M, N, K) bytes,
+ *                256-byte aligned, as for sgemm_cube_ws.
+ * Outputs must not overlap each other, an input or the workspace.
+ */
+int sgemm_cube_gated_linear(int64_t M, int64_t N, int64_t K, const float* X, int64_t ldx,
+                            const float* Wg, int64_t ldwg, const float* Wu, int64_t ldwu,
+                            int transpose_w, const float* bias_g, const float* bias_u,
+                            int activation, float* Y, int64_t ldy, float* G, int64_t ldg,
+                            float* U, int64_t ldu, float scale, int accum_order, void* ws,
+                            size_t ws_bytes, hipStream_t stream);
+size_t sgemm_cube_gated_linear_workspace_size(int64_t M, int64_t N, int64_t K);
+
+/*
+ * Its gradients: with dU = dY act(G) and dG = dY U act'(G), entry by entry,
+ *   dX = dG Wg^T + dU Wu^T,   dWg = X^T dG,   dWu = X^T dU,
+ * dbias_g and dbias_u the sums of dG's and dU's columns.  dG and dU are multiplied by
+ * powers of two for each row and column as in sgemm_cube_linear_backward.
+ *   dY, lddy     row-major M x N.
+ *   G, ldg, U, ldu  what the forward call kept.
+ *   X, Wg, Wu    as in the forward pass.
+ *   dX, dWg, dWu, dbias_g, dbias_u  NULL, or overwritten, dWg and dWu of the weights'
+ *                shape and layout (zeros for M == 0, and dX for N == 0).
+ *   ws, ws_bytes at least sgemm_cube_gated_linear_backward_workspace_size(M, N, K)
+ *                bytes, 256-byte aligned, as for sgemm_cube_ws.
+ * Outputs must not overlap each other, an input or the workspace.
+ */
+int sgemm_cube_gated_linear_backward(int64_t M, int64_t N, int64_t K, const float* dY,
+                                     int64_t lddy, const float* G, int64_t ldg, const float* U,
+                                     int64_t ldu, const float* X, int64_t ldx, const float* Wg,
+                                     int64_t ldwg, const float* Wu, int64_t ldwu, int transpose_w,
+                                     int activation, float* dX, int64_t lddx, float* dWg,
+                                     int64_t lddwg, float* dWu, int64_t lddwu, float* dbias_g,
+                                     float* dbias_u, float scale, int accum_order, void* ws,
+                                     size_t ws_bytes, hipStream_t stream);
+size_t sgemm_cube_gated_linear_backward_workspace_size(int64_t M, int64_t N, int64_t K);
 
 /* Values of an 8-bit AdamW state that share a scale. */
 enum { SGEMM_CUBE_ADAMW_BLOCK = 256 };

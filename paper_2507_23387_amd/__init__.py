@@ -45,10 +45,16 @@ _EXPORTS = (
 # The layers around the product (layers.py).
 _LAYERS = (
     "AdamW",
+    "embedding",
+    "embedding_backward",
+    "gated_linear",
+    "gated_linear_backward",
     "layer_norm",
     "layer_norm_backward",
     "linear",
     "linear_backward",
+    "linear_cross_entropy",
+    "linear_cross_entropy_backward",
 )
 
 __all__ = list(_EXPORTS + _LAYERS)

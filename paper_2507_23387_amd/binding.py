@@ -54,6 +54,13 @@ LAYER_EXPORTS = (
     "sgemm_cube_linear_backward", "sgemm_cube_linear_backward_workspace_size",
     "sgemm_cube_layer_norm", "sgemm_cube_layer_norm_backward",
     "sgemm_cube_layer_norm_backward_workspace_size",
+    "sgemm_cube_embedding", "sgemm_cube_embedding_backward",
+    "sgemm_cube_embedding_backward_workspace_size",
+    "sgemm_cube_linear_cross_entropy", "sgemm_cube_linear_cross_entropy_workspace_size",
+    "sgemm_cube_linear_cross_entropy_backward",
+    "sgemm_cube_linear_cross_entropy_backward_workspace_size",
+    "sgemm_cube_gated_linear", "sgemm_cube_gated_linear_workspace_size",
+    "sgemm_cube_gated_linear_backward", "sgemm_cube_gated_linear_backward_workspace_size",
     "sgemm_cube_adamw", "sgemm_cube_adamw_values",
 )
 ADAMW_BLOCK = 256
@@ -120,6 +127,25 @@ def _load() -> ctypes.CDLL:
         "sgemm_cube_layer_norm_backward": (i32, [i64, i64, i32, ptr, i64, ptr, i64, ptr, ptr,
                                                  ptr, ptr, i64, ptr, ptr, ptr, sz, ptr]),
         "sgemm_cube_layer_norm_backward_workspace_size": (sz, [i64, i64]),
+        "sgemm_cube_embedding": (i32, [i64, i64, i64, i32, ptr, i32, ptr, i64, f32, ptr, i64, ptr]),
+        "sgemm_cube_embedding_backward": (i32, [i64, i64, i64, i32, ptr, i64, ptr, i32, f32, i32,
+                                                ptr, i64, ptr, sz, ptr]),
+        "sgemm_cube_embedding_backward_workspace_size": (sz, [i64, i64]),
+        "sgemm_cube_linear_cross_entropy": (i32, [i64, i64, i64, ptr, i64, ptr, i64, i32, ptr, ptr,
+                                                  i32, ptr, ptr, f32, i32, ptr, sz, ptr]),
+        "sgemm_cube_linear_cross_entropy_workspace_size": (sz, [i64, i64, i64]),
+        "sgemm_cube_linear_cross_entropy_backward": (i32, [
+            i64, i64, i64, ptr, ptr, ptr, i64, ptr, i64, i32, ptr, ptr, i32, ptr, ptr, i64, ptr,
+            i64, ptr, f32, i32, ptr, sz, ptr]),
+        "sgemm_cube_linear_cross_entropy_backward_workspace_size": (sz, [i64, i64, i64]),
+        "sgemm_cube_gated_linear": (i32, [i64, i64, i64, ptr, i64, ptr, i64, ptr, i64, i32, ptr,
+                                          ptr, i32, ptr, i64, ptr, i64, ptr, i64, f32, i32, ptr,
+                                          sz, ptr]),
+        "sgemm_cube_gated_linear_workspace_size": (sz, [i64, i64, i64]),
+        "sgemm_cube_gated_linear_backward": (i32, [
+            i64, i64, i64, ptr, i64, ptr, i64, ptr, i64, ptr, i64, ptr, i64, ptr, i64, i32, i32,
+            ptr, i64, ptr, i64, ptr, i64, ptr, ptr, f32, i32, ptr, sz, ptr]),
+        "sgemm_cube_gated_linear_backward_workspace_size": (sz, [i64, i64, i64]),
         "sgemm_cube_adamw": (i32, [i64, ptr, i32, i32, f64, f64, f64, f64, f64, i64, ptr]),
         "sgemm_cube_adamw_values": (i32, [i64, ptr, ptr, ptr, ptr]),
     }
@@ -260,6 +286,72 @@ def sgemm_cube_layer_norm_backward(rows, cols, dtype, dY, lddy, X, ldx, weight, 
 
 def sgemm_cube_layer_norm_backward_workspace_size(rows, cols) -> int:
     return int(_lib.sgemm_cube_layer_norm_backward_workspace_size(rows, cols))
+
+
+def sgemm_cube_embedding(n, vocab, cols, dtype, ids, id_bits, W, ldw, scale, Y, ldy,
+                         stream) -> int:
+    return _lib.sgemm_cube_embedding(n, vocab, cols, dtype, ids, id_bits, W, ldw, scale, Y, ldy,
+                                     stream)
+
+
+def sgemm_cube_embedding_backward(n, vocab, cols, dtype, dY, lddy, ids, id_bits, scale, accumulate,
+                                  dW, lddw, ws, ws_bytes, stream) -> int:
+    return _lib.sgemm_cube_embedding_backward(n, vocab, cols, dtype, dY, lddy, ids, id_bits, scale,
+                                              accumulate, dW, lddw, ws, ws_bytes, stream)
+
+
+def sgemm_cube_embedding_backward_workspace_size(n, cols) -> int:
+    return int(_lib.sgemm_cube_embedding_backward_workspace_size(n, cols))
+
+
+def sgemm_cube_linear_cross_entropy(M, V, K, X, ldx, W, ldw, transpose_w, bias, targets,
+                                    target_bits, loss, lse, scale, accum_order, ws, ws_bytes,
+                                    stream) -> int:
+    return _lib.sgemm_cube_linear_cross_entropy(M, V, K, X, ldx, W, ldw, transpose_w, bias,
+                                                targets, target_bits, loss, lse, scale,
+                                                accum_order, ws, ws_bytes, stream)
+
+
+def sgemm_cube_linear_cross_entropy_workspace_size(M, V, K) -> int:
+    return int(_lib.sgemm_cube_linear_cross_entropy_workspace_size(M, V, K))
+
+
+def sgemm_cube_linear_cross_entropy_backward(M, V, K, dloss, dlse, X, ldx, W, ldw, transpose_w,
+                                             bias, targets, target_bits, lse, dX, lddx, dW, lddw,
+                                             dbias, scale, accum_order, ws, ws_bytes,
+                                             stream) -> int:
+    return _lib.sgemm_cube_linear_cross_entropy_backward(
+        M, V, K, dloss, dlse, X, ldx, W, ldw, transpose_w, bias, targets, target_bits, lse, dX,
+        lddx, dW, lddw, dbias, scale, accum_order, ws, ws_bytes, stream)
+
+
+def sgemm_cube_linear_cross_entropy_backward_workspace_size(M, V, K) -> int:
+    return int(_lib.sgemm_cube_linear_cross_entropy_backward_workspace_size(M, V, K))
+
+
+def sgemm_cube_gated_linear(M, N, K, X, ldx, Wg, ldwg, Wu, ldwu, transpose_w, bias_g, bias_u,
+                            activation, Y, ldy, G, ldg, U, ldu, scale, accum_order, ws, ws_bytes,
+                            stream) -> int:
+    return _lib.sgemm_cube_gated_linear(M, N, K, X, ldx, Wg, ldwg, Wu, ldwu, transpose_w, bias_g,
+                                        bias_u, activation, Y, ldy, G, ldg, U, ldu, scale,
+                                        accum_order, ws, ws_bytes, stream)
+
+
+def sgemm_cube_gated_linear_workspace_size(M, N, K) -> int:
+    return int(_lib.sgemm_cube_gated_linear_workspace_size(M, N, K))
+
+
+def sgemm_cube_gated_linear_backward(M, N, K, dY, lddy, G, ldg, U, ldu, X, ldx, Wg, ldwg, Wu, ldwu,
+                                     transpose_w, activation, dX, lddx, dWg, lddwg, dWu, lddwu,
+                                     dbias_g, dbias_u, scale, accum_order, ws, ws_bytes,
+                                     stream) -> int:
+    return _lib.sgemm_cube_gated_linear_backward(
+        M, N, K, dY, lddy, G, ldg, U, ldu, X, ldx, Wg, ldwg, Wu, ldwu, transpose_w, activation, dX,
+        lddx, dWg, lddwg, dWu, lddwu, dbias_g, dbias_u, scale, accum_order, ws, ws_bytes, stream)
+
+
+def sgemm_cube_gated_linear_backward_workspace_size(M, N, K) -> int:
+    return int(_lib.sgemm_cube_gated_linear_backward_workspace_size(M, N, K))
 
 
 def sgemm_cube_adamw(tensors, list, grad_dtype, state_bits, lr, beta1, beta2, eps, grad_scale,

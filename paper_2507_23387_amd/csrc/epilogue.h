@@ -34,7 +34,8 @@ struct LineShifts {
   }
 };
 
-// store_tile16, for Unscale each entry times 2^-shift of its row or column.
+// store_tile16, for Unscale each entry times 2^-shift of its row or column (and added to
+// C's).
 template <int kSubM, int kSubN, class Epi, typename F>
 __device__ __forceinline__ void store_product(const Epi& epi, float* __restrict__ C, int64_t ldc,
                                               int M, int N, int row0, int col0, bool full,
@@ -65,8 +66,10 @@ __device__ __forceinline__ void store_product(const Epi& epi, float* __restrict_
         float* const at = base + static_cast<int64_t>(rr) * ldc;
 #pragma unroll
         for (int j = 0; j < kSubN; ++j)
-          if (full || (row0 + rr < M && col0 + j * 16 < N))
-            at[j * 16] = __builtin_ldexpf(value(i, j, r), p[r]);
+          if (full || (row0 + rr < M && col0 + j * 16 < N)) {
+            const float v = __builtin_ldexpf(value(i, j, r), p[r]);
+            at[j * 16] = epi.add ? at[j * 16] + v : v;
+          }
       }
       SCHED_FENCE();
     }

@@ -91,10 +91,12 @@ struct Epilogue {
   float* z;           // null: not kept
   int64_t ldz;
 };
-// A gradient's product: row i (or column i) of P times 2^-shift[i].
+// A gradient's product: row i (or column i) of P times 2^-shift[i], by rows added to
+// what C holds where `add`.
 struct Unscale {
   const int* shift;
   bool columns;
+  bool add;
 };
 // The epilogue where K = 0: P = 0.
 hipError_t launch_epilogue(const Epilogue& e, int64_t M, int64_t N, float* Y, int64_t ldy,
@@ -149,13 +151,13 @@ struct LinearArgs {
 // The linear layer for few rows or few columns (linear_rows.hip), its sums termwise
 // whatever the variant.  linear_by_rows, linear_by_columns: the rules that choose
 // them.  With `row_shift`, row i of x, a gradient, is multiplied by 2^row_shift[i] as
-// it is split, and the result is freed of it again.  The workspace of N columns is
+// it is split, and the result is freed of it again (and added to y where `add`).  The workspace of N columns is
 // that of as many rows, linear_rows_ws(N, M, K).
 bool linear_by_rows(int64_t M, int64_t N);
 bool linear_by_columns(int64_t M, int64_t N);
 size_t linear_rows_ws(int64_t M, int64_t N, int64_t K);
 hipError_t launch_linear_rows(const LinearArgs& a, const int* row_shift, void* ws,
-                              hipStream_t stream);
+                              hipStream_t stream, bool add = false);
 hipError_t launch_linear_columns(const LinearArgs& a, void* ws, hipStream_t stream);
 
 // out = L^T R in FP32, L and R of M <= kOuterRows rows; a side with z is p times
@@ -197,9 +199,114 @@ struct LinearGradArgs {
   float* dbias;
   float scale;
   int variant;
+  bool add_dx = false;  // dX is added to what dx holds
 };
 size_t linear_grad_ws(int64_t M, int64_t N, int64_t K);
 hipError_t launch_linear_grad(const LinearGradArgs& a, void* ws, hipStream_t stream);
+
+// Token ids or targets: int32 or int64.
+struct Ids {
+  const void* p;
+  int bits;
+};
+
+struct EmbeddingArgs {
+  int64_t n, vocab, cols;
+  Ids ids;
+  const void* w;
+  int64_t ldw;
+  float scale;
+  void* y;
+  int64_t ldy;
+};
+hipError_t launch_embedding(const EmbeddingArgs& a, int dtype, hipStream_t stream);
+
+struct EmbeddingGradArgs {
+  int64_t n, vocab, cols;
+  const void* dy;
+  int64_t lddy;
+  Ids ids;
+  float scale;
+  bool accumulate;
+  float* dw;
+  int64_t lddw;
+};
+size_t embedding_grad_ws(int64_t n, int64_t cols);
+hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, int dtype, void* ws,
+                                 hipStream_t stream);
+
+// A linear layer onto a vocabulary of V entries and the cross entropy of its rows.
+struct XentArgs {
+  int64_t M, V, K;
+  const float* x;
+  int64_t ldx;
+  const float* w;
+  int64_t ldw;
+  bool transpose_w;
+  const float* bias;  // null: none
+  Ids targets;
+  float scale;
+  int variant;
+};
+size_t xent_ws(int64_t M, int64_t V, int64_t K);
+hipError_t launch_xent(const XentArgs& a, float* loss, float* lse, void* ws, hipStream_t stream);
+
+struct XentGradArgs {
+  XentArgs x;
+  const float* dloss;
+  const float* dlse;  // null: none
+  const float* lse;
+  float* dx;  // null: not wanted, as dw and dbias
+  int64_t lddx;
+  float* dw;
+  int64_t lddw;
+  float* dbias;
+};
+size_t xent_grad_ws(int64_t M, int64_t V, int64_t K);
+hipError_t launch_xent_grad(const XentGradArgs& a, void* ws, hipStream_t stream);
+
+// Y = act(G) U, G = X Wg + bg, U = X Wu + bu.
+struct GatedArgs {
+  int64_t M, N, K;
+  const float* x;
+  int64_t ldx;
+  const float* w[2];  // gate, up
+  int64_t ldw[2];
+  bool transpose_w;
+  const float* bias[2];  // null: none
+  int activation;
+  float* y;
+  int64_t ldy;
+  float* z[2];  // G and U, or null: not kept
+  int64_t ldz[2];
+  float scale;
+  int variant;
+};
+size_t gated_ws(int64_t M, int64_t N, int64_t K);
+hipError_t launch_gated(const GatedArgs& a, void* ws, hipStream_t stream);
+
+struct GatedGradArgs {
+  int64_t M, N, K;
+  const float* dy;
+  int64_t lddy;
+  const float* z[2];  // G, U
+  int64_t ldz[2];
+  const float* x;
+  int64_t ldx;
+  const float* w[2];
+  int64_t ldw[2];
+  bool transpose_w;
+  int activation;
+  float* dx;  // null: not wanted, as the others
+  int64_t lddx;
+  float* dw[2];
+  int64_t lddw[2];
+  float* dbias[2];
+  float scale;
+  int variant;
+};
+size_t gated_grad_ws(int64_t M, int64_t N, int64_t K);
+hipError_t launch_gated_grad(const GatedGradArgs& a, void* ws, hipStream_t stream);
 
 struct NormArgs {
   int64_t rows, cols;

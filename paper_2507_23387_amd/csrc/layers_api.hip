@@ -68,6 +68,23 @@ bool product_exceeds(int64_t M, int64_t N, int64_t K) {
   return M > kMaxDim || N > kMaxDim || K > kMaxDim || round_up_tiles_exceed(M, N);
 }
 
+bool valid_ids(const void* p, int bits, int64_t n) {
+  return (bits == 32 || bits == 64) &&
+         (n == 0 || (p && reinterpret_cast<uintptr_t>(p) % (bits / 8) == 0));
+}
+
+// Limits of the embedding's kernels.
+bool embedding_exceeds(int64_t n, int64_t vocab, int64_t cols) {
+  constexpr int64_t kMost = int64_t{1} << 28;
+  return n > kMost || vocab > kMost || cols > kMost;
+}
+
+// Limits of a product and its gradients.
+bool products_exceed(int64_t M, int64_t N, int64_t K) {
+  return product_exceeds(M, N, K) || product_exceeds(M, K, N) || product_exceeds(K, N, M) ||
+         product_exceeds(N, K, M);
+}
+
 size_t norm_grad_ws(int64_t rows, int64_t cols) {
   return static_cast<size_t>(round_up(norm_slabs(rows, cols) * 2 * cols * 4, 256));
 }
@@ -272,6 +289,205 @@ int sgemm_cube_adamw_values(int64_t tensors, const sgemm_cube_adamw_tensor_t* li
     if (hits(mo, {m, v, ms, vs, vo}) || hits(vo, {m, v, ms, vs})) return kInvalid;
   }
   return status_of(launch_adamw_values(tensors, list, exp_avg, exp_avg_sq, stream));
+}
+
+int sgemm_cube_embedding(int64_t n, int64_t vocab, int64_t cols, int dtype, const void* ids,
+                         int id_bits, const void* W, int64_t ldw, float scale, void* Y,
+                         int64_t ldy, hipStream_t stream) {
+  using namespace sgc;
+  if (n < 0 || vocab < 0 || cols < 0 || !valid_dtype(dtype) || !std::isfinite(scale) ||
+      !valid_ids(ids, id_bits, n))
+    return kInvalid;
+  const uint64_t elem = dtype_bytes(dtype);
+  if (!matrix_ok(vocab, cols, W, ldw, elem) || !matrix_ok(n, cols, Y, ldy, elem)) return kInvalid;
+  const Span y{Y, span_bytes(n, cols, ldy, elem)}, w{W, span_bytes(vocab, cols, ldw, elem)};
+  const Span id{ids, static_cast<uint64_t>(n) * (id_bits / 8)};
+  if (hits(y, {w, id})) return kInvalid;
+  if (embedding_exceeds(n, vocab, cols)) return SGEMM_CUBE_ERR_NOT_SUPPORTED;
+  if (n == 0 || cols == 0) return SGEMM_CUBE_OK;
+  const EmbeddingArgs a{n, vocab, cols, {ids, id_bits}, W, ldw, scale, Y, ldy};
+  return status_of(launch_embedding(a, dtype, stream));
+}
+
+size_t sgemm_cube_embedding_backward_workspace_size(int64_t n, int64_t cols) {
+  if (n <= 0 || cols <= 0 || sgc::embedding_exceeds(n, 0, cols)) return 0;
+  return sgc::embedding_grad_ws(n, cols);
+}
+
+int sgemm_cube_embedding_backward(int64_t n, int64_t vocab, int64_t cols, int dtype,
+                                  const void* dY, int64_t lddy, const void* ids, int id_bits,
+                                  float scale, int accumulate, float* dW, int64_t lddw, void* ws,
+                                  size_t ws_bytes, hipStream_t stream) {
+  using namespace sgc;
+  if (n < 0 || vocab < 0 || cols < 0 || !valid_dtype(dtype) || !std::isfinite(scale) ||
+      !valid_ids(ids, id_bits, n))
+    return kInvalid;
+  const uint64_t elem = dtype_bytes(dtype);
+  if (!matrix_ok(n, cols, dY, lddy, elem) || !matrix_ok(vocab, cols, dW, lddw, 4)) return kInvalid;
+  if (embedding_exceeds(n, vocab, cols)) return SGEMM_CUBE_ERR_NOT_SUPPORTED;
+  const size_t need = embedding_grad_ws(n, cols);
+  if (!workspace_ok(ws, ws_bytes, need)) return kInvalid;
+  const Span dy{dY, span_bytes(n, cols, lddy, elem)}, dw{dW, span_bytes(vocab, cols, lddw, 4)};
+  const Span id{ids, static_cast<uint64_t>(n) * (id_bits / 8)}, wsp{ws, need};
+  if (hits(dw, {dy, id, wsp}) || hits(wsp, {dy, id})) return kInvalid;
+  if (vocab == 0 || cols == 0) return SGEMM_CUBE_OK;
+  const EmbeddingGradArgs a{n, vocab, cols, dY, lddy, {ids, id_bits}, scale, accumulate != 0, dW,
+                            lddw};
+  return status_of(launch_embedding_grad(a, dtype, ws, stream));
+}
+
+size_t sgemm_cube_linear_cross_entropy_workspace_size(int64_t M, int64_t V, int64_t K) {
+  if (M < 0 || V < 0 || K < 0 || sgc::product_exceeds(M, V, K)) return 0;
+  return sgc::xent_ws(M, V, K);
+}
+
+int sgemm_cube_linear_cross_entropy(int64_t M, int64_t V, int64_t K, const float* X, int64_t ldx,
+                                    const float* W, int64_t ldw, int transpose_w,
+                                    const float* bias, const void* targets, int target_bits,
+                                    float* loss, float* lse, float scale, int accum_order,
+                                    void* ws, size_t ws_bytes, hipStream_t stream) {
+  using namespace sgc;
+  if (M < 0 || V < 0 || K < 0 || !valid_order(accum_order) || !valid_scale(scale) ||
+      !valid_ids(targets, target_bits, M))
+    return kInvalid;
+  const int64_t wr = transpose_w ? V : K, wc = transpose_w ? K : V;
+  if (!matrix_ok(M, K, X, ldx, 4) || !matrix_ok(wr, wc, W, ldw, 4) || !vector_ok(bias) ||
+      !vector_ok(loss) || !vector_ok(lse) || (M > 0 && (!loss || !lse)))
+    return kInvalid;
+  if (product_exceeds(M, V, K)) return SGEMM_CUBE_ERR_NOT_SUPPORTED;
+  const size_t need = xent_ws(M, V, K);
+  if (!workspace_ok(ws, ws_bytes, need)) return kInvalid;
+  const uint64_t m4 = 4 * static_cast<uint64_t>(M);
+  const Span x{X, span_bytes(M, K, ldx, 4)}, w{W, span_bytes(wr, wc, ldw, 4)};
+  const Span b{bias, 4 * static_cast<uint64_t>(V)}, l{loss, m4}, e{lse, m4}, wsp{ws, need};
+  const Span t{targets, static_cast<uint64_t>(M) * (target_bits / 8)};
+  if (hits(l, {x, w, b, t, e, wsp}) || hits(e, {x, w, b, t, wsp}) || hits(wsp, {x, w, b, t}))
+    return kInvalid;
+  if (M == 0) return SGEMM_CUBE_OK;
+  const XentArgs a{M, V, K, X, ldx, W, ldw, transpose_w != 0, bias, {targets, target_bits}, scale,
+                   variant_of(accum_order)};
+  return status_of(launch_xent(a, loss, lse, ws, stream));
+}
+
+size_t sgemm_cube_linear_cross_entropy_backward_workspace_size(int64_t M, int64_t V, int64_t K) {
+  if (M < 0 || V < 0 || K < 0 || sgc::products_exceed(M, V, K)) return 0;
+  return sgc::xent_grad_ws(M, V, K);
+}
+
+int sgemm_cube_linear_cross_entropy_backward(
+    int64_t M, int64_t V, int64_t K, const float* dloss, const float* dlse, const float* X,
+    int64_t ldx, const float* W, int64_t ldw, int transpose_w, const float* bias,
+    const void* targets, int target_bits, const float* lse, float* dX, int64_t lddx, float* dW,
+    int64_t lddw, float* dbias, float scale, int accum_order, void* ws, size_t ws_bytes,
+    hipStream_t stream) {
+  using namespace sgc;
+  if (M < 0 || V < 0 || K < 0 || !valid_order(accum_order) || !valid_scale(scale) ||
+      !valid_ids(targets, target_bits, M))
+    return kInvalid;
+  const int64_t wr = transpose_w ? V : K, wc = transpose_w ? K : V;
+  if (!matrix_ok(M, K, X, ldx, 4) || !matrix_ok(wr, wc, W, ldw, 4) || !vector_ok(bias) ||
+      !vector_ok(dloss) || !vector_ok(dlse) || !vector_ok(lse) || (M > 0 && (!dloss || !lse)) ||
+      (dX && !matrix_ok(M, K, dX, lddx, 4)) || (dW && !matrix_ok(wr, wc, dW, lddw, 4)) ||
+      !vector_ok(dbias))
+    return kInvalid;
+  if (products_exceed(M, V, K)) return SGEMM_CUBE_ERR_NOT_SUPPORTED;
+  const size_t need = xent_grad_ws(M, V, K);
+  if (!workspace_ok(ws, ws_bytes, need)) return kInvalid;
+  const uint64_t m4 = 4 * static_cast<uint64_t>(M), v4 = 4 * static_cast<uint64_t>(V);
+  const Span x{X, span_bytes(M, K, ldx, 4)}, w{W, span_bytes(wr, wc, ldw, 4)}, b{bias, v4};
+  const Span g{dloss, m4}, h{dlse, m4}, e{lse, m4}, db{dbias, v4}, wsp{ws, need};
+  const Span t{targets, static_cast<uint64_t>(M) * (target_bits / 8)};
+  const Span dx{dX, span_bytes(M, K, lddx, 4)}, dw{dW, span_bytes(wr, wc, lddw, 4)};
+  if (hits(dx, {x, w, b, g, h, e, t, dw, db, wsp}) || hits(dw, {x, w, b, g, h, e, t, db, wsp}) ||
+      hits(db, {x, w, b, g, h, e, t, wsp}) || hits(wsp, {x, w, b, g, h, e, t}))
+    return kInvalid;
+  const XentGradArgs a{{M, V, K, X, ldx, W, ldw, transpose_w != 0, bias, {targets, target_bits},
+                        scale, variant_of(accum_order)},
+                       dloss, dlse, lse, dX, lddx, dW, lddw, dbias};
+  return status_of(launch_xent_grad(a, ws, stream));
+}
+
+size_t sgemm_cube_gated_linear_workspace_size(int64_t M, int64_t N, int64_t K) {
+  if (M < 0 || N < 0 || K < 0 || N > sgc::kMaxDim || sgc::product_exceeds(M, 2 * N, K)) return 0;
+  return sgc::gated_ws(M, N, K);
+}
+
+int sgemm_cube_gated_linear(int64_t M, int64_t N, int64_t K, const float* X, int64_t ldx,
+                            const float* Wg, int64_t ldwg, const float* Wu, int64_t ldwu,
+                            int transpose_w, const float* bias_g, const float* bias_u,
+                            int activation, float* Y, int64_t ldy, float* G, int64_t ldg,
+                            float* U, int64_t ldu, float scale, int accum_order, void* ws,
+                            size_t ws_bytes, hipStream_t stream) {
+  using namespace sgc;
+  if (M < 0 || N < 0 || K < 0 || !valid_order(accum_order) || !valid_activation(activation) ||
+      !valid_scale(scale) || (G != nullptr) != (U != nullptr))
+    return kInvalid;
+  const int64_t wr = transpose_w ? N : K, wc = transpose_w ? K : N;
+  if (!matrix_ok(M, K, X, ldx, 4) || !matrix_ok(wr, wc, Wg, ldwg, 4) ||
+      !matrix_ok(wr, wc, Wu, ldwu, 4) || !vector_ok(bias_g) || !vector_ok(bias_u) ||
+      !matrix_ok(M, N, Y, ldy, 4) ||
+      (G && (!matrix_ok(M, N, G, ldg, 4) || !matrix_ok(M, N, U, ldu, 4))))
+    return kInvalid;
+  if (N > kMaxDim || product_exceeds(M, 2 * N, K)) return SGEMM_CUBE_ERR_NOT_SUPPORTED;
+  const size_t need = gated_ws(M, N, K);
+  if (!workspace_ok(ws, ws_bytes, need)) return kInvalid;
+  const uint64_t n4 = 4 * static_cast<uint64_t>(N);
+  const Span x{X, span_bytes(M, K, ldx, 4)}, bg{bias_g, n4}, bu{bias_u, n4}, wsp{ws, need};
+  const Span wg{Wg, span_bytes(wr, wc, ldwg, 4)}, wu{Wu, span_bytes(wr, wc, ldwu, 4)};
+  const Span y{Y, span_bytes(M, N, ldy, 4)}, g{G, span_bytes(M, N, ldg, 4)};
+  const Span u{U, span_bytes(M, N, ldu, 4)};
+  if (hits(y, {x, wg, wu, bg, bu, g, u, wsp}) || hits(g, {x, wg, wu, bg, bu, u, wsp}) ||
+      hits(u, {x, wg, wu, bg, bu, wsp}) || hits(wsp, {x, wg, wu, bg, bu}))
+    return kInvalid;
+  if (M == 0 || N == 0) return SGEMM_CUBE_OK;
+  const GatedArgs a{M, N, K, X, ldx, {Wg, Wu}, {ldwg, ldwu}, transpose_w != 0, {bias_g, bias_u},
+                    activation, Y, ldy, {G, U}, {ldg, ldu}, scale, variant_of(accum_order)};
+  return status_of(launch_gated(a, ws, stream));
+}
+
+size_t sgemm_cube_gated_linear_backward_workspace_size(int64_t M, int64_t N, int64_t K) {
+  if (M < 0 || N < 0 || K < 0 || N > sgc::kMaxDim || sgc::products_exceed(M, 2 * N, K)) return 0;
+  return sgc::gated_grad_ws(M, N, K);
+}
+
+int sgemm_cube_gated_linear_backward(int64_t M, int64_t N, int64_t K, const float* dY,
+                                     int64_t lddy, const float* G, int64_t ldg, const float* U,
+                                     int64_t ldu, const float* X, int64_t ldx, const float* Wg,
+                                     int64_t ldwg, const float* Wu, int64_t ldwu, int transpose_w,
+                                     int activation, float* dX, int64_t lddx, float* dWg,
+                                     int64_t lddwg, float* dWu, int64_t lddwu, float* dbias_g,
+                                     float* dbias_u, float scale, int accum_order, void* ws,
+                                     size_t ws_bytes, hipStream_t stream) {
+  using namespace sgc;
+  if (M < 0 || N < 0 || K < 0 || !valid_order(accum_order) || !valid_activation(activation) ||
+      !valid_scale(scale))
+    return kInvalid;
+  const int64_t wr = transpose_w ? N : K, wc = transpose_w ? K : N;
+  if (!matrix_ok(M, N, dY, lddy, 4) || !matrix_ok(M, N, G, ldg, 4) ||
+      !matrix_ok(M, N, U, ldu, 4) || !matrix_ok(M, K, X, ldx, 4) ||
+      !matrix_ok(wr, wc, Wg, ldwg, 4) || !matrix_ok(wr, wc, Wu, ldwu, 4) ||
+      (dX && !matrix_ok(M, K, dX, lddx, 4)) || (dWg && !matrix_ok(wr, wc, dWg, lddwg, 4)) ||
+      (dWu && !matrix_ok(wr, wc, dWu, lddwu, 4)) || !vector_ok(dbias_g) || !vector_ok(dbias_u))
+    return kInvalid;
+  if (N > kMaxDim || products_exceed(M, 2 * N, K)) return SGEMM_CUBE_ERR_NOT_SUPPORTED;
+  const size_t need = gated_grad_ws(M, N, K);
+  if (!workspace_ok(ws, ws_bytes, need)) return kInvalid;
+  const uint64_t n4 = 4 * static_cast<uint64_t>(N);
+  const Span dy{dY, span_bytes(M, N, lddy, 4)}, g{G, span_bytes(M, N, ldg, 4)};
+  const Span u{U, span_bytes(M, N, ldu, 4)}, x{X, span_bytes(M, K, ldx, 4)};
+  const Span wg{Wg, span_bytes(wr, wc, ldwg, 4)}, wu{Wu, span_bytes(wr, wc, ldwu, 4)};
+  const Span dx{dX, span_bytes(M, K, lddx, 4)}, dwg{dWg, span_bytes(wr, wc, lddwg, 4)};
+  const Span dwu{dWu, span_bytes(wr, wc, lddwu, 4)}, bg{dbias_g, n4}, bu{dbias_u, n4};
+  const Span wsp{ws, need};
+  if (hits(dx, {dy, g, u, x, wg, wu, dwg, dwu, bg, bu, wsp}) ||
+      hits(dwg, {dy, g, u, x, wg, wu, dwu, bg, bu, wsp}) ||
+      hits(dwu, {dy, g, u, x, wg, wu, bg, bu, wsp}) || hits(bg, {dy, g, u, x, wg, wu, bu, wsp}) ||
+      hits(bu, {dy, g, u, x, wg, wu, wsp}) || hits(wsp, {dy, g, u, x, wg, wu}))
+    return kInvalid;
+  const GatedGradArgs a{M, N, K, dY, lddy, {G, U}, {ldg, ldu}, X, ldx, {Wg, Wu}, {ldwg, ldwu},
+                        transpose_w != 0, activation, dX, lddx, {dWg, dWu}, {lddwg, lddwu},
+                        {dbias_g, dbias_u}, scale, variant_of(accum_order)};
+  return status_of(launch_gated_grad(a, ws, stream));
 }
 
 }  // extern "C"

@@ -184,7 +184,7 @@ hipError_t launch_linear_grad(const LinearGradArgs& a, void* ws, hipStream_t str
   const int64_t dw_rows = a.transpose_w ? a.N : a.K, dw_cols = a.transpose_w ? a.K : a.N;
   if (a.M == 0 || a.N == 0) {
     // No rows: the sums are empty.  No columns: dX = 0.
-    if (a.dx) err = launch_zero(a.M, a.K, a.dx, a.lddx, stream);
+    if (a.dx && !a.add_dx) err = launch_zero(a.M, a.K, a.dx, a.lddx, stream);
     if (err == hipSuccess && a.dw) err = launch_zero(dw_rows, dw_cols, a.dw, a.lddw, stream);
     if (err == hipSuccess && a.dbias) err = launch_zero(1, a.N, a.dbias, a.N, stream);
     return err;
@@ -214,7 +214,7 @@ hipError_t launch_linear_grad(const LinearGradArgs& a, void* ws, hipStream_t str
   SplitJob d = cols.d ? job_of(cols.d, a.N, a.M, a.N) : job_of(a.dy, a.lddy, a.M, a.N);
   if (!cols.d) d.z = a.z, d.ldz = a.ldz, d.activation = a.activation;
   // In dW, D's columns are the result's columns, or with N x K weights its rows.
-  const Unscale ex{g.row_shift, false}, ew{g.col_shift, !a.transpose_w};
+  const Unscale ex{g.row_shift, false, a.add_dx}, ew{g.col_shift, !a.transpose_w, false};
   if (dx && !dx_rows) {
     // dX = D W^T: D's rows and W's K rows, k over N.
     d.row_shift = g.row_shift;
@@ -249,7 +249,7 @@ hipError_t launch_linear_grad(const LinearGradArgs& a, void* ws, hipStream_t str
     r.w = a.w, r.ldw = a.ldw, r.transpose_w = !a.transpose_w;
     r.y = a.dx, r.ldy = a.lddx;
     r.scale = a.scale, r.variant = a.variant;
-    err = launch_linear_rows(r, g.row_shift, g.rows, stream);
+    err = launch_linear_rows(r, g.row_shift, g.rows, stream, a.add_dx);
   } else if (err == hipSuccess && dx) {
     if (dw) {
       const int64_t M[2] = {a.M, dw_rows}, N[2] = {a.K, dw_cols}, K[2] = {a.N, a.M};

@@ -110,6 +110,7 @@ __device__ __forceinline__ void load_strided(const float* col, int64_t ld, int64
 struct RowsArgs {
   LinearArgs a;
   const int* row_shift;  // of a gradient's rows, or null
+  bool add;      // with row_shift: to what Y holds
   bool swapped;  // Y^T = W^T X^T: entry (i, j) is row j, column i of Y
   float inv_s;
   int groups;      // of columns
@@ -122,7 +123,8 @@ __device__ __forceinline__ void finish(const RowsArgs& g, int64_t i, int64_t j, 
   float* const y = g.a.y + i * g.a.ldy + j;
   const Epilogue& e = g.a.e;
   if (g.row_shift) {
-    *y = __builtin_ldexpf(z, -g.row_shift[i]);
+    z = __builtin_ldexpf(z, -g.row_shift[i]);
+    *y = g.add ? *y + z : z;
     return;
   }
   if (e.bias) z += e.bias[j];
@@ -567,9 +569,9 @@ size_t linear_rows_ws(int64_t M, int64_t N, int64_t K) {
 }
 
 hipError_t launch_linear_rows(const LinearArgs& a, const int* row_shift, void* ws,
-                              hipStream_t stream) {
+                              hipStream_t stream, bool add) {
   const RowsPlan p = plan_rows(a.M, a.N, a.K, a.transpose_w);
-  const RowsArgs g{a, row_shift, false, 1.0f / a.scale, p.groups, p.splits,
+  const RowsArgs g{a, row_shift, add, false, 1.0f / a.scale, p.groups, p.splits,
                    static_cast<float*>(ws)};
   const hipError_t e =
       row_shift ? launch_plan<true>(g, p, stream) : launch_plan<false>(g, p, stream);
@@ -582,7 +584,7 @@ hipError_t launch_linear_columns(const LinearArgs& a, void* ws, hipStream_t stre
   t.x = a.w, t.ldx = a.ldw;
   t.w = a.x, t.ldw = a.ldx, t.transpose_w = true;
   const RowsPlan p = plan_rows(t.M, t.N, t.K, true);
-  const RowsArgs g{t, nullptr, true, 1.0f / a.scale, p.groups, p.splits,
+  const RowsArgs g{t, nullptr, false, true, 1.0f / a.scale, p.groups, p.splits,
                    static_cast<float*>(ws)};
   const hipError_t e =
       a.transpose_w ? launch_plan<false>(g, p, stream)

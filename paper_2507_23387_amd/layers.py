@@ -214,6 +214,206 @@ def layer_norm_backward(dy, x, weight, mean, rstd, out=None):
     return dx, dw, db
 
 
+_IDS = {torch.int32: 32, torch.int64: 64}
+
+
+def _ids(t, name, device, n=None):
+    """(address, bits) of a contiguous vector of ids."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in _IDS or t.get_device() != device:
+        _refuse(t, name, _IDS)
+    if t.dim() != 1 or (n is not None and t.numel() != n) or (t.numel() > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name} must be a contiguous vector"
+                         + ("" if n is None else f" of {n} ids"))
+    return t.data_ptr(), _IDS[t.dtype]
+
+
+def embedding(ids, W, scale: float = 1.0, out=None):
+    """scale * W[ids]: rows of the table W (vocabulary x columns; float32, float16 or
+    bfloat16) for a vector of ids (int32 or int64), rounded once to W's type.  A negative
+    id is a place without a token and gives zeros; an id past the table gives NaN.  The
+    result is not part of an autograd graph."""
+    device = _current_device()
+    pi, bits = _ids(ids, "ids", device)
+    pw, ldw = _matrix(W, "W", device, dtype=_DTYPES)
+    n, (vocab, cols) = ids.numel(), W.shape
+    if out is None:
+        y = _new((n, cols), W, W.dtype)
+        py, ldy = y.data_ptr(), max(cols, 1)
+    else:
+        y = out
+        py, ldy = _matrix(y, "out", device, (n, cols), (W.dtype,))
+    _check(binding.sgemm_cube_embedding(n, vocab, cols, _DTYPES[W.dtype], pi, bits, pw, ldw, scale,
+                                        py, ldy, _stream(device)), "sgemm_cube_embedding")
+    if out is not None:
+        _written(out)
+    return y
+
+
+def embedding_backward(dy, ids, vocab: int, scale: float = 1.0, add_to=None, workspace=None):
+    """The table's gradient, float32 vocabulary x columns: scale times the sums of dy's
+    rows (float32, float16 or bfloat16) of each id, zeros where there are none.  The sums'
+    order depends on the ids alone.  add_to: a gradient (that of an output layer which
+    shares the table, say) to which the sums are added, and which is returned.  workspace:
+    a byte tensor of sgemm_cube_embedding_backward_workspace_size bytes that a program
+    keeps between calls."""
+    device = _current_device()
+    pdy, lddy = _matrix(dy, "dy", device, dtype=_DTYPES)
+    n, cols = dy.shape
+    pi, bits = _ids(ids, "ids", device, n)
+    if vocab < 0:
+        raise ValueError("vocab must not be negative")
+    dW = _new((vocab, cols), dy) if add_to is None else add_to
+    pdw, lddw = _matrix(dW, "add_to", device, (vocab, cols))
+    held, ws, size = _workspace(workspace, device,
+                                binding.sgemm_cube_embedding_backward_workspace_size(n, cols), dy)
+    _check(binding.sgemm_cube_embedding_backward(
+        n, vocab, cols, _DTYPES[dy.dtype], pdy, lddy, pi, bits, scale, int(add_to is not None),
+        pdw, lddw, ws, size, _stream(device)), "sgemm_cube_embedding_backward")
+    if add_to is not None:
+        _written(add_to)
+    return dW
+
+
+def linear_cross_entropy(X, W, targets, bias=None, transpose_w: bool = False,
+                         scale: float = 2.0**11, order="elementwise", workspace=None):
+    """(loss, lse) of X's rows over a vocabulary: with z = X W + bias, lse = log(sum of
+    exp(z)) and loss = lse - z[target], the logits never kept.  X is M x K, W K x V, or
+    V x K (an embedding table) with transpose_w=True; bias may hold -inf.  targets: M ids
+    (int32 or int64); a negative one leaves its row out (loss 0), one past the vocabulary
+    gives NaN.  For a mean over the rows that count, the program divides.  order,
+    workspace: as for linear, sgemm_cube_linear_cross_entropy_workspace_size bytes.  The
+    results are not part of an autograd graph."""
+    device = _current_device()
+    px, ldx = _matrix(X, "X", device)
+    pw, ldw = _matrix(W, "W", device)
+    M, K = X.shape
+    K2, V = _weight_shape(W, transpose_w)
+    if K != K2:
+        raise ValueError(f"shape mismatch: X has {K} columns, W takes {K2}")
+    pt, bits = _ids(targets, "targets", device, M)
+    pb = _vector(bias, "bias", device, V)
+    loss, lse = X.new_empty((M,)), X.new_empty((M,))
+    held, ws, size = _workspace(
+        workspace, device, binding.sgemm_cube_linear_cross_entropy_workspace_size(M, V, K), X)
+    _check(binding.sgemm_cube_linear_cross_entropy(
+        M, V, K, px, ldx, pw, ldw, int(transpose_w), pb, pt, bits, loss.data_ptr(), lse.data_ptr(),
+        scale, _order(order), ws, size, _stream(device)), "sgemm_cube_linear_cross_entropy")
+    return loss, lse
+
+
+def linear_cross_entropy_backward(dloss, X, W, targets, lse, dlse=None, bias=None,
+                                  transpose_w: bool = False, need=_GRADIENTS,
+                                  scale: float = 2.0**11, order="elementwise", workspace=None):
+    """(dX, dW, db) of linear_cross_entropy from the gradients of its losses, M values,
+    and, where given, of its lse (of a penalty on lse, say).  lse: what the forward call
+    returned.  dloss of a row whose target is negative counts as 0.  dW has W's layout.
+    What `need` leaves out is None.  order, workspace: as for linear_cross_entropy,
+    sgemm_cube_linear_cross_entropy_backward_workspace_size bytes."""
+    device = _current_device()
+    px, ldx = _matrix(X, "X", device)
+    pw, ldw = _matrix(W, "W", device)
+    M, K = X.shape
+    K2, V = _weight_shape(W, transpose_w)
+    if K != K2:
+        raise ValueError(f"shape mismatch: X has {K} columns, W takes {K2}")
+    if dloss is None or lse is None:
+        raise TypeError("dloss and lse must be tensors")
+    if need is not _GRADIENTS and not set(need) <= set(_GRADIENTS):
+        raise ValueError("need may hold dX, dW and db")
+    pt, bits = _ids(targets, "targets", device, M)
+    pb = _vector(bias, "bias", device, V)
+    pg, ph = _vector(dloss, "dloss", device, M), _vector(dlse, "dlse", device, M)
+    pl = _vector(lse, "lse", device, M)
+    dX = X.new_empty((M, K)) if "dX" in need else None
+    dW = X.new_empty(W.shape) if "dW" in need else None
+    db = X.new_empty((V,)) if "db" in need else None
+    held, ws, size = _workspace(
+        workspace, device,
+        binding.sgemm_cube_linear_cross_entropy_backward_workspace_size(M, V, K), X)
+    _check(binding.sgemm_cube_linear_cross_entropy_backward(
+        M, V, K, pg, ph, px, ldx, pw, ldw, int(transpose_w), pb, pt, bits, pl,
+        None if dX is None else dX.data_ptr(), max(K, 1),
+        None if dW is None else dW.data_ptr(), max(W.shape[1], 1),
+        None if db is None else db.data_ptr(), scale, _order(order), ws, size, _stream(device)),
+        "sgemm_cube_linear_cross_entropy_backward")
+    return dX, dW, db
+
+
+def _gated_weights(X, W_gate, W_up, transpose_w, device):
+    """((address, leading dimension) of both weights, M, N, K)."""
+    pg, pu = _matrix(W_gate, "W_gate", device), _matrix(W_up, "W_up", device, W_gate.shape)
+    K, N = _weight_shape(W_gate, transpose_w)
+    if X.shape[1] != K:
+        raise ValueError(f"shape mismatch: X has {X.shape[1]} columns, W_gate takes {K}")
+    return pg, pu, X.shape[0], N, K
+
+
+def gated_linear(X, W_gate, W_up, bias_gate=None, bias_up=None, activation: str = "silu",
+                 transpose_w: bool = False, keep_preact: bool = False, scale: float = 2.0**11,
+                 order="elementwise", out=None, workspace=None):
+    """act(G) * U with G = X W_gate + bias_gate and U = X W_up + bias_up, the first half
+    of a gated feed-forward block.  X is M x K, both weights K x N, or N x K with
+    transpose_w=True (they may be halves of one matrix).  activation: none, relu, gelu,
+    gelu_tanh or silu.  With keep_preact=True returns (Y, G, U), what
+    gated_linear_backward needs.  order, workspace: as for linear,
+    sgemm_cube_gated_linear_workspace_size bytes.  The results are not part of an
+    autograd graph."""
+    device = _current_device()
+    px, ldx = _matrix(X, "X", device)
+    (pg, ldg), (pu, ldu), M, N, K = _gated_weights(X, W_gate, W_up, transpose_w, device)
+    bg, bu = _vector(bias_gate, "bias_gate", device, N), _vector(bias_up, "bias_up", device, N)
+    if out is None:
+        Y = X.new_empty((M, N))
+        py, ldy = Y.data_ptr(), max(N, 1)
+    else:
+        Y = out
+        py, ldy = _matrix(Y, "out", device, (M, N))
+    G, U = (X.new_empty((M, N)), X.new_empty((M, N))) if keep_preact else (None, None)
+    held, ws, size = _workspace(workspace, device,
+                                binding.sgemm_cube_gated_linear_workspace_size(M, N, K), X)
+    _check(binding.sgemm_cube_gated_linear(
+        M, N, K, px, ldx, pg, ldg, pu, ldu, int(transpose_w), bg, bu, _activation(activation), py,
+        ldy, G.data_ptr() if keep_preact else None, max(N, 1),
+        U.data_ptr() if keep_preact else None, max(N, 1), scale, _order(order), ws, size,
+        _stream(device)), "sgemm_cube_gated_linear")
+    if out is not None:
+        _written(out)
+    return (Y, G, U) if keep_preact else Y
+
+
+_GATED_GRADIENTS = ("dX", "dW_gate", "dW_up", "db_gate", "db_up")
+
+
+def gated_linear_backward(dY, X, W_gate, W_up, gate, up, activation: str = "silu",
+                          transpose_w: bool = False, need=_GATED_GRADIENTS,
+                          scale: float = 2.0**11, order="elementwise", workspace=None):
+    """(dX, dW_gate, dW_up, db_gate, db_up) of gated_linear from its output's gradient;
+    gate, up: the G and U that it kept.  The weights' gradients have their layout.  What
+    `need` leaves out is None.  order, workspace: as for gated_linear,
+    sgemm_cube_gated_linear_backward_workspace_size bytes."""
+    device = _current_device()
+    px, ldx = _matrix(X, "X", device)
+    (pg, ldg), (pu, ldu), M, N, K = _gated_weights(X, W_gate, W_up, transpose_w, device)
+    pdy, lddy = _matrix(dY, "dY", device, (M, N))
+    zg, ldzg = _matrix(gate, "gate", device, (M, N))
+    zu, ldzu = _matrix(up, "up", device, (M, N))
+    if need is not _GATED_GRADIENTS and not set(need) <= set(_GATED_GRADIENTS):
+        raise ValueError(f"need may hold {', '.join(_GATED_GRADIENTS)}")
+    shapes = ((M, K), W_gate.shape, W_gate.shape, (N,), (N,))
+    grads = [X.new_empty(shape) if name in need else None
+             for name, shape in zip(_GATED_GRADIENTS, shapes)]
+    dX, dWg, dWu, dbg, dbu = (None if g is None else g.data_ptr() for g in grads)
+    ld = max(W_gate.shape[1], 1)
+    held, ws, size = _workspace(workspace, device,
+                                binding.sgemm_cube_gated_linear_backward_workspace_size(M, N, K),
+                                X)
+    _check(binding.sgemm_cube_gated_linear_backward(
+        M, N, K, pdy, lddy, zg, ldzg, zu, ldzu, px, ldx, pg, ldg, pu, ldu, int(transpose_w),
+        _activation(activation), dX, max(K, 1), dWg, ld, dWu, ld, dbg, dbu, scale, _order(order),
+        ws, size, _stream(device)), "sgemm_cube_gated_linear_backward")
+    return tuple(grads)
+
+
 def _flat(t, name, device, n, dtype):
     """Address of a contiguous tensor of n values."""
     if not isinstance(t, torch.Tensor) or t.dtype not in dtype or t.get_device() != device:

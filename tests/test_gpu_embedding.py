@@ -1,0 +1,263 @@
+"""The embedding lookup and its gradient against their definitions.
+
+A looked-up value is one product in 32 bits, rounded once more to the table's type:
+torch's own two operations give the same bits.  A gradient's entry sums c rows in 32
+bits in some order, is scaled and, where asked, added to what was there: it is off by at
+most (c + 1) u of scale times the sum of magnitudes, and u of the result, u = 2^-24."""
+import pytest
+import torch
+
+from tests.gpu_util import log
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0**-24
+DTYPES = [torch.float32, torch.float16, torch.bfloat16]
+IDS = [torch.int64, torch.int32]
+# (ids, vocabulary, columns): one block of the sort, several, and more than one adds up
+# itself; one to three passes; rows shorter than a piece and longer than a workgroup's.
+SHAPES = [(1, 1, 1), (1, 5, 3), (2, 1, 70), (63, 7, 64), (65, 1000, 5), (200, 300, 129),
+          (777, 1003, 530), (4095, 511, 33), (4096, 512, 16), (4097, 513, 100), (5000, 70, 1030),
+          (300, 70000, 70), (9000, 262144, 20), (70, 40, 4100), (33, 50, 8200), (20000, 2000, 260),
+          (140000, 5000, 24), (150000, 3, 9)]
+
+
+def _wide(rows, cols, pad, dtype, gen, scale=1.0):
+    t = torch.full((rows, cols + pad), float("nan"), dtype=dtype, device="cuda")
+    t[:, :cols] = (torch.randn((rows, cols), generator=gen, device="cuda") * scale).to(dtype)
+    return t[:, :cols]
+
+
+def _ids(gen, n, vocab, dtype, kind):
+    u = torch.rand(n, generator=gen, device="cuda", dtype=torch.float64)
+    if kind == "one":
+        ids = torch.full((n,), vocab // 2, device="cuda")
+    elif kind == "often":  # the v-th id about 1 / v as often as the first
+        ids = ((vocab + 1.0)**u).long() - 1
+    else:
+        ids = (u * vocab).long()
+    ids = ids.clamp(0, vocab - 1)
+    if kind == "holes":
+        u = torch.rand(n, generator=gen, device="cuda")
+        ids = torch.where(u < 0.2, -1, torch.where(u < 0.3, vocab, ids))
+        ids[u < 0.02] = -2**31
+        ids[u > 0.98] = 2**31 - 1
+        if dtype == torch.int64:
+            ids[u > 0.99] = 2**40 + 1
+    return ids.to(dtype)
+
+
+def _forward(ids, W, scale):
+    live = (ids >= 0) & (ids < W.shape[0])
+    y = (W[torch.where(live, ids.long(), 0)].float() * scale).to(W.dtype)
+    y[ids < 0] = 0
+    y[ids >= W.shape[0]] = float("nan")
+    return y
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_forward(gpu, dtype):
+    import paper_2507_23387_amd as sgc
+
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(71)
+    for i, (n, vocab, cols) in enumerate(SHAPES):
+        pad, kind = (0, 1, 8)[i % 3], ("often", "holes", "one")[i % 3]
+        log(f"embedding {dtype} {n} of {vocab} x {cols} pad {pad} {kind}")
+        W = _wide(vocab, cols, pad, dtype, gen)
+        ids = _ids(gen, n, vocab, IDS[i % 2], kind)
+        scale = (1.0, 0.3, -7.0)[i // 2 % 3]
+        want = _forward(ids, W, scale)
+        got = sgc.embedding(ids, W, scale=scale)
+        assert got.dtype == dtype and torch.equal(got.isnan(), want.isnan())
+        assert torch.equal(got.nan_to_num(), want.nan_to_num())
+        exact = W.double()[ids.long().clamp(0, vocab - 1)] * scale
+        live = ((ids >= 0) & (ids < vocab))[:, None]
+        half = torch.finfo(dtype).eps / 2 + U
+        tiny = torch.finfo(dtype).tiny * torch.finfo(dtype).eps
+        assert torch.all(~live | ((got.double() - exact).abs() <= half * exact.abs() + tiny))
+        out = _wide(n, cols, 3, dtype, gen)
+        assert sgc.embedding(ids, W, scale=scale, out=out) is out
+        assert torch.equal(out.nan_to_num(), got.nan_to_num())
+        assert out._base is None or out._base[:, cols:].isnan().all()
+
+
+def _check_backward(dy, ids, vocab, scale, old, got):
+    ids, dy, got = ids.cpu(), dy.cpu(), got.cpu()  # many equal ids are slow on the GPU here
+    live = (ids >= 0) & (ids < vocab)
+    at, rows = ids[live].long(), dy[live].double()
+    shape = (vocab, dy.shape[1])
+    want = torch.zeros(shape, dtype=torch.float64).index_add_(0, at, rows) * scale
+    mass = torch.zeros(shape, dtype=torch.float64).index_add_(0, at, rows.abs())
+    count = torch.bincount(at, minlength=vocab).double()[:, None]
+    if old is not None:
+        old = old.cpu()
+        want = want + old.double()
+    tol = (count + 1) * U * abs(scale) * mass + U * want.abs() + 2.0**-149
+    worst = ((got.double() - want).abs() - tol).max().item()
+    assert worst <= 0, f"past the bound by {worst:.3e}"
+    untouched = count[:, 0] == 0
+    left = torch.zeros_like(got) if old is None else old
+    assert torch.equal(got[untouched], left[untouched])
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("kind", ["often", "even", "one", "holes"])
+def test_backward(gpu, dtype, kind):
+    import paper_2507_23387_amd as sgc
+
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(72)
+    for i, (n, vocab, cols) in enumerate(SHAPES):
+        pad = (1, 0, 8)[i % 3]
+        log(f"embedding_backward {dtype} {n} of {vocab} x {cols} pad {pad} {kind}")
+        ids = _ids(gen, n, vocab, IDS[i % 2], kind)
+        dy = _wide(n, cols, pad, dtype, gen, 1e-2)
+        dy[(ids < 0) | (ids >= vocab)] = float("nan")  # never read
+        scale = (1.0, 0.3, -7.0)[i // 2 % 3]
+        got = sgc.embedding_backward(dy, ids, vocab, scale=scale)
+        assert got.dtype == torch.float32
+        _check_backward(dy, ids, vocab, scale, None, got)
+        assert torch.equal(sgc.embedding_backward(dy, ids, vocab, scale=scale), got)
+        total = _wide(vocab, cols, pad, torch.float32, gen)
+        old = total.clone()
+        assert sgc.embedding_backward(dy, ids, vocab, scale=scale, add_to=total) is total
+        _check_backward(dy, ids, vocab, scale, old, total)
+        assert total._base is None or total._base[:, cols:].isnan().all()
+
+
+def test_backward_against_differences(gpu):
+    """<dW, E> against differences of the lookup in 64 bits (it is linear: one step)."""
+    import paper_2507_23387_amd as sgc
+
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(73)
+    ids = _ids(gen, 300, 50, torch.int64, "often")
+    W, dy = _wide(50, 40, 0, torch.float32, gen), _wide(300, 40, 0, torch.float32, gen)
+    E = torch.randn((50, 40), generator=gen, device="cuda", dtype=torch.float64)
+    look = lambda w: (w[ids] * 0.7 * dy.double()).sum().item()  # noqa: E731
+    want = look(W.double() + E) - look(W.double())
+    grad = sgc.embedding_backward(dy, ids, 50, scale=0.7).double()
+    # 300 terms at most a sum, and the differences' own rounding in 64 bits.
+    assert abs((grad * E).sum().item() - want) <= 302 * U * (0.7 * dy.double() * E[ids]).abs().sum()
+
+
+def test_empty(gpu):
+    import paper_2507_23387_amd as sgc
+
+    ids = torch.zeros(0, dtype=torch.int64, device="cuda")
+    W = torch.ones((5, 4), device="cuda")
+    assert sgc.embedding(ids, W).shape == (0, 4)
+    one = torch.zeros(3, dtype=torch.int32, device="cuda")
+    assert sgc.embedding(one, W[:, :0]).shape == (3, 0)
+    assert sgc.embedding(one, W[:0]).isnan().all()
+    assert torch.equal(sgc.embedding_backward(W[:0], ids, 5), torch.zeros_like(W))
+    assert torch.equal(sgc.embedding_backward(W[:0], ids, 5, add_to=W.clone()), W)
+    assert sgc.embedding_backward(W[:3], one, 0).shape == (0, 4)
+    assert sgc.embedding_backward(W[:3, :0], one, 5).shape == (5, 0)
+    none = torch.full((5000,), -1, device="cuda")
+    dy = torch.ones((5000, 4), device="cuda")
+    assert torch.equal(sgc.embedding_backward(dy, none, 5), torch.zeros_like(W))
+    assert torch.equal(sgc.embedding_backward(dy[:5], none[:5], 5, add_to=W.clone()), W)
+
+
+def test_infinities_stay_in_their_rows(gpu):
+    import paper_2507_23387_amd as sgc
+
+    ids = torch.arange(100, device="cuda") % 10
+    dy = torch.ones((100, 6), device="cuda")
+    dy[23, 2], dy[47, 0], dy[57, 0] = float("nan"), float("inf"), float("-inf")
+    got = sgc.embedding_backward(dy, ids, 10)
+    assert got[3, 2].isnan() and got[7, 0].isnan()
+    got[3, 2] = got[7, 0] = 10
+    assert torch.equal(got, torch.full_like(got, 10))
+
+
+def test_streams_workspace_and_graph(gpu):
+    import paper_2507_23387_amd as sgc
+    from paper_2507_23387_amd import binding
+
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(74)
+    for n, vocab, cols in ((50, 300, 100), (6000, 900, 260)):
+        W, dy = _wide(vocab, cols, 0, torch.float32, gen), _wide(n, cols, 0, torch.float32, gen)
+        ids = _ids(gen, n, vocab, torch.int64, "holes")
+        size = binding.sgemm_cube_embedding_backward_workspace_size(n, cols)
+        ws = torch.full((size,), 255, dtype=torch.uint8, device="cuda")
+
+        def step():
+            return (sgc.embedding(ids, W).nan_to_num(),
+                    sgc.embedding_backward(dy, ids, vocab, workspace=ws),
+                    sgc.embedding_backward(dy, ids, vocab, workspace=ws, add_to=W.clone()))
+
+        want = step()
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            other = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, other))
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            held = step()
+        for kind in ("often", "one", "even"):
+            ids.copy_(_ids(gen, n, vocab, torch.int64, kind))
+            dy.copy_(_wide(n, cols, 0, torch.float32, gen))
+            graph.replay()
+            torch.cuda.synchronize()
+            got = [h.clone() for h in held]
+            ws.fill_(255)
+            assert all(torch.equal(a, b) for a, b in zip(got, step()))
+
+
+def test_tables_past_2_to_the_32(gpu):
+    import paper_2507_23387_amd as sgc
+
+    vocab, cols = 600001, 8200  # 4.9e9 elements
+    W = torch.zeros((vocab, cols), dtype=torch.float16, device="cuda")
+    ids = torch.tensor([vocab - 1, 0, 523794, vocab - 1], device="cuda")  # 2^32 / 8200 = 523776
+    for k, v in enumerate(ids.tolist()[:3]):
+        W[v] = k + 1
+    got = sgc.embedding(ids, W)
+    assert torch.equal(got, got.new_tensor([1, 2, 3, 1])[:, None].expand(4, cols))
+    del W
+    vocab = 300001  # 2.5e9 values, 9.8e9 bytes
+    total = torch.zeros((vocab, cols), device="cuda")
+    ids = torch.tensor([vocab - 1, 5, vocab - 1], device="cuda")
+    sgc.embedding_backward(torch.ones((3, cols), device="cuda"), ids, vocab, add_to=total)
+    assert torch.all(total[vocab - 1] == 2) and torch.all(total[5] == 1)
+    assert total.sum(dtype=torch.float64).item() == 3 * cols
+    total.fill_(7)
+    fresh = sgc.embedding_backward(torch.ones((3, cols), device="cuda"), ids, vocab)
+    assert fresh.sum(dtype=torch.float64).item() == 3 * cols and torch.all(fresh[vocab - 1] == 2)
+
+
+def test_refused(gpu):
+    import paper_2507_23387_amd as sgc
+
+    W, dy = torch.zeros((5, 4), device="cuda"), torch.zeros((3, 4), device="cuda")
+    ids = torch.zeros(3, dtype=torch.int64, device="cuda")
+    small = torch.zeros(16, dtype=torch.uint8, device="cuda")
+    for bad in (lambda: sgc.embedding(ids.float(), W), lambda: sgc.embedding(ids.cpu(), W),
+                lambda: sgc.embedding(ids, W.double()), lambda: sgc.embedding([0, 1], W),
+                lambda: sgc.embedding(ids, W, out=dy.half()),
+                lambda: sgc.embedding_backward(dy.double(), ids, 5),
+                lambda: sgc.embedding_backward(dy, ids.short(), 5),
+                lambda: sgc.embedding_backward(dy, ids, 5, add_to=W.half())):
+        with pytest.raises(TypeError):
+            bad()
+    for bad in (lambda: sgc.embedding(ids[None], W), lambda: sgc.embedding(ids, W[0]),
+                lambda: sgc.embedding(ids.repeat(2)[::2], W), lambda: sgc.embedding(ids, W, out=W),
+                lambda: sgc.embedding(ids, W.t()), lambda: sgc.embedding_backward(dy, ids[:2], 5),
+                lambda: sgc.embedding_backward(dy, ids, -1),
+                lambda: sgc.embedding_backward(dy, ids, 5, add_to=W[:4]),
+                lambda: sgc.embedding_backward(dy, ids, 5, workspace=small.cpu())):
+        with pytest.raises(ValueError):
+            bad()
+    for bad in (lambda: sgc.embedding(ids, W, out=W[:3]),
+                lambda: sgc.embedding(ids, W, scale=float("inf")),
+                lambda: sgc.embedding_backward(dy, ids, 5, scale=float("nan")),
+                lambda: sgc.embedding_backward(dy, ids, 5, workspace=small),
+                lambda: sgc.embedding_backward(W[:3], ids, 5, add_to=W)):
+        with pytest.raises(sgc.SgemmCubeError):
+            bad()
