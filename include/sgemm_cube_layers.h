@@ -153,7 +153,7 @@ size_t sgemm_cube_layer_norm_backward_workspace_size(int64_t rows, int64_t cols)
  *   n            >= 0 ids, of 32 or 64 bits each (id_bits; int32_t, int64_t).  A
  *                negative id is a place without a token: its row is zeros.  An id
  *                of vocab or more gives a row of NaN.
- *   vocab, cols  >= 0, the table's size.  n, vocab, cols <= 2^28.
+ *   vocab, cols  >= 0, the table's size.  n <= 2^27; vocab, cols <= 2^28.
  *   dtype        sgemm_cube_dtype_t of W and Y.
  *   W, ldw       row-major vocab x cols, ldw >= max(1, cols).
  *   scale        finite.

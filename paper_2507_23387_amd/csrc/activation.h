@@ -3,6 +3,8 @@
 
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "sgemm_cube_layers.h"
 
 namespace sgc {
@@ -129,6 +131,31 @@ __device__ __forceinline__ void multiply_grad(int activation, V (&d)[kU], const 
       each([](float x) { return activate_grad(SGEMM_CUBE_ACT_SILU, x); });
       break;
     default: break;
+  }
+}
+
+// A gated layer's dG = dy u act'(g) in place of u, and dU = dy act(g), behind one branch.
+template <typename V, int kU>
+__device__ __forceinline__ void gate_gradients(int activation, const V (&dy)[kU],
+                                               const V (&g)[kU], V (&u)[kU], V (&du)[kU]) {
+  auto each = [&](auto act) {
+    constexpr int kAct = decltype(act)::value;
+#pragma unroll
+    for (int i = 0; i < kU; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        u[i][k] = dy[i][k] * u[i][k] * activate_grad(kAct, g[i][k]);
+        du[i][k] = dy[i][k] * activate(kAct, g[i][k]);
+      }
+  };
+  switch (activation) {
+    case SGEMM_CUBE_ACT_RELU: each(std::integral_constant<int, SGEMM_CUBE_ACT_RELU>{}); break;
+    case SGEMM_CUBE_ACT_GELU: each(std::integral_constant<int, SGEMM_CUBE_ACT_GELU>{}); break;
+    case SGEMM_CUBE_ACT_GELU_TANH:
+      each(std::integral_constant<int, SGEMM_CUBE_ACT_GELU_TANH>{});
+      break;
+    case SGEMM_CUBE_ACT_SILU: each(std::integral_constant<int, SGEMM_CUBE_ACT_SILU>{}); break;
+    default: each(std::integral_constant<int, SGEMM_CUBE_ACT_NONE>{}); break;
   }
 }
 

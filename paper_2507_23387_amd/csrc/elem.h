@@ -45,6 +45,22 @@ __device__ __forceinline__ void load_piece(const typename Elem<kDtype>::T* row, 
   }
 }
 
+// The same piece as it lies.
+template <int kDtype>
+__device__ __forceinline__ typename Elem<kDtype>::Piece raw_piece(
+    const typename Elem<kDtype>::T* row, int j, int n) {
+  using L = Elem<kDtype>;
+  typename L::Piece p;
+  if (j + L::kE <= n) {
+    p = *reinterpret_cast<const typename L::Piece*>(row + j);
+  } else {
+#pragma unroll
+    for (int e = 0; e < L::kE; ++e)
+      p[e] = j + e < n ? row[j + e] : static_cast<typename L::T>(0.0f);
+  }
+  return p;
+}
+
 template <int kDtype>
 __device__ __forceinline__ void store_piece(typename Elem<kDtype>::T* row, int j, int n,
                                             const float* v) {

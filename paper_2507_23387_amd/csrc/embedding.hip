@@ -153,50 +153,6 @@ __device__ __forceinline__ void scan_bins(uint32_t count, uint32_t* first) {
   __syncthreads();
 }
 
-// Up to 4096 positions: all passes in one workgroup.
-__global__ __launch_bounds__(kSortThreads) void sort_small_kernel(Ids ids, int64_t vocab, int n,
-                                                                  int key_bits, Sorted out) {
-  __shared__ uint16_t waves[kSortWaves][kBins];
-  __shared__ uint32_t first[kBins], keys[kSortItems];
-  __shared__ uint16_t at[kSortItems];
-  const int begin = (threadIdx.x >> 6) * (64 * kSortRounds) + (threadIdx.x & 63);
-  uint32_t key[kSortRounds], pos[kSortRounds], digit[kSortRounds], rank[kSortRounds];
-  bool live[kSortRounds];
-#pragma unroll
-  for (int r = 0; r < kSortRounds; ++r) {
-    pos[r] = begin + 64 * r;
-    live[r] = static_cast<int>(pos[r]) < n;
-    key[r] = live[r] ? key_of(ids, vocab, pos[r]) : 0;
-  }
-  for (int shift = 0; shift < key_bits; shift += kDigitBits) {
-    const int bits = min(kDigitBits, key_bits - shift);
-#pragma unroll
-    for (int r = 0; r < kSortRounds; ++r) digit[r] = key[r] >> shift & (kBins - 1);
-    rank_items(digit, live, bits, waves, rank);
-    scan_bins(sum_waves(waves), first);
-#pragma unroll
-    for (int r = 0; r < kSortRounds; ++r) {
-      if (!live[r]) continue;
-      const uint32_t to = first[digit[r]] + waves[threadIdx.x >> 6][digit[r]] + rank[r];
-      keys[to] = key[r];
-      at[to] = static_cast<uint16_t>(pos[r]);
-    }
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < kSortRounds; ++r) {
-      if (!live[r]) continue;
-      key[r] = keys[begin + 64 * r];
-      pos[r] = at[begin + 64 * r];
-    }
-  }
-#pragma unroll
-  for (int r = 0; r < kSortRounds; ++r) {
-    if (!live[r]) continue;
-    out.keys[begin + 64 * r] = key[r];
-    out.at[begin + 64 * r] = pos[r];
-  }
-}
-
 // A workgroup's items of one pass: from the ids (the first pass) or the pass before.
 __device__ __forceinline__ void load_items(const SortPass& p, const Ids& ids, int64_t vocab,
                                            const Sorted& from, uint32_t (&key)[kSortRounds],
@@ -295,6 +251,76 @@ __global__ __launch_bounds__(kSortThreads) void sort_scatter_kernel(SortPass p, 
   }
 }
 
+// The median of three: k clamped to a .. b where a <= b.
+__device__ __forceinline__ int clamp_of(int k, int a, int b) {
+  int r;
+  asm("v_med3_i32 %0, %1, %2, %3" : "=v"(r) : "v"(k), "v"(a), "v"(b));
+  return r;
+}
+
+// Few positions: each one's place is the number of pairs (id, position) below its own,
+// counted against all of them.  A workgroup places 64 positions, one a lane, and its
+// waves share the keys, which LDS hands to all lanes at once.  Against `key`, a key k
+// clamped to key - 1 .. key (before it: key .. key + 1) is one less where it counts, so
+// that one instruction compares and half of one adds up; with carries there are two, and
+// two waits between them.  RANK_TIMES
+constexpr int64_t kRankItems = 16384;
+constexpr int kRankChunk = 8192, kPastKeys = 0x7fffffff;
+__global__ __launch_bounds__(kSortThreads) void rank_kernel(Ids ids, int64_t vocab, int n,
+                                                            Sorted out) {
+  __shared__ __align__(16) int keys[kRankChunk];
+  __shared__ uint32_t counts[kSortWaves][64];
+  typedef int i32x4 __attribute__((ext_vector_type(4)));
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int i0 = blockIdx.x * 64, i = i0 + lane;
+  auto key_at = [&](int j) {
+    return j < n ? static_cast<int>(key_of(ids, vocab, j)) : kPastKeys;
+  };
+  const int key = i < n ? key_at(i) : 0;
+  uint32_t below = 0;
+  // Adds how many of 64 keys are below hi.
+  auto count = [&](const int* group, int hi) {
+    const i32x4* const at = reinterpret_cast<const i32x4*>(group);
+    uint32_t sum = 0;
+#pragma unroll
+    for (int q = 0; q < 16; ++q) {
+      const i32x4 k = at[q];
+#pragma unroll
+      for (int e = 0; e < 4; e += 2)
+        sum += static_cast<uint32_t>(clamp_of(k[e], hi - 1, hi)) +
+               static_cast<uint32_t>(clamp_of(k[e + 1], hi - 1, hi));
+    }
+    below += 64 * static_cast<uint32_t>(hi) - sum;
+  };
+  for (int c0 = 0; c0 < n; c0 += kRankChunk) {
+    const int size = min(kRankChunk, (n - c0 + 63) / 64 * 64);
+    __syncthreads();  // the chunk before has been read
+    for (int j = threadIdx.x; j < size; j += kSortThreads) keys[j] = key_at(c0 + j);
+    __syncthreads();
+    for (int g = wave * 64; g < size; g += kSortThreads) {
+      if (c0 + g != i0) {
+        count(keys + g, c0 + g < i0 ? key + 1 : key);
+        continue;
+      }
+#pragma unroll 1
+      for (int j = 0; j < 64; j += 4) {
+        const i32x4 k = *reinterpret_cast<const i32x4*>(keys + g + j);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) below += k[e] < key + (j + e < lane ? 1 : 0);
+      }
+    }
+  }
+  counts[wave][lane] = below;
+  __syncthreads();
+  if (wave != 0 || i >= n) return;
+  uint32_t to = 0;
+#pragma unroll
+  for (int w = 0; w < kSortWaves; ++w) to += counts[w][lane];
+  out.keys[to] = key;
+  out.at[to] = i;
+}
+
 // --- the sums -------------------------------------------------------------------------
 
 struct SumArgs {
@@ -307,13 +333,17 @@ struct SumArgs {
   uint32_t sum_blocks, tiles;  // workgroups of the sums, tiles of columns
 };
 
-// The first position whose key is not below k.
-__device__ __forceinline__ int64_t lower_bound(const uint32_t* keys, int64_t n, uint32_t k) {
-  int64_t lo = 0, hi = n;
-  while (lo < hi) {
-    const int64_t mid = lo + (hi - lo) / 2;
-    if (keys[mid] < k) lo = mid + 1;
-    else hi = mid;
+// The first position whose key is not below k, by a wave: 64 places at a time.
+__device__ __forceinline__ int64_t wave_lower_bound(const uint32_t* keys, int64_t n, uint32_t k) {
+  int64_t lo = 0, size = n;  // the answer is in lo .. lo + size
+  while (size > 0) {
+    const int64_t step = (size + 63) / 64, p = lo + (threadIdx.x & 63) * step;
+    // The lanes' last places of their stretches: below k in a run from lane 0 on.
+    const int64_t last = min(p + step, lo + size) - 1;
+    const int below = __builtin_popcountll(__ballot(p < lo + size && keys[last] < k));
+    const int64_t end = lo + size;
+    lo = min(lo + below * step, end);
+    size = min(step - 1, end - lo);
   }
   return lo;
 }
@@ -348,17 +378,22 @@ template <int kDtype>
 __global__ __launch_bounds__(kThreads) void embedding_sum_kernel(SumArgs g) {
   using L = Elem<kDtype>;
   typedef typename L::T T;
-  constexpr int kE = L::kE, kU = 4;
+  constexpr int kE = L::kE, kU = 8;
   const EmbeddingGradArgs& a = g.a;
   const int cols = static_cast<int>(a.cols);
   if (blockIdx.x >= g.sum_blocks) {
     __shared__ bool absent[kZeroRows];
+    __shared__ int64_t ends[2];
     const int64_t v0 = static_cast<int64_t>(blockIdx.x - g.sum_blocks) * kZeroRows;
-    if (threadIdx.x < kZeroRows) {
-      const int64_t v = v0 + threadIdx.x;
-      const int64_t p = lower_bound(g.sorted.keys, a.n, static_cast<uint32_t>(v));
-      absent[threadIdx.x] = v < a.vocab && (p >= a.n || g.sorted.keys[p] != v);
+    const int64_t v1 = min(a.vocab, v0 + kZeroRows);
+    if (threadIdx.x < kZeroRows) absent[threadIdx.x] = v0 + threadIdx.x < v1;
+    if (threadIdx.x < 128) {
+      const int wave = threadIdx.x >> 6;
+      ends[wave] = wave_lower_bound(g.sorted.keys, a.n, static_cast<uint32_t>(wave ? v1 : v0));
     }
+    __syncthreads();
+    for (int64_t p = ends[0] + threadIdx.x; p < ends[1]; p += kThreads)
+      absent[g.sorted.keys[p] - v0] = false;
     __syncthreads();
     const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     const int per = kThreads / g.lanes;
@@ -378,9 +413,20 @@ __global__ __launch_bounds__(kThreads) void embedding_sum_kernel(SumArgs g) {
   const uint32_t* const keys = g.sorted.keys;
   const uint32_t none = static_cast<uint32_t>(a.vocab);
   const int64_t p0 = c * g.chunk, p1 = min(a.n, p0 + g.chunk);
-  uint32_t run = keys[p0];
+  // The next positions' keys and rows' numbers are asked for before this turn's rows.
+  uint32_t k[kU], at[kU];
+  auto ask = [&](int64_t p) {
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      k[u] = p + u < p1 ? keys[p + u] : none;
+      at[u] = p + u < p1 ? g.sorted.at[p + u] : 0;
+    }
+  };
+  ask(p0);
+  const uint32_t before = p0 > 0 ? keys[p0 - 1] : none, after = p1 < a.n ? keys[p1] : none;
+  uint32_t run = k[0];
   if (run == none) return;
-  bool begun = p0 > 0 && keys[p0 - 1] == run;  // before the chunk
+  bool begun = before == run;  // before the chunk
   float sum[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
   auto leave = [&](int which) {
     float* const to = g.partial + (2 * c + which) * a.cols;
@@ -389,75 +435,70 @@ __global__ __launch_bounds__(kThreads) void embedding_sum_kernel(SumArgs g) {
       if (j + q < cols) store_piece<kF32>(to, j + q, cols, sum + q);
   };
   for (int64_t p = p0; p < p1; p += kU) {
-    uint32_t k[kU];
-    float v[kU][kE];
+    uint32_t now[kU];
+    typename L::Piece v[kU];
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
-      k[u] = p + u < p1 ? keys[p + u] : none;
-      if (k[u] != none)
-        load_piece<kDtype>(static_cast<const T*>(a.dy) + static_cast<int64_t>(g.sorted.at[p + u]) * a.lddy,
-                           j, cols, v[u]);
+      now[u] = k[u];
+      if (now[u] != none)
+        v[u] = raw_piece<kDtype>(
+            static_cast<const T*>(a.dy) + static_cast<int64_t>(at[u]) * a.lddy, j, cols);
     }
+    ask(p + kU);
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
       if (p + u >= p1) break;
-      if (k[u] != run) {
+      if (now[u] != run) {
         if (begun) leave(0);
         else write_row(a, run, j, kE, sum);
         begun = false;
-        run = k[u];
+        run = now[u];
         if (run == none) return;  // the last of the sorted keys
 #pragma unroll
         for (int e = 0; e < kE; ++e) sum[e] = 0.0f;
       }
 #pragma unroll
-      for (int e = 0; e < kE; ++e) sum[e] += v[u][e];
+      for (int e = 0; e < kE; ++e) sum[e] += static_cast<float>(v[u][e]);
     }
   }
-  const bool goes_on = p1 < a.n && keys[p1] == run;
+  const bool goes_on = after == run;
   if (begun) leave(0);
   else if (goes_on) leave(1);
   else write_row(a, run, j, kE, sum);
 }
 
-constexpr int kJoinCols = 256;
-
-// A run that begins in a chunk and goes past it: the chunks' sums, every fourth a wave.
+// Runs that begin in a chunk and go past it, a chunk a workgroup, 1024 columns: the sums
+// that the chunks left, in their order.
+constexpr int kJoinCols = 4 * kThreads;
 __global__ __launch_bounds__(kThreads) void embedding_join_kernel(SumArgs g) {
-  __shared__ float part[kThreads / 64][kJoinCols];
   const EmbeddingGradArgs& a = g.a;
   const uint32_t* const keys = g.sorted.keys;
-  const int64_t c = blockIdx.x, p0 = c * g.chunk, p1 = p0 + g.chunk;
   const int cols = static_cast<int>(a.cols);
+  const int64_t c = blockIdx.x, p0 = c * g.chunk, p1 = p0 + g.chunk;
   if (p1 >= a.n) return;
-  const uint32_t run = keys[p1];
-  if (run >= a.vocab || keys[p1 - 1] != run || (p0 > 0 && keys[p0 - 1] == run)) return;
-  const int64_t last = (lower_bound(keys, a.n, run + 1) - 1) / g.chunk;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint32_t run = keys[p1], in = keys[p1 - 1], before = p0 > 0 ? keys[p0 - 1] : ~0u;
+  if (run >= a.vocab || in != run || before == run) return;
+  // How many chunks begin with the run, 64 at a time.
+  int64_t last = c;
+  for (uint64_t more = ~uint64_t{0}; more == ~uint64_t{0};) {
+    const int64_t p = (last + 1 + (threadIdx.x & 63)) * g.chunk;
+    more = __ballot(p < a.n && keys[p] == run);
+    last += more == ~uint64_t{0} ? 64 : __builtin_ctzll(~more);
+  }
   for (int64_t j0 = static_cast<int64_t>(blockIdx.y) * kJoinCols; j0 < cols;
        j0 += static_cast<int64_t>(gridDim.y) * kJoinCols) {
-    const int j = static_cast<int>(j0) + 4 * lane;
+    const int j = static_cast<int>(j0) + 4 * threadIdx.x;
+    if (j >= cols) break;
     float sum[8] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (j < cols) {
-#pragma unroll 4
-      for (int64_t d = c + wave; d <= last; d += kThreads / 64) {
-        float v[4];
-        load_piece<kF32>(g.partial + (2 * d + (d == c ? 1 : 0)) * a.cols, j, cols, v);
+    load_piece<kF32>(g.partial + (2 * c + 1) * a.cols, j, cols, sum);
+#pragma unroll 8
+    for (int64_t d = c + 1; d <= last; ++d) {
+      float v[4];
+      load_piece<kF32>(g.partial + 2 * d * a.cols, j, cols, v);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum[e] += v[e];
-      }
+      for (int e = 0; e < 4; ++e) sum[e] += v[e];
     }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) part[wave][4 * lane + e] = sum[e];
-    __syncthreads();
-    if (wave == 0 && j < cols) {
-#pragma unroll
-      for (int w = 1; w < kThreads / 64; ++w)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sum[e] += part[w][4 * lane + e];
-      write_row(a, run, j, 4, sum);
-    }
-    __syncthreads();
+    write_row(a, run, j, 4, sum);
   }
 }
 
@@ -468,13 +509,12 @@ int row_lanes(int64_t cols, int per) {
   return lanes;
 }
 
-// Positions to a chunk: longer ones leave fewer sums to join, shorter ones spread few
-// positions over more compute units.
-int chunk_length(int64_t n, int64_t cols, int per) {
-  const int64_t tiles = (cols + int64_t{kThreads} * per - 1) / (int64_t{kThreads} * per);
-  const int64_t groups = kThreads / row_lanes(cols, per);
-  int chunk = 4;
-  while (chunk < 64 && n * tiles / (chunk * groups) > 2048) chunk *= 2;
+// Positions to a chunk: the rows of one id are added one after the other within it, and
+// an id's chunks after each other, so that a long run takes as many steps of either kind
+// (text's most frequent id has a tenth of all positions).  CHUNK_TIMES
+int chunk_length(int64_t n) {
+  int chunk = 8;
+  while (chunk < 64 && int64_t{16} * chunk * chunk < n) chunk *= 2;
   return chunk;
 }
 
@@ -498,16 +538,16 @@ GradWorkspace carve(void* ws, int64_t n, int64_t cols) {
   };
   GradWorkspace g{};
   const int64_t blocks = (n + kSortItems - 1) / kSortItems;
-  for (int s = 0; s < (blocks > 1 ? 2 : 1); ++s) {
+  const bool passes = n > kRankItems;
+  for (int s = 0; s < (passes ? 2 : 1); ++s) {
     g.sorted[s].keys = reinterpret_cast<uint32_t*>(take(4 * n));
     g.sorted[s].at = reinterpret_cast<uint32_t*>(take(4 * n));
   }
-  if (blocks > 1) {
+  if (passes) {
     g.counts = reinterpret_cast<uint32_t*>(take(4 * kBins * blocks));
     g.totals = reinterpret_cast<uint32_t*>(take(4 * kBins));
   }
-  // The chunks of the type that has more of them.
-  const int64_t chunk = std::min(chunk_length(n, cols, 4), chunk_length(n, cols, 8));
+  const int64_t chunk = chunk_length(n);
   g.partial = reinterpret_cast<float*>(take((n + chunk - 1) / chunk * 2 * cols * 4));
   g.bytes = used;
   return g;
@@ -518,9 +558,10 @@ hipError_t launch_sort(const EmbeddingGradArgs& a, const GradWorkspace& ws, Sort
   int key_bits = 1;
   while (a.vocab >> key_bits) ++key_bits;
   sorted = ws.sorted[0];
-  if (a.n <= kSortItems) {
-    hipLaunchKernelGGL(sort_small_kernel, dim3(1), dim3(kSortThreads), 0, stream, a.ids, a.vocab,
-                       static_cast<int>(a.n), key_bits, sorted);
+  if (a.n <= kRankItems) {
+    hipLaunchKernelGGL(rank_kernel, dim3(static_cast<unsigned>((a.n + 63) / 64)),
+                       dim3(kSortThreads), 0, stream, a.ids, a.vocab, static_cast<int>(a.n),
+                       sorted);
     return hipGetLastError();
   }
   const int64_t blocks = (a.n + kSortItems - 1) / kSortItems;
@@ -574,7 +615,7 @@ hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, int dtype, void* ws
   const int per = dtype == kF32 ? 4 : 8;
   g.partial = w.partial;
   g.lanes = row_lanes(a.cols, per);
-  g.chunk = chunk_length(a.n, a.cols, per);
+  g.chunk = chunk_length(a.n);
   g.chunks = (a.n + g.chunk - 1) / g.chunk;
   g.tiles = static_cast<uint32_t>((a.cols + int64_t{g.lanes} * per - 1) / (int64_t{g.lanes} * per));
   const int64_t groups = kThreads / g.lanes;

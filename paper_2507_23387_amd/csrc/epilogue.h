@@ -14,7 +14,8 @@ namespace {
 // In place of an epilogue: C is stored as the product (store_tile16).
 struct NoEpilogue {};
 template <class Epi>
-constexpr bool kThroughLds = std::is_same<Epi, Epilogue>::value;
+constexpr bool kThroughLds =
+    std::is_same<Epi, Epilogue>::value || std::is_same<Epi, GateEpilogue>::value;
 
 // The shifts of a wave's kBlocks x 16 rows (or columns) from `first` on, 64 lines at a
 // time, one a lane, which hand them out: all of a lane's own are more than the wide
@@ -123,6 +124,36 @@ __device__ __forceinline__ void epilogue_edge(const Epilogue& e, float* Y, int64
   }
 }
 
+// Column c of row r of a wave's staged accumulators is at c ^ 16 ((r / 4) % 4) of the row
+// (as far as its width allows), which spreads the 4 row groups of an accumulator over the
+// banks.
+template <int kSubN>
+constexpr int kStageSwap = kSubN % 4 == 0 ? 3 : kSubN % 2 == 0 ? 1 : 0;
+
+// A wave's rows of blocks i0 .. i0 + kN - 1 in its own LDS.
+template <int i0, int kN, int kSubN, typename F>
+__device__ __forceinline__ void stage_rows(float* stage, F value) {
+  constexpr int kWidth = 16 * kSubN;
+  const int lane = threadIdx.x & 63;
+  // The wave's reads of the rows before are done.
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int i = 0; i < kN; ++i)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int row = 16 * i + 4 * (lane >> 4) + r, swap = ((lane >> 4) & kStageSwap<kSubN>) << 4;
+#pragma unroll
+      for (int j = 0; j < kSubN; ++j)
+        stage[row * kWidth + ((16 * j + (lane & 15)) ^ swap)] = value(i0 + i, j, r);
+      // Row by row, so that no more accumulators are read ahead than there are
+      // registers for.
+      SCHED_FENCE();
+    }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // Y = act(Z) + R, Z = value(i, j, r) + bias for a wave's kSubM x kSubN accumulators
 // of 16 x 16 (store_tile16's layout; row0, col0: its first row and column).  kChunk
 // rows of blocks at a time go through `stage`, the wave's own LDS, so that lane l
@@ -130,37 +161,19 @@ __device__ __forceinline__ void epilogue_edge(const Epilogue& e, float* Y, int64
 // whole rows, and the activation is one rolled loop of four pieces and not one copy
 // per accumulator (one piece at a time, a lone wave per SIMD waited out each step of
 // it: 8192 x 8192 x 4096 with GELU and Z 1289 us in all, so 1199 to 1269, of which
-// the split is 94 to 98; the product alone 1170 to 1198).  Column c of row r is at
-// c ^ 16 ((r / 4) % 4) of the row (as far as its width allows), which spreads the 4
-// row groups of an accumulator over the banks.
+// the split is 94 to 98; the product alone 1170 to 1198). 
 template <int kSubM, int kSubN, int kChunk, typename F>
 __device__ __forceinline__ void epilogue_tile(const Epilogue& e, float* stage, float* Y,
                                               int64_t ldy, int M, int N, int row0, int col0,
                                               F value) {
   constexpr int kWidth = 16 * kSubN, kQuads = kWidth / 4;
-  constexpr int kSwap = kSubN % 4 == 0 ? 3 : kSubN % 2 == 0 ? 1 : 0;
+  constexpr int kSwap = kStageSwap<kSubN>;
   const int lane = threadIdx.x & 63;
   const bool full = row0 + 16 * kSubM <= M && col0 + kWidth <= N;
   static_for<(kSubM + kChunk - 1) / kChunk>([&](auto Cc) {
     constexpr int i0 = decltype(Cc)::value * kChunk;
     constexpr int kN = i0 + kChunk <= kSubM ? kChunk : kSubM - i0;
-    // The wave's reads of the chunk before are done.
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-#pragma unroll
-    for (int i = 0; i < kN; ++i)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int row = 16 * i + 4 * (lane >> 4) + r, swap = ((lane >> 4) & kSwap) << 4;
-#pragma unroll
-        for (int j = 0; j < kSubN; ++j)
-          stage[row * kWidth + ((16 * j + (lane & 15)) ^ swap)] = value(i0 + i, j, r);
-        // Row by row, so that no more accumulators are read ahead than there are
-        // registers for.
-        SCHED_FENCE();
-      }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
+    stage_rows<i0, kN, kSubN>(stage, value);
     constexpr int kPieces = kN * kSubN;  // of this lane
     constexpr int kU = kPieces % 4 == 0 ? 4 : kPieces % 2 == 0 ? 2 : 1;
 #pragma unroll 1
@@ -209,6 +222,77 @@ __device__ __forceinline__ void epilogue_tile(const Epilogue& e, float* stage, f
 #pragma unroll
       for (int u = 0; u < kU; ++u)
         store_any(Y + static_cast<int64_t>(gr[u]) * ldy + gc[u], v[u]);
+    }
+  });
+}
+
+// The gated layer's: G and U, 8 columns of each in turn, lie side by side in a wave's
+// accumulators, so that a lane that reads four adjacent columns of both from the staged
+// rows has what an output needs.  M, N: the product's; a piece is 16 bytes of each output.
+template <int kSubM, int kSubN, int kChunk, typename F>
+__device__ __forceinline__ void epilogue_tile(const GateEpilogue& e, float* stage, float* Y,
+                                              int64_t ldy, int M, int N, int row0, int col0,
+                                              F value) {
+  constexpr int kWidth = 16 * kSubN, kQuads = kWidth / 8, kSwap = kStageSwap<kSubN>;
+  const int lane = threadIdx.x & 63, cols = static_cast<int>(e.N);
+  const bool full = row0 + 16 * kSubM <= M && (col0 + kWidth) / 2 <= cols;
+  static_for<(kSubM + kChunk - 1) / kChunk>([&](auto Cc) {
+    constexpr int i0 = decltype(Cc)::value * kChunk;
+    constexpr int kN = i0 + kChunk <= kSubM ? kChunk : kSubM - i0;
+    stage_rows<i0, kN, kSubN>(stage, value);
+    constexpr int kAll = 16 * kN * kQuads, kPieces = (kAll + 63) / 64;
+    constexpr int kU = kPieces % 4 == 0 ? 4 : kPieces % 2 == 0 ? 2 : 1;
+#pragma unroll 1
+    for (int p0 = 0; p0 < kPieces; p0 += kU) {
+      floatx4 v[kU], w[kU];
+      int gr[kU], gc[kU];
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        const int q = lane + 64 * (p0 + u), row = q / kQuads, c = 4 * (q - row * kQuads);
+        gr[u] = kAll % 64 && q >= kAll ? M : row0 + 16 * i0 + row;
+        gc[u] = col0 / 2 + c;
+        const int at = (row < 16 * kN ? row : 0) * kWidth +
+                       ((c / 8 * 16 + c % 8) ^ (((row >> 2) & kSwap) << 4));
+        v[u] = *reinterpret_cast<const floatx4*>(stage + at);
+        w[u] = *reinterpret_cast<const floatx4*>(stage + at + 8);
+      }
+      if (!full || kAll % 64) {
+        // The last columns and rows, value by value.
+#pragma unroll
+        for (int u = 0; u < kU; ++u)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            if (gr[u] >= M || gc[u] + k >= cols) continue;
+            float x = v[u][k], y = w[u][k];
+            if (e.bias[0]) x += e.bias[0][gc[u] + k];
+            if (e.bias[1]) y += e.bias[1][gc[u] + k];
+            if (e.z[0]) {
+              e.z[0][static_cast<int64_t>(gr[u]) * e.ldz[0] + gc[u] + k] = x;
+              e.z[1][static_cast<int64_t>(gr[u]) * e.ldz[1] + gc[u] + k] = y;
+            }
+            Y[static_cast<int64_t>(gr[u]) * ldy + gc[u] + k] = activate(e.activation, x) * y;
+          }
+        continue;
+      }
+      if (e.bias[0]) {
+#pragma unroll
+        for (int u = 0; u < kU; ++u) v[u] += load_any(e.bias[0] + gc[u]);
+      }
+      if (e.bias[1]) {
+#pragma unroll
+        for (int u = 0; u < kU; ++u) w[u] += load_any(e.bias[1] + gc[u]);
+      }
+      if (e.z[0]) {
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+          store_any(e.z[0] + static_cast<int64_t>(gr[u]) * e.ldz[0] + gc[u], v[u]);
+          store_any(e.z[1] + static_cast<int64_t>(gr[u]) * e.ldz[1] + gc[u], w[u]);
+        }
+      }
+      activate_all(e.activation, v);
+#pragma unroll
+      for (int u = 0; u < kU; ++u)
+        store_any(Y + static_cast<int64_t>(gr[u]) * ldy + gc[u], v[u] * w[u]);
     }
   });
 }

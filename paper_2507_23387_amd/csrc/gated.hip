@@ -1,10 +1,14 @@
 // The gated linear layer and its gradients (gfx950):
 //   G = X Wg + bg, U = X Wu + bu, Y = act(G) U;
-//   dU = dY act(G), dG = dY U act'(G), and the gradients of two linear layers.
+//   dU = dY act(G), dG = dY U act'(G), dX = dG Wg^T + dU Wu^T, dW = X^T dG and X^T dU.
+//
+// Forward: one product onto the columns of both weights, 8 of each in turn, whose epilogue
+// has an entry of G and the same of U in one lane.  Backward: [dG | dU] is formed once, as
+// one matrix D that gives dX in one product with a k of both halves.
 #include <algorithm>
 
 #include "activation.h"
-#include "layers.h"
+#include "linear_plan.h"
 
 namespace sgc {
 namespace {
@@ -26,38 +30,35 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(CombineArgs a) {
     a.y[i * a.ldy + j] = activate(a.activation, a.g[i * a.ldg + j]) * a.u[i * a.ldu + j];
 }
 
-__global__ __launch_bounds__(kThreads) void gate_grad_kernel(GatedGradArgs a, float* dg, float* du) {
-  const int64_t j = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-  if (j >= a.N) return;
-  for (int64_t i = blockIdx.y; i < a.M; i += gridDim.y) {
-    const float dy = a.dy[i * a.lddy + j], g = a.z[0][i * a.ldz[0] + j];
-    const float u = a.z[1][i * a.ldz[1] + j];
-    dg[i * a.N + j] = dy * u * activate_grad(a.activation, g);
-    du[i * a.N + j] = dy * activate(a.activation, g);
-  }
+// Whether G and U are two linear layers' results: few rows, few columns, and no k.
+bool gated_apart(int64_t M, int64_t N, int64_t K) {
+  return K == 0 || linear_by_rows(M, N) || linear_by_columns(M, 2 * N);
 }
 
-dim3 grid_of(int64_t M, int64_t N) {
-  return dim3(static_cast<unsigned>((N + kThreads - 1) / kThreads),
-              static_cast<unsigned>(std::min<int64_t>(M, 65535)));
+// Columns of the product of both weights.
+int64_t pair_cols(int64_t N) { return 2 * round_up(N, 8); }
+
+struct ApartWorkspace {
+  float* z[2];
+  void* linear;
+  size_t bytes;
+};
+
+ApartWorkspace carve_apart(void* ws, int64_t M, int64_t N, int64_t K) {
+  Carver c{static_cast<char*>(ws), 0};
+  ApartWorkspace w{};
+  for (float*& z : w.z) z = c.take<float>(M * N);
+  w.linear = c.take<char>(static_cast<int64_t>(linear_ws(M, N, K)));
+  w.bytes = c.used;
+  return w;
 }
 
-int64_t matrix_bytes(int64_t M, int64_t N) { return round_up(4 * M * N, 256); }
-
-}  // namespace
-
-size_t gated_ws(int64_t M, int64_t N, int64_t K) {
-  if (M == 0 || N == 0) return 0;
-  return static_cast<size_t>(2 * matrix_bytes(M, N)) + linear_ws(M, N, K);
-}
-
-hipError_t launch_gated(const GatedArgs& a, void* ws, hipStream_t stream) {
-  char* const base = static_cast<char*>(ws);
-  void* const linear = base + 2 * matrix_bytes(a.M, a.N);
+hipError_t launch_gated_apart(const GatedArgs& a, void* ws, hipStream_t stream) {
+  const ApartWorkspace w = carve_apart(ws, a.M, a.N, a.K);
   float* z[2];
   int64_t ldz[2];
   for (int i = 0; i < 2; ++i) {
-    z[i] = a.z[i] ? a.z[i] : reinterpret_cast<float*>(base + i * matrix_bytes(a.M, a.N));
+    z[i] = a.z[i] ? a.z[i] : w.z[i];
     ldz[i] = a.z[i] ? a.ldz[i] : a.N;
     LinearArgs l{};
     l.M = a.M, l.N = a.N, l.K = a.K;
@@ -66,42 +67,197 @@ hipError_t launch_gated(const GatedArgs& a, void* ws, hipStream_t stream) {
     l.e.bias = a.bias[i];
     l.y = z[i], l.ldy = ldz[i];
     l.scale = a.scale, l.variant = a.variant;
-    const hipError_t err = launch_linear(l, linear, stream);
+    const hipError_t err = launch_linear(l, w.linear, stream);
     if (err != hipSuccess) return err;
   }
   const CombineArgs c{a.M, a.N, a.activation, z[0], z[1], ldz[0], ldz[1], a.y, a.ldy};
-  hipLaunchKernelGGL(combine_kernel, grid_of(a.M, a.N), dim3(kThreads), 0, stream, c);
+  const dim3 grid(static_cast<unsigned>((a.N + kThreads - 1) / kThreads),
+                  static_cast<unsigned>(std::min<int64_t>(a.M, 65535)));
+  hipLaunchKernelGGL(combine_kernel, grid, dim3(kThreads), 0, stream, c);
   return hipGetLastError();
 }
 
+}  // namespace
+
+size_t gated_ws(int64_t M, int64_t N, int64_t K) {
+  if (M == 0 || N == 0) return 0;
+  if (gated_apart(M, N, K)) return carve_apart(nullptr, M, N, K).bytes;
+  Carver c{nullptr, 0};
+  (void)carve_planes(c, M, pair_cols(N), K);
+  return c.used;
+}
+
+hipError_t launch_gated(const GatedArgs& a, void* ws, hipStream_t stream) {
+  if (gated_apart(a.M, a.N, a.K)) return launch_gated_apart(a, ws, stream);
+  Carver c{static_cast<char*>(ws), 0};
+  const Planes p = carve_planes(c, a.M, pair_cols(a.N), a.K);
+  SplitJob jobs[3];
+  for (int i = 0; i < 2; ++i) {
+    jobs[i] = a.transpose_w ? job_of(a.w[i], a.ldw[i], a.N, a.K)
+                            : job_of(a.w[i], a.ldw[i], a.K, a.N);
+    to_planes(jobs[i], p, true, !a.transpose_w);
+    jobs[i].pair = i + 1;
+  }
+  // Both write the words of one operand.
+  jobs[1].row_stamp = jobs[0].row_stamp, jobs[1].col_stamp = jobs[0].col_stamp;
+  jobs[2] = job_of(a.x, a.ldx, a.M, a.K);
+  to_planes(jobs[2], p, false, false);
+  const hipError_t err = launch_split_jobs(jobs, 3, a.scale, stream);
+  if (err != hipSuccess) return err;
+  const GateEpilogue e{{a.bias[0], a.bias[1]}, a.activation, a.N, {a.z[0], a.z[1]},
+                       {a.ldz[0], a.ldz[1]}};
+  return launch_gemm_epilogue(p, a.M, pair_cols(a.N), a.y, a.ldy, a.scale, a.variant, e, false,
+                              stream);
+}
+
+namespace {
+
+struct GradWorkspace {
+  int64_t half;  // columns of D to each of dG and dU
+  float *d, *row_top, *col_top, *sums;
+  int *row_shift, *col_shift;
+  void* linear;  // the gradients' of one weight, where they go apart
+  Planes dx, dw;
+  size_t bytes;
+};
+
+// Whether each weight's gradients are a linear layer's.
+bool grad_apart(int64_t M, int64_t N, int64_t K) { return linear_grad_by_rows(M, N, K) || K == 0; }
+
+GradWorkspace carve_grad(void* ws, int64_t M, int64_t N, int64_t K, bool transpose_w) {
+  Carver c{static_cast<char*>(ws), 0};
+  GradWorkspace w{};
+  w.half = round_up(N, kColumnStrip);
+  w.d = c.take<float>(M * 2 * w.half);
+  if (grad_apart(M, N, K)) {
+    w.linear = c.take<char>(static_cast<int64_t>(linear_grad_ws(M, N, K)));
+  } else {
+    const int64_t slabs = column_slabs(M, w.half);
+    w.row_top = c.take<float>(row_pieces(2 * w.half) * M);
+    w.col_top = c.take<float>(slabs * 2 * w.half);
+    w.sums = c.take<float>(slabs * 2 * w.half);
+    w.row_shift = c.take<int>(round_up(M, kKPad));
+    w.col_shift = c.take<int>(2 * w.half);
+    w.dx = carve_planes(c, M, K, 2 * w.half);
+    // The second half's tiles of 256 may reach a panel past D's columns.
+    const int64_t lines = 2 * w.half + kPanel;
+    w.dw = transpose_w ? carve_planes(c, lines, K, M) : carve_planes(c, K, lines, M);
+  }
+  w.bytes = c.used;
+  return w;
+}
+
+// dW of one half of D.
+GroupProduct weight_product(const GatedGradArgs& a, const GradWorkspace& w, int i) {
+  GroupProduct g{};
+  g.p = w.dw;
+  g.M = a.transpose_w ? a.N : a.K;
+  g.N = a.transpose_w ? a.K : a.N;
+  g.K = a.M;
+  const int64_t skip = i * w.half * g.p.Kp;
+  if (a.transpose_w)
+    g.p.a_hi += skip, g.p.a_lo += skip, g.p.Mp = round_up(a.N, kRowPad);
+  else
+    g.p.b_hi += skip, g.p.b_lo += skip, g.p.Np = round_up(a.N, kRowPad);
+  g.C = a.dw[i], g.ldc = a.lddw[i];
+  g.epi = Unscale{w.col_shift + i * w.half, !a.transpose_w, false};
+  return g;
+}
+
+}  // namespace
+
 size_t gated_grad_ws(int64_t M, int64_t N, int64_t K) {
   if (M == 0 || N == 0) return 0;
-  return static_cast<size_t>(2 * matrix_bytes(M, N)) + linear_grad_ws(M, N, K);
+  return std::max(carve_grad(nullptr, M, N, K, false).bytes,
+                  carve_grad(nullptr, M, N, K, true).bytes);
 }
 
 hipError_t launch_gated_grad(const GatedGradArgs& a, void* ws, hipStream_t stream) {
-  char* const base = static_cast<char*>(ws);
-  float* d[2] = {reinterpret_cast<float*>(base),
-                 reinterpret_cast<float*>(base + matrix_bytes(a.M, a.N))};
-  if (a.M > 0 && a.N > 0) {
-    hipLaunchKernelGGL(gate_grad_kernel, grid_of(a.M, a.N), dim3(kThreads), 0, stream, a, d[0],
-                       d[1]);
-    const hipError_t err = hipGetLastError();
-    if (err != hipSuccess) return err;
+  const bool empty = a.M == 0 || a.N == 0, apart = empty || grad_apart(a.M, a.N, a.K);
+  GradWorkspace w{};
+  hipError_t err = hipSuccess;
+  if (!empty) {
+    w = carve_grad(ws, a.M, a.N, a.K, a.transpose_w);
+    // (Sums and magnitudes are wanted below, or again from D's halves.)
+    const GateColumnArgs d{a.M, a.N, w.half, a.dy, a.lddy, a.z[0], a.ldz[0], a.z[1], a.ldz[1],
+                           a.activation, a.dx ? w.row_top : nullptr,
+                           a.dw[0] || a.dw[1] ? w.col_top : nullptr, w.sums, w.d};
+    err = launch_gate_columns(d, stream);
   }
-  for (int i = 0; i < 2; ++i) {
-    LinearGradArgs l{};
-    l.M = a.M, l.N = a.N, l.K = a.K;
-    l.dy = d[i], l.lddy = a.N;
-    l.x = a.x, l.ldx = a.ldx;
-    l.w = a.w[i], l.ldw = a.ldw[i], l.transpose_w = a.transpose_w;
-    l.dx = a.dx, l.lddx = a.lddx, l.add_dx = i > 0;
-    l.dw = a.dw[i], l.lddw = a.lddw[i], l.dbias = a.dbias[i];
-    l.scale = a.scale, l.variant = a.variant;
-    const hipError_t err = launch_linear_grad(l, base + 2 * matrix_bytes(a.M, a.N), stream);
-    if (err != hipSuccess) return err;
+  if (apart) {
+    for (int i = 0; i < 2 && err == hipSuccess; ++i) {
+      LinearGradArgs l{};
+      l.M = a.M, l.N = a.N, l.K = a.K;
+      l.dy = empty ? nullptr : w.d + i * w.half, l.lddy = 2 * w.half;
+      l.x = a.x, l.ldx = a.ldx;
+      l.w = a.w[i], l.ldw = a.ldw[i], l.transpose_w = a.transpose_w;
+      l.dx = a.dx, l.lddx = a.lddx, l.add_dx = i > 0;
+      l.dw = a.dw[i], l.lddw = a.lddw[i], l.dbias = a.dbias[i];
+      l.scale = a.scale, l.variant = a.variant;
+      err = launch_linear_grad(l, w.linear, stream);
+    }
+    return err;
   }
-  return hipSuccess;
+  if (err != hipSuccess) return err;
+  const bool weights = a.dw[0] || a.dw[1];
+  ColumnJoin join{};
+  join.M = a.M, join.N = 2 * w.half;
+  join.pieces = static_cast<int>(row_pieces(2 * w.half));
+  join.slabs = static_cast<int>(column_slabs(a.M, w.half));
+  join.row_top = w.row_top, join.col_top = w.col_top, join.sums = w.sums;
+  join.row_target = target_a(a.scale);
+  join.col_target = a.transpose_w ? target_a(a.scale) : target_b(a.scale, a.variant);
+  join.row_shift = a.dx ? w.row_shift : nullptr;
+  join.col_shift = weights ? w.col_shift : nullptr;
+  join.dbias = a.dbias[0], join.dbias_second = a.dbias[1];
+  join.half = w.half, join.cols = a.N;
+
+  SplitJob jobs[kSplitJobs];
+  int count = 0;
+  SplitJob d = job_of(w.d, 2 * w.half, a.M, 2 * w.half);
+  if (a.dx) {
+    // dX: D's rows and both weights' K rows, k over dG's columns and then dU's.
+    d.row_shift = w.row_shift;
+    to_planes(d, w.dx, false, false);
+    for (int i = 0; i < 2; ++i) {
+      SplitJob& j = jobs[count++];
+      j = a.transpose_w ? job_of(a.w[i], a.ldw[i], a.N, a.K) : job_of(a.w[i], a.ldw[i], a.K, a.N);
+      to_planes(j, w.dx, true, a.transpose_w);
+      j.k0 = i * w.half, j.kp = 2 * w.half;
+    }
+    jobs[1].row_stamp = jobs[0].row_stamp, jobs[1].col_stamp = jobs[0].col_stamp;
+  }
+  if (weights) {
+    // Both dW: columns of X and of D, k over M.
+    d.col_shift = w.col_shift;
+    to_planes(d, w.dw, !a.transpose_w, true);
+    jobs[count] = job_of(a.x, a.ldx, a.M, a.K);
+    to_planes(jobs[count++], w.dw, a.transpose_w, true);
+  }
+  if (count > 0) jobs[count++] = d;
+  const bool split_joins = count > 0 && split_jobs_blocks(jobs, count) <= kSplitJoinBlocks;
+  if (!split_joins) err = launch_columns_join(join, stream);
+  if (err == hipSuccess && count > 0)
+    err = launch_split_jobs(jobs, count, a.scale, stream, split_joins ? &join : nullptr);
+
+  GroupProduct list[kGroupProducts];
+  count = 0;
+  if (a.dx)
+    list[count++] = GroupProduct{w.dx, a.M, a.K, 2 * w.half, a.dx, a.lddx,
+                                 Unscale{w.row_shift, false, false}};
+  for (int i = 0; i < 2; ++i)
+    if (a.dw[i]) list[count++] = weight_product(a, w, i);
+  if (err == hipSuccess && count > 1) {
+    if (const int tile = group_gemm_tile(list, count, a.variant, !scaled_kernel_ok(a.scale)))
+      return launch_gemm_group(tile, list, count, a.scale, a.variant, stream);
+  }
+  for (int i = 0; i < count && err == hipSuccess; ++i) {
+    // As B, D never asks for the fallback (launch_linear_grad).
+    const GroupProduct& g = list[i];
+    err = launch_gemm_epilogue(g.p, g.M, g.N, g.C, g.ldc, a.scale, a.variant, g.epi,
+                               g.epi.columns, stream);
+  }
+  return err;
 }
 
 }  // namespace sgc

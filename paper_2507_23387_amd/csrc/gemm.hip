@@ -1224,6 +1224,9 @@ hipError_t launch_gemm_fused_a_epilogue(const Planes& p, int64_t M, int64_t N, i
 template hipError_t launch_gemm_epilogue<Epilogue>(const Planes&, int64_t, int64_t, float*,
                                                    int64_t, float, int, const Epilogue&, bool,
                                                    hipStream_t);
+template hipError_t launch_gemm_epilogue<GateEpilogue>(const Planes&, int64_t, int64_t, float*,
+                                                       int64_t, float, int, const GateEpilogue&,
+                                                       bool, hipStream_t);
 template hipError_t launch_gemm_epilogue<Unscale>(const Planes&, int64_t, int64_t, float*, int64_t,
                                                   float, int, const Unscale&, bool, hipStream_t);
 

@@ -377,20 +377,22 @@ __global__ __launch_bounds__(64 * kWM * kWN, 1) void linear_small_kernel(SmallAr
   small_body<V, SmallShape<kBM, kBN, kWM, kWN, kStages, false>>(g, unscaled_only, epi, blockIdx.x);
 }
 
-// Two products in one launch (a layer's two gradients), the first `first`
-// workgroups on the one.  Alone, neither fills the GPU for long: 777 x 530 x 1003 and
+// Several products in one launch (a layer's gradients), workgroups first[i - 1] ..
+// first[i] - 1 on the i-th.  Alone, none fills the GPU for long: 777 x 530 x 1003 and
 // 1003 x 530 x 777 took 11 and 14 us, and a launch between.  The arguments are an
 // array, so that a scalar index into it keeps them in scalar registers.
-struct PairArgs {
-  SmallArgs g[2];
-  Unscale e[2];
-  int first, unscaled_only;
+struct GroupArgs {
+  SmallArgs g[kGroupProducts];
+  Unscale e[kGroupProducts];
+  int first[kGroupProducts];
+  int unscaled_only;
 };
 template <int V, int kBM, int kBN, int kWM, int kWN, int kStages>
-__global__ __launch_bounds__(64 * kWM * kWN, 1) void linear_pair_kernel(PairArgs a) {
+__global__ __launch_bounds__(64 * kWM * kWN, 1) void linear_group_kernel(GroupArgs a) {
   using S = SmallShape<kBM, kBN, kWM, kWN, kStages, false>;
-  const int i = static_cast<int>(blockIdx.x) >= a.first ? 1 : 0;
-  small_body<V, S>(a.g[i], a.unscaled_only, a.e[i], blockIdx.x - (i ? a.first : 0));
+  const int b = static_cast<int>(blockIdx.x);
+  const int i = b >= a.first[1] ? 2 : b >= a.first[0] ? 1 : 0;
+  small_body<V, S>(a.g[i], a.unscaled_only, a.e[i], b - (i ? a.first[i - 1] : 0));
 }
 
 // The unscaled body alone, on 256 x 128 tiles: the fallback of the 256-wide
@@ -547,29 +549,31 @@ hipError_t launch_config_epilogue(int tile, const Planes& p, int64_t M, int64_t 
 }
 
 template <int V>
-hipError_t launch_config_pair(int tile, const Planes (&p)[2], const int64_t (&M)[2],
-                              const int64_t (&N)[2], float* const (&C)[2],
-                              const int64_t (&ldc)[2], float s, const Unscale (&epi)[2],
-                              hipStream_t stream) {
+hipError_t launch_config_group(int tile, const GroupProduct* list, int count, float s,
+                               hipStream_t stream) {
   return with_config<V>(tile, [&](auto c) {
     using T = decltype(c);
     if constexpr (T::kBM > 128) {
-      return hipErrorInvalidValue;  // pair_gemm_tile offers none
+      return hipErrorInvalidValue;  // group_gemm_tile offers none
     } else {
       using S = SmallShape<T::kBM, T::kBN, T::kWM, T::kWN, T::kStages, false>;
       static std::atomic<bool> done[kMaxDevices];
-      constexpr auto kernel = &linear_pair_kernel<V, T::kBM, T::kBN, T::kWM, T::kWN, T::kStages>;
+      constexpr auto kernel = &linear_group_kernel<V, T::kBM, T::kBN, T::kWM, T::kWN, T::kStages>;
       const hipError_t attr = set_lds(kernel, S::kLdsBytes, done);
       if (attr != hipSuccess) return attr;
-      PairArgs a;
-      for (int i = 0; i < 2; ++i) {
-        a.g[i] = small_args<S>(p[i], M[i], N[i], C[i], ldc[i], s, RangeOpts{}, nullptr);
-        a.e[i] = epi[i];
+      GroupArgs a{};
+      int blocks = 0;
+      for (int i = 0; i < kGroupProducts; ++i) {
+        if (i < count) {
+          const GroupProduct& g = list[i];
+          a.g[i] = small_args<S>(g.p, g.M, g.N, g.C, g.ldc, s, RangeOpts{}, nullptr);
+          a.e[i] = g.epi;
+          blocks += a.g[i].tiles_m * a.g[i].tiles_n;
+        }
+        a.first[i] = blocks;
       }
-      a.first = a.g[0].tiles_m * a.g[0].tiles_n;
       a.unscaled_only = scaled_kernel_ok(s) ? 0 : 1;
-      hipLaunchKernelGGL(kernel, dim3(a.first + a.g[1].tiles_m * a.g[1].tiles_n),
-                         dim3(S::kThreads), S::kLdsBytes, stream, a);
+      hipLaunchKernelGGL(kernel, dim3(blocks), dim3(S::kThreads), S::kLdsBytes, stream, a);
       return hipGetLastError();
     }
   });
@@ -686,48 +690,48 @@ int small_gemm_tile(int64_t M, int64_t N, int64_t K, int variant, bool unscaled,
   return tile;
 }
 
-int pair_gemm_tile(const int64_t (&M)[2], const int64_t (&N)[2], const int64_t (&K)[2],
-                   int variant, bool unscaled) {
+int group_gemm_tile(const GroupProduct* list, int count, int variant, bool unscaled) {
   const int row = unscaled && variant == kElementwise ? 4 : variant;
   auto side_cost = [&](int side) -> const GridCost& {
     return side == 32 ? k32[row] : side == 64 ? k64[row] : side == 128 ? k128[row] : k192[row];
   };
   auto together = [](int side) { return side <= 64 ? 512 : 256; };
-  auto tiles = [&](int i, int side) {
-    return ((M[i] + side - 1) / side) * ((N[i] + side - 1) / side);
+  auto tiles = [&](const GroupProduct& g, int side) {
+    return ((g.M + side - 1) / side) * ((g.N + side - 1) / side);
   };
-  int64_t steps[2];
+  auto steps = [](const GroupProduct& g) { return round_up(g.K, kKPad) / kSmallStep; };
   double apart = 0.0;
-  for (int i = 0; i < 2; ++i) {
-    steps[i] = round_up(K[i], kKPad) / kSmallStep;
-    const int side = small_gemm_tile(M[i], N[i], K[i], variant, unscaled);
+  int64_t longest = 0;
+  for (int i = 0; i < count; ++i) {
+    const GroupProduct& g = list[i];
+    const int side = small_gemm_tile(g.M, g.N, g.K, variant, unscaled);
     if (side == 0) return 0;
-    apart += grid_time(side_cost(side), tiles(i, side), together(side), steps[i]);
+    apart += grid_time(side_cost(side), tiles(g, side), together(side), steps(g));
+    longest = std::max(longest, steps(g));
   }
   int best = 0;
   for (int side : {32, 64, 128}) {
     const GridCost& c = side_cost(side);
-    const int64_t t0 = tiles(0, side), t1 = tiles(1, side);
-    if ((t0 + t1) * small_tile_threads(side, variant) > UINT32_MAX) continue;
-    const int64_t rounds = (t0 + t1 + together(side) - 1) / together(side);
-    const double us = c.launch + rounds * (c.start + std::max(steps[0], steps[1]) * c.round) +
-                      c.tile * (t0 * steps[0] + t1 * steps[1]) / 256;
+    int64_t all = 0;
+    double work = 0.0;
+    for (int i = 0; i < count; ++i) {
+      all += tiles(list[i], side);
+      work += static_cast<double>(tiles(list[i], side) * steps(list[i]));
+    }
+    if (all * small_tile_threads(side, variant) > UINT32_MAX) continue;
+    const int64_t rounds = (all + together(side) - 1) / together(side);
+    const double us = c.launch + rounds * (c.start + longest * c.round) + c.tile * work / 256;
     if (us < apart) apart = us, best = side;
   }
   return best;
 }
 
-hipError_t launch_gemm_pair(int tile, const Planes (&p)[2], const int64_t (&M)[2],
-                            const int64_t (&N)[2], float* const (&C)[2], const int64_t (&ldc)[2],
-                            float scale, int variant, const Unscale (&epi)[2],
-                            hipStream_t stream) {
+hipError_t launch_gemm_group(int tile, const GroupProduct* list, int count, float scale,
+                             int variant, hipStream_t stream) {
   switch (variant) {
-    case kElementwise:
-      return launch_config_pair<kElementwise>(tile, p, M, N, C, ldc, scale, epi, stream);
-    case kTermwise:
-      return launch_config_pair<kTermwise>(tile, p, M, N, C, ldc, scale, epi, stream);
-    case kCrossFirst:
-      return launch_config_pair<kCrossFirst>(tile, p, M, N, C, ldc, scale, epi, stream);
+    case kElementwise: return launch_config_group<kElementwise>(tile, list, count, scale, stream);
+    case kTermwise: return launch_config_group<kTermwise>(tile, list, count, scale, stream);
+    case kCrossFirst: return launch_config_group<kCrossFirst>(tile, list, count, scale, stream);
     default: return hipErrorInvalidValue;
   }
 }
@@ -792,6 +796,12 @@ template hipError_t launch_gemm_small_epilogue<Epilogue>(int, const Planes&, int
 template hipError_t launch_gemm_small_epilogue<Unscale>(int, const Planes&, int64_t, int64_t,
                                                         float*, int64_t, float, int,
                                                         const Unscale&, hipStream_t);
+template hipError_t launch_gemm_small_epilogue<GateEpilogue>(int, const Planes&, int64_t, int64_t,
+                                                             float*, int64_t, float, int,
+                                                             const GateEpilogue&, hipStream_t);
+template hipError_t launch_gemm_unscaled_epilogue<GateEpilogue>(const Planes&, int64_t, int64_t,
+                                                                float*, int64_t, float, int, bool,
+                                                                const GateEpilogue&, hipStream_t);
 template hipError_t launch_gemm_unscaled_epilogue<Epilogue>(const Planes&, int64_t, int64_t, float*,
                                                             int64_t, float, int, bool,
                                                             const Epilogue&, hipStream_t);

@@ -37,8 +37,18 @@ struct SplitJob {
   uint32_t* row_range;
   uint32_t* col_range;
   uint32_t row_stamp, col_stamp;
+  // A gated layer's weights.  pair 1 or 2: the planes hold the lines of two matrices, 8 of
+  // the first and 8 of the second in turn, and these are the first's or the second's.
+  // kp > 0: the planes' k is that of two matrices, kp in all, and this one's begins at k0
+  // and goes on to k0 + kp / 2 (zeros past its end).
+  int pair;
+  int64_t k0, kp;
 };
-constexpr int kSplitJobs = 3;
+constexpr int kSplitJobs = 4;
+// The plane row of line r of such a matrix.
+__host__ __device__ inline int64_t pair_row(int64_t r, int pair) {
+  return pair ? r / 8 * 16 + r % 8 + 8 * (pair - 1) : r;
+}
 // The join of what launch_columns left: for each of D's M rows and N columns the
 // shift that brings its largest finite magnitude to 2^target (prescale_shift), and
 // the sums of the columns.  Null: not wanted.  A split launch can do it on the way:
@@ -54,6 +64,10 @@ struct ColumnJoin {
   int* row_shift;
   int* col_shift;
   float* dbias;
+  // half > 0: D is two matrices of `cols` columns side by side, the second from column
+  // `half` on, whose sums go to dbias_second.
+  int64_t half, cols;
+  float* dbias_second;
 };
 hipError_t launch_split_jobs(const SplitJob* jobs, int count, float scale, hipStream_t stream,
                              const ColumnJoin* join = nullptr);
@@ -80,6 +94,24 @@ struct ColumnArgs {
   float* d;  // null, or M x N that receives D
 };
 hipError_t launch_columns(const ColumnArgs& a, hipStream_t stream);
+// The same for a gated layer: D = [dY U act'(G) | dY act(G)], M x 2 half, half = N rounded
+// up to kColumnStrip and zeros in between, is written; row_top, col_top and sums (null: not
+// wanted) are D's.
+struct GateColumnArgs {
+  int64_t M, N, half;
+  const float* dy;
+  int64_t lddy;
+  const float* g;
+  int64_t ldg;
+  const float* u;
+  int64_t ldu;
+  int activation;
+  float* row_top;
+  float* col_top;
+  float* sums;
+  float* d;
+};
+hipError_t launch_gate_columns(const GateColumnArgs& a, hipStream_t stream);
 hipError_t launch_columns_join(const ColumnJoin& j, hipStream_t stream);
 
 // What follows a product P: Y = act(Z) + R, Z = P + bias.
@@ -97,6 +129,15 @@ struct Unscale {
   const int* shift;
   bool columns;
   bool add;
+};
+// A gated layer's product: columns 16 b + c of P (c < 8) are columns 8 b + c of G, those
+// 16 b + 8 + c of U.  Y = act(G + bias[0]) (U + bias[1]).
+struct GateEpilogue {
+  const float* bias[2];  // null: none
+  int activation;
+  int64_t N;    // of Y
+  float* z[2];  // G and U with their biases; null: not kept
+  int64_t ldz[2];
 };
 // The epilogue where K = 0: P = 0.
 hipError_t launch_epilogue(const Epilogue& e, int64_t M, int64_t N, float* Y, int64_t ldy,
@@ -125,14 +166,19 @@ hipError_t launch_gemm_fused_a_epilogue(const Planes& p, int64_t M, int64_t N, i
                                         float scale, int variant, const Epilogue& epi,
                                         hipStream_t stream);
 
-// Two gradients' products in one launch, on tiles of 32, 64 or 128.
-// pair_gemm_tile: the tile where that takes less time than two launches, or 0.
-int pair_gemm_tile(const int64_t (&M)[2], const int64_t (&N)[2], const int64_t (&K)[2],
-                   int variant, bool unscaled);
-hipError_t launch_gemm_pair(int tile, const Planes (&p)[2], const int64_t (&M)[2],
-                            const int64_t (&N)[2], float* const (&C)[2], const int64_t (&ldc)[2],
-                            float scale, int variant, const Unscale (&epi)[2],
-                            hipStream_t stream);
+// Several gradients' products in one launch, on tiles of 32, 64 or 128.
+// group_gemm_tile: the tile where that takes less time than a launch each, or 0.
+constexpr int kGroupProducts = 3;
+struct GroupProduct {
+  Planes p;
+  int64_t M, N, K;
+  float* C;
+  int64_t ldc;
+  Unscale epi;
+};
+int group_gemm_tile(const GroupProduct* list, int count, int variant, bool unscaled);
+hipError_t launch_gemm_group(int tile, const GroupProduct* list, int count, float scale,
+                             int variant, hipStream_t stream);
 
 struct LinearArgs {
   int64_t M, N, K;
@@ -201,6 +247,8 @@ struct LinearGradArgs {
   int variant;
   bool add_dx = false;  // dX is added to what dx holds
 };
+// Whether dX is formed by rows (linear.hip has the rule).
+bool linear_grad_by_rows(int64_t M, int64_t N, int64_t K);
 size_t linear_grad_ws(int64_t M, int64_t N, int64_t K);
 hipError_t launch_linear_grad(const LinearGradArgs& a, void* ws, hipStream_t stream);
 

@@ -76,7 +76,7 @@ bool valid_ids(const void* p, int bits, int64_t n) {
 // Limits of the embedding's kernels.
 bool embedding_exceeds(int64_t n, int64_t vocab, int64_t cols) {
   constexpr int64_t kMost = int64_t{1} << 28;
-  return n > kMost || vocab > kMost || cols > kMost;
+  return n > kMost / 2 || vocab > kMost || cols > kMost;
 }
 
 // Limits of a product and its gradients.

@@ -1,75 +1,9 @@
 // The linear layer and its gradients: workspace, operands and launches.
 #include <algorithm>
-#include <cmath>
 
-#include "layers.h"
+#include "linear_plan.h"
 
 namespace sgc {
-namespace {
-
-// One product's planes, carved from a workspace: a_rows x k and b_rows x k.
-struct Carver {
-  char* base;
-  size_t used;
-  template <typename T>
-  T* take(int64_t count) {
-    char* const at = base + used;
-    used += static_cast<size_t>(round_up(count * static_cast<int64_t>(sizeof(T)), 256));
-    return reinterpret_cast<T*>(at);
-  }
-};
-
-Planes carve_planes(Carver& c, int64_t M, int64_t N, int64_t K) {
-  Planes p{};
-  p.Mp = round_up(M, kRowPad);
-  p.Np = round_up(N, kRowPad);
-  p.Kp = round_up(K, kKPad);
-  p.range = c.take<uint32_t>(kFlagBytes / 4);
-  p.a_hi = c.take<uint16_t>(p.Mp * p.Kp);
-  p.a_lo = c.take<uint16_t>(p.Mp * p.Kp);
-  p.b_hi = c.take<uint16_t>(p.Np * p.Kp);
-  p.b_lo = c.take<uint16_t>(p.Np * p.Kp);
-  return p;
-}
-
-SplitJob job_of(const float* s, int64_t ld, int64_t rows, int64_t cols) {
-  SplitJob j{};
-  j.s = s;
-  j.ld = ld;
-  j.rows = rows;
-  j.cols = cols;
-  return j;
-}
-
-// Adds planes to a job: the A or the B side of p, from its rows or its columns.
-void to_planes(SplitJob& j, const Planes& p, bool side_b, bool columns) {
-  uint16_t* const hi = side_b ? p.b_hi : p.a_hi;
-  uint16_t* const lo = side_b ? p.b_lo : p.a_lo;
-  if (columns) {
-    j.col_hi = hi, j.col_lo = lo;
-    if (side_b) j.col_range = p.range, j.col_stamp = next_stamp();
-  } else {
-    j.row_hi = hi, j.row_lo = lo;
-    if (side_b) j.row_range = p.range, j.row_stamp = next_stamp();
-  }
-}
-
-// Most tiles of a split that also joins what the pass over D left: each of D's tiles
-// then joins its own lines' magnitudes, 2 us and more where they are many, instead of
-// a launch between (us, so and with it: 256 x 1024 x 1024 27.9 and 28.9, 777 x 1003 x 530
-// 30.8 and 32.7, 4096 x 256 x 256 39.8 and 41.6, 1024 x 1024 x 512 30.3 and 30.6; of more
-// tiles 2048 x 1024 x 1024 56.1 and 55.4, 2048 x 2560 x 512 79.5 and 73.0).
-constexpr int64_t kSplitJoinBlocks = 1024;
-
-// Target exponents of a pre-scaled operand (api.hip's range_opts): as A, and as
-// B, where the scaled kernels form s B_hi in FP16.
-int target_a(float scale) { return std::min(14, 26 - std::ilogb(scale)); }
-int target_b(float scale, int variant) {
-  return variant == kTermwise || !scaled_kernel_ok(scale) ? target_a(scale)
-                                                          : 14 - std::ilogb(scale);
-}
-
-}  // namespace
 
 // Few rows: every 64 rows read W once more, as FP32, where the tiles read it,
 // write its planes and read those for every 32 to 256 rows.  On N, K = 256 .. 8192,
@@ -120,8 +54,6 @@ hipError_t launch_linear(const LinearArgs& a, void* ws, hipStream_t stream) {
                               stream);
 }
 
-namespace {
-
 // Whether dX = D W^T (M x K, k over N) goes by rows.  D is then written as FP32 by
 // the kernel that sums its columns, where an activation makes it other than dY.  A
 // small W is split with the rest instead, and both products take one launch (us,
@@ -130,14 +62,16 @@ namespace {
 // for few tiles takes longer still, while rows share it (N x K, 1 and 128 rows: 2048 x
 // 512 25 and 27 against 27 and 29, 3000 x 128 25 and 27 against 23 and 25, 4096 x 128 28
 // against 32, 8192 x 64 28 and 31 against 45 and 48).
-bool grad_by_rows(int64_t M, int64_t N, int64_t K) {
+bool linear_grad_by_rows(int64_t M, int64_t N, int64_t K) {
   return M <= 128 && (N * K >= 1500000 || static_cast<double>(N) * N * K >= 1.6e9);
 }
+
+namespace {
 
 // Whether dW = X^T D is formed in FP32 from few rows, where dX needs no planes of D
 // either.
 bool grad_outer(int64_t M, int64_t N, int64_t K) {
-  return M <= kOuterRows && grad_by_rows(M, N, K);
+  return M <= kOuterRows && linear_grad_by_rows(M, N, K);
 }
 
 struct GradWorkspace {
@@ -159,7 +93,7 @@ GradWorkspace carve_grad(void* ws, int64_t M, int64_t N, int64_t K, bool transpo
   g.row_shift = c.take<int>(round_up(M, kKPad));
   g.col_shift = c.take<int>(round_up(N, kColumnStrip));
   if (K > 0) {
-    if (grad_by_rows(M, N, K)) {
+    if (linear_grad_by_rows(M, N, K)) {
       g.rows = c.take<char>(static_cast<int64_t>(linear_rows_ws(M, K, N)));
       g.d = c.take<float>(M * N);
     } else {
@@ -192,7 +126,7 @@ hipError_t launch_linear_grad(const LinearGradArgs& a, void* ws, hipStream_t str
   const GradWorkspace g = carve_grad(ws, a.M, a.N, a.K, a.transpose_w);
   const bool dx = a.dx && a.K > 0, outer = a.dw && a.K > 0 && grad_outer(a.M, a.N, a.K);
   const bool dw = a.dw && a.K > 0 && !outer;
-  const bool dx_rows = dx && grad_by_rows(a.M, a.N, a.K);
+  const bool dx_rows = dx && linear_grad_by_rows(a.M, a.N, a.K);
   // dX is scaled by rows, dW by columns: each of their entries sums one line of D, so
   // that a line far below the others keeps its digits.
   const ColumnArgs cols{a.M, a.N, a.dy, a.lddy, a.z, a.ldz, a.activation,
@@ -252,14 +186,10 @@ hipError_t launch_linear_grad(const LinearGradArgs& a, void* ws, hipStream_t str
     err = launch_linear_rows(r, g.row_shift, g.rows, stream, a.add_dx);
   } else if (err == hipSuccess && dx) {
     if (dw) {
-      const int64_t M[2] = {a.M, dw_rows}, N[2] = {a.K, dw_cols}, K[2] = {a.N, a.M};
-      if (const int tile = pair_gemm_tile(M, N, K, a.variant, !scaled_kernel_ok(a.scale))) {
-        const Planes p[2] = {g.dx, g.dw};
-        float* const C[2] = {a.dx, a.dw};
-        const int64_t ldc[2] = {a.lddx, a.lddw};
-        const Unscale epi[2] = {ex, ew};
-        return launch_gemm_pair(tile, p, M, N, C, ldc, a.scale, a.variant, epi, stream);
-      }
+      const GroupProduct both[2] = {{g.dx, a.M, a.K, a.N, a.dx, a.lddx, ex},
+                                    {g.dw, dw_rows, dw_cols, a.M, a.dw, a.lddw, ew}};
+      if (const int tile = group_gemm_tile(both, 2, a.variant, !scaled_kernel_ok(a.scale)))
+        return launch_gemm_group(tile, both, 2, a.scale, a.variant, stream);
     }
     err = launch_gemm_epilogue(g.dx, a.M, a.K, a.dx, a.lddx, a.scale, a.variant, ex, false,
                                stream);

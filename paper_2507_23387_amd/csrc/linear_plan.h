@@ -1,0 +1,77 @@
+// What the linear and the gated layer's workspaces, operands and launches share.
+// Internal; every function has internal linkage.
+#pragma once
+
+#include <algorithm>
+#include <cmath>
+
+#include "layers.h"
+
+namespace sgc {
+namespace {
+
+// Pieces of a workspace, in 256-byte units; from null only their sum.
+struct Carver {
+  char* base;
+  size_t used;
+  template <typename T>
+  T* take(int64_t count) {
+    char* const at = base + used;
+    used += static_cast<size_t>(round_up(count * static_cast<int64_t>(sizeof(T)), 256));
+    return reinterpret_cast<T*>(at);
+  }
+};
+
+// One product's planes, carved from a workspace: a_rows x k and b_rows x k.
+inline Planes carve_planes(Carver& c, int64_t M, int64_t N, int64_t K) {
+  Planes p{};
+  p.Mp = round_up(M, kRowPad);
+  p.Np = round_up(N, kRowPad);
+  p.Kp = round_up(K, kKPad);
+  p.range = c.take<uint32_t>(kFlagBytes / 4);
+  p.a_hi = c.take<uint16_t>(p.Mp * p.Kp);
+  p.a_lo = c.take<uint16_t>(p.Mp * p.Kp);
+  p.b_hi = c.take<uint16_t>(p.Np * p.Kp);
+  p.b_lo = c.take<uint16_t>(p.Np * p.Kp);
+  return p;
+}
+
+inline SplitJob job_of(const float* s, int64_t ld, int64_t rows, int64_t cols) {
+  SplitJob j{};
+  j.s = s;
+  j.ld = ld;
+  j.rows = rows;
+  j.cols = cols;
+  return j;
+}
+
+// Adds planes to a job: the A or the B side of p, from its rows or its columns.
+inline void to_planes(SplitJob& j, const Planes& p, bool side_b, bool columns) {
+  uint16_t* const hi = side_b ? p.b_hi : p.a_hi;
+  uint16_t* const lo = side_b ? p.b_lo : p.a_lo;
+  if (columns) {
+    j.col_hi = hi, j.col_lo = lo;
+    if (side_b) j.col_range = p.range, j.col_stamp = next_stamp();
+  } else {
+    j.row_hi = hi, j.row_lo = lo;
+    if (side_b) j.row_range = p.range, j.row_stamp = next_stamp();
+  }
+}
+
+// Most tiles of a split that also joins what the pass over D left: each of D's tiles
+// then joins its own lines' magnitudes, 2 us and more where they are many, instead of
+// a launch between (us, so and with it: 256 x 1024 x 1024 27.9 and 28.9, 777 x 1003 x 530
+// 30.8 and 32.7, 4096 x 256 x 256 39.8 and 41.6, 1024 x 1024 x 512 30.3 and 30.6; of more
+// tiles 2048 x 1024 x 1024 56.1 and 55.4, 2048 x 2560 x 512 79.5 and 73.0).
+constexpr int64_t kSplitJoinBlocks = 1024;
+
+// Target exponents of a pre-scaled operand (api.hip's range_opts): as A, and as
+// B, where the scaled kernels form s B_hi in FP16.
+inline int target_a(float scale) { return std::min(14, 26 - std::ilogb(scale)); }
+inline int target_b(float scale, int variant) {
+  return variant == kTermwise || !scaled_kernel_ok(scale) ? target_a(scale)
+                                                          : 14 - std::ilogb(scale);
+}
+
+}  // namespace
+}  // namespace sgc

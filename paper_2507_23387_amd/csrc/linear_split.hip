@@ -78,7 +78,14 @@ __device__ __forceinline__ int shift_of(float top, int target) {
 __device__ void join_sums(const ColumnJoin& g, uint32_t block, float* part) {
   const int64_t j = static_cast<int64_t>(block) * kJoinLines + threadIdx.x % kJoinLines;
   const float s = join_line<false>(g.sums, g.slabs, g.N, g.N, j, part);
-  if (threadIdx.x < kJoinLines && j < g.N) g.dbias[j] = s;
+  if (threadIdx.x >= kJoinLines || j >= g.N) return;
+  if (g.half == 0) {
+    g.dbias[j] = s;
+  } else if (j < g.half) {
+    if (g.dbias && j < g.cols) g.dbias[j] = s;
+  } else if (g.dbias_second && j - g.half < g.cols) {
+    g.dbias_second[j - g.half] = s;
+  }
 }
 
 // The shifts of 32 rows or columns.
@@ -128,8 +135,10 @@ __device__ __forceinline__ void split_tile(const SplitArgs& a, const SplitJob& g
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[u][e] *= activate_grad(g.activation, z[u][e]);
   }
-  const int64_t kp_row = (g.cols + kKPad - 1) / kKPad * kKPad;
-  const int64_t kp_col = (g.rows + kKPad - 1) / kKPad * kKPad;
+  // k of the planes, and where this matrix's ends in them.
+  const int64_t kp_row = g.kp ? g.kp : (g.cols + kKPad - 1) / kKPad * kKPad;
+  const int64_t kp_col = g.kp ? g.kp : (g.rows + kKPad - 1) / kKPad * kKPad;
+  const int64_t row_end = g.kp ? g.kp / 2 : kp_row;
   bool big = false;
   auto too_big = [&](uint32_t h) {
     typedef _Float16 half2 __attribute__((ext_vector_type(2)));
@@ -145,7 +154,7 @@ __device__ __forceinline__ void split_tile(const SplitArgs& a, const SplitJob& g
     if (t == 0 && scaled) range[kWordBOverflow] = 0;  // no stamp is 0
     if (t == 0) range[kWordBStamp] = stamp;
   };
-  if (g.row_hi && j < kp_row) {
+  if (g.row_hi && j < row_end) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       float w[8];
@@ -155,7 +164,7 @@ __device__ __forceinline__ void split_tile(const SplitArgs& a, const SplitJob& g
       u32x4 hv, lv;
       split8(w, a.s, hv, lv);
       if (g.row_range) too_big(hv[0]), too_big(hv[1]), too_big(hv[2]), too_big(hv[3]);
-      const int64_t at = tiled_index(i + u, j, kp_row);
+      const int64_t at = tiled_index(pair_row(i + u, g.pair), g.k0 + j, kp_row);
       store_chunk(g.row_hi + at, hv);
       store_chunk(g.row_lo + at, lv);
     }
@@ -180,10 +189,15 @@ __device__ __forceinline__ void split_tile(const SplitArgs& a, const SplitJob& g
   }
   if (g.col_range) flag(g.col_range, g.col_stamp);
   __syncthreads();
-  const int r = t >> 1, c = (t & 1) ^ tile_swizzle(r);
+  // Chunk t & 1 of plane row p (t & 1 of the tile's own order where lines are not paired).
+  const int r = t >> 1;
+  const int64_t p = pair_row(tc * kTileCols + r, g.pair);
+  const int c = (t & 1) ^ tile_swizzle(static_cast<int>(p % kPanel));
+  const int64_t panel = p / kPanel * (kp_col / kSlice) + g.k0 / kSlice;
+  const int64_t in_tile = p % kPanel * kSlice + 8 * (t & 1);
 #pragma unroll
   for (int sl = 0; sl < kTileRows / kSlice; ++sl) {
-    const int64_t at = (tc * (kp_col / kSlice) + tr * (kTileRows / kSlice) + sl) * kTileHalves + t * 8;
+    const int64_t at = (panel + tr * (kTileRows / kSlice) + sl) * kTileHalves + in_tile;
     store_chunk(g.col_hi + at, *reinterpret_cast<const u32x4*>(ph + r * kPitch + sl * 8 + c * 4));
     store_chunk(g.col_lo + at, *reinterpret_cast<const u32x4*>(pl + r * kPitch + sl * 8 + c * 4));
   }
@@ -379,6 +393,74 @@ __global__ __launch_bounds__(kThreads) void columns_kernel(ColumnArgs a, int64_t
     a.col_top[blockIdx.y * (static_cast<int64_t>(gridDim.x) * kColumnStrip) + col] = most;
 }
 
+// columns_kernel for a gated layer: the strip's columns of dG and dU from the same three
+// loads, both written as a half of D.  HBM bounds it, 20 bytes an entry: GATE_COLUMNS_TIME.
+__global__ __launch_bounds__(kThreads) void gate_columns_kernel(GateColumnArgs a,
+                                                                int64_t slab_rows) {
+  constexpr int kStride = kThreads / 32;
+  __shared__ float sums[2][kStride][kColumnStrip], tops[2][kStride][kColumnStrip];
+  const int t = threadIdx.x;
+  const int64_t j = static_cast<int64_t>(blockIdx.x) * kColumnStrip + 4 * (t & 31);
+  const int64_t i0 = blockIdx.y * slab_rows, i1 = min(a.M, i0 + slab_rows);
+  float s[2][4] = {}, top[2][4] = {};
+  auto rows = [&](int64_t i, auto count) {
+    constexpr int kU = decltype(count)::value;
+    floatx4v y[kU], g[kU], d[2][kU];
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const int64_t row = i + u * kStride;
+      y[u] = load4(a.dy + row * a.lddy, j, a.N);
+      g[u] = load4(a.g + row * a.ldg, j, a.N);
+      d[0][u] = load4(a.u + row * a.ldu, j, a.N);
+    }
+    gate_gradients(a.activation, y, g, d[0], d[1]);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        const int64_t row = i + u * kStride;
+        *reinterpret_cast<floatx4v*>(a.d + row * (2 * a.half) + h * a.half + j) = d[h][u];
+        float b[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          s[h][e] += d[h][u][e];
+          b[e] = __builtin_fabsf(d[h][u][e]);
+          b[e] = b[e] <= 3.4028235e38f ? b[e] : 0.0f;
+          top[h][e] = __builtin_fmaxf(top[h][e], b[e]);
+        }
+        if (a.row_top) {
+          const float m = quarter_max(__builtin_fmaxf(__builtin_fmaxf(b[0], b[1]),
+                                                      __builtin_fmaxf(b[2], b[3])));
+          if ((t & 15) == 0)
+            a.row_top[(2 * (h * gridDim.x + blockIdx.x) + (t >> 4 & 1)) * a.M + row] = m;
+        }
+      }
+  };
+  int64_t i = i0 + (t >> 5);
+  for (; i + (kColumnRows - 1) * kStride < i1; i += kColumnRows * kStride)
+    rows(i, std::integral_constant<int, kColumnRows>{});
+  for (; i < i1; i += kStride) rows(i, std::integral_constant<int, 1>{});
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      sums[h][t >> 5][4 * (t & 31) + e] = s[h][e];
+      tops[h][t >> 5][4 * (t & 31) + e] = top[h][e];
+    }
+  __syncthreads();
+  const int h = t / kColumnStrip, c = t % kColumnStrip;
+  float sum = 0.0f, most = 0.0f;
+#pragma unroll
+  for (int g = 0; g < kStride; ++g) {
+    sum += sums[h][g][c];
+    most = __builtin_fmaxf(most, tops[h][g][c]);
+  }
+  const int64_t at = blockIdx.y * (2 * a.half) + h * a.half +
+                     static_cast<int64_t>(blockIdx.x) * kColumnStrip + c;
+  if (a.sums) a.sums[at] = sum;
+  if (a.col_top) a.col_top[at] = most;
+}
+
 // The join alone, 32 columns or rows a workgroup: dbias, the columns' shifts, the rows'.
 __global__ __launch_bounds__(kThreads) void columns_join_kernel(ColumnJoin g, uint32_t sums,
                                                                 uint32_t cols) {
@@ -409,10 +491,14 @@ __global__ __launch_bounds__(kThreads) void epilogue_kernel(Epilogue e, int64_t 
 
 namespace {
 
-// Tiles of a job.  Rows up to a multiple of 64: the padding of k in column planes.
+// Tiles of a job.  Rows up to a multiple of 64, the padding of k in column planes, or to
+// where the matrix's share of a k ends.
 int64_t job_blocks(const SplitJob& j) {
-  return round_up(j.rows, kKPad) / kTileRows * ((j.cols + kTileCols - 1) / kTileCols);
+  const int64_t rows = j.kp && j.col_hi ? j.kp / 2 : round_up(j.rows, kKPad);
+  return rows / kTileRows * ((j.cols + kTileCols - 1) / kTileCols);
 }
+
+const void* wants_sums(const ColumnJoin& j) { return j.dbias ? j.dbias : j.dbias_second; }
 
 unsigned join_blocks(const void* wanted, int64_t lines) {
   return wanted ? static_cast<unsigned>((lines + kJoinLines - 1) / kJoinLines) : 0u;
@@ -442,7 +528,7 @@ hipError_t launch_split_jobs(const SplitJob* jobs, int count, float scale, hipSt
   if (blocks == 0) return hipSuccess;
   if (join) {
     a.join = *join;
-    hipLaunchKernelGGL(split_join_kernel, dim3(a.first[count] + join_blocks(join->dbias, join->N)),
+    hipLaunchKernelGGL(split_join_kernel, dim3(a.first[count] + join_blocks(wants_sums(*join), join->N)),
                        dim3(kThreads), 0, stream, a);
     return hipGetLastError();
   }
@@ -465,8 +551,16 @@ hipError_t launch_columns(const ColumnArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
+hipError_t launch_gate_columns(const GateColumnArgs& a, hipStream_t stream) {
+  const int64_t slabs = column_slabs(a.M, a.half);
+  hipLaunchKernelGGL(gate_columns_kernel, dim3(static_cast<unsigned>(a.half / kColumnStrip),
+                                               static_cast<unsigned>(slabs)),
+                     dim3(kThreads), 0, stream, a, (a.M + slabs - 1) / slabs);
+  return hipGetLastError();
+}
+
 hipError_t launch_columns_join(const ColumnJoin& j, hipStream_t stream) {
-  const unsigned sums = join_blocks(j.dbias, j.N), cols = join_blocks(j.col_shift, j.N);
+  const unsigned sums = join_blocks(wants_sums(j), j.N), cols = join_blocks(j.col_shift, j.N);
   const unsigned rows = join_blocks(j.row_shift, j.M);
   if (sums + cols + rows == 0) return hipSuccess;
   hipLaunchKernelGGL(columns_join_kernel, dim3(sums + cols + rows), dim3(kThreads), 0, stream, j,

@@ -31,18 +31,9 @@ __device__ __forceinline__ void load_row(const typename Elem<kDtype>::T* row, in
 template <int kDtype, int kT, int kP>
 __device__ __forceinline__ void load_raw(const typename Elem<kDtype>::T* row, int t, int n,
                                          typename Elem<kDtype>::Piece (&p)[kP / Elem<kDtype>::kE]) {
-  using L = Elem<kDtype>;
+  constexpr int kE = Elem<kDtype>::kE;
 #pragma unroll
-  for (int c = 0; c < kP / L::kE; ++c) {
-    const int j = (c * kT + t) * L::kE;
-    if (j + L::kE <= n) {
-      p[c] = *reinterpret_cast<const typename L::Piece*>(row + j);
-    } else {
-#pragma unroll
-      for (int e = 0; e < L::kE; ++e)
-        p[c][e] = j + e < n ? row[j + e] : static_cast<typename L::T>(0.0f);
-    }
-  }
+  for (int c = 0; c < kP / kE; ++c) p[c] = raw_piece<kDtype>(row, (c * kT + t) * kE, n);
 }
 
 // Values j .. j + kE - 1 of an FP32 vector, `fill` where there is no vector.
