@@ -215,8 +215,8 @@ size_t sgemm_cube_linear_cross_entropy_workspace_size(int64_t M, int64_t V, int6
  * dloss_i taken as 0 where the target is negative.  The logits are computed again, a
  * piece of the vocabulary at a time, and D is multiplied by powers of two for each row
  * and column of a piece as in sgemm_cube_linear_backward.  A row whose dloss + dlse is 0
- * has p = 0 whatever its logits (its X must be finite, as it enters dW times 0); a
- * target of V or more gives a D of NaN.
+ * has p = 0 whatever its lse (its X must be finite, as it enters dW times 0); a target
+ * of V or more gives a D of NaN.
  *   dloss        M values; dlse: NULL (zeros), or M values.
  *   lse          what the forward call gave for the same operands.
  *   dX, lddx     NULL, or row-major M x K, overwritten.

@@ -1,14 +1,17 @@
 // Cross entropy of a linear layer's rows over a vocabulary, and its gradients (gfx950).
 //
 // With z = X W + b: lse_i = log sum_j exp(z_ij), loss_i = lse_i - z_i,t.  The vocabulary
-// is taken in pieces, of which no more than one piece's logits are in memory.  A row's
-// maximum and sum of exponentials are kept for stretches of its columns and joined at
-// the end, so that each logit is looked at once.
+// is taken in pieces.  A row's maximum and sum of exponentials are kept for stretches of
+// its columns and joined at the end, so that each logit is looked at once: by the product's
+// own epilogue, or, where few rows or columns or another order take other kernels, from one
+// piece's logits in the workspace.
 // Gradients, from g = dloss and h = dlse: D_ij = exp(z_ij - lse_i) (g_i + h_i) -
-// [j = t_i] g_i, whose products are those of a linear layer (linear.hip).
+// [j = t_i] g_i, a piece at a time, whose products are those of a linear layer: X is split
+// once for all pieces, W's piece once for the logits and dX, D as linear.hip says.
 #include <algorithm>
 
-#include "layers.h"
+#include "lanes.h"
+#include "linear_plan.h"
 
 namespace sgc {
 namespace {
@@ -16,27 +19,13 @@ namespace {
 constexpr int kThreads = 256;
 typedef float floatx4_u __attribute__((ext_vector_type(4), aligned(4)));
 
-// exp(x) on the hardware's exp2: off by (|x| + 2) 2^-24 of itself.
-__device__ __forceinline__ float exp_of(float x) {
-  return __builtin_amdgcn_exp2f(1.44269504f * x);
-}
-
-// Sums of exponentials: sum exp(z) = sum * exp(top).
-struct Exps {
-  float top, sum;
-  // Without a finite entry (top = -inf) the sum is 0.  A NaN or +inf makes it NaN.
-  __device__ __forceinline__ void join(const Exps& o) {
-    const float t = __builtin_fmaxf(top, o.top);
-    const float s = t == -__builtin_inff() ? sum + o.sum
-                                           : sum * exp_of(top - t) + o.sum * exp_of(o.top - t);
-    top = t;
-    sum = s;
-  }
-};
-
-__device__ __forceinline__ int64_t target_at(const Ids& ids, int64_t i) {
-  return ids.bits == 32 ? static_cast<const int32_t*>(ids.p)[i]
-                        : static_cast<const int64_t*>(ids.p)[i];
+// a becomes the sum of both.  Without a finite entry (top = -inf) the sum is 0.  A NaN or
+// +inf makes it NaN.
+__device__ __forceinline__ void join(Exps& a, const Exps& b) {
+  const float t = __builtin_fmaxf(a.top, b.top);
+  a.sum = t == -__builtin_inff() ? a.sum + b.sum
+                                 : a.sum * exp_of(a.top - t) + b.sum * exp_of(b.top - t);
+  a.top = t;
 }
 
 // What the rows of a piece's logits leave.
@@ -71,46 +60,50 @@ __global__ __launch_bounds__(kThreads) void exps_kernel(PieceArgs g) {
       const float base = o.top == -__builtin_inff() ? 0.0f : o.top;
 #pragma unroll
       for (int k = 0; k < 4; ++k) o.sum += exp_of(v[k] - base);
-      e.join(o);
+      join(e, o);
     }
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) e.join(Exps{__shfl_xor(e.top, d), __shfl_xor(e.sum, d)});
+    for (int d = 1; d < 64; d *= 2) join(e, Exps{__shfl_xor(e.top, d), __shfl_xor(e.sum, d)});
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = e;
     __syncthreads();
     if (threadIdx.x == 0) {
 #pragma unroll
-      for (int w = 1; w < kThreads / 64; ++w) e.join(part[w]);
+      for (int w = 1; w < kThreads / 64; ++w) join(e, part[w]);
       g.exps[(g.slot0 + blockIdx.y) * g.M + i] = e;
-      const int64_t t = target_at(g.targets, i) - g.first;
+      const int64_t t = id_at(g.targets, i) - g.first;
       if (t >= c0 && t < c1) g.at[i] = row[t];
     }
     __syncthreads();  // the sums are read before the next row's are written
   }
 }
 
-// The rows' results from `slots` stretches: 16 rows a workgroup, every 16th stretch a
-// thread.
-constexpr int kJoinRows = 16, kJoinGroups = kThreads / kJoinRows;
-__global__ __launch_bounds__(kThreads) void xent_join_kernel(int64_t M, int64_t V, int64_t slots,
-                                                             const Exps* exps, const float* at,
-                                                             Ids targets, float* loss,
-                                                             float* lse) {
-  __shared__ Exps part[kJoinGroups][kJoinRows];
-  const int r = threadIdx.x % kJoinRows, q = threadIdx.x / kJoinRows;
+// The rows' results from `slots` stretches: 16 rows a workgroup, every 64th stretch a
+// thread (every 16th, of 256 threads: 1024 slots of 4096 rows 35 us).
+constexpr int kJoinThreads = 1024, kJoinRows = 16, kJoinGroups = kJoinThreads / kJoinRows;
+constexpr int kJoinWaves = kJoinThreads / 64;
+__global__ __launch_bounds__(kJoinThreads) void xent_join_kernel(int64_t M, int64_t V,
+                                                                 int64_t slots, const Exps* exps,
+                                                                 const float* at, Ids targets,
+                                                                 float* loss, float* lse) {
+  __shared__ Exps part[kJoinWaves][kJoinRows];
+  const int r = threadIdx.x % kJoinRows, q = threadIdx.x / kJoinRows, wave = threadIdx.x >> 6;
   for (int64_t i0 = static_cast<int64_t>(blockIdx.x) * kJoinRows; i0 < M;
        i0 += static_cast<int64_t>(gridDim.x) * kJoinRows) {
     const int64_t i = i0 + r;
     Exps e{-__builtin_inff(), 0.0f};
     if (i < M) {
 #pragma unroll 4
-      for (int64_t s = q; s < slots; s += kJoinGroups) e.join(exps[s * M + i]);
+      for (int64_t s = q; s < slots; s += kJoinGroups) join(e, exps[s * M + i]);
     }
-    part[q][r] = e;
+#pragma unroll
+    for (int d = 16; d < 64; d *= 2) join(e, Exps{__shfl_xor(e.top, d), __shfl_xor(e.sum, d)});
+    if ((threadIdx.x & 63) < kJoinRows) part[wave][r] = e;
     __syncthreads();
     if (q == 0 && i < M) {
-      for (int k = 1; k < kJoinGroups; ++k) e.join(part[k][r]);
+#pragma unroll
+      for (int w = 1; w < kJoinWaves; ++w) join(e, part[w][r]);
       const float l = e.top + __builtin_logf(e.sum);
-      const int64_t t = target_at(targets, i);
+      const int64_t t = id_at(targets, i);
       lse[i] = l;
       loss[i] = t < 0 ? 0.0f : t >= V ? __builtin_nanf("") : l - at[i];
     }
@@ -129,23 +122,36 @@ __global__ __launch_bounds__(kThreads) void xent_grad_kernel(GradArgs g) {
   const int64_t j = (static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x) * 4;
   if (j >= g.cols) return;
   for (int64_t i = blockIdx.y; i < g.M; i += gridDim.y) {
-    const int64_t t = target_at(g.targets, i);
-    const float d = t < 0 ? 0.0f : t >= g.vocab ? __builtin_nanf("") : g.dloss[i];
-    const float c = g.dlse ? d + g.dlse[i] : d, l = g.lse[i];
+    const RowTerms t(i, g.vocab, g.targets, g.dloss, g.dlse, g.lse);
     float* const at = g.z + i * g.cols + j;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       if (j + k >= g.cols) break;
-      const float p = c == 0.0f ? 0.0f : exp_of(at[k] - l) * c;
-      at[k] = g.first + j + k == t ? p - d : p;
+      const float p = exp_of(at[k] - t.lse) * t.c;
+      at[k] = g.first + j + k == t.target ? p - t.d : p;
     }
   }
 }
 
-// Columns of a piece: what keeps its logits within 256 MiB, whole tiles of 256 columns.
-int64_t piece_cols(int64_t M, int64_t V) {
-  const int64_t most = std::max<int64_t>(1, (int64_t{64} << 20) / std::max<int64_t>(M, 1) / 256);
-  return std::min(V, most * 256);
+// Workgroups that take rows in turn, within a grid of 2^32 threads.
+unsigned rows_grid(int64_t workgroups) {
+  return static_cast<unsigned>(std::min<int64_t>(workgroups, int64_t{1} << 20));
+}
+
+// Columns of a piece, `bytes` for each of them: whole tiles of 256 columns within the
+// budget.  Each piece ends with workgroups that wait for the last ones: 4096 x 65536 x 4096
+// in pieces of 128 MiB of planes 4827 us, 256 4717, 512 4682, 1 GiB 4694; the gradient of
+// 4096 x 32768 x 4096 in pieces of 256 MiB of D and W 7438, 512 7231, 1 GiB 7100, 2 GiB
+// 7102.
+constexpr int64_t kPieceBytes = int64_t{512} << 20, kGradPieceBytes = int64_t{1} << 30;
+int64_t piece_of(int64_t V, int64_t budget, int64_t bytes) {
+  return std::min(V, std::max<int64_t>(1, budget / std::max<int64_t>(bytes, 1) / 256) * 256);
+}
+
+// Whether the pieces' logits are written: where few rows or columns go by kernels of their
+// own (a piece of few columns alone, not), and in the orders without the epilogues.
+bool logits_apart(int64_t M, int64_t V, int64_t K, int variant) {
+  return K == 0 || variant != kElementwise || linear_by_rows(M, V) || linear_by_columns(M, V);
 }
 
 // Columns of a row that one workgroup reduces: few rows are shared by more of them.
@@ -159,78 +165,66 @@ int64_t stretches(int64_t M, int64_t cols) {
   return (cols + s - 1) / s;
 }
 
-// Workgroups that take rows in turn, within a grid of 2^32 threads.
-unsigned rows_grid(int64_t workgroups) {
-  return static_cast<unsigned>(std::min<int64_t>(workgroups, int64_t{1} << 20));
+const float* weights_of(const XentArgs& a, int64_t first) {
+  return a.w + (a.transpose_w ? first * a.ldw : first);
 }
 
-struct Carver {
-  char* base;
-  size_t used;
-  template <typename T>
-  T* take(int64_t bytes) {
-    char* const at = base + used;
-    used += static_cast<size_t>(round_up(bytes, 256));
-    return reinterpret_cast<T*>(at);
-  }
-};
-
-const float* piece_of(const XentArgs& a, int64_t first) {
-  return a.w + (a.transpose_w ? first * a.ldw : first);
+SplitJob weights_job(const XentArgs& a, int64_t first, int64_t cols) {
+  const float* const w = weights_of(a, first);
+  return a.transpose_w ? job_of(w, a.ldw, cols, a.K) : job_of(w, a.ldw, a.K, cols);
 }
 
 LinearArgs logits_of(const XentArgs& a, int64_t first, int64_t cols, float* z) {
   LinearArgs l{};
   l.M = a.M, l.N = cols, l.K = a.K;
   l.x = a.x, l.ldx = a.ldx;
-  l.w = piece_of(a, first), l.ldw = a.ldw, l.transpose_w = a.transpose_w;
+  l.w = weights_of(a, first), l.ldw = a.ldw, l.transpose_w = a.transpose_w;
   l.e.bias = a.bias ? a.bias + first : nullptr;
   l.y = z, l.ldy = cols;
   l.scale = a.scale, l.variant = a.variant;
   return l;
 }
 
-struct Workspace {
-  float* z;
-  Exps* exps;
-  float* at;
-  void* linear;
-  int64_t piece, slots;
-  size_t bytes;
-};
-
-Workspace carve(void* ws, int64_t M, int64_t V, int64_t K) {
-  Carver c{static_cast<char*>(ws), 0};
-  Workspace w{};
-  w.piece = piece_cols(M, V);
-  const int64_t rest = V % w.piece;
-  w.slots = V / w.piece * stretches(M, w.piece) + (rest ? stretches(M, rest) : 0);
-  w.z = c.take<float>(4 * M * w.piece);
-  w.exps = c.take<Exps>(8 * M * w.slots);
-  w.at = c.take<float>(4 * M);
-  // Of both widths: fewer columns may take another path.
-  w.linear = c.take<void>(static_cast<int64_t>(
-      std::max(linear_ws(M, w.piece, K), linear_ws(M, rest, K))));
-  w.bytes = c.used;
-  return w;
+// Of whichever body the scale takes.
+TileGrain finest_grain(int64_t M, int64_t N, int64_t K) {
+  const TileGrain a = tile_grain(M, N, K, kElementwise, false);
+  const TileGrain b = tile_grain(M, N, K, kElementwise, true);
+  return {std::min(a.rows, b.rows), std::min(a.cols, b.cols)};
 }
 
-struct GradWorkspace {
-  float* z;
-  void* linear;
+int64_t pieces_of(int64_t n, int64_t size) { return (n + size - 1) / size; }
+
+struct Workspace {
   int64_t piece;
+  Exps* exps;
+  float* at;
+  float* z;  // apart: a piece's logits
+  void* linear;
+  Planes p;  // otherwise
   size_t bytes;
 };
 
-GradWorkspace carve_grad(void* ws, int64_t M, int64_t V, int64_t K) {
+Workspace carve(void* ws, int64_t M, int64_t V, int64_t K, bool apart) {
   Carver c{static_cast<char*>(ws), 0};
-  GradWorkspace w{};
-  w.piece = piece_cols(M, V);
+  Workspace w{};
+  // A piece's logits, or its planes.
+  w.piece = piece_of(V, kPieceBytes, 4 * (apart ? M : round_up(K, kKPad)));
   const int64_t rest = V % w.piece;
-  w.z = c.take<float>(4 * M * w.piece);
-  w.linear = c.take<void>(static_cast<int64_t>(
-      std::max(std::max(linear_ws(M, w.piece, K), linear_ws(M, rest, K)),
-               std::max(linear_grad_ws(M, w.piece, K), linear_grad_ws(M, rest, K)))));
+  auto parts = [&](int64_t cols) {
+    if (cols == 0) return int64_t{0};
+    if (apart) return stretches(M, cols);
+    return pieces_of(cols, finest_grain(M, cols, K).cols);
+  };
+  const int64_t slots = V / w.piece * parts(w.piece) + parts(rest);
+  w.exps = c.take<Exps>(M * slots);
+  w.at = c.take<float>(M);
+  if (apart) {
+    w.z = c.take<float>(M * w.piece);
+    w.linear = c.take<char>(static_cast<int64_t>(
+        std::max(linear_ws(M, w.piece, K), linear_ws(M, rest, K))));
+  } else {
+    w.p = carve_planes(c, M, w.piece, K);
+  }
   w.bytes = c.used;
   return w;
 }
@@ -238,36 +232,197 @@ GradWorkspace carve_grad(void* ws, int64_t M, int64_t V, int64_t K) {
 }  // namespace
 
 size_t xent_ws(int64_t M, int64_t V, int64_t K) {
-  return M > 0 && V > 0 ? carve(nullptr, M, V, K).bytes : 0;
+  if (M == 0 || V == 0) return 0;
+  const size_t apart = carve(nullptr, M, V, K, true).bytes;
+  return logits_apart(M, V, K, kElementwise)
+             ? apart : std::max(apart, carve(nullptr, M, V, K, false).bytes);
 }
 
 hipError_t launch_xent(const XentArgs& a, float* loss, float* lse, void* ws, hipStream_t stream) {
+  const bool apart = a.V == 0 || logits_apart(a.M, a.V, a.K, a.variant);
   Workspace w{};
-  if (a.V > 0) w = carve(ws, a.M, a.V, a.K);
+  if (a.V > 0) w = carve(ws, a.M, a.V, a.K, apart);
   hipError_t err = hipSuccess;
   int64_t slot = 0;
   for (int64_t first = 0; first < a.V && err == hipSuccess; first += w.piece) {
     const int64_t cols = std::min(w.piece, a.V - first);
+    if (!apart) {
+      SplitJob jobs[2] = {weights_job(a, first, cols), job_of(a.x, a.ldx, a.M, a.K)};
+      to_planes(jobs[0], w.p, true, !a.transpose_w);
+      to_planes(jobs[1], w.p, false, false);
+      Planes p = w.p;
+      p.Np = round_up(cols, kRowPad);
+      err = launch_split_jobs(jobs, first == 0 ? 2 : 1, a.scale, stream);
+      if (err != hipSuccess) break;
+      const ExpsEpilogue e{a.bias, w.exps, slot, w.at, a.targets, first, a.V};
+      const int stretch =
+          tile_grain(a.M, cols, p.Kp, a.variant, !scaled_kernel_ok(a.scale)).cols;
+      err = launch_gemm_epilogue(p, a.M, cols, nullptr, 0, a.scale, a.variant, e, false, stream);
+      slot += pieces_of(cols, stretch);
+      continue;
+    }
     err = launch_linear(logits_of(a, first, cols, w.z), w.linear, stream);
     if (err != hipSuccess) break;
+    const int64_t parts = stretches(a.M, cols);
     const PieceArgs g{a.M, cols, first, w.z, a.targets, w.exps, w.at, slot,
                       stretch_cols(a.M, cols)};
-    const int64_t parts = stretches(a.M, cols);
     hipLaunchKernelGGL(exps_kernel, dim3(rows_grid(a.M), static_cast<unsigned>(parts)),
                        dim3(kThreads), 0, stream, g);
     err = hipGetLastError();
     slot += parts;
   }
   if (err != hipSuccess) return err;
-  hipLaunchKernelGGL(xent_join_kernel,
-                     dim3(rows_grid((a.M + kJoinRows - 1) / kJoinRows)),
-                     dim3(kThreads), 0, stream, a.M, a.V, slot, w.exps, w.at, a.targets, loss,
+  hipLaunchKernelGGL(xent_join_kernel, dim3(rows_grid((a.M + kJoinRows - 1) / kJoinRows)),
+                     dim3(kJoinThreads), 0, stream, a.M, a.V, slot, w.exps, w.at, a.targets, loss,
                      lse);
   return hipGetLastError();
 }
 
+namespace {
+
+struct GradWorkspace {
+  int64_t piece;
+  float* d;  // a piece's logits, then D
+  // Apart: each piece is two linear layers'.
+  void* linear;
+  // Otherwise: launch_columns' arrays and the planes of the three products.
+  float *row_top, *col_top, *sums;
+  int *row_shift, *col_shift;
+  Planes logits, dx, dw;
+  size_t bytes;
+};
+
+bool grad_apart(int64_t M, int64_t V, int64_t K, int variant) {
+  return logits_apart(M, V, K, variant) || linear_grad_by_rows(M, V, K);
+}
+
+GradWorkspace carve_grad(void* ws, int64_t M, int64_t V, int64_t K, bool transpose_w, bool apart) {
+  Carver c{static_cast<char*>(ws), 0};
+  GradWorkspace w{};
+  w.piece = piece_of(V, kGradPieceBytes, 4 * (M + K));
+  const int64_t rest = V % w.piece;
+  w.d = c.take<float>(M * w.piece);
+  if (apart) {
+    // Of both widths: fewer columns may take another path.
+    w.linear = c.take<char>(static_cast<int64_t>(
+        std::max(std::max(linear_ws(M, w.piece, K), linear_ws(M, rest, K)),
+                 std::max(linear_grad_ws(M, w.piece, K), linear_grad_ws(M, rest, K)))));
+  } else {
+    int64_t pieces = 0, top = 0;
+    for (const int64_t cols : {w.piece, rest}) {
+      if (cols == 0) continue;
+      const TileGrain g = finest_grain(M, cols, K);
+      pieces = std::max(pieces, pieces_of(cols, g.cols));
+      top = std::max(top, pieces_of(M, g.rows) * round_up(cols, kColumnStrip));
+    }
+    w.row_top = c.take<float>(pieces * M);
+    w.col_top = c.take<float>(top);
+    w.sums = c.take<float>(top);
+    w.row_shift = c.take<int>(round_up(M, kKPad));
+    w.col_shift = c.take<int>(round_up(w.piece, kColumnStrip));
+    w.logits = carve_planes(c, M, w.piece, K);
+    w.dx = carve_planes(c, M, K, w.piece);
+    w.dw = transpose_w ? carve_planes(c, w.piece, K, M) : carve_planes(c, K, w.piece, M);
+  }
+  w.bytes = c.used;
+  return w;
+}
+
+hipError_t launch_piece_apart(const XentGradArgs& a, const GradWorkspace& w, int64_t first,
+                              int64_t cols, hipStream_t stream) {
+  const XentArgs& x = a.x;
+  hipError_t err = launch_linear(logits_of(x, first, cols, w.d), w.linear, stream);
+  if (err != hipSuccess) return err;
+  const GradArgs g{x.M, cols, first, x.V, w.d, x.targets, a.dloss, a.dlse, a.lse};
+  hipLaunchKernelGGL(xent_grad_kernel,
+                     dim3(static_cast<unsigned>((cols + 4 * kThreads - 1) / (4 * kThreads)),
+                          static_cast<unsigned>(std::min<int64_t>(x.M, 65535))),
+                     dim3(kThreads), 0, stream, g);
+  err = hipGetLastError();
+  if (err != hipSuccess) return err;
+  LinearGradArgs l{};
+  l.M = x.M, l.N = cols, l.K = x.K;
+  l.dy = w.d, l.lddy = cols;
+  l.x = x.x, l.ldx = x.ldx;
+  l.w = weights_of(x, first), l.ldw = x.ldw, l.transpose_w = x.transpose_w;
+  l.dx = a.dx, l.lddx = a.lddx, l.add_dx = first > 0;
+  l.dw = a.dw ? a.dw + (x.transpose_w ? first * a.lddw : first) : nullptr, l.lddw = a.lddw;
+  l.dbias = a.dbias ? a.dbias + first : nullptr;
+  l.scale = x.scale, l.variant = x.variant;
+  return launch_linear_grad(l, w.linear, stream);
+}
+
+hipError_t launch_piece(const XentGradArgs& a, const GradWorkspace& w, int64_t first, int64_t cols,
+                        hipStream_t stream) {
+  const XentArgs& x = a.x;
+  Planes logits = w.logits, dx = w.dx, dw = w.dw;
+  logits.Np = round_up(cols, kRowPad);
+  dx.Kp = round_up(cols, kKPad);
+  (x.transpose_w ? dw.Mp : dw.Np) = round_up(cols, kRowPad);
+  // W's rows or columns for the logits, the others for dX; X the first time, its rows for
+  // the logits and its columns, k over M, for dW.
+  SplitJob jobs[kSplitJobs] = {weights_job(x, first, cols), job_of(x.x, x.ldx, x.M, x.K)};
+  to_planes(jobs[0], logits, true, !x.transpose_w);
+  if (a.dx) to_planes(jobs[0], dx, true, x.transpose_w);
+  to_planes(jobs[1], logits, false, false);
+  if (a.dw) to_planes(jobs[1], dw, x.transpose_w, true);
+  hipError_t err = launch_split_jobs(jobs, first == 0 ? 2 : 1, x.scale, stream);
+  if (err != hipSuccess) return err;
+  const XentGradEpilogue e{x.bias, x.targets, a.dloss, a.dlse, a.lse, first, x.V,
+                           a.dx ? w.row_top : nullptr, a.dw ? w.col_top : nullptr, w.sums};
+  err = launch_gemm_epilogue(logits, x.M, cols, w.d, cols, x.scale, x.variant, e, false, stream);
+  if (err != hipSuccess) return err;
+  const TileGrain grain =
+      tile_grain(x.M, cols, logits.Kp, x.variant, !scaled_kernel_ok(x.scale));
+  ColumnJoin join{};
+  join.M = x.M, join.N = cols;
+  join.pieces = static_cast<int>(pieces_of(cols, grain.cols));
+  join.slabs = static_cast<int>(pieces_of(x.M, grain.rows));
+  join.row_top = w.row_top, join.col_top = w.col_top, join.sums = w.sums;
+  join.row_target = target_a(x.scale);
+  join.col_target = x.transpose_w ? target_a(x.scale) : target_b(x.scale, x.variant);
+  join.row_shift = a.dx ? w.row_shift : nullptr;
+  join.col_shift = a.dw ? w.col_shift : nullptr;
+  join.dbias = a.dbias ? a.dbias + first : nullptr;
+  SplitJob d = job_of(w.d, cols, x.M, cols);
+  if (a.dx) d.row_shift = w.row_shift, to_planes(d, dx, false, false);
+  if (a.dw) d.col_shift = w.col_shift, to_planes(d, dw, !x.transpose_w, true);
+  const bool split = a.dx || a.dw;
+  const bool split_joins = split && split_jobs_blocks(&d, 1) <= kSplitJoinBlocks;
+  if (!split_joins) err = launch_columns_join(join, stream);
+  if (err == hipSuccess && split)
+    err = launch_split_jobs(&d, 1, x.scale, stream, split_joins ? &join : nullptr);
+
+  GroupProduct list[2];
+  int count = 0;
+  if (a.dx)
+    list[count++] = GroupProduct{dx, x.M, x.K, cols, a.dx, a.lddx,
+                                 Unscale{w.row_shift, false, first > 0}};
+  if (a.dw)
+    list[count++] = GroupProduct{dw, x.transpose_w ? cols : x.K, x.transpose_w ? x.K : cols, x.M,
+                                 a.dw + (x.transpose_w ? first * a.lddw : first), a.lddw,
+                                 Unscale{w.col_shift, !x.transpose_w, false}};
+  if (err == hipSuccess && count == 2) {
+    if (const int tile = group_gemm_tile(list, 2, x.variant, !scaled_kernel_ok(x.scale)))
+      return launch_gemm_group(tile, list, 2, x.scale, x.variant, stream);
+  }
+  for (int i = 0; i < count && err == hipSuccess; ++i) {
+    // As B, D never asks for the fallback (launch_linear_grad).
+    const GroupProduct& g = list[i];
+    err = launch_gemm_epilogue(g.p, g.M, g.N, g.C, g.ldc, x.scale, x.variant, g.epi,
+                               g.epi.columns, stream);
+  }
+  return err;
+}
+
+}  // namespace
+
 size_t xent_grad_ws(int64_t M, int64_t V, int64_t K) {
-  return M > 0 && V > 0 ? carve_grad(nullptr, M, V, K).bytes : 0;
+  if (M == 0 || V == 0) return 0;
+  const size_t apart = carve_grad(nullptr, M, V, K, false, true).bytes;
+  if (grad_apart(M, V, K, kElementwise)) return apart;
+  return std::max(apart, std::max(carve_grad(nullptr, M, V, K, false, false).bytes,
+                                  carve_grad(nullptr, M, V, K, true, false).bytes));
 }
 
 hipError_t launch_xent_grad(const XentGradArgs& a, void* ws, hipStream_t stream) {
@@ -280,28 +435,12 @@ hipError_t launch_xent_grad(const XentGradArgs& a, void* ws, hipStream_t stream)
     if (err == hipSuccess && a.dbias) err = launch_zero(1, x.V, a.dbias, x.V, stream);
     return err;
   }
-  const GradWorkspace w = carve_grad(ws, x.M, x.V, x.K);
+  const bool apart = grad_apart(x.M, x.V, x.K, x.variant);
+  const GradWorkspace w = carve_grad(ws, x.M, x.V, x.K, x.transpose_w, apart);
   for (int64_t first = 0; first < x.V && err == hipSuccess; first += w.piece) {
     const int64_t cols = std::min(w.piece, x.V - first);
-    err = launch_linear(logits_of(x, first, cols, w.z), w.linear, stream);
-    if (err != hipSuccess) break;
-    const GradArgs g{x.M, cols, first, x.V, w.z, x.targets, a.dloss, a.dlse, a.lse};
-    hipLaunchKernelGGL(xent_grad_kernel,
-                       dim3(static_cast<unsigned>((cols + 4 * kThreads - 1) / (4 * kThreads)),
-                            static_cast<unsigned>(std::min<int64_t>(x.M, 65535))),
-                       dim3(kThreads), 0, stream, g);
-    err = hipGetLastError();
-    if (err != hipSuccess) break;
-    LinearGradArgs l{};
-    l.M = x.M, l.N = cols, l.K = x.K;
-    l.dy = w.z, l.lddy = cols;
-    l.x = x.x, l.ldx = x.ldx;
-    l.w = piece_of(x, first), l.ldw = x.ldw, l.transpose_w = x.transpose_w;
-    l.dx = a.dx, l.lddx = a.lddx, l.add_dx = first > 0;
-    l.dw = a.dw ? a.dw + (x.transpose_w ? first * a.lddw : first) : nullptr, l.lddw = a.lddw;
-    l.dbias = a.dbias ? a.dbias + first : nullptr;
-    l.scale = x.scale, l.variant = x.variant;
-    err = launch_linear_grad(l, w.linear, stream);
+    err = apart ? launch_piece_apart(a, w, first, cols, stream)
+                : launch_piece(a, w, first, cols, stream);
   }
   return err;
 }

@@ -15,11 +15,6 @@ namespace {
 
 constexpr int kThreads = 256;
 
-__device__ __forceinline__ int64_t id_at(const Ids& ids, int64_t i) {
-  return ids.bits == 32 ? static_cast<const int32_t*>(ids.p)[i]
-                        : static_cast<const int64_t*>(ids.p)[i];
-}
-
 // A row's pieces by `lanes` threads (a power of two), four pieces in flight each.  HBM
 // bounds it, or for few rows the two dependent loads' latency.
 template <int kDtype>

@@ -6,10 +6,16 @@
 
 #include "activation.h"
 #include "gemm_common.h"
+#include "lanes.h"
 #include "layers.h"
 
 namespace sgc {
 namespace {
+
+// The cross entropy's epilogues are there for the elementwise order alone.
+template <class Epi>
+constexpr bool kElementwiseOnly =
+    std::is_same<Epi, ExpsEpilogue>::value || std::is_same<Epi, XentGradEpilogue>::value;
 
 // In place of an epilogue: C is stored as the product (store_tile16).
 struct NoEpilogue {};
@@ -35,13 +41,163 @@ struct LineShifts {
   }
 };
 
+// Blocks of 16 rows or columns to a stretch (TileGrain): a wave's, but of its 128 half,
+// which the fallback's waves have.
+template <int kSub>
+constexpr int kGrainBlocks = kSub == 8 ? 4 : kSub;
+
+// Each row's largest logit in a stretch and the sum of the exponentials below it, by the 16
+// lanes that hold them; the lane with a row's target leaves that.
+template <bool kFull, int kSubM, int kSubN, typename F>
+__device__ __forceinline__ void exps_tile(const ExpsEpilogue& e, int M, int N, int row0, int col0,
+                                          F value) {
+  constexpr int kB = kGrainBlocks<kSubN>;
+  const int lane = threadIdx.x & 63, l16 = lane & 15;
+  // The rows' targets as columns of the piece, 64 rows at a time, one a lane (LineShifts).
+  const int first_row = row0 - 4 * (lane >> 4);
+  int held[(kSubM + 3) / 4];
+#pragma unroll
+  for (int h = 0; h < (kSubM + 3) / 4; ++h) {
+    const int64_t t = id_at(e.targets, min(first_row + 64 * h + lane, M - 1));
+    held[h] = t < 0 || t >= e.vocab ? INT32_MIN : static_cast<int>(t - e.first);
+  }
+#pragma unroll
+  for (int j0 = 0; j0 < kSubN; j0 += kB) {
+    const int col = col0 + 16 * j0;  // this lane's first
+    if (!kFull && col - l16 >= N) break;
+    Exps* const out = e.exps + (e.slot0 + (col - l16) / (16 * kB)) * M;
+    float bias[kB];
+#pragma unroll
+    for (int j = 0; j < kB; ++j)
+      bias[j] = e.bias && (kFull || col + 16 * j < N) ? e.bias[e.first + col + 16 * j] : 0.0f;
+#pragma unroll
+    for (int i = 0; i < kSubM; ++i) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int row = row0 + 16 * i + r;
+        float v[kB], top = -__builtin_inff();
+#pragma unroll
+        for (int j = 0; j < kB; ++j) {
+          v[j] = kFull || col + 16 * j < N ? value(i, j0 + j, r) + bias[j] : -__builtin_inff();
+          top = __builtin_fmaxf(top, v[j]);
+        }
+        top = max_of_16(top);
+        const float base = top == -__builtin_inff() ? 0.0f : top;
+        float sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < kB; ++j) sum += exp_of(v[j] - base);
+        sum = sum_of_16(sum);
+        if (l16 == 0 && (kFull || row < M)) out[row] = Exps{top, sum};
+        const int t = __shfl(held[i / 4], i % 4 * 16 + 4 * (lane >> 4) + r) - col;
+        const bool hit = static_cast<unsigned>(t) < 16 * kB && t % 16 == 0 && (kFull || row < M);
+        if (__ballot(hit)) {
+          float z = v[0];
+#pragma unroll
+          for (int j = 1; j < kB; ++j) z = t == 16 * j ? v[j] : z;
+          if (hit) e.at[row] = z;
+        }
+      }
+      SCHED_FENCE();
+    }
+  }
+}
+
+// D in place of the product, and its lines' largest magnitudes and sums.  A lane holds the
+// terms of one of 64 rows and hands them out: read by all from memory they made a tile of
+// 256 x 256 wait 30 us longer.
+template <bool kFull, int kSubM, int kSubN, typename F>
+__device__ __forceinline__ void xent_grad_tile(const XentGradEpilogue& e, float* __restrict__ C,
+                                               int64_t ldc, int M, int N, int row0, int col0,
+                                               F value) {
+  constexpr int kBM = kGrainBlocks<kSubM>, kBN = kGrainBlocks<kSubN>, kParts = kSubN / kBN;
+  const int lane = threadIdx.x & 63, l16 = lane & 15;
+  const int64_t ld_top = (N + kColumnStrip - 1) / kColumnStrip * kColumnStrip;
+  float bias[kSubN];
+#pragma unroll
+  for (int j = 0; j < kSubN; ++j)
+    bias[j] = e.bias && (kFull || col0 + 16 * j < N) ? e.bias[e.first + col0 + 16 * j] : 0.0f;
+#pragma unroll
+  for (int i0 = 0; i0 < kSubM; i0 += kBM) {
+    const int first_row = row0 - 4 * (lane >> 4) + 16 * i0;
+    if (!kFull && first_row >= M) break;
+    const RowTerms mine(min(first_row + (lane < 16 * kBM ? lane : 0), M - 1), e.vocab, e.targets,
+                        e.dloss, e.dlse, e.lse);
+    const int target = mine.target < 0 ? INT32_MIN : static_cast<int>(mine.target - e.first);
+    float sum[kSubN], top[kSubN];
+#pragma unroll
+    for (int j = 0; j < kSubN; ++j) sum[j] = top[j] = 0.0f;
+#pragma unroll
+    for (int i = i0; i < i0 + kBM; ++i) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int row = row0 + 16 * i + r, from = 16 * (i - i0) + 4 * (lane >> 4) + r;
+        const float lse = __shfl(mine.lse, from), c = __shfl(mine.c, from);
+        const int hit = __shfl(target, from) - col0;
+        float d[kSubN];
+#pragma unroll
+        for (int j = 0; j < kSubN; ++j) d[j] = exp_of(value(i, j, r) + bias[j] - lse) * c;
+        if (__ballot(static_cast<unsigned>(hit) < 16 * kSubN)) {
+          const float off = __shfl(mine.d, from);
+#pragma unroll
+          for (int j = 0; j < kSubN; ++j) d[j] = hit == 16 * j ? d[j] - off : d[j];
+        }
+        float* const at = C + static_cast<int64_t>(row) * ldc + col0;
+        float most[kParts];
+#pragma unroll
+        for (int q = 0; q < kParts; ++q) most[q] = 0.0f;
+#pragma unroll
+        for (int j = 0; j < kSubN; ++j) {
+          if (kFull || (row < M && col0 + 16 * j < N)) at[16 * j] = d[j];
+          else d[j] = 0.0f;
+          const float b = finite_magnitude(d[j]);
+          sum[j] += d[j];
+          top[j] = __builtin_fmaxf(top[j], b);
+          most[j / kBN] = __builtin_fmaxf(most[j / kBN], b);
+        }
+        if (e.row_top) {
+#pragma unroll
+          for (int q = 0; q < kParts; ++q) {
+            const int col = col0 - l16 + 16 * kBN * q;
+            const float m = max_of_16(most[q]);
+            if (l16 == 0 && (kFull || (row < M && col < N)))
+              e.row_top[static_cast<int64_t>(col / (16 * kBN)) * M + row] = m;
+          }
+        }
+        SCHED_FENCE();
+      }
+    }
+    const int64_t slab = first_row / (16 * kBM);
+#pragma unroll
+    for (int j = 0; j < kSubN; ++j) {
+      sum[j] += __shfl_xor(sum[j], 16);
+      top[j] = __builtin_fmaxf(top[j], __shfl_xor(top[j], 16));
+      sum[j] += __shfl_xor(sum[j], 32);
+      top[j] = __builtin_fmaxf(top[j], __shfl_xor(top[j], 32));
+      const int col = col0 + 16 * j;
+      if (lane >= 16 || (!kFull && col >= N)) continue;
+      e.sums[slab * N + col] = sum[j];
+      if (e.col_top) e.col_top[slab * ld_top + col] = top[j];
+    }
+  }
+}
+
 // store_tile16, for Unscale each entry times 2^-shift of its row or column (and added to
 // C's).
 template <int kSubM, int kSubN, class Epi, typename F>
 __device__ __forceinline__ void store_product(const Epi& epi, float* __restrict__ C, int64_t ldc,
                                               int M, int N, int row0, int col0, bool full,
                                               F value) {
-  if constexpr (!std::is_same<Epi, Unscale>::value) {
+  if constexpr (std::is_same<Epi, ExpsEpilogue>::value) {
+    if (full)
+      exps_tile<true, kSubM, kSubN>(epi, M, N, row0, col0, value);
+    else
+      exps_tile<false, kSubM, kSubN>(epi, M, N, row0, col0, value);
+  } else if constexpr (std::is_same<Epi, XentGradEpilogue>::value) {
+    if (full)
+      xent_grad_tile<true, kSubM, kSubN>(epi, C, ldc, M, N, row0, col0, value);
+    else
+      xent_grad_tile<false, kSubM, kSubN>(epi, C, ldc, M, N, row0, col0, value);
+  } else if constexpr (!std::is_same<Epi, Unscale>::value) {
     store_tile16<kSubM, kSubN>(C, ldc, M, N, row0, col0, full, value);
   } else if (epi.columns) {
     const int i0 = threadIdx.x & 15;

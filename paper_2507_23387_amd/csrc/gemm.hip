@@ -1197,14 +1197,18 @@ hipError_t launch_gemm_epilogue(const Planes& p, int64_t M, int64_t N, float* C,
                                 hipStream_t stream) {
   if (const int tile = small_gemm_tile(M, N, p.Kp, variant, !scaled_kernel_ok(scale)))
     return launch_gemm_small_epilogue(tile, p, M, N, C, ldc, scale, variant, epi, stream);
-  if (variant == kTermwise)
-    return launch_linear_n128<kTermwise>(p, M, N, C, ldc, scale, epi, stream);
   const bool scaled = scaled_kernel_ok(scale);
-  if (scaled) {
-    const hipError_t e =
-        variant == kElementwise
-            ? launch_linear_el(p, M, N, C, ldc, scale, epi, stream)
-            : launch_linear_n128<kCrossScaled>(p, M, N, C, ldc, scale, epi, stream);
+  if constexpr (!kElementwiseOnly<Epi>) {
+    if (variant == kTermwise)
+      return launch_linear_n128<kTermwise>(p, M, N, C, ldc, scale, epi, stream);
+    if (variant == kCrossFirst && scaled) {
+      const hipError_t e =
+          launch_linear_n128<kCrossScaled>(p, M, N, C, ldc, scale, epi, stream);
+      if (e != hipSuccess || no_overflow) return e;
+    }
+  }
+  if (variant == kElementwise && scaled) {
+    const hipError_t e = launch_linear_el(p, M, N, C, ldc, scale, epi, stream);
     if (e != hipSuccess || no_overflow) return e;
   }
   return launch_gemm_unscaled_epilogue(p, M, N, C, ldc, scale, variant, !scaled, epi, stream);
@@ -1227,6 +1231,13 @@ template hipError_t launch_gemm_epilogue<Epilogue>(const Planes&, int64_t, int64
 template hipError_t launch_gemm_epilogue<GateEpilogue>(const Planes&, int64_t, int64_t, float*,
                                                        int64_t, float, int, const GateEpilogue&,
                                                        bool, hipStream_t);
+template hipError_t launch_gemm_epilogue<ExpsEpilogue>(const Planes&, int64_t, int64_t, float*,
+                                                       int64_t, float, int, const ExpsEpilogue&,
+                                                       bool, hipStream_t);
+template hipError_t launch_gemm_epilogue<XentGradEpilogue>(const Planes&, int64_t, int64_t, float*,
+                                                           int64_t, float, int,
+                                                           const XentGradEpilogue&, bool,
+                                                           hipStream_t);
 template hipError_t launch_gemm_epilogue<Unscale>(const Planes&, int64_t, int64_t, float*, int64_t,
                                                   float, int, const Unscale&, bool, hipStream_t);
 

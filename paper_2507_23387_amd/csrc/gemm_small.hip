@@ -690,6 +690,20 @@ int small_gemm_tile(int64_t M, int64_t N, int64_t K, int variant, bool unscaled,
   return tile;
 }
 
+TileGrain tile_grain(int64_t M, int64_t N, int64_t K, int variant, bool unscaled) {
+  const int tile = small_gemm_tile(M, N, K, variant, unscaled);
+  if (tile == 0) return {16 * kGrainBlocks<8>, 16 * kGrainBlocks<8>};
+  static_assert(UnscaledShape::kRT == kGrainBlocks<8> && UnscaledShape::kCT == kGrainBlocks<8>,
+                "the fallback of the wide kernel leaves as much");
+  TileGrain g{};
+  (void)with_config<kElementwise>(tile, [&](auto c) {
+    using T = decltype(c);
+    g = {16 * kGrainBlocks<T::kBM / T::kWM / 16>, 16 * kGrainBlocks<T::kBN / T::kWN / 16>};
+    return hipSuccess;
+  });
+  return g;
+}
+
 int group_gemm_tile(const GroupProduct* list, int count, int variant, bool unscaled) {
   const int row = unscaled && variant == kElementwise ? 4 : variant;
   auto side_cost = [&](int side) -> const GridCost& {
@@ -766,7 +780,11 @@ template <class Epi>
 hipError_t launch_gemm_small_epilogue(int tile, const Planes& p, int64_t M, int64_t N, float* C,
                                       int64_t ldc, float scale, int variant, const Epi& epi,
                                       hipStream_t stream) {
-  switch (variant) {
+  if constexpr (kElementwiseOnly<Epi>)
+    return variant != kElementwise ? hipErrorInvalidValue
+                                   : launch_config_epilogue<kElementwise>(tile, p, M, N, C, ldc,
+                                                                          scale, epi, stream);
+  else switch (variant) {
     case kElementwise:
       return launch_config_epilogue<kElementwise>(tile, p, M, N, C, ldc, scale, epi, stream);
     case kTermwise:
@@ -781,7 +799,11 @@ template <class Epi>
 hipError_t launch_gemm_unscaled_epilogue(const Planes& p, int64_t M, int64_t N, float* C,
                                          int64_t ldc, float scale, int variant, bool only,
                                          const Epi& epi, hipStream_t stream) {
-  switch (variant) {
+  if constexpr (kElementwiseOnly<Epi>)
+    return variant != kElementwise
+               ? hipErrorInvalidValue
+               : launch_unscaled_epilogue<kElementwise>(p, M, N, C, ldc, scale, only, epi, stream);
+  else switch (variant) {
     case kElementwise:
       return launch_unscaled_epilogue<kElementwise>(p, M, N, C, ldc, scale, only, epi, stream);
     case kCrossFirst:
@@ -796,6 +818,18 @@ template hipError_t launch_gemm_small_epilogue<Epilogue>(int, const Planes&, int
 template hipError_t launch_gemm_small_epilogue<Unscale>(int, const Planes&, int64_t, int64_t,
                                                         float*, int64_t, float, int,
                                                         const Unscale&, hipStream_t);
+template hipError_t launch_gemm_small_epilogue<ExpsEpilogue>(int, const Planes&, int64_t, int64_t, float*,
+                                                    int64_t, float, int, const ExpsEpilogue&,
+                                                    hipStream_t);
+template hipError_t launch_gemm_unscaled_epilogue<ExpsEpilogue>(const Planes&, int64_t, int64_t, float*,
+                                                       int64_t, float, int, bool, const ExpsEpilogue&,
+                                                       hipStream_t);
+template hipError_t launch_gemm_small_epilogue<XentGradEpilogue>(int, const Planes&, int64_t, int64_t, float*,
+                                                    int64_t, float, int, const XentGradEpilogue&,
+                                                    hipStream_t);
+template hipError_t launch_gemm_unscaled_epilogue<XentGradEpilogue>(const Planes&, int64_t, int64_t, float*,
+                                                       int64_t, float, int, bool, const XentGradEpilogue&,
+                                                       hipStream_t);
 template hipError_t launch_gemm_small_epilogue<GateEpilogue>(int, const Planes&, int64_t, int64_t,
                                                              float*, int64_t, float, int,
                                                              const GateEpilogue&, hipStream_t);

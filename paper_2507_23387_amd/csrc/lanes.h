@@ -1,0 +1,62 @@
+// Reductions over 16 adjacent lanes, exponentials, and a cross entropy's gradient.  Internal; every function has
+// internal linkage.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "layers.h"
+
+namespace sgc {
+namespace {
+
+// f of the values of 16 lanes, in every one of them, by rotations.
+template <typename F>
+__device__ __forceinline__ float join_16(float v, F f) {
+  auto step = [&](auto control) {
+    const int o = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v),
+                                              decltype(control)::value, 0xf, 0xf, true);
+    v = f(v, __builtin_bit_cast(float, o));
+  };
+  step(std::integral_constant<int, 0x121>{});  // row_ror:1
+  step(std::integral_constant<int, 0x122>{});
+  step(std::integral_constant<int, 0x124>{});
+  step(std::integral_constant<int, 0x128>{});
+  return v;
+}
+__device__ __forceinline__ float max_of_16(float v) {
+  return join_16(v, [](float a, float b) { return __builtin_fmaxf(a, b); });
+}
+__device__ __forceinline__ float sum_of_16(float v) {
+  return join_16(v, [](float a, float b) { return a + b; });
+}
+
+// exp(x) on the hardware's exp2: off by (|x| + 2) 2^-24 of itself.
+__device__ __forceinline__ float exp_of(float x) {
+  return __builtin_amdgcn_exp2f(1.44269504f * x);
+}
+
+// The magnitude of a finite value, 0 of others.
+__device__ __forceinline__ float finite_magnitude(float v) {
+  const float b = __builtin_fabsf(v);
+  return b <= 3.4028235e38f ? b : 0.0f;
+}
+
+// What a row's D_ij = exp(z_ij - lse) c - [j = target] d needs.
+struct RowTerms {
+  float lse, c, d;
+  int64_t target;  // -1: none
+  __device__ __forceinline__ RowTerms(int64_t i, int64_t vocab, const Ids& targets,
+                                      const float* dloss, const float* dlse, const float* lses) {
+    target = id_at(targets, i);
+    d = target < 0 ? 0.0f : target >= vocab ? __builtin_nanf("") : dloss[i];
+    c = dlse ? d + dlse[i] : d;
+    // exp(z - inf) c = 0, whatever the row's lse.
+    lse = c == 0.0f ? __builtin_inff() : lses[i];
+    if (target < 0 || target >= vocab) target = -1;
+  }
+};
+
+}  // namespace
+}  // namespace sgc

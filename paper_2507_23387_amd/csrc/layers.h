@@ -11,6 +11,16 @@ namespace sgc {
 enum Dtype : int { kF32 = 0, kF16 = 1, kBF16 = 2 };
 inline int dtype_bytes(int dtype) { return dtype == kF32 ? 4 : 2; }
 
+// Token ids or targets: int32 or int64.
+struct Ids {
+  const void* p;
+  int bits;
+};
+__device__ inline int64_t id_at(const Ids& ids, int64_t i) {
+  return ids.bits == 32 ? static_cast<const int32_t*>(ids.p)[i]
+                        : static_cast<const int64_t*>(ids.p)[i];
+}
+
 // --- linear layer ---------------------------------------------------------------
 
 // One matrix of a split launch: S is rows x cols row-major, times act'(Z) where z
@@ -139,6 +149,37 @@ struct GateEpilogue {
   float* z[2];  // G and U with their biases; null: not kept
   int64_t ldz[2];
 };
+// The logits z = P + bias of a piece of a vocabulary, its columns those from `first` on.
+// Sums of exponentials: sum exp(z) = sum * exp(top).
+struct Exps {
+  float top, sum;
+};
+// What follows is left for the rows and columns of each wave's part of a tile, which this
+// says for the kernels that launch_gemm_epilogue picks.
+struct TileGrain {
+  int rows, cols;
+};
+TileGrain tile_grain(int64_t M, int64_t N, int64_t K, int variant, bool unscaled);
+// What a row's logits leave: exps[slot * rows + row] for each stretch of columns, and
+// at[row], the target's logit.
+struct ExpsEpilogue {
+  const float* bias;  // null: none
+  Exps* exps;
+  int64_t slot0;
+  float* at;
+  Ids targets;
+  int64_t first, vocab;
+};
+// C_ij = D_ij = exp(z_ij - lse_i) (dloss_i + dlse_i) - [j = target_i] dloss_i, and
+// launch_columns' arrays of D: its rows' largest finite magnitudes for each stretch of
+// columns, its columns' and their sums for each stretch of rows.
+struct XentGradEpilogue {
+  const float* bias;
+  Ids targets;
+  const float *dloss, *dlse, *lse;  // dlse null: zeros
+  int64_t first, vocab;
+  float *row_top, *col_top, *sums;  // the tops null: not wanted
+};
 // The epilogue where K = 0: P = 0.
 hipError_t launch_epilogue(const Epilogue& e, int64_t M, int64_t N, float* Y, int64_t ldy,
                            hipStream_t stream);
@@ -251,12 +292,6 @@ struct LinearGradArgs {
 bool linear_grad_by_rows(int64_t M, int64_t N, int64_t K);
 size_t linear_grad_ws(int64_t M, int64_t N, int64_t K);
 hipError_t launch_linear_grad(const LinearGradArgs& a, void* ws, hipStream_t stream);
-
-// Token ids or targets: int32 or int64.
-struct Ids {
-  const void* p;
-  int bits;
-};
 
 struct EmbeddingArgs {
   int64_t n, vocab, cols;
