@@ -28,11 +28,25 @@ __device__ __forceinline__ void join(Exps& a, const Exps& b) {
   a.top = t;
 }
 
+// A row's results: its loss and lse.
+struct Results {
+  int64_t V;
+  Ids targets;
+  float *loss, *lse;
+  __device__ __forceinline__ void store(int64_t i, const Exps& e, const float* at) const {
+    const float l = e.top + __builtin_logf(e.sum);
+    const int64_t t = id_at(targets, i);
+    lse[i] = l;
+    loss[i] = t < 0 ? 0.0f : t >= V ? __builtin_nanf("") : l - *at;
+  }
+};
+
 // What the rows of a piece's logits leave.
 struct PieceArgs {
   int64_t M, cols, first;  // columns first .. first + cols - 1 of the vocabulary
   const float* z;          // M x cols
-  Ids targets;
+  Results out;
+  bool all;       // one stretch, of all columns: the results
   Exps* exps;     // slots x M
   float* at;      // the target's logit
   int64_t slot0;  // of this piece's first stretch
@@ -40,27 +54,38 @@ struct PieceArgs {
 };
 
 // A stretch of one row a workgroup.
-__global__ __launch_bounds__(kThreads) void exps_kernel(PieceArgs g) {
-  __shared__ Exps part[kThreads / 64];
+constexpr int kExpsThreads = 1024;
+__global__ __launch_bounds__(kExpsThreads) void exps_kernel(PieceArgs g) {
+  __shared__ Exps part[kExpsThreads / 64];
   const int64_t c0 = blockIdx.y * g.stretch, c1 = min(g.cols, c0 + g.stretch);
   for (int64_t i = blockIdx.x; i < g.M; i += gridDim.x) {
     const float* const row = g.z + i * g.cols;
     Exps e{-__builtin_inff(), 0.0f};
-    for (int64_t j = c0 + 4 * threadIdx.x; j < c1; j += 4 * kThreads) {
-      float v[4];
-      if (j + 3 < c1) {
-        const floatx4_u p = *reinterpret_cast<const floatx4_u*>(row + j);
+    // Four quads of this thread's in flight.
+    constexpr int kU = 4;
+    for (int64_t j0 = c0 + 4 * threadIdx.x; j0 < c1; j0 += 4 * kU * kExpsThreads) {
+      float v[kU][4];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = p[k];
-      } else {
+      for (int u = 0; u < kU; ++u) {
+        const int64_t j = j0 + 4 * u * kExpsThreads;
+        if (j + 3 < c1) {
+          const floatx4_u p = *reinterpret_cast<const floatx4_u*>(row + j);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = j + k < c1 ? row[j + k] : -__builtin_inff();
+          for (int k = 0; k < 4; ++k) v[u][k] = p[k];
+        } else {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[u][k] = j + k < c1 ? row[j + k] : -__builtin_inff();
+        }
       }
-      Exps o{__builtin_fmaxf(__builtin_fmaxf(v[0], v[1]), __builtin_fmaxf(v[2], v[3])), 0.0f};
-      const float base = o.top == -__builtin_inff() ? 0.0f : o.top;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) o.sum += exp_of(v[k] - base);
-      join(e, o);
+      for (int u = 0; u < kU; ++u) {
+        const float(&q)[4] = v[u];
+        Exps o{__builtin_fmaxf(__builtin_fmaxf(q[0], q[1]), __builtin_fmaxf(q[2], q[3])), 0.0f};
+        const float base = o.top == -__builtin_inff() ? 0.0f : o.top;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o.sum += exp_of(q[k] - base);
+        join(e, o);
+      }
     }
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) join(e, Exps{__shfl_xor(e.top, d), __shfl_xor(e.sum, d)});
@@ -68,10 +93,15 @@ __global__ __launch_bounds__(kThreads) void exps_kernel(PieceArgs g) {
     __syncthreads();
     if (threadIdx.x == 0) {
 #pragma unroll
-      for (int w = 1; w < kThreads / 64; ++w) join(e, part[w]);
-      g.exps[(g.slot0 + blockIdx.y) * g.M + i] = e;
-      const int64_t t = id_at(g.targets, i) - g.first;
-      if (t >= c0 && t < c1) g.at[i] = row[t];
+      for (int w = 1; w < kExpsThreads / 64; ++w) join(e, part[w]);
+      const int64_t t = id_at(g.out.targets, i) - g.first;
+      const bool here = t >= c0 && t < c1;
+      if (g.all) {
+        g.out.store(i, e, row + (here ? t : 0));
+      } else {
+        g.exps[(g.slot0 + blockIdx.y) * g.M + i] = e;
+        if (here) g.at[i] = row[t];
+      }
     }
     __syncthreads();  // the sums are read before the next row's are written
   }
@@ -81,10 +111,9 @@ __global__ __launch_bounds__(kThreads) void exps_kernel(PieceArgs g) {
 // thread (every 16th, of 256 threads: 1024 slots of 4096 rows 35 us).
 constexpr int kJoinThreads = 1024, kJoinRows = 16, kJoinGroups = kJoinThreads / kJoinRows;
 constexpr int kJoinWaves = kJoinThreads / 64;
-__global__ __launch_bounds__(kJoinThreads) void xent_join_kernel(int64_t M, int64_t V,
-                                                                 int64_t slots, const Exps* exps,
-                                                                 const float* at, Ids targets,
-                                                                 float* loss, float* lse) {
+__global__ __launch_bounds__(kJoinThreads) void xent_join_kernel(int64_t M, int64_t slots,
+                                                                 const Exps* exps, const float* at,
+                                                                 Results out) {
   __shared__ Exps part[kJoinWaves][kJoinRows];
   const int r = threadIdx.x % kJoinRows, q = threadIdx.x / kJoinRows, wave = threadIdx.x >> 6;
   for (int64_t i0 = static_cast<int64_t>(blockIdx.x) * kJoinRows; i0 < M;
@@ -102,10 +131,7 @@ __global__ __launch_bounds__(kJoinThreads) void xent_join_kernel(int64_t M, int6
     if (q == 0 && i < M) {
 #pragma unroll
       for (int w = 1; w < kJoinWaves; ++w) join(e, part[w][r]);
-      const float l = e.top + __builtin_logf(e.sum);
-      const int64_t t = id_at(targets, i);
-      lse[i] = l;
-      loss[i] = t < 0 ? 0.0f : t >= V ? __builtin_nanf("") : l - at[i];
+      out.store(i, e, at + i);
     }
     __syncthreads();  // the sums are read before the next rows' are written
   }
@@ -142,10 +168,10 @@ unsigned rows_grid(int64_t workgroups) {
 // budget.  Each piece ends with workgroups that wait for the last ones: 4096 x 65536 x 4096
 // in pieces of 128 MiB of planes 4827 us, 256 4717, 512 4682, 1 GiB 4694; the gradient of
 // 4096 x 32768 x 4096 in pieces of 256 MiB of D and W 7438, 512 7231, 1 GiB 7100, 2 GiB
-// 7102.
+// 7102.  (At least 2048 columns, as each piece adds to all of dX.)
 constexpr int64_t kPieceBytes = int64_t{512} << 20, kGradPieceBytes = int64_t{1} << 30;
 int64_t piece_of(int64_t V, int64_t budget, int64_t bytes) {
-  return std::min(V, std::max<int64_t>(1, budget / std::max<int64_t>(bytes, 1) / 256) * 256);
+  return std::min(V, std::max<int64_t>(2048, budget / std::max<int64_t>(bytes, 1) / 256 * 256));
 }
 
 // Whether the pieces' logits are written: where few rows or columns go by kernels of their
@@ -154,9 +180,10 @@ bool logits_apart(int64_t M, int64_t V, int64_t K, int variant) {
   return K == 0 || variant != kElementwise || linear_by_rows(M, V) || linear_by_columns(M, V);
 }
 
-// Columns of a row that one workgroup reduces: few rows are shared by more of them.
+// Columns of a row that one workgroup reduces: few long rows are shared by more of them.
+// (One row of 32768 in one workgroup 8.6 us, in 32 and a join 4.7 and 4.7.)
 int64_t stretch_cols(int64_t M, int64_t cols) {
-  const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(cols / 1024, 1024 / M));
+  const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(cols / 32768, 1024 / M));
   return round_up((cols + parts - 1) / parts, 4);
 }
 
@@ -240,6 +267,7 @@ size_t xent_ws(int64_t M, int64_t V, int64_t K) {
 
 hipError_t launch_xent(const XentArgs& a, float* loss, float* lse, void* ws, hipStream_t stream) {
   const bool apart = a.V == 0 || logits_apart(a.M, a.V, a.K, a.variant);
+  const Results out{a.V, a.targets, loss, lse};
   Workspace w{};
   if (a.V > 0) w = carve(ws, a.M, a.V, a.K, apart);
   hipError_t err = hipSuccess;
@@ -264,17 +292,18 @@ hipError_t launch_xent(const XentArgs& a, float* loss, float* lse, void* ws, hip
     err = launch_linear(logits_of(a, first, cols, w.z), w.linear, stream);
     if (err != hipSuccess) break;
     const int64_t parts = stretches(a.M, cols);
-    const PieceArgs g{a.M, cols, first, w.z, a.targets, w.exps, w.at, slot,
+    const bool all = cols == a.V && parts == 1;
+    const PieceArgs g{a.M, cols, first, w.z, out, all, w.exps, w.at, slot,
                       stretch_cols(a.M, cols)};
     hipLaunchKernelGGL(exps_kernel, dim3(rows_grid(a.M), static_cast<unsigned>(parts)),
-                       dim3(kThreads), 0, stream, g);
+                       dim3(kExpsThreads), 0, stream, g);
     err = hipGetLastError();
+    if (all) return err;
     slot += parts;
   }
   if (err != hipSuccess) return err;
   hipLaunchKernelGGL(xent_join_kernel, dim3(rows_grid((a.M + kJoinRows - 1) / kJoinRows)),
-                     dim3(kJoinThreads), 0, stream, a.M, a.V, slot, w.exps, w.at, a.targets, loss,
-                     lse);
+                     dim3(kJoinThreads), 0, stream, a.M, slot, w.exps, w.at, out);
   return hipGetLastError();
 }
 

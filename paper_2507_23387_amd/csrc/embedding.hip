@@ -258,7 +258,9 @@ __device__ __forceinline__ int clamp_of(int k, int a, int b) {
 // waves share the keys, which LDS hands to all lanes at once.  Against `key`, a key k
 // clamped to key - 1 .. key (before it: key .. key + 1) is one less where it counts, so
 // that one instruction compares and half of one adds up; with carries there are two, and
-// two waits between them.  RANK_TIMES
+// two waits between them.  LDS's handing out bounds it past 8192 positions: 777 4.8 us, 4096
+// 8.8, 16384 24.4 (26.7 with carries; the passes above 29.4 in four launches), of which 3.5
+// are the launch.
 constexpr int64_t kRankItems = 16384;
 constexpr int kRankChunk = 8192, kPastKeys = 0x7fffffff;
 __global__ __launch_bounds__(kSortThreads) void rank_kernel(Ids ids, int64_t vocab, int n,
@@ -324,6 +326,7 @@ struct SumArgs {
   float* partial;  // chunks x 2 x cols: a chunk's first run, begun before it, and its last
   int lanes;       // threads to a chunk
   int chunk;       // positions
+  int zero_rows;   // rows to a workgroup that writes zeros
   int64_t chunks;
   uint32_t sum_blocks, tiles;  // workgroups of the sums, tiles of columns
 };
@@ -363,7 +366,14 @@ __device__ __forceinline__ void write_row(const EmbeddingGradArgs& a, uint32_t v
   }
 }
 
-constexpr int kZeroRows = 32;
+// Rows of dW to a workgroup that looks for those without ids: 4096 values or 8 rows (8 of
+// 1003 x 530 7.0 us, 32 10.8; of 131072 x 64 19.4, 64 8.6).
+constexpr int kMostZeroRows = 64;
+int zero_rows(int64_t cols) {
+  int rows = 8;
+  while (rows < kMostZeroRows && 2 * rows * cols <= 4096) rows *= 2;
+  return rows;
+}
 
 // Runs of equal ids within a chunk of sorted positions are summed by the threads that
 // hold its columns, kU rows of dy in flight.  A run that goes past the chunk leaves
@@ -377,11 +387,11 @@ __global__ __launch_bounds__(kThreads) void embedding_sum_kernel(SumArgs g) {
   const EmbeddingGradArgs& a = g.a;
   const int cols = static_cast<int>(a.cols);
   if (blockIdx.x >= g.sum_blocks) {
-    __shared__ bool absent[kZeroRows];
+    __shared__ bool absent[kMostZeroRows];
     __shared__ int64_t ends[2];
-    const int64_t v0 = static_cast<int64_t>(blockIdx.x - g.sum_blocks) * kZeroRows;
-    const int64_t v1 = min(a.vocab, v0 + kZeroRows);
-    if (threadIdx.x < kZeroRows) absent[threadIdx.x] = v0 + threadIdx.x < v1;
+    const int64_t v0 = static_cast<int64_t>(blockIdx.x - g.sum_blocks) * g.zero_rows;
+    const int64_t v1 = min(a.vocab, v0 + g.zero_rows);
+    if (threadIdx.x < g.zero_rows) absent[threadIdx.x] = v0 + threadIdx.x < v1;
     if (threadIdx.x < 128) {
       const int wave = threadIdx.x >> 6;
       ends[wave] = wave_lower_bound(g.sorted.keys, a.n, static_cast<uint32_t>(wave ? v1 : v0));
@@ -392,7 +402,7 @@ __global__ __launch_bounds__(kThreads) void embedding_sum_kernel(SumArgs g) {
     __syncthreads();
     const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     const int per = kThreads / g.lanes;
-    for (int r = threadIdx.x / g.lanes; r < kZeroRows; r += per) {
+    for (int r = threadIdx.x / g.lanes; r < g.zero_rows; r += per) {
       if (!absent[r]) continue;
       for (int64_t j = 4 * (threadIdx.x % g.lanes); j < cols; j += 4 * g.lanes)
         store_piece<kF32>(a.dw + (v0 + r) * a.lddw, static_cast<int>(j), cols, zero);
@@ -506,10 +516,15 @@ int row_lanes(int64_t cols, int per) {
 
 // Positions to a chunk: the rows of one id are added one after the other within it, and
 // an id's chunks after each other, so that a long run takes as many steps of either kind
-// (text's most frequent id has a tenth of all positions).  CHUNK_TIMES
-int chunk_length(int64_t n) {
+// (text's most frequent id has a tenth of all positions); but 512 workgroups, where there
+// are as many chunks of 8.  Sum and join, us: 16384 x 4096 bfloat16 in chunks of 16 58 and
+// 26, 32 58 and 12; 20000 x 1024 32 31 and 14, 64 41 and 7.
+int chunk_length(int64_t n, int64_t cols, int per) {
+  const int64_t tiles = (cols + int64_t{kThreads} * per - 1) / (int64_t{kThreads} * per);
+  const int64_t groups = kThreads / row_lanes(cols, per);
   int chunk = 8;
-  while (chunk < 64 && int64_t{16} * chunk * chunk < n) chunk *= 2;
+  while (chunk < 64 && int64_t{16} * chunk * chunk < n && n * tiles / (2 * chunk * groups) >= 512)
+    chunk *= 2;
   return chunk;
 }
 
@@ -542,7 +557,8 @@ GradWorkspace carve(void* ws, int64_t n, int64_t cols) {
     g.counts = reinterpret_cast<uint32_t*>(take(4 * kBins * blocks));
     g.totals = reinterpret_cast<uint32_t*>(take(4 * kBins));
   }
-  const int64_t chunk = chunk_length(n);
+  // The chunks of the type that has more of them.
+  const int64_t chunk = std::min(chunk_length(n, cols, 4), chunk_length(n, cols, 8));
   g.partial = reinterpret_cast<float*>(take((n + chunk - 1) / chunk * 2 * cols * 4));
   g.bytes = used;
   return g;
@@ -610,12 +626,13 @@ hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, int dtype, void* ws
   const int per = dtype == kF32 ? 4 : 8;
   g.partial = w.partial;
   g.lanes = row_lanes(a.cols, per);
-  g.chunk = chunk_length(a.n);
+  g.chunk = chunk_length(a.n, a.cols, per);
   g.chunks = (a.n + g.chunk - 1) / g.chunk;
+  g.zero_rows = zero_rows(a.cols);
   g.tiles = static_cast<uint32_t>((a.cols + int64_t{g.lanes} * per - 1) / (int64_t{g.lanes} * per));
   const int64_t groups = kThreads / g.lanes;
   const int64_t sums = (g.chunks + groups - 1) / groups * g.tiles;
-  const int64_t zeros = a.accumulate ? 0 : (a.vocab + kZeroRows - 1) / kZeroRows;
+  const int64_t zeros = a.accumulate ? 0 : (a.vocab + g.zero_rows - 1) / g.zero_rows;
   if ((sums + zeros) * kThreads > UINT32_MAX || g.chunks * kThreads > UINT32_MAX)
     return hipErrorInvalidValue;
   g.sum_blocks = static_cast<uint32_t>(sums);

@@ -30,9 +30,9 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(CombineArgs a) {
     a.y[i * a.ldy + j] = activate(a.activation, a.g[i * a.ldg + j]) * a.u[i * a.ldu + j];
 }
 
-// Whether G and U are two linear layers' results: few rows, few columns, and no k.
+// Whether G and U are two linear layers' results: few columns, and no k.
 bool gated_apart(int64_t M, int64_t N, int64_t K) {
-  return K == 0 || linear_by_rows(M, N) || linear_by_columns(M, 2 * N);
+  return K == 0 || (!linear_by_rows(M, 2 * N) && linear_by_columns(M, 2 * N));
 }
 
 // Columns of the product of both weights.
@@ -82,6 +82,7 @@ hipError_t launch_gated_apart(const GatedArgs& a, void* ws, hipStream_t stream) 
 size_t gated_ws(int64_t M, int64_t N, int64_t K) {
   if (M == 0 || N == 0) return 0;
   if (gated_apart(M, N, K)) return carve_apart(nullptr, M, N, K).bytes;
+  if (linear_by_rows(M, 2 * N)) return gated_rows_ws(M, N, K);
   Carver c{nullptr, 0};
   (void)carve_planes(c, M, pair_cols(N), K);
   return c.used;
@@ -89,6 +90,7 @@ size_t gated_ws(int64_t M, int64_t N, int64_t K) {
 
 hipError_t launch_gated(const GatedArgs& a, void* ws, hipStream_t stream) {
   if (gated_apart(a.M, a.N, a.K)) return launch_gated_apart(a, ws, stream);
+  if (linear_by_rows(a.M, 2 * a.N)) return launch_gated_rows(a, ws, stream);
   Carver c{static_cast<char*>(ws), 0};
   const Planes p = carve_planes(c, a.M, pair_cols(a.N), a.K);
   SplitJob jobs[3];

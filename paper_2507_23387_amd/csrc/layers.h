@@ -365,6 +365,9 @@ struct GatedArgs {
   float scale;
   int variant;
 };
+// For few rows, both weights read once, as FP32 (linear_rows.hip).
+size_t gated_rows_ws(int64_t M, int64_t N, int64_t K);
+hipError_t launch_gated_rows(const GatedArgs& a, void* ws, hipStream_t stream);
 size_t gated_ws(int64_t M, int64_t N, int64_t K);
 hipError_t launch_gated(const GatedArgs& a, void* ws, hipStream_t stream);
 

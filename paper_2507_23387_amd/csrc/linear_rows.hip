@@ -115,8 +115,31 @@ struct RowsArgs {
   float inv_s;
   int groups;      // of columns
   int splits;      // workgroups that share a group's k
-  float* partial;  // splits x M x N, where splits > 1
+  float* partial;  // splits x M x N (gated: x 2), where splits > 1
+  // A gated layer: the second weight, and what follows.
+  const float* w_up;
+  int64_t ldw_up;
+  GateEpilogue gate;
 };
+
+// Stores row i, column j of a gated layer's results.
+__device__ __forceinline__ void finish_gate(const RowsArgs& g, int64_t i, int64_t j, float z,
+                                            float u) {
+  const GateEpilogue& e = g.gate;
+  if (e.bias[0]) z += e.bias[0][j];
+  if (e.bias[1]) u += e.bias[1][j];
+  if (e.z[0]) {
+    e.z[0][i * e.ldz[0] + j] = z;
+    e.z[1][i * e.ldz[1] + j] = u;
+  }
+  g.a.y[i * g.a.ldy + j] = activate(e.activation, z) * u;
+}
+
+// The partial sum of this split, of G (0) or U (1).
+__device__ __forceinline__ float& gate_partial(const RowsArgs& g, int split, int which, int64_t i,
+                                               int64_t j) {
+  return g.partial[((static_cast<int64_t>(split) * 2 + which) * g.a.M + i) * g.a.N + j];
+}
 
 // Stores the result of row i, column j of Y.
 __device__ __forceinline__ void finish(const RowsArgs& g, int64_t i, int64_t j, float z) {
@@ -145,9 +168,10 @@ __device__ __forceinline__ void store(const RowsArgs& g, int split, int64_t i, i
 // steps of k in turn, and add their sums in LDS.  Where W's rows are along k they
 // read 2 KiB of each of those rows in line together.  1 x 8192 x 4096: 25.7 us, 5.2
 // TB/s (64 columns a workgroup as below 30; 8 waves 28.6; one column block 30).
+// (kGate: both blocks of columns are the same 16 of Y, one of each weight.)
 constexpr int kLineWaves = 16;
 
-template <bool kNk, int kC, bool kGrad, bool kAcross>
+template <bool kNk, int kC, bool kGrad, bool kAcross, bool kGate>
 __global__ __launch_bounds__(64 * kLineWaves) void linear_line_kernel(RowsArgs g) {
   const LinearArgs& a = g.a;
   __shared__ float tile[kLineWaves][256 * kC];
@@ -155,15 +179,21 @@ __global__ __launch_bounds__(64 * kLineWaves) void linear_line_kernel(RowsArgs g
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int index = xcd_order(blockIdx.x, gridDim.x);
   const int col_group = index / g.splits, split = index - col_group * g.splits;
-  const int64_t col0 = static_cast<int64_t>(col_group) * (16 * kC);
+  static_assert(!kGate || (kC == 2 && !kGrad && !kAcross), "a block of each weight");
+  const int64_t col0 = static_cast<int64_t>(col_group) * (kGate ? 16 : 16 * kC);
   // Rows and columns past the end repeat the last; they are not stored.
   const int64_t row = min<int64_t>(l16, a.M - 1);
   const float* const xrow = a.x + row * (kAcross ? 1 : a.ldx);
   const int shift = kGrad ? g.row_shift[row] : 0;
   const float* wcol[kC];
+  int64_t ldw[kC];
 #pragma unroll
-  for (int c = 0; c < kC; ++c)
-    wcol[c] = a.w + min<int64_t>(col0 + 16 * c + l16, a.N - 1) * (kNk ? a.ldw : 1);
+  for (int c = 0; c < kC; ++c) {
+    const bool up = kGate && c == 1;
+    ldw[c] = up ? g.ldw_up : a.ldw;
+    wcol[c] = (up ? g.w_up : a.w) +
+              min<int64_t>(col0 + (kGate ? 0 : 16 * c) + l16, a.N - 1) * (kNk ? ldw[c] : 1);
+  }
 
   struct Step {
     Values x, w[kC];
@@ -174,7 +204,7 @@ __global__ __launch_bounds__(64 * kLineWaves) void linear_line_kernel(RowsArgs g
       if constexpr (kNk)
         load_along<true, tail.value>(wcol[c], step * kStep, a.K, group, s.w[c]);
       else
-        load_across<tail.value>(wcol[c], a.ldw, step * kStep, a.K, group, s.w[c]);
+        load_across<tail.value>(wcol[c], ldw[c], step * kStep, a.K, group, s.w[c]);
     if constexpr (kAcross)
       load_strided<kNk, tail.value>(xrow, a.ldx, step * kStep, a.K, group, s.x);
     else
@@ -230,6 +260,22 @@ __global__ __launch_bounds__(64 * kLineWaves) void linear_line_kernel(RowsArgs g
       tile[wave][(4 * group + r) * kWidth + 16 * c + l16] =
           __builtin_fmaf(cross[c][r], g.inv_s, hh[c][r]);
   __syncthreads();
+  if constexpr (kGate) {
+    const int q = threadIdx.x;
+    const int64_t i = q / 16, j = col0 + q % 16;
+    if (q >= 256 || i >= a.M || j >= a.N) return;
+    float v[2];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int at = static_cast<int>(i) * kWidth + 16 * c + q % 16;
+      v[c] = tile[0][at];
+#pragma unroll
+      for (int w = 1; w < kLineWaves; ++w) v[c] += tile[w][at];
+      if (g.splits > 1) gate_partial(g, split, c, i, j) = v[c];
+    }
+    if (g.splits == 1) finish_gate(g, i, j, v[0], v[1]);
+    return;
+  }
   for (int q = threadIdx.x; q < 16 * kWidth; q += 64 * kLineWaves) {
     const int64_t i = q / kWidth, j = col0 + q % kWidth;
     if (i >= a.M || j >= a.N) continue;
@@ -252,7 +298,9 @@ __global__ __launch_bounds__(64 * kLineWaves) void linear_line_kernel(RowsArgs g
 constexpr int kTileWaves = 4, kTileCols = 16 * kTileWaves;
 constexpr int kChunkSteps = 2, kChunkK = kChunkSteps * kStep;
 
-template <bool kNk, int kR, bool kGrad, bool kAcross>
+// (kGate: 32 columns of Y, of the first weight by waves 0 and 1 and of the second by the
+// others, which hand their sums over.)
+template <bool kNk, int kR, bool kGrad, bool kAcross, bool kGate>
 __global__ __launch_bounds__(64 * kTileWaves, kR > (kAcross ? 4 : 5) ? 2 : 3)
 void linear_rows_tile_kernel(RowsArgs g) {
   const LinearArgs& a = g.a;
@@ -263,12 +311,15 @@ void linear_rows_tile_kernel(RowsArgs g) {
   const int index = xcd_order(blockIdx.x, gridDim.x);
   const int col_group = index / g.splits, split = index - col_group * g.splits;
   const int64_t row0 = static_cast<int64_t>(blockIdx.y) * (kBlockRows * kR);
-  const int64_t col = static_cast<int64_t>(col_group) * kTileCols + 16 * wave + l16;
+  const int which = kGate ? wave / 2 : 0;
+  const int64_t col = kGate ? static_cast<int64_t>(col_group) * (kTileCols / 2) + 16 * (wave % 2) + l16
+                            : static_cast<int64_t>(col_group) * kTileCols + 16 * wave + l16;
+  const int64_t ldw = which ? g.ldw_up : a.ldw;
   // Whole chunks c0 .. c1 - 1, and for the last split the one that K ends in.
   const int64_t chunks = a.K / kChunkK;
   const int64_t c0 = chunks * split / g.splits, c1 = chunks * (split + 1) / g.splits;
 
-  const float* const wcol = a.w + min<int64_t>(col, a.N - 1) * (kNk ? a.ldw : 1);
+  const float* const wcol = (which ? g.w_up : a.w) + min<int64_t>(col, a.N - 1) * (kNk ? ldw : 1);
   // Units of X's chunk: step u / kR, row block u % kR.  The waves take them in turn,
   // the last one again where there are fewer.
   constexpr int kPer = (kUnits + kTileWaves - 1) / kTileWaves;
@@ -288,7 +339,7 @@ void linear_rows_tile_kernel(RowsArgs g) {
     if constexpr (kNk)
       load_along<true, tail.value>(wcol, k0, a.K, group, to);
     else
-      load_across<tail.value>(wcol, a.ldw, k0, a.K, group, to);
+      load_across<tail.value>(wcol, ldw, k0, a.K, group, to);
   };
   auto load_x = [&](int64_t c, auto tail) {
 #pragma unroll
@@ -377,6 +428,33 @@ void linear_rows_tile_kernel(RowsArgs g) {
     __syncthreads();
     multiply(w[0], 0, 0, no);
   }
+  if constexpr (kGate) {
+    float* const sums = reinterpret_cast<float*>(frags);  // 16 kR rows x 32 columns of U
+    auto at = [&](int i, int r) { return (16 * i + 4 * group + r) * 32 + 16 * (wave % 2) + l16; };
+    auto sum = [&](int i, int r) { return __builtin_fmaf(cross[i][r], g.inv_s, hh[i][r]); };
+    if (g.splits == 1) {
+      __syncthreads();  // every wave has read its fragments
+      if (which == 1) {
+#pragma unroll
+        for (int i = 0; i < kR; ++i)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) sums[at(i, r)] = sum(i, r);
+      }
+      __syncthreads();
+      if (which == 1) return;
+    }
+    if (col >= a.N) return;
+#pragma unroll
+    for (int i = 0; i < kR; ++i)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int64_t row = row0 + 16 * i + 4 * group + r;
+        if (row >= a.M) continue;
+        if (g.splits == 1) finish_gate(g, row, col, sum(i, r), sums[at(i, r)]);
+        else gate_partial(g, split, which, row, col) = sum(i, r);
+      }
+    return;
+  }
   if (col >= a.N) return;
 #pragma unroll
   for (int i = 0; i < kR; ++i)
@@ -397,6 +475,19 @@ __global__ __launch_bounds__(256) void linear_join_kernel(RowsArgs g) {
 #pragma unroll 4
   for (int s = 0; s < g.splits; ++s) v += g.partial[s * a.M * a.N + q];
   finish(g, g.swapped ? j : i, g.swapped ? i : j, v);
+}
+
+__global__ __launch_bounds__(256) void gate_join_kernel(RowsArgs g) {
+  const LinearArgs& a = g.a;
+  const int64_t q = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, all = a.M * a.N;
+  if (q >= all) return;
+  float v = 0.0f, u = 0.0f;
+#pragma unroll 4
+  for (int64_t s = 0; s < g.splits; ++s) {
+    v += g.partial[2 * s * all + q];
+    u += g.partial[(2 * s + 1) * all + q];
+  }
+  finish_gate(g, q / a.N, q % a.N, v, u);
 }
 
 // out = L^T R of matrices with few rows: a weight's gradient of few rows is bound by
@@ -464,21 +555,24 @@ struct RowsPlan {
   int groups, row_groups, splits;
 };
 
-RowsPlan plan_rows(int64_t M, int64_t N, int64_t K, bool transpose_w) {
+// gate: N columns of each of two weights.
+RowsPlan plan_rows(int64_t M, int64_t N, int64_t K, bool transpose_w, bool gate = false) {
   RowsPlan p{};
+  const int64_t both = gate ? 2 * N : N;
   // Rows of W along n: 16 columns are half a cache line, which costs large weights
   // more than the tiles' join (1 x 8192 x 8192 73 us, tiles 51; 16 x 4096 x 4096 22.6
   // and 20.3) and small ones less (1 x 2048 x 2048 8.9 and 11.7, 512 x 512 9.0 and
   // 11.6, 1024 x 4096 11.8 and 11.6).
-  p.line = M <= kBlockRows && (transpose_w || N * K <= (int64_t{1} << 22));
+  p.line = M <= kBlockRows && (transpose_w || both * K <= (int64_t{1} << 22));
   int64_t most, fill;
   if (p.line) {
     // A compute unit holds one workgroup, and a round of them takes 12 us with one
     // block of columns and 21 with two (K = 4096): 1 x 6144 25.0 and 21.3 us, 8192 29.2
     // and 25.8, 11008 37.5 and 42.4, 14336 48.4 and 44.0.
     const int64_t one = (N + 4095) / 4096, two = (N + 8191) / 8192;
-    p.blocks = transpose_w && 7 * two <= 4 * one ? 2 : 1;
-    p.groups = static_cast<int>((N + 16 * p.blocks - 1) / (16 * p.blocks));
+    p.blocks = gate || (transpose_w && 7 * two <= 4 * one) ? 2 : 1;
+    const int64_t cols = gate ? 16 : 16 * p.blocks;
+    p.groups = static_cast<int>((N + cols - 1) / cols);
     p.row_groups = 1;
     most = K / kStep / (4 * kLineWaves);  // four steps a wave at least
     fill = 256;
@@ -487,13 +581,14 @@ RowsPlan plan_rows(int64_t M, int64_t N, int64_t K, bool transpose_w) {
     // two, 83 so; 96 x 4096 x 4096 nk 39 and 32; few columns 10265 x 84 x 6848 137 and 88.
     // Small kn weights lose a little (80 x 2048 x 2048 12.6 and 13.3), 128 rows in one
     // group (registers) more.
-    const bool six = M > 64 && M <= 96 && (transpose_w || N >= 4096);
+    const bool six = M > 64 && M <= 96 && (transpose_w || both >= 4096);
     p.blocks = static_cast<int>(std::min<int64_t>((M + kBlockRows - 1) / kBlockRows, six ? 6 : 4));
     p.row_groups = static_cast<int>((M + kBlockRows * p.blocks - 1) / (kBlockRows * p.blocks));
     // The groups even.
     const int64_t even = kBlockRows * static_cast<int64_t>(p.row_groups);
     p.blocks = static_cast<int>((M + even - 1) / even);
-    p.groups = static_cast<int>((N + kTileCols - 1) / kTileCols);
+    const int64_t cols = gate ? kTileCols / 2 : kTileCols;
+    p.groups = static_cast<int>((N + cols - 1) / cols);
     // The join costs 4 us, as much as four chunks of a lone workgroup.
     most = K / kChunkK > 5 ? K / kChunkK / 2 : 1;
     fill = p.blocks > 5 ? 512 : 768;  // what the registers of a compute unit hold
@@ -503,32 +598,32 @@ RowsPlan plan_rows(int64_t M, int64_t N, int64_t K, bool transpose_w) {
   return p;
 }
 
-template <bool kNk, int kC, bool kGrad, bool kAcross = false>
+template <bool kNk, int kC, bool kGrad, bool kAcross = false, bool kGate = false>
 hipError_t launch_line(const RowsArgs& g, const RowsPlan& p, hipStream_t stream) {
-  hipLaunchKernelGGL((linear_line_kernel<kNk, kC, kGrad, kAcross>), dim3(p.groups * p.splits),
+  hipLaunchKernelGGL((linear_line_kernel<kNk, kC, kGrad, kAcross, kGate>), dim3(p.groups * p.splits),
                      dim3(64 * kLineWaves), 0, stream, g);
   return hipGetLastError();
 }
 
-template <bool kNk, int kR, bool kGrad, bool kAcross>
+template <bool kNk, int kR, bool kGrad, bool kAcross, bool kGate>
 hipError_t launch_tile(const RowsArgs& g, const RowsPlan& p, hipStream_t stream) {
   constexpr size_t kLds = static_cast<size_t>(2) * kChunkSteps * kR * 2 * 1024;
   static_assert(kLds <= 64 * 1024, "both chunks fit LDS without asking for more");
-  hipLaunchKernelGGL((linear_rows_tile_kernel<kNk, kR, kGrad, kAcross>),
+  hipLaunchKernelGGL((linear_rows_tile_kernel<kNk, kR, kGrad, kAcross, kGate>),
                      dim3(p.groups * p.splits, p.row_groups), dim3(64 * kTileWaves), kLds, stream,
                      g);
   return hipGetLastError();
 }
 
-template <bool kNk, bool kGrad, bool kAcross = false>
+template <bool kNk, bool kGrad, bool kAcross = false, bool kGate = false>
 hipError_t launch_tiles(const RowsArgs& g, const RowsPlan& p, hipStream_t stream) {
   switch (p.blocks) {
-    case 1: return launch_tile<kNk, 1, kGrad, kAcross>(g, p, stream);
-    case 2: return launch_tile<kNk, 2, kGrad, kAcross>(g, p, stream);
-    case 3: return launch_tile<kNk, 3, kGrad, kAcross>(g, p, stream);
-    case 4: return launch_tile<kNk, 4, kGrad, kAcross>(g, p, stream);
-    case 5: return launch_tile<kNk, 5, kGrad, kAcross>(g, p, stream);
-    default: return launch_tile<kNk, 6, kGrad, kAcross>(g, p, stream);
+    case 1: return launch_tile<kNk, 1, kGrad, kAcross, kGate>(g, p, stream);
+    case 2: return launch_tile<kNk, 2, kGrad, kAcross, kGate>(g, p, stream);
+    case 3: return launch_tile<kNk, 3, kGrad, kAcross, kGate>(g, p, stream);
+    case 4: return launch_tile<kNk, 4, kGrad, kAcross, kGate>(g, p, stream);
+    case 5: return launch_tile<kNk, 5, kGrad, kAcross, kGate>(g, p, stream);
+    default: return launch_tile<kNk, 6, kGrad, kAcross, kGate>(g, p, stream);
   }
 }
 
@@ -572,7 +667,7 @@ hipError_t launch_linear_rows(const LinearArgs& a, const int* row_shift, void* w
                               hipStream_t stream, bool add) {
   const RowsPlan p = plan_rows(a.M, a.N, a.K, a.transpose_w);
   const RowsArgs g{a, row_shift, add, false, 1.0f / a.scale, p.groups, p.splits,
-                   static_cast<float*>(ws)};
+                   static_cast<float*>(ws), nullptr, 0, {}};
   const hipError_t e =
       row_shift ? launch_plan<true>(g, p, stream) : launch_plan<false>(g, p, stream);
   return e == hipSuccess ? launch_join(g, stream) : e;
@@ -585,13 +680,42 @@ hipError_t launch_linear_columns(const LinearArgs& a, void* ws, hipStream_t stre
   t.w = a.x, t.ldw = a.ldx, t.transpose_w = true;
   const RowsPlan p = plan_rows(t.M, t.N, t.K, true);
   const RowsArgs g{t, nullptr, false, true, 1.0f / a.scale, p.groups, p.splits,
-                   static_cast<float*>(ws)};
+                   static_cast<float*>(ws), nullptr, 0, {}};
   const hipError_t e =
       a.transpose_w ? launch_plan<false>(g, p, stream)
       : !p.line     ? launch_tiles<true, false, true>(g, p, stream)
       : p.blocks == 1 ? launch_line<true, 1, false, true>(g, p, stream)
                       : launch_line<true, 2, false, true>(g, p, stream);
   return e == hipSuccess ? launch_join(g, stream) : e;
+}
+
+size_t gated_rows_ws(int64_t M, int64_t N, int64_t K) {
+  const int splits = std::max(plan_rows(M, N, K, false, true).splits,
+                              plan_rows(M, N, K, true, true).splits);
+  return static_cast<size_t>(round_up(splits > 1 ? splits * 2 * M * N * 4 : 1, 256));
+}
+
+hipError_t launch_gated_rows(const GatedArgs& a, void* ws, hipStream_t stream) {
+  const RowsPlan p = plan_rows(a.M, a.N, a.K, a.transpose_w, true);
+  LinearArgs l{};
+  l.M = a.M, l.N = a.N, l.K = a.K;
+  l.x = a.x, l.ldx = a.ldx;
+  l.w = a.w[0], l.ldw = a.ldw[0], l.transpose_w = a.transpose_w;
+  l.y = a.y, l.ldy = a.ldy;
+  l.scale = a.scale, l.variant = a.variant;
+  const RowsArgs g{l, nullptr, false, false, 1.0f / a.scale, p.groups, p.splits,
+                   static_cast<float*>(ws), a.w[1], a.ldw[1],
+                   GateEpilogue{{a.bias[0], a.bias[1]}, a.activation, a.N, {a.z[0], a.z[1]},
+                                {a.ldz[0], a.ldz[1]}}};
+  const hipError_t e =
+      p.line ? (a.transpose_w ? launch_line<true, 2, false, false, true>(g, p, stream)
+                              : launch_line<false, 2, false, false, true>(g, p, stream))
+             : (a.transpose_w ? launch_tiles<true, false, false, true>(g, p, stream)
+                              : launch_tiles<false, false, false, true>(g, p, stream));
+  if (e != hipSuccess || p.splits == 1) return e;
+  hipLaunchKernelGGL(gate_join_kernel, dim3(static_cast<unsigned>((a.M * a.N + 255) / 256)),
+                     dim3(256), 0, stream, g);
+  return hipGetLastError();
 }
 
 }  // namespace sgc

@@ -380,7 +380,8 @@ __global__ __launch_bounds__(kThreads) void columns_kernel(ColumnArgs a, int64_t
 }
 
 // columns_kernel for a gated layer: the strip's columns of dG and dU from the same three
-// loads, both written as a half of D.  HBM bounds it, 20 bytes an entry: GATE_COLUMNS_TIME.
+// loads, both written as a half of D.  HBM bounds it, 20 bytes an entry: 4096 x 8192
+// with SiLU 134 us, 5.0 TB/s.
 __global__ __launch_bounds__(kThreads) void gate_columns_kernel(GateColumnArgs a,
                                                                 int64_t slab_rows) {
   constexpr int kStride = kThreads / 32;
