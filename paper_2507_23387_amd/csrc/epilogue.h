@@ -21,7 +21,7 @@ constexpr bool kElementwiseOnly =
 struct NoEpilogue {};
 template <class Epi>
 constexpr bool kThroughLds =
-    std::is_same<Epi, Epilogue>::value || std::is_same<Epi, GateEpilogue>::value;
+    !std::is_same<Epi, NoEpilogue>::value && !std::is_same<Epi, Unscale>::value;
 
 // The shifts of a wave's kBlocks x 16 rows (or columns) from `first` on, 64 lines at a
 // time, one a lane, which hand them out: all of a lane's own are more than the wide
@@ -41,163 +41,13 @@ struct LineShifts {
   }
 };
 
-// Blocks of 16 rows or columns to a stretch (TileGrain): a wave's, but of its 128 half,
-// which the fallback's waves have.
-template <int kSub>
-constexpr int kGrainBlocks = kSub == 8 ? 4 : kSub;
-
-// Each row's largest logit in a stretch and the sum of the exponentials below it, by the 16
-// lanes that hold them; the lane with a row's target leaves that.
-template <bool kFull, int kSubM, int kSubN, typename F>
-__device__ __forceinline__ void exps_tile(const ExpsEpilogue& e, int M, int N, int row0, int col0,
-                                          F value) {
-  constexpr int kB = kGrainBlocks<kSubN>;
-  const int lane = threadIdx.x & 63, l16 = lane & 15;
-  // The rows' targets as columns of the piece, 64 rows at a time, one a lane (LineShifts).
-  const int first_row = row0 - 4 * (lane >> 4);
-  int held[(kSubM + 3) / 4];
-#pragma unroll
-  for (int h = 0; h < (kSubM + 3) / 4; ++h) {
-    const int64_t t = id_at(e.targets, min(first_row + 64 * h + lane, M - 1));
-    held[h] = t < 0 || t >= e.vocab ? INT32_MIN : static_cast<int>(t - e.first);
-  }
-#pragma unroll
-  for (int j0 = 0; j0 < kSubN; j0 += kB) {
-    const int col = col0 + 16 * j0;  // this lane's first
-    if (!kFull && col - l16 >= N) break;
-    Exps* const out = e.exps + (e.slot0 + (col - l16) / (16 * kB)) * M;
-    float bias[kB];
-#pragma unroll
-    for (int j = 0; j < kB; ++j)
-      bias[j] = e.bias && (kFull || col + 16 * j < N) ? e.bias[e.first + col + 16 * j] : 0.0f;
-#pragma unroll
-    for (int i = 0; i < kSubM; ++i) {
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int row = row0 + 16 * i + r;
-        float v[kB], top = -__builtin_inff();
-#pragma unroll
-        for (int j = 0; j < kB; ++j) {
-          v[j] = kFull || col + 16 * j < N ? value(i, j0 + j, r) + bias[j] : -__builtin_inff();
-          top = __builtin_fmaxf(top, v[j]);
-        }
-        top = max_of_16(top);
-        const float base = top == -__builtin_inff() ? 0.0f : top;
-        float sum = 0.0f;
-#pragma unroll
-        for (int j = 0; j < kB; ++j) sum += exp_of(v[j] - base);
-        sum = sum_of_16(sum);
-        if (l16 == 0 && (kFull || row < M)) out[row] = Exps{top, sum};
-        const int t = __shfl(held[i / 4], i % 4 * 16 + 4 * (lane >> 4) + r) - col;
-        const bool hit = static_cast<unsigned>(t) < 16 * kB && t % 16 == 0 && (kFull || row < M);
-        if (__ballot(hit)) {
-          float z = v[0];
-#pragma unroll
-          for (int j = 1; j < kB; ++j) z = t == 16 * j ? v[j] : z;
-          if (hit) e.at[row] = z;
-        }
-      }
-      SCHED_FENCE();
-    }
-  }
-}
-
-// D in place of the product, and its lines' largest magnitudes and sums.  A lane holds the
-// terms of one of 64 rows and hands them out: read by all from memory they made a tile of
-// 256 x 256 wait 30 us longer.
-template <bool kFull, int kSubM, int kSubN, typename F>
-__device__ __forceinline__ void xent_grad_tile(const XentGradEpilogue& e, float* __restrict__ C,
-                                               int64_t ldc, int M, int N, int row0, int col0,
-                                               F value) {
-  constexpr int kBM = kGrainBlocks<kSubM>, kBN = kGrainBlocks<kSubN>, kParts = kSubN / kBN;
-  const int lane = threadIdx.x & 63, l16 = lane & 15;
-  const int64_t ld_top = (N + kColumnStrip - 1) / kColumnStrip * kColumnStrip;
-  float bias[kSubN];
-#pragma unroll
-  for (int j = 0; j < kSubN; ++j)
-    bias[j] = e.bias && (kFull || col0 + 16 * j < N) ? e.bias[e.first + col0 + 16 * j] : 0.0f;
-#pragma unroll
-  for (int i0 = 0; i0 < kSubM; i0 += kBM) {
-    const int first_row = row0 - 4 * (lane >> 4) + 16 * i0;
-    if (!kFull && first_row >= M) break;
-    const RowTerms mine(min(first_row + (lane < 16 * kBM ? lane : 0), M - 1), e.vocab, e.targets,
-                        e.dloss, e.dlse, e.lse);
-    const int target = mine.target < 0 ? INT32_MIN : static_cast<int>(mine.target - e.first);
-    float sum[kSubN], top[kSubN];
-#pragma unroll
-    for (int j = 0; j < kSubN; ++j) sum[j] = top[j] = 0.0f;
-#pragma unroll
-    for (int i = i0; i < i0 + kBM; ++i) {
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int row = row0 + 16 * i + r, from = 16 * (i - i0) + 4 * (lane >> 4) + r;
-        const float lse = __shfl(mine.lse, from), c = __shfl(mine.c, from);
-        const int hit = __shfl(target, from) - col0;
-        float d[kSubN];
-#pragma unroll
-        for (int j = 0; j < kSubN; ++j) d[j] = exp_of(value(i, j, r) + bias[j] - lse) * c;
-        if (__ballot(static_cast<unsigned>(hit) < 16 * kSubN)) {
-          const float off = __shfl(mine.d, from);
-#pragma unroll
-          for (int j = 0; j < kSubN; ++j) d[j] = hit == 16 * j ? d[j] - off : d[j];
-        }
-        float* const at = C + static_cast<int64_t>(row) * ldc + col0;
-        float most[kParts];
-#pragma unroll
-        for (int q = 0; q < kParts; ++q) most[q] = 0.0f;
-#pragma unroll
-        for (int j = 0; j < kSubN; ++j) {
-          if (kFull || (row < M && col0 + 16 * j < N)) at[16 * j] = d[j];
-          else d[j] = 0.0f;
-          const float b = finite_magnitude(d[j]);
-          sum[j] += d[j];
-          top[j] = __builtin_fmaxf(top[j], b);
-          most[j / kBN] = __builtin_fmaxf(most[j / kBN], b);
-        }
-        if (e.row_top) {
-#pragma unroll
-          for (int q = 0; q < kParts; ++q) {
-            const int col = col0 - l16 + 16 * kBN * q;
-            const float m = max_of_16(most[q]);
-            if (l16 == 0 && (kFull || (row < M && col < N)))
-              e.row_top[static_cast<int64_t>(col / (16 * kBN)) * M + row] = m;
-          }
-        }
-        SCHED_FENCE();
-      }
-    }
-    const int64_t slab = first_row / (16 * kBM);
-#pragma unroll
-    for (int j = 0; j < kSubN; ++j) {
-      sum[j] += __shfl_xor(sum[j], 16);
-      top[j] = __builtin_fmaxf(top[j], __shfl_xor(top[j], 16));
-      sum[j] += __shfl_xor(sum[j], 32);
-      top[j] = __builtin_fmaxf(top[j], __shfl_xor(top[j], 32));
-      const int col = col0 + 16 * j;
-      if (lane >= 16 || (!kFull && col >= N)) continue;
-      e.sums[slab * N + col] = sum[j];
-      if (e.col_top) e.col_top[slab * ld_top + col] = top[j];
-    }
-  }
-}
-
 // store_tile16, for Unscale each entry times 2^-shift of its row or column (and added to
 // C's).
 template <int kSubM, int kSubN, class Epi, typename F>
 __device__ __forceinline__ void store_product(const Epi& epi, float* __restrict__ C, int64_t ldc,
                                               int M, int N, int row0, int col0, bool full,
                                               F value) {
-  if constexpr (std::is_same<Epi, ExpsEpilogue>::value) {
-    if (full)
-      exps_tile<true, kSubM, kSubN>(epi, M, N, row0, col0, value);
-    else
-      exps_tile<false, kSubM, kSubN>(epi, M, N, row0, col0, value);
-  } else if constexpr (std::is_same<Epi, XentGradEpilogue>::value) {
-    if (full)
-      xent_grad_tile<true, kSubM, kSubN>(epi, C, ldc, M, N, row0, col0, value);
-    else
-      xent_grad_tile<false, kSubM, kSubN>(epi, C, ldc, M, N, row0, col0, value);
-  } else if constexpr (!std::is_same<Epi, Unscale>::value) {
+  if constexpr (!std::is_same<Epi, Unscale>::value) {
     store_tile16<kSubM, kSubN>(C, ldc, M, N, row0, col0, full, value);
   } else if (epi.columns) {
     const int i0 = threadIdx.x & 15;
@@ -450,6 +300,236 @@ __device__ __forceinline__ void epilogue_tile(const GateEpilogue& e, float* stag
       for (int u = 0; u < kU; ++u)
         store_any(Y + static_cast<int64_t>(gr[u]) * ldy + gc[u], v[u] * w[u]);
     }
+  });
+}
+
+// The cross entropy's epilogues.  A wave's rows are staged as above and read back by 4 to 16
+// lanes to a row, each with four adjacent columns of a stretch; taken from the accumulators
+// as they lie, 256 of them in as many copies of the code, registers ran out.  Blocks of 16
+// rows or columns to a stretch (TileGrain): a wave's, but of its 128 half, which the
+// fallback's waves have, and of its 96 half, within 16 lanes' reach.
+template <int kSub>
+constexpr int kGrainBlocks = kSub == 8 ? 4 : kSub == 6 ? 3 : kSub;
+
+// How the rows of a chunk of kN blocks are shared: kLanes lanes to a row (of which kUsed
+// have columns), kU rows a lane at a time.
+template <int kSubN, int kN>
+struct RowLanes {
+  static constexpr int kB = kGrainBlocks<kSubN>;
+  static constexpr int kUsed = 4 * kB, kLanes = kB > 2 ? 16 : kUsed;
+  static constexpr int kRows = 64 / kLanes;  // of a wave
+  static constexpr int kU = 16 * kN < 4 * kRows ? 16 * kN / kRows : 4;
+  static constexpr int kTurns = 16 * kN / (kRows * kU);
+  static_assert(kTurns * kRows * kU == 16 * kN, "whole turns");
+  // The row of this lane in turn p, and its first column of the stretch.
+  static __device__ __forceinline__ int row(int p, int u) {
+    return (p * kU + u) * kRows + static_cast<int>(threadIdx.x & 63) / kLanes;
+  }
+  static __device__ __forceinline__ int column() { return 4 * (threadIdx.x % kLanes); }
+  static __device__ __forceinline__ bool in() {
+    return kUsed == kLanes || threadIdx.x % kLanes < kUsed;
+  }
+
+  // Quads of stretch kPart of turn p's rows, with the bias; lanes past the stretch get
+  // `fill`, as do columns past N.
+  template <int kPart>
+  static __device__ __forceinline__ void read(const float* stage, int p, int col, int N, bool full,
+                                              floatx4 bias, float fill, floatx4 (&v)[kU]) {
+    const int c = 16 * kB * kPart + column();
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const int r = row(p, u);
+      const int at = r * (16 * kSubN) + (c ^ (((r >> 2) & kStageSwap<kSubN>) << 4));
+      v[u] = *reinterpret_cast<const floatx4*>(stage + (in() ? at : 0));
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        v[u][k] += bias[k];
+        if (!in() || (!full && col + k >= N)) v[u][k] = fill;
+      }
+    }
+  }
+};
+
+// Four values of the bias from column `col` of a piece of N, zeros past its end.
+__device__ __forceinline__ floatx4 piece_bias(const float* bias, int64_t first, int col, int N) {
+  floatx4 b{};
+  if (bias) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (col + k < N) b[k] = bias[first + col + k];
+  }
+  return b;
+}
+
+// Each row's largest logit in a stretch and the sum of the exponentials below it; the lane
+// with a row's target leaves that logit.
+template <int kSubM, int kSubN, int kChunk, typename F>
+__device__ __forceinline__ void epilogue_tile(const ExpsEpilogue& e, float* stage, float*,
+                                              int64_t, int M, int N, int row0, int col0, F value) {
+  constexpr int kB = kGrainBlocks<kSubN>, kParts = kSubN / kB;
+  const int lane = threadIdx.x & 63;
+  const bool full = row0 + 16 * kSubM <= M && col0 + 16 * kSubN <= N;
+  // The rows' targets as columns of the piece, 64 rows at a time, one a lane.
+  int held[(kSubM + 3) / 4];
+#pragma unroll
+  for (int h = 0; h < (kSubM + 3) / 4; ++h) {
+    const int64_t t = id_at(e.targets, min(row0 + 64 * h + lane, M - 1));
+    held[h] = t < 0 || t >= e.vocab ? INT32_MIN : static_cast<int>(t - e.first);
+  }
+  static_for<(kSubM + kChunk - 1) / kChunk>([&](auto Cc) {
+    constexpr int i0 = decltype(Cc)::value * kChunk;
+    constexpr int kN = i0 + kChunk <= kSubM ? kChunk : kSubM - i0;
+    static_assert(i0 / 4 == (i0 + kN - 1) / 4, "a chunk's rows are in one register of targets");
+    using L = RowLanes<kSubN, kN>;
+    constexpr int kU = L::kU;
+    stage_rows<i0, kN, kSubN>(stage, value);
+    static_for<kParts>([&](auto Pc) {
+      constexpr int kPart = decltype(Pc)::value;
+      const int first_col = col0 + 16 * kB * kPart, col = first_col + L::column();
+      if (first_col >= N) return;
+      const floatx4 bias = piece_bias(e.bias, e.first, L::in() ? col : N, N);
+      Exps* const out = e.exps + (e.slot0 + first_col / (16 * kB)) * M;
+#pragma unroll 1
+      for (int p = 0; p < L::kTurns; ++p) {
+        floatx4 v[kU];
+        L::template read<kPart>(stage, p, col, N, full, bias, -__builtin_inff(), v);
+        float top[kU], sum[kU];
+        int t[kU];
+        bool any = false;
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+          top[u] = max_of<L::kLanes>(__builtin_fmaxf(__builtin_fmaxf(v[u][0], v[u][1]),
+                                                     __builtin_fmaxf(v[u][2], v[u][3])));
+          const float base = top[u] == -__builtin_inff() ? 0.0f : top[u];
+          sum[u] = 0.0f;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) sum[u] += exp_of(v[u][k] - base);
+          sum[u] = sum_of<L::kLanes>(sum[u]);
+          t[u] = __shfl(held[i0 / 4], (16 * i0 + L::row(p, u)) % 64) - col;
+          any |= static_cast<unsigned>(t[u]) < 4 && L::in();
+        }
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+          const int row = row0 + 16 * i0 + L::row(p, u);
+          if (L::column() == 0 && row < M) out[row] = Exps{top[u], sum[u]};
+        }
+        if (any) {
+#pragma unroll
+          for (int u = 0; u < kU; ++u) {
+            const int row = row0 + 16 * i0 + L::row(p, u);
+            if (static_cast<unsigned>(t[u]) < 4 && row < M)
+              e.at[row] = t[u] == 0 ? v[u][0] : t[u] == 1 ? v[u][1] : t[u] == 2 ? v[u][2] : v[u][3];
+          }
+        }
+      }
+    });
+  });
+}
+
+// D in place of the product, and its lines' largest magnitudes and sums.  A lane holds the
+// terms of one of 64 rows and hands them out: read by all from memory they made a tile of
+// 256 x 256 wait 30 us longer.
+template <int kSubM, int kSubN, int kChunk, typename F>
+__device__ __forceinline__ void epilogue_tile(const XentGradEpilogue& e, float* stage, float* D,
+                                              int64_t ldd, int M, int N, int row0, int col0,
+                                              F value) {
+  constexpr int kBM = kGrainBlocks<kSubM>, kB = kGrainBlocks<kSubN>, kParts = kSubN / kB;
+  const int lane = threadIdx.x & 63;
+  const bool full = row0 + 16 * kSubM <= M && col0 + 16 * kSubN <= N;
+  const int64_t ld_top = (N + kColumnStrip - 1) / kColumnStrip * kColumnStrip;
+  float lse, c, d;
+  int target;
+  floatx4 sum[kParts], top[kParts];
+  static_for<(kSubM + kChunk - 1) / kChunk>([&](auto Cc) {
+    constexpr int i0 = decltype(Cc)::value * kChunk;
+    constexpr int kN = i0 + kChunk <= kSubM ? kChunk : kSubM - i0;
+    static_assert(i0 / kBM == (i0 + kN - 1) / kBM, "a chunk's rows are in one stretch");
+    using L = RowLanes<kSubN, kN>;
+    constexpr int kU = L::kU;
+    if constexpr (i0 % kBM == 0) {
+      const int r = lane < 16 * kBM ? lane : 0;
+      const RowTerms mine(min(row0 + 16 * i0 + r, M - 1), e.vocab, e.targets, e.dloss, e.dlse,
+                          e.lse);
+      lse = mine.lse, c = mine.c, d = mine.d;
+      target = mine.target < 0 ? INT32_MIN : static_cast<int>(mine.target - e.first);
+#pragma unroll
+      for (int q = 0; q < kParts; ++q) sum[q] = top[q] = floatx4{};
+    }
+    stage_rows<i0, kN, kSubN>(stage, value);
+    static_for<kParts>([&](auto Pc) {
+      constexpr int kPart = decltype(Pc)::value;
+      const int first_col = col0 + 16 * kB * kPart, col = first_col + L::column();
+      if (first_col >= N) return;
+      const floatx4 bias = piece_bias(e.bias, e.first, L::in() ? col : N, N);
+#pragma unroll 1
+      for (int p = 0; p < L::kTurns; ++p) {
+        floatx4 v[kU];
+        L::template read<kPart>(stage, p, col, N, full, bias, 0.0f, v);
+        int hit[kU];
+        bool any = false;
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+          const int from = (16 * i0 + L::row(p, u)) % (16 * kBM);
+          const float l = __shfl(lse, from), f = __shfl(c, from);
+          hit[u] = __shfl(target, from) - col;
+          any |= static_cast<unsigned>(hit[u]) < 4;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) v[u][k] = exp_of(v[u][k] - l) * f;
+        }
+        if (__ballot(any)) {
+#pragma unroll
+          for (int u = 0; u < kU; ++u) {
+            const float off = __shfl(d, (16 * i0 + L::row(p, u)) % (16 * kBM));
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[u][k] = hit[u] == k ? v[u][k] - off : v[u][k];
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+          const int row = row0 + 16 * i0 + L::row(p, u);
+          float most = 0.0f;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            if (!L::in() || (!full && (row >= M || col + k >= N))) v[u][k] = 0.0f;
+            const float b = finite_magnitude(v[u][k]);
+            sum[kPart][k] += v[u][k];
+            top[kPart][k] = __builtin_fmaxf(top[kPart][k], b);
+            most = __builtin_fmaxf(most, b);
+          }
+          most = max_of<L::kLanes>(most);
+          if (e.row_top && L::column() == 0 && row < M)
+            e.row_top[static_cast<int64_t>(first_col / (16 * kB)) * M + row] = most;
+        }
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+          const int row = row0 + 16 * i0 + L::row(p, u);
+          float* const at = D + static_cast<int64_t>(row) * ldd + col;
+          if (full) {
+            if (L::in()) store_any(at, v[u]);
+          } else if (L::in() && row < M) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              if (col + k < N) at[k] = v[u][k];
+          }
+        }
+      }
+      if constexpr ((i0 + kN) % kBM == 0) {
+        const int64_t slab = (row0 + 16 * i0) / (16 * kBM);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          float s = sum[kPart][k], m = top[kPart][k];
+#pragma unroll
+          for (int w = L::kLanes; w < 64; w *= 2) {
+            s += __shfl_xor(s, w);
+            m = __builtin_fmaxf(m, __shfl_xor(m, w));
+          }
+          if (lane >= L::kLanes || !L::in() || col + k >= N || row0 + 16 * (i0 / kBM * kBM) >= M)
+            continue;
+          e.sums[slab * N + col + k] = s;
+          if (e.col_top) e.col_top[slab * ld_top + col + k] = m;
+        }
+      }
+    });
   });
 }
 

@@ -1,4 +1,4 @@
-// Reductions over 16 adjacent lanes, exponentials, and a cross entropy's gradient.  Internal; every function has
+// Reductions over adjacent lanes, exponentials, and a cross entropy's gradient.  Internal; every function has
 // internal linkage.
 #pragma once
 
@@ -11,25 +11,28 @@
 namespace sgc {
 namespace {
 
-// f of the values of 16 lanes, in every one of them, by rotations.
-template <typename F>
-__device__ __forceinline__ float join_16(float v, F f) {
+// f of the values of kL (4, 8 or 16) adjacent lanes, in every one of them: with the
+// neighbour, the other pair of four, the mirrored lanes of eight and of sixteen.
+template <int kL, typename F>
+__device__ __forceinline__ float join_lanes(float v, F f) {
   auto step = [&](auto control) {
     const int o = __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v),
                                               decltype(control)::value, 0xf, 0xf, true);
     v = f(v, __builtin_bit_cast(float, o));
   };
-  step(std::integral_constant<int, 0x121>{});  // row_ror:1
-  step(std::integral_constant<int, 0x122>{});
-  step(std::integral_constant<int, 0x124>{});
-  step(std::integral_constant<int, 0x128>{});
+  step(std::integral_constant<int, 0xb1>{});  // quad_perm:[1,0,3,2]
+  step(std::integral_constant<int, 0x4e>{});  // quad_perm:[2,3,0,1]
+  if constexpr (kL > 4) step(std::integral_constant<int, 0x141>{});  // row_half_mirror
+  if constexpr (kL > 8) step(std::integral_constant<int, 0x140>{});  // row_mirror
   return v;
 }
-__device__ __forceinline__ float max_of_16(float v) {
-  return join_16(v, [](float a, float b) { return __builtin_fmaxf(a, b); });
+template <int kL>
+__device__ __forceinline__ float max_of(float v) {
+  return join_lanes<kL>(v, [](float a, float b) { return __builtin_fmaxf(a, b); });
 }
-__device__ __forceinline__ float sum_of_16(float v) {
-  return join_16(v, [](float a, float b) { return a + b; });
+template <int kL>
+__device__ __forceinline__ float sum_of(float v) {
+  return join_lanes<kL>(v, [](float a, float b) { return a + b; });
 }
 
 // exp(x) on the hardware's exp2: off by (|x| + 2) 2^-24 of itself.

@@ -343,7 +343,7 @@ __global__ __launch_bounds__(kThreads) void columns_kernel(ColumnArgs a, int64_t
         top[e] = __builtin_fmaxf(top[e], b[e]);
       }
       if (a.row_top) {
-        const float m = max_of_16(__builtin_fmaxf(__builtin_fmaxf(b[0], b[1]),
+        const float m = max_of<16>(__builtin_fmaxf(__builtin_fmaxf(b[0], b[1]),
                                                     __builtin_fmaxf(b[2], b[3])));
         if ((t & 15) == 0)
           a.row_top[(2 * blockIdx.x + (t >> 4 & 1)) * a.M + i + u * kStride] = m;
@@ -415,7 +415,7 @@ __global__ __launch_bounds__(kThreads) void gate_columns_kernel(GateColumnArgs a
           top[h][e] = __builtin_fmaxf(top[h][e], b[e]);
         }
         if (a.row_top) {
-          const float m = max_of_16(__builtin_fmaxf(__builtin_fmaxf(b[0], b[1]),
+          const float m = max_of<16>(__builtin_fmaxf(__builtin_fmaxf(b[0], b[1]),
                                                       __builtin_fmaxf(b[2], b[3])));
           if ((t & 15) == 0)
             a.row_top[(2 * (h * gridDim.x + blockIdx.x) + (t >> 4 & 1)) * a.M + row] = m;
