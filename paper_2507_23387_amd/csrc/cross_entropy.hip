@@ -33,11 +33,11 @@ struct Results {
   int64_t V;
   Ids targets;
   float *loss, *lse;
-  __device__ __forceinline__ void store(int64_t i, const Exps& e, const float* at) const {
+  __device__ __forceinline__ void store(int64_t i, const Exps& e, int64_t target,
+                                        float at) const {
     const float l = e.top + __builtin_logf(e.sum);
-    const int64_t t = id_at(targets, i);
     lse[i] = l;
-    loss[i] = t < 0 ? 0.0f : t >= V ? __builtin_nanf("") : l - *at;
+    loss[i] = target < 0 ? 0.0f : target >= V ? __builtin_nanf("") : l - at;
   }
 };
 
@@ -54,12 +54,16 @@ struct PieceArgs {
 };
 
 // A stretch of one row a workgroup.
-constexpr int kExpsThreads = 1024;
+constexpr int kExpsThreads = 1024, kExpsWaves = kExpsThreads / 64;
 __global__ __launch_bounds__(kExpsThreads) void exps_kernel(PieceArgs g) {
-  __shared__ Exps part[kExpsThreads / 64];
+  __shared__ Exps part[kExpsWaves];
   const int64_t c0 = blockIdx.y * g.stretch, c1 = min(g.cols, c0 + g.stretch);
   for (int64_t i = blockIdx.x; i < g.M; i += gridDim.x) {
     const float* const row = g.z + i * g.cols;
+    // The target's logit is asked for first: one load waits for the other.
+    const int64_t target = id_at(g.out.targets, i), t = target - g.first;
+    const bool here = t >= c0 && t < c1;
+    const float at = row[here ? t : c0];
     Exps e{-__builtin_inff(), 0.0f};
     // Four quads of this thread's in flight.
     constexpr int kU = 4;
@@ -91,16 +95,18 @@ __global__ __launch_bounds__(kExpsThreads) void exps_kernel(PieceArgs g) {
     for (int d = 1; d < 64; d *= 2) join(e, Exps{__shfl_xor(e.top, d), __shfl_xor(e.sum, d)});
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = e;
     __syncthreads();
-    if (threadIdx.x == 0) {
+    if (threadIdx.x < kExpsWaves) {
+      e = part[threadIdx.x];
 #pragma unroll
-      for (int w = 1; w < kExpsThreads / 64; ++w) join(e, part[w]);
-      const int64_t t = id_at(g.out.targets, i) - g.first;
-      const bool here = t >= c0 && t < c1;
+      for (int d = 1; d < kExpsWaves; d *= 2)
+        join(e, Exps{__shfl_xor(e.top, d), __shfl_xor(e.sum, d)});
+    }
+    if (threadIdx.x == 0) {
       if (g.all) {
-        g.out.store(i, e, row + (here ? t : 0));
+        g.out.store(i, e, target, at);
       } else {
         g.exps[(g.slot0 + blockIdx.y) * g.M + i] = e;
-        if (here) g.at[i] = row[t];
+        if (here) g.at[i] = at;
       }
     }
     __syncthreads();  // the sums are read before the next row's are written
@@ -131,7 +137,8 @@ __global__ __launch_bounds__(kJoinThreads) void xent_join_kernel(int64_t M, int6
     if (q == 0 && i < M) {
 #pragma unroll
       for (int w = 1; w < kJoinWaves; ++w) join(e, part[w][r]);
-      out.store(i, e, at + i);
+      const int64_t t = id_at(out.targets, i);
+      out.store(i, e, t, t >= 0 && t < out.V ? at[i] : 0.0f);
     }
     __syncthreads();  // the sums are read before the next rows' are written
   }
@@ -318,6 +325,7 @@ struct GradWorkspace {
   float *row_top, *col_top, *sums;
   int *row_shift, *col_shift;
   Planes logits, dx, dw;
+  float* part;  // launch_gradients'
   size_t bytes;
 };
 
@@ -352,6 +360,14 @@ GradWorkspace carve_grad(void* ws, int64_t M, int64_t V, int64_t K, bool transpo
     w.logits = carve_planes(c, M, w.piece, K);
     w.dx = carve_planes(c, M, K, w.piece);
     w.dw = transpose_w ? carve_planes(c, w.piece, K, M) : carve_planes(c, K, w.piece, M);
+    int64_t part = 0;
+    for (const int64_t cols : {w.piece, rest}) {
+      if (cols == 0) continue;
+      part = std::max(part, std::max(shares_floats(M, K, cols),
+                                     transpose_w ? shares_floats(cols, K, M)
+                                                 : shares_floats(K, cols, M)));
+    }
+    w.part = c.take<float>(part);
   }
   w.bytes = c.used;
   return w;
@@ -431,17 +447,8 @@ hipError_t launch_piece(const XentGradArgs& a, const GradWorkspace& w, int64_t f
     list[count++] = GroupProduct{dw, x.transpose_w ? cols : x.K, x.transpose_w ? x.K : cols, x.M,
                                  a.dw + (x.transpose_w ? first * a.lddw : first), a.lddw,
                                  Unscale{w.col_shift, !x.transpose_w, false}};
-  if (err == hipSuccess && count == 2) {
-    if (const int tile = group_gemm_tile(list, 2, x.variant, !scaled_kernel_ok(x.scale)))
-      return launch_gemm_group(tile, list, 2, x.scale, x.variant, stream);
-  }
-  for (int i = 0; i < count && err == hipSuccess; ++i) {
-    // As B, D never asks for the fallback (launch_linear_grad).
-    const GroupProduct& g = list[i];
-    err = launch_gemm_epilogue(g.p, g.M, g.N, g.C, g.ldc, x.scale, x.variant, g.epi,
-                               g.epi.columns, stream);
-  }
-  return err;
+  return err == hipSuccess && count > 0
+             ? launch_gradients(list, count, x.scale, x.variant, w.part, stream) : err;
 }
 
 }  // namespace

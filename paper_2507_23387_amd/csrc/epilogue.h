@@ -19,9 +19,12 @@ constexpr bool kElementwiseOnly =
 
 // In place of an epilogue: C is stored as the product (store_tile16).
 struct NoEpilogue {};
+// The same, of a share of k that blockIdx.y names (gemm_shares_kernel).
+struct Share {};
 template <class Epi>
 constexpr bool kThroughLds =
-    !std::is_same<Epi, NoEpilogue>::value && !std::is_same<Epi, Unscale>::value;
+    !std::is_same<Epi, NoEpilogue>::value && !std::is_same<Epi, Share>::value &&
+    !std::is_same<Epi, Unscale>::value;
 
 // The shifts of a wave's kBlocks x 16 rows (or columns) from `first` on, 64 lines at a
 // time, one a lane, which hand them out: all of a lane's own are more than the wide

@@ -120,6 +120,7 @@ struct GradWorkspace {
   int *row_shift, *col_shift;
   void* linear;  // the gradients' of one weight, where they go apart
   Planes dx, dw;
+  float* part;  // launch_gradients'
   size_t bytes;
 };
 
@@ -144,6 +145,8 @@ GradWorkspace carve_grad(void* ws, int64_t M, int64_t N, int64_t K, bool transpo
     // The second half's tiles of 256 may reach a panel past D's columns.
     const int64_t lines = 2 * w.half + kPanel;
     w.dw = transpose_w ? carve_planes(c, lines, K, M) : carve_planes(c, K, lines, M);
+    w.part = c.take<float>(std::max(shares_floats(M, K, 2 * w.half),
+                                    transpose_w ? shares_floats(N, K, M) : shares_floats(K, N, M)));
   }
   w.bytes = c.used;
   return w;
@@ -249,17 +252,8 @@ hipError_t launch_gated_grad(const GatedGradArgs& a, void* ws, hipStream_t strea
                                  Unscale{w.row_shift, false, false}};
   for (int i = 0; i < 2; ++i)
     if (a.dw[i]) list[count++] = weight_product(a, w, i);
-  if (err == hipSuccess && count > 1) {
-    if (const int tile = group_gemm_tile(list, count, a.variant, !scaled_kernel_ok(a.scale)))
-      return launch_gemm_group(tile, list, count, a.scale, a.variant, stream);
-  }
-  for (int i = 0; i < count && err == hipSuccess; ++i) {
-    // As B, D never asks for the fallback (launch_linear_grad).
-    const GroupProduct& g = list[i];
-    err = launch_gemm_epilogue(g.p, g.M, g.N, g.C, g.ldc, a.scale, a.variant, g.epi,
-                               g.epi.columns, stream);
-  }
-  return err;
+  return err == hipSuccess && count > 0
+             ? launch_gradients(list, count, a.scale, a.variant, w.part, stream) : err;
 }
 
 }  // namespace sgc

@@ -82,6 +82,7 @@ struct SmallArgs {
   const uint32_t* col_max;
   int exp_a, exp_b;
   uint32_t* report;  // range report word, or null
+  int steps;  // of k, 32 wide: all of them, or those of a share
 };
 
 // `index`: the workgroup's place in the grid of this product.
@@ -97,7 +98,14 @@ __device__ __forceinline__ void small_tile(const SmallArgs& g, uint16_t* lds, co
   const int lane = threadIdx.x & 63;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int wm = w / S::kWavesN, wn = w % S::kWavesN;
-  const int ksteps = g.Kp / kSmallStep;
+  // All of k, or a share of it.
+  int first_step = 0, ksteps = g.steps;
+  float* C = g.C;
+  if constexpr (std::is_same<Epi, Share>::value) {
+    first_step = blockIdx.y * g.steps;
+    ksteps = min(ksteps, g.Kp / kSmallStep - first_step);
+    C += static_cast<int64_t>(blockIdx.y) * g.M * g.N;
+  }
 
   // Copy u of a stage is 1 KiB: rows 32 r .. 32 r + 31 of one slice of one
   // plane, contiguous in the tiled plane; the A planes come first, and wave w
@@ -120,7 +128,8 @@ __device__ __forceinline__ void small_tile(const SmallArgs& g, uint16_t* lds, co
     const int row = min((is_a ? tm * S::kBM : tn * S::kBN) + 32 * r, (is_a ? g.Mp : g.Np) - 32);
     const uint16_t* plane = is_a ? (p ? g.a_lo : g.a_hi) : (p ? g.b_lo : g.b_hi);
     src[i] = reinterpret_cast<const char*>(plane) + (row / kPanel) * panel_bytes +
-             sl * (kTileHalves * 2) + (row % kPanel) * (kSlice * 2);
+             static_cast<int64_t>(2 * first_step + sl) * (kTileHalves * 2) +
+             (row % kPanel) * (kSlice * 2);
     dst[i] = lds_base + ((is_a ? p * S::kAPlane : S::kBBase + p * S::kBPlane) +
                          (sl * (is_a ? S::kBM : S::kBN) + 32 * r) * kSlice) * 2;
   }
@@ -315,7 +324,7 @@ __device__ __forceinline__ void small_tile(const SmallArgs& g, uint16_t* lds, co
                   "the waves' staging fits the ring");
     lds_barrier();  // every wave is done with the ring
     epilogue_tile<kRT, kCT, kChunk>(epi, reinterpret_cast<float*>(lds) + w * kChunk * kCT * 256,
-                                    g.C, g.ldc, g.M, g.N, tm * S::kBM + wm * S::kWRows,
+                                    C, g.ldc, g.M, g.N, tm * S::kBM + wm * S::kWRows,
                                     tn * S::kBN + wn * S::kWCols, value);
     return;
   }
@@ -335,13 +344,13 @@ __device__ __forceinline__ void small_tile(const SmallArgs& g, uint16_t* lds, co
         const int col = col0 + 16 * j;
         q[j] = col < g.N ? prescale_shift(g.col_max[col], g.exp_b) : 0;
       }
-      store_tile16<kRT, kCT>(g.C, g.ldc, g.M, g.N, row0, col0, full, [&](int i, int j, int r) {
+      store_tile16<kRT, kCT>(C, g.ldc, g.M, g.N, row0, col0, full, [&](int i, int j, int r) {
         return __builtin_ldexpf(value(i, j, r), -(p[i][r] + q[j]));
       });
       return;
     }
   }
-  store_product<kRT, kCT>(epi, g.C, g.ldc, g.M, g.N, row0, col0, full, value);
+  store_product<kRT, kCT>(epi, C, g.ldc, g.M, g.N, row0, col0, full, value);
 }
 
 template <int V, class S, class Epi>
@@ -395,6 +404,34 @@ __global__ __launch_bounds__(64 * kWM * kWN, 1) void linear_group_kernel(GroupAr
   small_body<V, S>(a.g[i], a.unscaled_only, a.e[i], b - (i ? a.first[i - 1] : 0));
 }
 
+// A product of few tiles and a long k in shares of it, blockIdx.y the share, each an M x N
+// matrix of its own: C + share M N.  g.steps: those of every share but the last, which has
+// what is left.
+template <int V, int kBM, int kBN, int kWM, int kWN, int kStages>
+__global__ __launch_bounds__(64 * kWM * kWN, 1) void gemm_shares_kernel(SmallArgs g,
+                                                                        int unscaled_only) {
+  small_body<V, SmallShape<kBM, kBN, kWM, kWN, kStages, false>>(g, unscaled_only, Share{},
+                                                                blockIdx.x);
+}
+
+// The shares' sum, always in the same order, with the gradient's powers of two.
+constexpr int kJoinThreads = 256;
+__global__ __launch_bounds__(kJoinThreads) void shares_join_kernel(const float* part, int shares,
+                                                                   int64_t M, int64_t N, float* C,
+                                                                   int64_t ldc, Unscale e) {
+  const int64_t all = M * N;
+  for (int64_t q = static_cast<int64_t>(blockIdx.x) * kJoinThreads + threadIdx.x; q < all;
+       q += static_cast<int64_t>(gridDim.x) * kJoinThreads) {
+    const int64_t i = q / N, j = q - i * N;
+    float v = 0.0f;
+#pragma unroll 8
+    for (int s = 0; s < shares; ++s) v += part[s * all + q];
+    v = __builtin_ldexpf(v, -e.shift[e.columns ? j : i]);
+    float* const at = C + i * ldc + j;
+    *at = e.add ? *at + v : v;
+  }
+}
+
 // The unscaled body alone, on 256 x 128 tiles: the fallback of the 256-wide
 // scaled kernels (gemm.hip).  Unless the host routed the call here (unscaled_only:
 // s is not a finite FP16 value) it returns at once where the range flag is
@@ -436,7 +473,8 @@ SmallArgs small_args(const Planes& p, int64_t M, int64_t N, float* C, int64_t ld
                    static_cast<int>(p.Np), static_cast<int>(p.Kp), tiles_m, tiles_n, by_xcd, C,
                    ldc, static_cast<int>(M),
                    static_cast<int>(N), s, 1.0f / s, opt.prescale ? p.row_max : nullptr,
-                   opt.prescale ? p.col_max : nullptr, opt.exp_a, opt.exp_b, report};
+                   opt.prescale ? p.col_max : nullptr, opt.exp_a, opt.exp_b, report,
+                   static_cast<int>(p.Kp / kSmallStep)};
 }
 
 template <int V>
@@ -702,6 +740,68 @@ TileGrain tile_grain(int64_t M, int64_t N, int64_t K, int variant, bool unscaled
     return hipSuccess;
   });
   return g;
+}
+
+// The rule: the shares whose grid and join take less than 0.85 of the whole by the model
+// above.  150 x 2048 of k = 32768: whole, on 32-wide tiles, 266 us; eight shares on 64-wide
+// ones 130, the join 5.  1024 x 1024 of the same k 199 and 8.
+GemmShares gemm_shares(int64_t M, int64_t N, int64_t K, int variant, bool unscaled) {
+  GemmShares best{0, 1, 0};
+  const int row = unscaled && variant == kElementwise ? 4 : variant;
+  const int64_t steps = round_up(K, kKPad) / kSmallStep;
+  auto tiles = [&](int side) { return ((M + side - 1) / side) * ((N + side - 1) / side); };
+  const int whole = small_gemm_tile(M, N, K, variant, unscaled);
+  if (variant != kElementwise || whole == 0) return best;
+  const GridCost* const cost[] = {&k32[row], &k64[row], &k128[row], &k192[row]};
+  const int side_of[] = {32, 64, 128, 192}, together[] = {512, 512, 256, 256};
+  double limit = 0.0;
+  for (int n = 0; n < 4; ++n)
+    if (side_of[n] == whole) limit = 0.85 * grid_time(*cost[n], tiles(whole), together[n], steps);
+  for (int n = 0; n < 3; ++n) {
+    for (int want = 2; want <= kMaxShares; ++want) {
+      // Whole pairs of steps (small_tile takes two a turn), ten steps at least, and what the
+      // join reads within the cache.
+      const int64_t each = round_up((steps + want - 1) / want, 2);
+      const int shares = static_cast<int>((steps + each - 1) / each);
+      if (each < 10 || 4.0 * shares * M * N > 128.0 * (1 << 20)) break;
+      const int64_t all = tiles(side_of[n]) * shares;
+      if (all * small_tile_threads(side_of[n], variant) > UINT32_MAX) break;
+      // The join: a launch, and the shares written and read.
+      const double us = grid_time(*cost[n], all, together[n], each) + 4.0 +
+                        8.0 * shares * M * N / 4.0e6;
+      if (shares > 1 && us < limit) limit = us, best = {side_of[n], shares, static_cast<int>(each)};
+    }
+  }
+  return best;
+}
+
+hipError_t launch_gemm_shares(const GemmShares& s, const GroupProduct& g, float scale,
+                              float* part, hipStream_t stream) {
+  auto launch = [&](auto c) {
+    using T = decltype(c);
+    if constexpr (T::kBM > 128) {
+      return hipErrorInvalidValue;  // gemm_shares offers none
+    } else {
+      using S = SmallShape<T::kBM, T::kBN, T::kWM, T::kWN, T::kStages, false>;
+      static std::atomic<bool> done[kMaxDevices];
+      constexpr auto kernel =
+          &gemm_shares_kernel<kElementwise, T::kBM, T::kBN, T::kWM, T::kWN, T::kStages>;
+      const hipError_t attr = set_lds(kernel, S::kLdsBytes, done);
+      if (attr != hipSuccess) return attr;
+      SmallArgs a = small_args<S>(g.p, g.M, g.N, part, g.N, scale, RangeOpts{}, nullptr);
+      a.steps = s.steps;
+      hipLaunchKernelGGL(kernel, dim3(a.tiles_m * a.tiles_n, s.shares), dim3(S::kThreads),
+                         S::kLdsBytes, stream, a, scaled_kernel_ok(scale) ? 0 : 1);
+      return hipGetLastError();
+    }
+  };
+  const hipError_t err = with_config<kElementwise>(s.tile, launch);
+  if (err != hipSuccess) return err;
+  const int64_t blocks = (g.M * g.N + kJoinThreads - 1) / kJoinThreads;
+  hipLaunchKernelGGL(shares_join_kernel,
+                     dim3(static_cast<unsigned>(std::min<int64_t>(blocks, int64_t{1} << 20))),
+                     dim3(kJoinThreads), 0, stream, part, s.shares, g.M, g.N, g.C, g.ldc, g.epi);
+  return hipGetLastError();
 }
 
 int group_gemm_tile(const GroupProduct* list, int count, int variant, bool unscaled) {

@@ -221,6 +221,17 @@ int group_gemm_tile(const GroupProduct* list, int count, int variant, bool unsca
 hipError_t launch_gemm_group(int tile, const GroupProduct* list, int count, float scale,
                              int variant, hipStream_t stream);
 
+// A gradient's product of few tiles and a long k, in shares of it that a second launch
+// joins: one share where that takes no less time than the whole.  `part`: shares x M x N.
+// In the elementwise order.
+constexpr int kMaxShares = 16;
+struct GemmShares {
+  int tile, shares, steps;  // steps of 32 k to a share, the last what is left
+};
+GemmShares gemm_shares(int64_t M, int64_t N, int64_t K, int variant, bool unscaled);
+hipError_t launch_gemm_shares(const GemmShares& s, const GroupProduct& g, float scale,
+                              float* part, hipStream_t stream);
+
 struct LinearArgs {
   int64_t M, N, K;
   const float* x;

@@ -73,5 +73,44 @@ inline int target_b(float scale, int variant) {
                                                           : 14 - std::ilogb(scale);
 }
 
+// Workspace of a gradient's product: its shares, whatever the scale.
+inline int64_t shares_floats(int64_t M, int64_t N, int64_t K) {
+  int64_t most = 0;
+  for (const bool unscaled : {false, true}) {
+    const GemmShares s = gemm_shares(M, N, K, kElementwise, unscaled);
+    if (s.shares > 1) most = std::max(most, s.shares * M * N);
+  }
+  return most;
+}
+
+// The products of a layer's gradients: all in one launch, or one after the other, each
+// whole or in shares, as the rules say for it alone (so that it has the same bits whichever
+// others are wanted).  part: shares_floats of the largest.
+inline hipError_t launch_gradients(const GroupProduct* list, int count, float scale, int variant,
+                                   float* part, hipStream_t stream) {
+  const bool unscaled = !scaled_kernel_ok(scale);
+  GemmShares shares[kGroupProducts];
+  bool any = false;
+  for (int i = 0; i < count; ++i) {
+    shares[i] = gemm_shares(list[i].M, list[i].N, list[i].K, variant, unscaled);
+    any |= shares[i].shares > 1;
+  }
+  if (count > 1 && !any) {
+    if (const int tile = group_gemm_tile(list, count, variant, unscaled))
+      return launch_gemm_group(tile, list, count, scale, variant, stream);
+  }
+  for (int i = 0; i < count; ++i) {
+    const GroupProduct& g = list[i];
+    // As B, D never asks for the fallback (launch_linear_grad).
+    const hipError_t err =
+        shares[i].shares > 1
+            ? launch_gemm_shares(shares[i], g, scale, part, stream)
+            : launch_gemm_epilogue(g.p, g.M, g.N, g.C, g.ldc, scale, variant, g.epi,
+                                   g.epi.columns, stream);
+    if (err != hipSuccess) return err;
+  }
+  return hipSuccess;
+}
+
 }  // namespace
 }  // namespace sgc
