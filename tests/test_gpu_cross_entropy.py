@@ -345,6 +345,25 @@ def test_large_weights(gpu):
             _check_backward(g, None, X, Wkn, None, t, lse, True, dX, dW, db)
 
 
+@pytest.mark.parametrize("m,v,k", [(3, 700, 130), (300, 900, 128), (260, 9000, 65),
+                                   (4200, 4300, 64)])
+def test_large_scale(gpu, m, v, k):
+    """A scale past what the scaled kernels take, on entries that it fits."""
+    import paper_2507_23387_amd as sgc
+
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(88)
+    X, W, Wkn = _case(gen, m, v, k, "nk", 0)
+    t, g = _targets(gen, m, v, torch.int64), torch.ones(m, device="cuda")
+    for order in ORDERS:
+        log(f"linear_cross_entropy, scale 2^16, {order} {m}x{v}x{k}")
+        kw = dict(transpose_w=True, order=order, scale=2.0**16)
+        loss, lse = sgc.linear_cross_entropy(X, W, t, **kw)
+        _check_forward(X, Wkn, None, t, loss, lse)
+        dX, dW, db = sgc.linear_cross_entropy_backward(g, X, W, t, lse, **kw)
+        _check_backward(g, None, X, Wkn, None, t, lse, True, dX, dW, db)
+
+
 def test_refused(gpu):
     import paper_2507_23387_amd as sgc
 

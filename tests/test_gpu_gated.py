@@ -257,10 +257,13 @@ def test_large_weights(gpu):
             dY = _mat(gen, m, n)
             grads = sgc.gated_linear_backward(dY, X, *W, G, Up, **kw)
             _check_backward(dY, X, Wkn, G, Up, "silu", True, grads)
-            kw["scale"] = 2.0**16  # past what the scaled kernels take
-            small = [w / 64 for w in W]
-            Y, G, Up = sgc.gated_linear(X / 64, *small, keep_preact=True, **{**kw, "scale": 2.0**12})
-            _check_forward(X / 64, [w / 64 for w in Wkn], (None, None), "silu", Y, G, Up)
+            # A scale past what the scaled kernels take, on entries that it fits.
+            kw["scale"] = 2.0**16
+            args, small = (X / 64, *(w / 64 for w in W)), [w / 64 for w in Wkn]
+            Y, G, Up = sgc.gated_linear(*args, keep_preact=True, **kw)
+            _check_forward(args[0], small, (None, None), "silu", Y, G, Up)
+            grads = sgc.gated_linear_backward(dY, *args, G, Up, **kw)
+            _check_backward(dY, args[0], small, G, Up, "silu", True, grads)
 
 
 def test_empty(gpu):
