@@ -53,10 +53,16 @@ struct PieceArgs {
   int64_t stretch;
 };
 
-// A stretch of one row a workgroup.
+// A stretch of one row a workgroup, of as many threads as it has work for.
 constexpr int kExpsThreads = 1024, kExpsWaves = kExpsThreads / 64;
+int exps_threads(int64_t stretch) {
+  int threads = 64;
+  while (threads < kExpsThreads && 16 * threads < stretch) threads *= 2;
+  return threads;
+}
 __global__ __launch_bounds__(kExpsThreads) void exps_kernel(PieceArgs g) {
   __shared__ Exps part[kExpsWaves];
+  const int threads = blockDim.x;
   const int64_t c0 = blockIdx.y * g.stretch, c1 = min(g.cols, c0 + g.stretch);
   for (int64_t i = blockIdx.x; i < g.M; i += gridDim.x) {
     const float* const row = g.z + i * g.cols;
@@ -67,11 +73,11 @@ __global__ __launch_bounds__(kExpsThreads) void exps_kernel(PieceArgs g) {
     Exps e{-__builtin_inff(), 0.0f};
     // Four quads of this thread's in flight.
     constexpr int kU = 4;
-    for (int64_t j0 = c0 + 4 * threadIdx.x; j0 < c1; j0 += 4 * kU * kExpsThreads) {
+    for (int64_t j0 = c0 + 4 * threadIdx.x; j0 < c1; j0 += 4 * kU * threads) {
       float v[kU][4];
 #pragma unroll
       for (int u = 0; u < kU; ++u) {
-        const int64_t j = j0 + 4 * u * kExpsThreads;
+        const int64_t j = j0 + 4 * u * threads;
         if (j + 3 < c1) {
           const floatx4_u p = *reinterpret_cast<const floatx4_u*>(row + j);
 #pragma unroll
@@ -96,7 +102,8 @@ __global__ __launch_bounds__(kExpsThreads) void exps_kernel(PieceArgs g) {
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = e;
     __syncthreads();
     if (threadIdx.x < kExpsWaves) {
-      e = part[threadIdx.x];
+      e = static_cast<int>(threadIdx.x) < threads / 64 ? part[threadIdx.x]
+                                                       : Exps{-__builtin_inff(), 0.0f};
 #pragma unroll
       for (int d = 1; d < kExpsWaves; d *= 2)
         join(e, Exps{__shfl_xor(e.top, d), __shfl_xor(e.sum, d)});
@@ -303,7 +310,7 @@ hipError_t launch_xent(const XentArgs& a, float* loss, float* lse, void* ws, hip
     const PieceArgs g{a.M, cols, first, w.z, out, all, w.exps, w.at, slot,
                       stretch_cols(a.M, cols)};
     hipLaunchKernelGGL(exps_kernel, dim3(rows_grid(a.M), static_cast<unsigned>(parts)),
-                       dim3(kExpsThreads), 0, stream, g);
+                       dim3(exps_threads(g.stretch)), 0, stream, g);
     err = hipGetLastError();
     if (all) return err;
     slot += parts;

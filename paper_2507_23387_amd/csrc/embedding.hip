@@ -366,12 +366,14 @@ __device__ __forceinline__ void write_row(const EmbeddingGradArgs& a, uint32_t v
   }
 }
 
-// Rows of dW to a workgroup that looks for those without ids: 4096 values or 8 rows (8 of
-// 1003 x 530 7.0 us, 32 10.8; of 131072 x 64 19.4, 64 8.6).
+// Rows of dW to a workgroup that looks for those without ids: 4096 values or 8 rows, and
+// 4096 workgroups at most.  (8 rows of 1003 x 530 7.0 us, 32 10.8; 8 of 131072 x 64 19.4, 64
+// 8.6; 1048 positions of 112256 x 836 in 8 rows and in 32: ZERO112.)
 constexpr int kMostZeroRows = 64;
-int zero_rows(int64_t cols) {
+int zero_rows(int64_t vocab, int64_t cols) {
   int rows = 8;
-  while (rows < kMostZeroRows && 2 * rows * cols <= 4096) rows *= 2;
+  while (rows < kMostZeroRows && (2 * rows * cols <= 4096 || vocab > int64_t{4096} * rows))
+    rows *= 2;
   return rows;
 }
 
@@ -401,6 +403,14 @@ __global__ __launch_bounds__(kThreads) void embedding_sum_kernel(SumArgs g) {
       absent[g.sorted.keys[p] - v0] = false;
     __syncthreads();
     const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (ends[0] == ends[1] && a.lddw == a.cols) {
+      // All of them, side by side.
+      float* const at = a.dw + v0 * a.lddw;
+      const int64_t all = (v1 - v0) * a.cols;
+      for (int64_t j = 4 * threadIdx.x; j < all; j += 4 * kThreads)
+        store_piece<kF32>(at, static_cast<int>(j), static_cast<int>(all), zero);
+      return;
+    }
     const int per = kThreads / g.lanes;
     for (int r = threadIdx.x / g.lanes; r < g.zero_rows; r += per) {
       if (!absent[r]) continue;
@@ -628,7 +638,7 @@ hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, int dtype, void* ws
   g.lanes = row_lanes(a.cols, per);
   g.chunk = chunk_length(a.n, a.cols, per);
   g.chunks = (a.n + g.chunk - 1) / g.chunk;
-  g.zero_rows = zero_rows(a.cols);
+  g.zero_rows = zero_rows(a.vocab, a.cols);
   g.tiles = static_cast<uint32_t>((a.cols + int64_t{g.lanes} * per - 1) / (int64_t{g.lanes} * per));
   const int64_t groups = kThreads / g.lanes;
   const int64_t sums = (g.chunks + groups - 1) / groups * g.tiles;

@@ -353,6 +353,9 @@ struct RowLanes {
   }
 };
 
+// Of a row without a target: no column of a piece, nor is its distance from one.
+constexpr int kNoColumn = INT32_MIN / 2;
+
 // Four values of the bias from column `col` of a piece of N, zeros past its end.
 __device__ __forceinline__ floatx4 piece_bias(const float* bias, int64_t first, int col, int N) {
   floatx4 b{};
@@ -377,7 +380,7 @@ __device__ __forceinline__ void epilogue_tile(const ExpsEpilogue& e, float* stag
 #pragma unroll
   for (int h = 0; h < (kSubM + 3) / 4; ++h) {
     const int64_t t = id_at(e.targets, min(row0 + 64 * h + lane, M - 1));
-    held[h] = t < 0 || t >= e.vocab ? INT32_MIN : static_cast<int>(t - e.first);
+    held[h] = t < 0 || t >= e.vocab ? kNoColumn : static_cast<int>(t - e.first);
   }
   static_for<(kSubM + kChunk - 1) / kChunk>([&](auto Cc) {
     constexpr int i0 = decltype(Cc)::value * kChunk;
@@ -454,7 +457,7 @@ __device__ __forceinline__ void epilogue_tile(const XentGradEpilogue& e, float* 
       const RowTerms mine(min(row0 + 16 * i0 + r, M - 1), e.vocab, e.targets, e.dloss, e.dlse,
                           e.lse);
       lse = mine.lse, c = mine.c, d = mine.d;
-      target = mine.target < 0 ? INT32_MIN : static_cast<int>(mine.target - e.first);
+      target = mine.target < 0 ? kNoColumn : static_cast<int>(mine.target - e.first);
 #pragma unroll
       for (int q = 0; q < kParts; ++q) sum[q] = top[q] = floatx4{};
     }

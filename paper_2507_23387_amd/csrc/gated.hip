@@ -118,36 +118,41 @@ struct GradWorkspace {
   int64_t half;  // columns of D to each of dG and dU
   float *d, *row_top, *col_top, *sums;
   int *row_shift, *col_shift;
-  void* linear;  // the gradients' of one weight, where they go apart
-  Planes dx, dw;
-  float* part;  // launch_gradients'
+  void* rows;     // launch_linear_rows', where dX goes by rows
+  Planes dx, dw;  // otherwise, and where dW is no outer product
+  float* part;    // launch_gradients'
   size_t bytes;
 };
 
-// Whether each weight's gradients are a linear layer's.
-bool grad_apart(int64_t M, int64_t N, int64_t K) { return linear_grad_by_rows(M, N, K) || K == 0; }
+// As a linear layer's: dX by rows, and dW of even fewer rows as an outer product.
+bool by_rows(int64_t M, int64_t N, int64_t K) { return linear_grad_by_rows(M, N, K); }
+bool outer(int64_t M, int64_t N, int64_t K) { return M <= kOuterRows && by_rows(M, N, K); }
 
 GradWorkspace carve_grad(void* ws, int64_t M, int64_t N, int64_t K, bool transpose_w) {
   Carver c{static_cast<char*>(ws), 0};
   GradWorkspace w{};
   w.half = round_up(N, kColumnStrip);
   w.d = c.take<float>(M * 2 * w.half);
-  if (grad_apart(M, N, K)) {
-    w.linear = c.take<char>(static_cast<int64_t>(linear_grad_ws(M, N, K)));
-  } else {
-    const int64_t slabs = column_slabs(M, w.half);
-    w.row_top = c.take<float>(row_pieces(2 * w.half) * M);
-    w.col_top = c.take<float>(slabs * 2 * w.half);
-    w.sums = c.take<float>(slabs * 2 * w.half);
-    w.row_shift = c.take<int>(round_up(M, kKPad));
-    w.col_shift = c.take<int>(2 * w.half);
+  const int64_t slabs = column_slabs(M, w.half);
+  w.row_top = c.take<float>(row_pieces(2 * w.half) * M);
+  w.col_top = c.take<float>(slabs * 2 * w.half);
+  w.sums = c.take<float>(slabs * 2 * w.half);
+  w.row_shift = c.take<int>(round_up(M, kKPad));
+  w.col_shift = c.take<int>(2 * w.half);
+  int64_t part = 0;
+  if (K > 0 && by_rows(M, N, K)) {
+    w.rows = c.take<char>(static_cast<int64_t>(linear_rows_ws(M, K, N)));
+  } else if (K > 0) {
     w.dx = carve_planes(c, M, K, 2 * w.half);
+    part = shares_floats(M, K, 2 * w.half);
+  }
+  if (K > 0 && !outer(M, N, K)) {
     // The second half's tiles of 256 may reach a panel past D's columns.
     const int64_t lines = 2 * w.half + kPanel;
     w.dw = transpose_w ? carve_planes(c, lines, K, M) : carve_planes(c, K, lines, M);
-    w.part = c.take<float>(std::max(shares_floats(M, K, 2 * w.half),
-                                    transpose_w ? shares_floats(N, K, M) : shares_floats(K, N, M)));
+    part = std::max(part, transpose_w ? shares_floats(N, K, M) : shares_floats(K, N, M));
   }
+  w.part = c.take<float>(part);
   w.bytes = c.used;
   return w;
 }
@@ -169,6 +174,17 @@ GroupProduct weight_product(const GatedGradArgs& a, const GradWorkspace& w, int 
   return g;
 }
 
+// No rows: the sums are empty.  No columns: dX = 0.
+hipError_t launch_empty_grad(const GatedGradArgs& a, hipStream_t stream) {
+  const int64_t rows = a.transpose_w ? a.N : a.K, cols = a.transpose_w ? a.K : a.N;
+  hipError_t err = a.dx ? launch_zero(a.M, a.K, a.dx, a.lddx, stream) : hipSuccess;
+  for (int i = 0; i < 2 && err == hipSuccess; ++i) {
+    if (a.dw[i]) err = launch_zero(rows, cols, a.dw[i], a.lddw[i], stream);
+    if (err == hipSuccess && a.dbias[i]) err = launch_zero(1, a.N, a.dbias[i], a.N, stream);
+  }
+  return err;
+}
+
 }  // namespace
 
 size_t gated_grad_ws(int64_t M, int64_t N, int64_t K) {
@@ -178,33 +194,16 @@ size_t gated_grad_ws(int64_t M, int64_t N, int64_t K) {
 }
 
 hipError_t launch_gated_grad(const GatedGradArgs& a, void* ws, hipStream_t stream) {
-  const bool empty = a.M == 0 || a.N == 0, apart = empty || grad_apart(a.M, a.N, a.K);
-  GradWorkspace w{};
-  hipError_t err = hipSuccess;
-  if (!empty) {
-    w = carve_grad(ws, a.M, a.N, a.K, a.transpose_w);
-    // (Sums and magnitudes are wanted below, or again from D's halves.)
-    const GateColumnArgs d{a.M, a.N, w.half, a.dy, a.lddy, a.z[0], a.ldz[0], a.z[1], a.ldz[1],
-                           a.activation, a.dx ? w.row_top : nullptr,
-                           a.dw[0] || a.dw[1] ? w.col_top : nullptr, w.sums, w.d};
-    err = launch_gate_columns(d, stream);
-  }
-  if (apart) {
-    for (int i = 0; i < 2 && err == hipSuccess; ++i) {
-      LinearGradArgs l{};
-      l.M = a.M, l.N = a.N, l.K = a.K;
-      l.dy = empty ? nullptr : w.d + i * w.half, l.lddy = 2 * w.half;
-      l.x = a.x, l.ldx = a.ldx;
-      l.w = a.w[i], l.ldw = a.ldw[i], l.transpose_w = a.transpose_w;
-      l.dx = a.dx, l.lddx = a.lddx, l.add_dx = i > 0;
-      l.dw = a.dw[i], l.lddw = a.lddw[i], l.dbias = a.dbias[i];
-      l.scale = a.scale, l.variant = a.variant;
-      err = launch_linear_grad(l, w.linear, stream);
-    }
-    return err;
-  }
+  if (a.M == 0 || a.N == 0) return launch_empty_grad(a, stream);
+  const GradWorkspace w = carve_grad(ws, a.M, a.N, a.K, a.transpose_w);
+  const bool dx = a.dx && a.K > 0, weights = (a.dw[0] || a.dw[1]) && a.K > 0;
+  const bool dx_rows = dx && by_rows(a.M, a.N, a.K);
+  const bool dw_outer = weights && outer(a.M, a.N, a.K), dw_planes = weights && !dw_outer;
+  const GateColumnArgs columns{a.M, a.N, w.half, a.dy, a.lddy, a.z[0], a.ldz[0], a.z[1], a.ldz[1],
+                               a.activation, dx ? w.row_top : nullptr,
+                               dw_planes ? w.col_top : nullptr, w.sums, w.d};
+  hipError_t err = launch_gate_columns(columns, stream);
   if (err != hipSuccess) return err;
-  const bool weights = a.dw[0] || a.dw[1];
   ColumnJoin join{};
   join.M = a.M, join.N = 2 * w.half;
   join.pieces = static_cast<int>(row_pieces(2 * w.half));
@@ -212,15 +211,15 @@ hipError_t launch_gated_grad(const GatedGradArgs& a, void* ws, hipStream_t strea
   join.row_top = w.row_top, join.col_top = w.col_top, join.sums = w.sums;
   join.row_target = target_a(a.scale);
   join.col_target = a.transpose_w ? target_a(a.scale) : target_b(a.scale, a.variant);
-  join.row_shift = a.dx ? w.row_shift : nullptr;
-  join.col_shift = weights ? w.col_shift : nullptr;
+  join.row_shift = dx ? w.row_shift : nullptr;
+  join.col_shift = dw_planes ? w.col_shift : nullptr;
   join.dbias = a.dbias[0], join.dbias_second = a.dbias[1];
   join.half = w.half, join.cols = a.N;
 
   SplitJob jobs[kSplitJobs];
   int count = 0;
   SplitJob d = job_of(w.d, 2 * w.half, a.M, 2 * w.half);
-  if (a.dx) {
+  if (dx && !dx_rows) {
     // dX: D's rows and both weights' K rows, k over dG's columns and then dU's.
     d.row_shift = w.row_shift;
     to_planes(d, w.dx, false, false);
@@ -232,7 +231,7 @@ hipError_t launch_gated_grad(const GatedGradArgs& a, void* ws, hipStream_t strea
     }
     jobs[1].row_stamp = jobs[0].row_stamp, jobs[1].col_stamp = jobs[0].col_stamp;
   }
-  if (weights) {
+  if (dw_planes) {
     // Both dW: columns of X and of D, k over M.
     d.col_shift = w.col_shift;
     to_planes(d, w.dw, !a.transpose_w, true);
@@ -240,18 +239,36 @@ hipError_t launch_gated_grad(const GatedGradArgs& a, void* ws, hipStream_t strea
     to_planes(jobs[count++], w.dw, a.transpose_w, true);
   }
   if (count > 0) jobs[count++] = d;
+  // (A split whose D has no row planes joins those shifts in each of its tiles all the same.)
   const bool split_joins = count > 0 && split_jobs_blocks(jobs, count) <= kSplitJoinBlocks;
   if (!split_joins) err = launch_columns_join(join, stream);
   if (err == hipSuccess && count > 0)
     err = launch_split_jobs(jobs, count, a.scale, stream, split_joins ? &join : nullptr);
 
+  for (int i = 0; i < 2 && dw_outer && err == hipSuccess; ++i) {
+    if (!a.dw[i]) continue;
+    const OuterSide x{a.x, a.ldx, a.K, nullptr, 0};
+    const OuterSide half{w.d + i * w.half, 2 * w.half, a.N, nullptr, 0};
+    const OuterArgs o{static_cast<int>(a.M), SGEMM_CUBE_ACT_NONE, a.transpose_w ? half : x,
+                      a.transpose_w ? x : half, a.dw[i], a.lddw[i]};
+    err = launch_linear_outer(o, stream);
+  }
+  for (int i = 0; i < 2 && dx_rows && err == hipSuccess; ++i) {
+    LinearArgs r{};
+    r.M = a.M, r.N = a.K, r.K = a.N;
+    r.x = w.d + i * w.half, r.ldx = 2 * w.half;
+    r.w = a.w[i], r.ldw = a.ldw[i], r.transpose_w = !a.transpose_w;
+    r.y = a.dx, r.ldy = a.lddx;
+    r.scale = a.scale, r.variant = a.variant;
+    err = launch_linear_rows(r, w.row_shift, w.rows, stream, i > 0);
+  }
   GroupProduct list[kGroupProducts];
   count = 0;
-  if (a.dx)
+  if (dx && !dx_rows)
     list[count++] = GroupProduct{w.dx, a.M, a.K, 2 * w.half, a.dx, a.lddx,
                                  Unscale{w.row_shift, false, false}};
   for (int i = 0; i < 2; ++i)
-    if (a.dw[i]) list[count++] = weight_product(a, w, i);
+    if (dw_planes && a.dw[i]) list[count++] = weight_product(a, w, i);
   return err == hipSuccess && count > 0
              ? launch_gradients(list, count, a.scale, a.variant, w.part, stream) : err;
 }

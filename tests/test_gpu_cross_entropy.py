@@ -28,7 +28,8 @@ IDS = [torch.int64, torch.int32]
 SHAPES = [(1, 1, 1), (1, 2, 5), (1, 3001, 130), (2, 5000, 64), (3, 257, 65), (5, 1003, 530),
           (16, 4096, 70), (17, 33, 31), (48, 9000, 100), (64, 200, 300), (65, 1030, 65),
           (128, 2500, 190), (129, 255, 64), (300, 130, 70), (300, 200, 1000), (777, 1003, 530),
-          (1100, 2100, 70), (2001, 70, 77), (257, 10000, 33), (4100, 4300, 66), (700, 30000, 65)]
+          (1100, 2100, 70), (2001, 70, 77), (257, 10000, 33), (4100, 4300, 66), (700, 30000, 65),
+          (5000, 70, 40), (4, 70000, 33)]
 # Several pieces of the vocabulary: 512 MiB of W's planes, or of few rows' logits, a piece;
 # of the gradients 1 GiB of W and D.
 MANY = [(130, 40000, 8200), (9000, 40000, 20), (20, 40000, 8200), (128, 1100000, 3)]

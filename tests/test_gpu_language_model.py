@@ -97,6 +97,26 @@ def test_a_captured_step(gpu, example):
             assert torch.equal(a, b)
 
 
+def test_a_graph_refuses_values_that_were_written_over(gpu):
+    """autograd is told of what the calls write to; results require no gradient."""
+    import paper_2507_23387_amd as sgc
+
+    x, w = torch.randn((4, 8), device="cuda"), torch.randn((8, 8), device="cuda")
+    ids = torch.arange(4, device="cuda")
+    parameter = torch.nn.Parameter(w)
+    for write in (lambda t: sgc.embedding(ids, parameter, out=t),
+                  lambda t: sgc.embedding_backward(x, ids, 4, add_to=t),
+                  lambda t: sgc.gated_linear(x, parameter, w, out=t)):
+        t = torch.randn((4, 8), device="cuda")
+        ones = torch.ones((4, 8), device="cuda", requires_grad=True)
+        loss, before = (ones * t).sum(), t.clone()
+        assert not write(t).requires_grad and not torch.equal(t, before)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+    loss, lse = sgc.linear_cross_entropy(x, parameter, ids)
+    assert not loss.requires_grad and not lse.requires_grad
+
+
 def test_the_example_runs(gpu, example, capsys):
     means = example.main(["--tokens", "512", "--vocab", "1000", "--hidden", "128", "--inner",
                           "256", "--steps", "6"])

@@ -27,7 +27,7 @@ def test_embedding_validation(lib):
                dict(Y=W), dict(Y=W + 32), dict(Y=I), dict(Y=I - 64), dict(n=1 << 60, ldy=1 << 10)):
         assert call(**kw) == INVALID, kw
     far = dict(Y=FAKE << 1, W=FAKE << 2)
-    assert call(n=(1 << 28) + 1, **far) == NOT_SUPPORTED
+    assert call(n=(1 << 27) + 1, **far) == NOT_SUPPORTED
     assert call(v=(1 << 28) + 1, **far) == NOT_SUPPORTED
     assert call(cols=(1 << 28) + 1, ldw=1 << 29, ldy=1 << 29, **far) == NOT_SUPPORTED
     assert call(n=0, I=None, Y=None) == 0 and call(cols=0, W=None, Y=None) == 0
@@ -37,7 +37,7 @@ def test_embedding_backward_validation(lib):
     DY, I, DW, WS = (FAKE + i * GIB for i in range(4))
     need = lib.sgemm_cube_embedding_backward_workspace_size(4, 8)
     assert need > 0 and need % 256 == 0
-    for sizes in ((0, 8), (4, 0), (-1, 8), (4, -1), ((1 << 28) + 1, 8)):
+    for sizes in ((0, 8), (4, 0), (-1, 8), (4, -1), ((1 << 27) + 1, 8)):
         assert lib.sgemm_cube_embedding_backward_workspace_size(*sizes) == 0
 
     def call(n=4, v=9, cols=8, dtype=2, DY=DY, lddy=8, I=I, bits=32, scale=1.0, add=0, DW=DW,
