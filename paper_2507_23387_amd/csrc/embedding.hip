@@ -327,6 +327,7 @@ struct SumArgs {
   int lanes;       // threads to a chunk
   int chunk;       // positions
   int zero_rows;   // rows to a workgroup that writes zeros
+  bool past;       // dW goes past the caches
   int64_t chunks;
   uint32_t sum_blocks, tiles;  // workgroups of the sums, tiles of columns
 };
@@ -346,8 +347,31 @@ __device__ __forceinline__ int64_t wave_lower_bound(const uint32_t* keys, int64_
   return lo;
 }
 
-__device__ __forceinline__ void write_row(const EmbeddingGradArgs& a, uint32_t v, int j, int count,
+// A gradient that the 256 MB last cache cannot hold goes past it, which leaves the cache
+// to dy.  4096 positions of 32768 x 4096 take 126 us otherwise, with the zeros past it 112,
+// with all rows 115; 16384 take 191, 186 and 156; 1048 of 112256 x 836 84, 64 and 64.  A
+// smaller one stays where its reader finds it (20000 of 100000 x 512: 70, 75 past it).
+// Lines that two rows share are put together in the cache (single rows of 836 values past
+// it: 92).
+constexpr int64_t kCacheBytes = int64_t{256} << 20;
+
+__device__ __forceinline__ bool whole_lines(const EmbeddingGradArgs& a) {
+  return (a.cols | a.lddw) % 32 == 0 && reinterpret_cast<uintptr_t>(a.dw) % 128 == 0;
+}
+
+__device__ __forceinline__ void store_grad(float* row, int j, int n, const float* v, bool past) {
+  typedef Elem<kF32>::Piece Piece;
+  if (past && j + 4 <= n) {
+    const Piece p = {v[0], v[1], v[2], v[3]};
+    __builtin_nontemporal_store(p, reinterpret_cast<Piece*>(row + j));
+  } else {
+    store_piece<kF32>(row, j, n, v);
+  }
+}
+
+__device__ __forceinline__ void write_row(const SumArgs& g, uint32_t v, int j, int count,
                                           float* sum) {
+  const EmbeddingGradArgs& a = g.a;
   float* const row = a.dw + static_cast<int64_t>(v) * a.lddw;
   const int cols = static_cast<int>(a.cols);
 #pragma unroll
@@ -362,13 +386,13 @@ __device__ __forceinline__ void write_row(const EmbeddingGradArgs& a, uint32_t v
 #pragma unroll
       for (int e = 0; e < 4; ++e) sum[q + e] *= a.scale;
     }
-    store_piece<kF32>(row, j + q, cols, sum + q);
+    store_grad(row, j + q, cols, sum + q, g.past && whole_lines(a));
   }
 }
 
 // Rows of dW to a workgroup that looks for those without ids: 4096 values or 8 rows, and
 // 4096 workgroups at most.  (8 rows of 1003 x 530 7.0 us, 32 10.8; 8 of 131072 x 64 19.4, 64
-// 8.6; 1048 positions of 112256 x 836 in 8 rows and in 32: ZERO112.)
+// 8.6; the call with 20000 positions of 100000 x 512 76 us in 8, 70 in 32.)
 constexpr int kMostZeroRows = 64;
 int zero_rows(int64_t vocab, int64_t cols) {
   int rows = 8;
@@ -403,19 +427,20 @@ __global__ __launch_bounds__(kThreads) void embedding_sum_kernel(SumArgs g) {
       absent[g.sorted.keys[p] - v0] = false;
     __syncthreads();
     const float zero[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    if (ends[0] == ends[1] && a.lddw == a.cols) {
+    const int64_t all = (v1 - v0) * a.cols;
+    if (ends[0] == ends[1] && a.lddw == a.cols && all < INT32_MAX - 4) {
       // All of them, side by side.
       float* const at = a.dw + v0 * a.lddw;
-      const int64_t all = (v1 - v0) * a.cols;
       for (int64_t j = 4 * threadIdx.x; j < all; j += 4 * kThreads)
-        store_piece<kF32>(at, static_cast<int>(j), static_cast<int>(all), zero);
+        store_grad(at, static_cast<int>(j), static_cast<int>(all), zero, g.past);
       return;
     }
     const int per = kThreads / g.lanes;
+    const bool past = g.past && whole_lines(a);
     for (int r = threadIdx.x / g.lanes; r < g.zero_rows; r += per) {
       if (!absent[r]) continue;
       for (int64_t j = 4 * (threadIdx.x % g.lanes); j < cols; j += 4 * g.lanes)
-        store_piece<kF32>(a.dw + (v0 + r) * a.lddw, static_cast<int>(j), cols, zero);
+        store_grad(a.dw + (v0 + r) * a.lddw, static_cast<int>(j), cols, zero, past);
     }
     return;
   }
@@ -465,7 +490,7 @@ __global__ __launch_bounds__(kThreads) void embedding_sum_kernel(SumArgs g) {
       if (p + u >= p1) break;
       if (now[u] != run) {
         if (begun) leave(0);
-        else write_row(a, run, j, kE, sum);
+        else write_row(g, run, j, kE, sum);
         begun = false;
         run = now[u];
         if (run == none) return;  // the last of the sorted keys
@@ -479,7 +504,7 @@ __global__ __launch_bounds__(kThreads) void embedding_sum_kernel(SumArgs g) {
   const bool goes_on = after == run;
   if (begun) leave(0);
   else if (goes_on) leave(1);
-  else write_row(a, run, j, kE, sum);
+  else write_row(g, run, j, kE, sum);
 }
 
 // Runs that begin in a chunk and go past it, a chunk a workgroup, 1024 columns: the sums
@@ -513,7 +538,7 @@ __global__ __launch_bounds__(kThreads) void embedding_join_kernel(SumArgs g) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) sum[e] += v[e];
     }
-    write_row(a, run, j, 4, sum);
+    write_row(g, run, j, 4, sum);
   }
 }
 
@@ -639,6 +664,7 @@ hipError_t launch_embedding_grad(const EmbeddingGradArgs& a, int dtype, void* ws
   g.chunk = chunk_length(a.n, a.cols, per);
   g.chunks = (a.n + g.chunk - 1) / g.chunk;
   g.zero_rows = zero_rows(a.vocab, a.cols);
+  g.past = a.vocab * a.cols * 4 > kCacheBytes;
   g.tiles = static_cast<uint32_t>((a.cols + int64_t{g.lanes} * per - 1) / (int64_t{g.lanes} * per));
   const int64_t groups = kThreads / g.lanes;
   const int64_t sums = (g.chunks + groups - 1) / groups * g.tiles;

@@ -126,6 +126,26 @@ def test_backward(gpu, dtype, kind):
         assert total._base is None or total._base[:, cols:].isnan().all()
 
 
+@pytest.mark.parametrize("n,vocab,cols,pad", [(900, 66000, 1024, 0), (300, 66000, 1020, 0),
+                                              (300, 66000, 1024, 32), (300, 66000, 1024, 3)])
+def test_gradients_larger_than_the_cache(gpu, n, vocab, cols, pad):
+    import paper_2507_23387_amd as sgc
+
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(78)
+    ids = _ids(gen, n, vocab, torch.int64, "often")
+    dy = _wide(n, cols, pad, torch.bfloat16, gen)
+    torch.full((vocab, cols), float("nan"), device="cuda")  # what the gradient's memory holds
+    got = sgc.embedding_backward(dy, ids, vocab)
+    _check_backward(dy, ids, vocab, 1.0, None, got)
+    del got
+    total = _wide(vocab, cols, pad, torch.float32, gen)
+    old = total.clone()
+    sgc.embedding_backward(dy, ids, vocab, add_to=total)
+    _check_backward(dy, ids, vocab, 1.0, old, total)
+    assert total._base is None or total._base[:, cols:].isnan().all()
+
+
 def test_backward_against_differences(gpu):
     """<dW, E> against differences of the lookup in 64 bits (it is linear: one step)."""
     import paper_2507_23387_amd as sgc
